@@ -57,6 +57,9 @@ typedef struct CUstream_st* eogp_stream_t;
 /* ---- element types ----------------------------------------------------- */
 #define EOGP_F32  0 /* float32 inputs; computed with fp32 CUDA-core kernels */
 #define EOGP_BF16 1 /* bfloat16 inputs; tcgen05 tensor-core kernels, fp32 accumulation */
+/* Types of token numbers (the calls under "model ends" below). */
+#define EOGP_I32  2
+#define EOGP_I64  3
 
 /* ---- eogp_compress_layer output modes ---------------------------------- */
 #define EOGP_OUT_FIRST_STAGE 0 /* z = (Lambda_m + lambda I)^{-1/2} Q_m^T g   [B x m] fp32 */
@@ -92,7 +95,10 @@ int eogp_sync_status(eogp_stream_t stream);
 #define EOGP_K_PACK     3 /* sign/scale packing (also the split-K finalise)    */
 #define EOGP_K_SCORE    4 /* scoring kernels                                   */
 #define EOGP_K_SIMT     5 /* fp32 CUDA-core kernels of the EOGP_F32 path       */
-#define EOGP_K_COUNT    6
+#define EOGP_K_EMBED    6 /* token embedding and its gradient (a call's launches counted as one) */
+#define EOGP_K_NORM     7 /* normalisation and its gradient (likewise)         */
+#define EOGP_K_LOSS     8 /* token loss and its gradient                       */
+#define EOGP_K_COUNT    9
 int eogp_profile_enable(int on);
 int eogp_profile_read(int kind, int* launches, double* total_ms, int reset);
 
@@ -540,6 +546,105 @@ int eogp_score_topk(const void* train, int ld_train, const float* train_scales, 
                     int ld_query, const float* query_scales, int ld_qscale, int Q, int topk,
                     float* top_scores, int ld_top_scores, int* top_index, int ld_top_index,
                     void* ws, size_t ws_bytes, eogp_stream_t stream);
+
+/* ========================================================================
+ * Model ends: token embedding, normalisation and token loss, with gradients
+ *
+ * What a program runs around the linear modules to get their activations a_t
+ * and output gradients s_t: the embedding starts the forward pass, a
+ * normalisation writes most modules' inputs, and the loss gradient starts the
+ * backward pass. The paper takes a and s as given; these calls are a library
+ * convenience with no counterpart in it.
+ *
+ * Conventions of these calls:
+ *  - B examples of T tokens, B * T <= 2^30. Rows of width n (d or V) are
+ *    contiguous; row (b, t) of an array starts at element b * bs + t * ld of its
+ *    base ("_bs" and "_ld" arguments, in elements, long long; any offset that
+ *    fits 63 bits). Inputs may use any strides >= 0 (0 repeats a row); outputs
+ *    must not overlap themselves: ld >= n and bs >= (T - 1) ld + n, or
+ *    bs >= n and ld >= (B - 1) bs + n (a stride whose extent is 1 is ignored).
+ *  - Token numbers (tokens, targets) are EOGP_I32 or EOGP_I64, row b at element
+ *    b * bs, contiguous over t.
+ *  - lengths: device int32 [B] or NULL. Positions t >= lengths[b] are padding, as
+ *    in eogp_layer_desc: nothing of theirs is read, their output rows are 0, and
+ *    they add nothing to any sum.
+ *  - EOGP_F32 or EOGP_BF16 arrays, aligned to their element; sums, statistics
+ *    and exponentials are formed in fp32, each result rounded once to its type.
+ *    16-byte aligned bases and strides run fastest; nothing else needs them.
+ *  - Sums have a fixed order: results are bitwise reproducible.
+ *  - B = 0 or T = 0: nothing is read; arrays that sum over tokens become 0
+ *    (unless accumulated into).
+ *  - A token number outside its range sets EOGP_EDEVICE in the device status
+ *    word (eogp_sync_status); that position is then treated as padding.
+ * Errors: EOGP_EINVAL, EOGP_EUNSUPPORTED, EOGP_EWORKSPACE, EOGP_ECUDA.
+ * ======================================================================== */
+
+/* out[b][t] = scale * table[tokens[b][t]] (+ pos[t]), [d] wide, type `dtype` as
+ * table and pos. table [V x ld_table]; pos [>= T x ld_pos] holds the position
+ * rows of t = 0..T-1, or is NULL (one token at position p: T = 1 and pos at row
+ * p). Gradients: eogp_embed_grad, for `pos` with the numbers 0..T-1 as tokens,
+ * V = rows of pos and scale = 1. */
+int eogp_embed(const void* tokens, int index_type, long long tokens_bs, const void* table, int dtype, int V,
+               int d, long long ld_table, float scale, const void* pos, long long ld_pos, const int32_t* lengths,
+               int B, int T, void* out, long long out_bs, long long out_ld, eogp_stream_t stream);
+
+/* dtable[v] (+)= scale * sum of dout[b][t] over the positions with
+ * tokens[b][t] = v, in ascending order of (b, t): positions are sorted by token
+ * and each token's run of rows is summed, with no floating-point atomics. Every
+ * row of dtable [V x ld_dtable] (type `grad_dtype`) is written, 0 for tokens that
+ * do not occur; with `accumulate` the sums are added instead and rows of other
+ * tokens are left alone. dout has type `dtype`. */
+int eogp_embed_grad_workspace_size(int V, int d, int B, int T, size_t* bytes);
+int eogp_embed_grad(const void* tokens, int index_type, long long tokens_bs, const void* dout, int dtype,
+                    long long dout_bs, long long dout_ld, const int32_t* lengths, int B, int T, int V, int d,
+                    float scale, void* dtable, int grad_dtype, long long ld_dtable, int accumulate, void* ws,
+                    size_t ws_bytes, eogp_stream_t stream);
+
+/* Normalisation over the d channels of each row, then weight and bias:
+ *   EOGP_NORM_LAYER: y = (x - mean) * rstd * weight + bias,
+ *                    rstd = (mean((x - mean)^2) + eps)^(-1/2);
+ *   EOGP_NORM_RMS:   y = x * rstd * weight + bias, rstd = (mean(x^2) + eps)^(-1/2).
+ * x and y [B x T x d] of type `dtype`; weight and bias [d] of type param_dtype,
+ * NULL for 1 and 0. mean and rstd (fp32 [B x T], dense) are written when not
+ * NULL; the gradient needs them (rstd alone for EOGP_NORM_RMS). y may be x with
+ * the same strides. */
+#define EOGP_NORM_LAYER 0
+#define EOGP_NORM_RMS   1
+int eogp_norm(int kind, const void* x, int dtype, long long x_bs, long long x_ld, const void* weight,
+              const void* bias, int param_dtype, float eps, const int32_t* lengths, int B, int T, int d, void* y,
+              long long y_bs, long long y_ld, float* mean, float* rstd, eogp_stream_t stream);
+
+/* Gradient of eogp_norm. With xh = (x - mean) * rstd and g = dy * weight:
+ *   dx = rstd * (g - mean_d(g) - xh * mean_d(g * xh))  (EOGP_NORM_RMS: without
+ *        mean_d(g), and xh = x * rstd; the mean argument is ignored),
+ *   dweight = sum dy * xh,  dbias = sum dy,
+ * the sums over an example's tokens with per_example nonzero (dweight, dbias
+ * [B x ld_dparam], row b of example b: the per-example gradients influence
+ * functions are made of) and over all tokens otherwise ([d]). They are fp32 and
+ * added to when `accumulate` is nonzero. Any of dx, dweight, dbias may be NULL.
+ * dy, x and dx [B x T x d] of type `dtype`; dx may be dy or x with the same
+ * strides. */
+int eogp_norm_grad_workspace_size(int B, int T, int d, int per_example, size_t* bytes);
+int eogp_norm_grad(int kind, const void* dy, long long dy_bs, long long dy_ld, const void* x, int dtype,
+                   long long x_bs, long long x_ld, const float* mean, const float* rstd, const void* weight,
+                   int param_dtype, const int32_t* lengths, int B, int T, int d, void* dx, long long dx_bs,
+                   long long dx_ld, float* dweight, float* dbias, long long ld_dparam, int per_example,
+                   int accumulate, void* ws, size_t ws_bytes, eogp_stream_t stream);
+
+/* Token loss (cross entropy) over V classes and the gradient of its sum:
+ *   lse[b][t]  = log sum_v exp(x_v),   x = logits[b][t],
+ *   loss[b][t] = w * (lse - x_target),  dlogits[b][t] = w * (softmax(x) - e_target),
+ * w = weights[b][t] (fp32 [B x T] dense, or NULL for 1). dlogits is the gradient of
+ * sum loss[b][t]: divide the weights for a mean. A position is left out
+ * (loss, lse and gradient 0, its logits not read) when it is padding, when its
+ * target equals ignore_index, or when its weight is 0. Logits of -inf have
+ * probability 0; rows without a finite logit, or with a NaN or +inf, give NaN.
+ * loss and lse fp32 [B x T], dense; lse and dlogits may be NULL; dlogits has the
+ * type of logits and may be logits itself with the same strides. */
+int eogp_cross_entropy(const void* logits, int dtype, long long logits_bs, long long logits_ld,
+                       const void* targets, int index_type, long long targets_bs, const float* weights,
+                       long long ignore_index, const int32_t* lengths, int B, int T, int V, float* loss, float* lse,
+                       void* dlogits, long long dlogits_bs, long long dlogits_ld, eogp_stream_t stream);
 
 #ifdef __cplusplus
 }

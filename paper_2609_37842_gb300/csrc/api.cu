@@ -1470,3 +1470,194 @@ extern "C" int eogp_score_topk(const void* train, int ld_train, const float* tra
                              ld_top_index, st));
   return EOGP_OK;
 }
+
+// ============================================================ model ends
+
+namespace {
+
+bool elem_type(int t) { return t == EOGP_F32 || t == EOGP_BF16; }
+bool index_type_ok(int t) { return t == EOGP_I32 || t == EOGP_I64; }
+int elem_bytes(int t) { return t == EOGP_F32 || t == EOGP_I32 ? 4 : t == EOGP_I64 ? 8 : 2; }
+
+bool aligned_to(const void* p, int type) { return reinterpret_cast<uintptr_t>(p) % elem_bytes(type) == 0; }
+
+// Strides of a [B x T] array of n-wide rows that is written: rows may not overlap.
+bool out_strides_ok(long long bs, long long ld, int B, int T, int n) {
+  if (T > 1 && ld < n) return false;
+  if (B > 1 && bs < n) return false;
+  if (B == 1 || T == 1) return true;
+  return (bs - n) / (T - 1) >= ld || (ld - n) / (B - 1) >= bs;
+}
+
+bool in_strides_ok(long long bs, long long ld) { return bs >= 0 && ld >= 0; }
+
+int check_rows(int B, int T) {
+  if (B < 0 || T < 0) return set_error(EOGP_EINVAL, "B and T must be >= 0");
+  if (static_cast<long long>(B) * T > (1LL << 30)) return set_error(EOGP_EUNSUPPORTED, "B * T must be <= 2^30");
+  return EOGP_OK;
+}
+
+}  // namespace
+
+extern "C" int eogp_embed(const void* tokens, int index_type, long long tokens_bs, const void* table, int dtype,
+                          int V, int d, long long ld_table, float scale, const void* pos, long long ld_pos,
+                          const int32_t* lengths, int B, int T, void* out, long long out_bs, long long out_ld,
+                          eogp_stream_t stream) {
+  clear_error();
+  if (int rc = check_rows(B, T)) return rc;
+  if (!index_type_ok(index_type)) return set_error(EOGP_EINVAL, "bad index_type");
+  if (!elem_type(dtype)) return set_error(EOGP_EINVAL, "bad dtype");
+  if (V < 1 || d < 1) return set_error(EOGP_EINVAL, "V and d must be >= 1");
+  if (B == 0 || T == 0) return EOGP_OK;
+  if (!tokens || !table || !out) return set_error(EOGP_EINVAL, "NULL argument");
+  if (!aligned_to(tokens, index_type) || !aligned_to(table, dtype) || !aligned_to(pos, dtype) ||
+      !aligned_to(out, dtype) || !aligned_to(lengths, EOGP_I32))
+    return set_error(EOGP_EINVAL, "an array is not aligned to its elements");
+  if (tokens_bs < 0 || ld_table < 0 || (pos && ld_pos < 0)) return set_error(EOGP_EINVAL, "negative stride");
+  if (!out_strides_ok(out_bs, out_ld, B, T, d)) return set_error(EOGP_EINVAL, "rows of out overlap");
+  unsigned* status = status_word();
+  if (!status) return set_error(EOGP_ECUDA, "device status word unavailable");
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  ProfScope ps(EOGP_K_EMBED, st);
+  CUDA_TRY(launch_embed(RowSet{B, T, lengths}, TokenView{tokens, index_type == EOGP_I64, tokens_bs}, table,
+                        dtype == EOGP_BF16, V, d, ld_table, scale, pos, ld_pos, RowView{out, out_bs, out_ld}, status,
+                        st));
+  return EOGP_OK;
+}
+
+extern "C" int eogp_embed_grad_workspace_size(int V, int d, int B, int T, size_t* bytes) {
+  clear_error();
+  if (!bytes) return set_error(EOGP_EINVAL, "bytes is NULL");
+  if (int rc = check_rows(B, T)) return rc;
+  if (V < 1 || d < 1) return set_error(EOGP_EINVAL, "V and d must be >= 1");
+  *bytes = embed_grad_ws_bytes(V, d, static_cast<long long>(B) * T);
+  return EOGP_OK;
+}
+
+extern "C" int eogp_embed_grad(const void* tokens, int index_type, long long tokens_bs, const void* dout, int dtype,
+                               long long dout_bs, long long dout_ld, const int32_t* lengths, int B, int T, int V,
+                               int d, float scale, void* dtable, int grad_dtype, long long ld_dtable, int accumulate,
+                               void* ws, size_t ws_bytes, eogp_stream_t stream) {
+  clear_error();
+  size_t need = 0;
+  if (int rc = eogp_embed_grad_workspace_size(V, d, B, T, &need)) return rc;
+  if (!index_type_ok(index_type)) return set_error(EOGP_EINVAL, "bad index_type");
+  if (!elem_type(dtype) || !elem_type(grad_dtype)) return set_error(EOGP_EINVAL, "bad dtype");
+  const bool empty = B == 0 || T == 0;
+  if (!dtable || (!empty && (!tokens || !dout))) return set_error(EOGP_EINVAL, "NULL argument");
+  if (!aligned_to(tokens, index_type) || !aligned_to(dout, dtype) || !aligned_to(dtable, grad_dtype) ||
+      !aligned_to(lengths, EOGP_I32))
+    return set_error(EOGP_EINVAL, "an array is not aligned to its elements");
+  if (tokens_bs < 0 || !in_strides_ok(dout_bs, dout_ld)) return set_error(EOGP_EINVAL, "negative stride");
+  if (V > 1 && ld_dtable < d) return set_error(EOGP_EINVAL, "ld_dtable < d");
+  if (need && (!ws || ws_bytes < need)) return set_error(EOGP_EWORKSPACE, "workspace of %zu bytes needed", need);
+  if (need && (reinterpret_cast<uintptr_t>(ws) & 255))
+    return set_error(EOGP_EINVAL, "workspace must be 256-byte aligned");
+  unsigned* status = status_word();
+  if (!status) return set_error(EOGP_ECUDA, "device status word unavailable");
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  ProfScope ps(EOGP_K_EMBED, st);
+  CUDA_TRY(launch_embed_grad(RowSet{B, T, lengths}, TokenView{tokens, index_type == EOGP_I64, tokens_bs},
+                             RowView{dout, dout_bs, dout_ld}, dtype == EOGP_BF16, V, d, scale, dtable,
+                             grad_dtype == EOGP_BF16, ld_dtable, accumulate != 0, ws, status, sm_count(), st));
+  return EOGP_OK;
+}
+
+extern "C" int eogp_norm(int kind, const void* x, int dtype, long long x_bs, long long x_ld, const void* weight,
+                         const void* bias, int param_dtype, float eps, const int32_t* lengths, int B, int T, int d,
+                         void* y, long long y_bs, long long y_ld, float* mean, float* rstd, eogp_stream_t stream) {
+  clear_error();
+  if (int rc = check_rows(B, T)) return rc;
+  if (kind != EOGP_NORM_LAYER && kind != EOGP_NORM_RMS) return set_error(EOGP_EINVAL, "bad norm kind");
+  if (!elem_type(dtype) || !elem_type(param_dtype)) return set_error(EOGP_EINVAL, "bad dtype");
+  if (d < 1) return set_error(EOGP_EINVAL, "d must be >= 1");
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return set_error(EOGP_EINVAL, "eps must be finite and >= 0");
+  if (B == 0 || T == 0) return EOGP_OK;
+  if (!x || !y) return set_error(EOGP_EINVAL, "NULL argument");
+  if (!aligned_to(x, dtype) || !aligned_to(y, dtype) || !aligned_to(weight, param_dtype) ||
+      !aligned_to(bias, param_dtype) || !aligned_to(mean, EOGP_F32) || !aligned_to(rstd, EOGP_F32) ||
+      !aligned_to(lengths, EOGP_I32))
+    return set_error(EOGP_EINVAL, "an array is not aligned to its elements");
+  if (!in_strides_ok(x_bs, x_ld)) return set_error(EOGP_EINVAL, "negative stride");
+  if (!out_strides_ok(y_bs, y_ld, B, T, d)) return set_error(EOGP_EINVAL, "rows of y overlap");
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  ProfScope ps(EOGP_K_NORM, st);
+  CUDA_TRY(launch_norm(kind == EOGP_NORM_RMS, RowSet{B, T, lengths}, RowView{x, x_bs, x_ld}, dtype == EOGP_BF16,
+                       weight, bias, param_dtype == EOGP_BF16, eps, d, RowView{y, y_bs, y_ld}, mean, rstd, sm_count(),
+                       st));
+  return EOGP_OK;
+}
+
+extern "C" int eogp_norm_grad_workspace_size(int B, int T, int d, int per_example, size_t* bytes) {
+  clear_error();
+  if (!bytes) return set_error(EOGP_EINVAL, "bytes is NULL");
+  if (int rc = check_rows(B, T)) return rc;
+  if (d < 1) return set_error(EOGP_EINVAL, "d must be >= 1");
+  *bytes = norm_grad_ws_bytes(B, T, d, per_example != 0, sm_count());
+  return EOGP_OK;
+}
+
+extern "C" int eogp_norm_grad(int kind, const void* dy, long long dy_bs, long long dy_ld, const void* x, int dtype,
+                              long long x_bs, long long x_ld, const float* mean, const float* rstd,
+                              const void* weight, int param_dtype, const int32_t* lengths, int B, int T, int d,
+                              void* dx, long long dx_bs, long long dx_ld, float* dweight, float* dbias,
+                              long long ld_dparam, int per_example, int accumulate, void* ws, size_t ws_bytes,
+                              eogp_stream_t stream) {
+  clear_error();
+  size_t need = 0;
+  if (int rc = eogp_norm_grad_workspace_size(B, T, d, per_example, &need)) return rc;
+  if (kind != EOGP_NORM_LAYER && kind != EOGP_NORM_RMS) return set_error(EOGP_EINVAL, "bad norm kind");
+  if (!elem_type(dtype) || !elem_type(param_dtype)) return set_error(EOGP_EINVAL, "bad dtype");
+  const bool empty = B == 0 || T == 0;
+  const bool sums = dweight || dbias;
+  if (!empty && (!dy || !x || !rstd || (kind == EOGP_NORM_LAYER && !mean)))
+    return set_error(EOGP_EINVAL, "NULL argument");
+  if (!aligned_to(dy, dtype) || !aligned_to(x, dtype) || !aligned_to(dx, dtype) || !aligned_to(weight, param_dtype) ||
+      !aligned_to(mean, EOGP_F32) || !aligned_to(rstd, EOGP_F32) || !aligned_to(dweight, EOGP_F32) ||
+      !aligned_to(dbias, EOGP_F32) || !aligned_to(lengths, EOGP_I32))
+    return set_error(EOGP_EINVAL, "an array is not aligned to its elements");
+  if (!in_strides_ok(dy_bs, dy_ld) || !in_strides_ok(x_bs, x_ld)) return set_error(EOGP_EINVAL, "negative stride");
+  if (dx && !empty && !out_strides_ok(dx_bs, dx_ld, B, T, d)) return set_error(EOGP_EINVAL, "rows of dx overlap");
+  if (sums && per_example && B > 1 && ld_dparam < d) return set_error(EOGP_EINVAL, "ld_dparam < d");
+  if (sums && need && (!ws || ws_bytes < need))
+    return set_error(EOGP_EWORKSPACE, "workspace of %zu bytes needed", need);
+  if (sums && need && (reinterpret_cast<uintptr_t>(ws) & 255))
+    return set_error(EOGP_EINVAL, "workspace must be 256-byte aligned");
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  ProfScope ps(EOGP_K_NORM, st);
+  const NormGrad g{kind == EOGP_NORM_RMS, dtype == EOGP_BF16, param_dtype == EOGP_BF16, per_example != 0,
+                   accumulate != 0, RowSet{B, T, lengths}, d, RowView{dy, dy_bs, dy_ld}, RowView{x, x_bs, x_ld},
+                   RowView{dx, dx_bs, dx_ld}, mean, rstd, weight, dweight, dbias, ld_dparam};
+  CUDA_TRY(launch_norm_grad(g, ws, sm_count(), st));
+  return EOGP_OK;
+}
+
+extern "C" int eogp_cross_entropy(const void* logits, int dtype, long long logits_bs, long long logits_ld,
+                                  const void* targets, int index_type, long long targets_bs, const float* weights,
+                                  long long ignore_index, const int32_t* lengths, int B, int T, int V, float* loss,
+                                  float* lse, void* dlogits, long long dlogits_bs, long long dlogits_ld,
+                                  eogp_stream_t stream) {
+  clear_error();
+  if (int rc = check_rows(B, T)) return rc;
+  if (!elem_type(dtype)) return set_error(EOGP_EINVAL, "bad dtype");
+  if (!index_type_ok(index_type)) return set_error(EOGP_EINVAL, "bad index_type");
+  if (V < 1) return set_error(EOGP_EINVAL, "V must be >= 1");
+  if (B == 0 || T == 0) return EOGP_OK;
+  if (!logits || !targets || !loss) return set_error(EOGP_EINVAL, "NULL argument");
+  if (!aligned_to(logits, dtype) || !aligned_to(dlogits, dtype) || !aligned_to(targets, index_type) ||
+      !aligned_to(weights, EOGP_F32) || !aligned_to(loss, EOGP_F32) || !aligned_to(lse, EOGP_F32) ||
+      !aligned_to(lengths, EOGP_I32))
+    return set_error(EOGP_EINVAL, "an array is not aligned to its elements");
+  if (targets_bs < 0 || !in_strides_ok(logits_bs, logits_ld)) return set_error(EOGP_EINVAL, "negative stride");
+  if (dlogits && !out_strides_ok(dlogits_bs, dlogits_ld, B, T, V))
+    return set_error(EOGP_EINVAL, "rows of dlogits overlap");
+  unsigned* status = status_word();
+  if (!status) return set_error(EOGP_ECUDA, "device status word unavailable");
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  ProfScope ps(EOGP_K_LOSS, st);
+  const LossArgs a{RowSet{B, T, lengths}, RowView{logits, logits_bs, logits_ld},
+                   RowView{dlogits, dlogits_bs, dlogits_ld}, TokenView{targets, index_type == EOGP_I64, targets_bs},
+                   weights, ignore_index, V, loss, lse};
+  CUDA_TRY(launch_cross_entropy(a, dtype == EOGP_BF16, status, sm_count(), st));
+  return EOGP_OK;
+}

@@ -216,3 +216,60 @@ int fit_pca_device(const float* Z, int n, int m, int ldz, int k, void* Pt, int l
 cudaError_t second_moment_device(const float* Z, int n, int m, int ldz, double* C, int ldc, int accumulate,
                                  cudaStream_t st);
 size_t fit_pca_ws_bytes(int n, int m, int k);
+
+// ------------------------------------------------------------ model ends
+// A [B x T] array of rows: row (b, t) starts at element b * bs + t * ld.
+struct RowView {
+  const void* p;
+  long long bs, ld;
+};
+// Token numbers [B x T]: int32 or int64, row b at element b * bs.
+struct TokenView {
+  const void* p;
+  bool i64;
+  long long bs;
+};
+// Which rows take part: B examples of T tokens, kept tokens per example or NULL.
+struct RowSet {
+  int B, T;
+  const int32_t* lengths;
+  long long rows() const { return static_cast<long long>(B) * T; }
+};
+
+// k_embed.cu
+cudaError_t launch_embed(RowSet rs, TokenView tok, const void* table, bool bf16, int V, int d, long long ld_table,
+                         float scale, const void* pos, long long ld_pos, RowView out, unsigned* status,
+                         cudaStream_t st);
+size_t embed_grad_ws_bytes(int V, int d, long long M);
+cudaError_t launch_embed_grad(RowSet rs, TokenView tok, RowView dout, bool bf16, int V, int d, float scale,
+                              void* dtable, bool grad_bf16, long long ld_dtable, bool accumulate, void* ws,
+                              unsigned* status, int num_sms, cudaStream_t st);
+
+// k_norm.cu
+cudaError_t launch_norm(bool rms, RowSet rs, RowView x, bool bf16, const void* weight, const void* bias,
+                        bool param_bf16, float eps, int d, RowView y, float* mean, float* rstd, int num_sms,
+                        cudaStream_t st);
+struct NormGrad {
+  bool rms, bf16, param_bf16, per_example, accumulate;
+  RowSet rs;
+  int d;
+  RowView dy, x, dx;  // dx.p NULL: not wanted
+  const float *mean, *rstd;
+  const void* weight;
+  float *dweight, *dbias;  // either NULL: not wanted
+  long long ld_dparam;
+};
+size_t norm_grad_ws_bytes(int B, int T, int d, bool per_example, int num_sms);
+cudaError_t launch_norm_grad(const NormGrad& g, void* ws, int num_sms, cudaStream_t st);
+
+// k_loss.cu
+struct LossArgs {
+  RowSet rs;
+  RowView logits, dlogits;  // dlogits.p NULL: not wanted
+  TokenView targets;
+  const float* weights;
+  long long ignore;
+  int V;
+  float *loss, *lse;
+};
+cudaError_t launch_cross_entropy(const LossArgs& a, bool bf16, unsigned* status, int num_sms, cudaStream_t st);

@@ -7,9 +7,10 @@ fallback implementation.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
-from ctypes import POINTER, c_double, c_float, c_int, c_int32, c_size_t, c_uint32, c_void_p
+from ctypes import POINTER, c_double, c_float, c_int, c_int32, c_longlong, c_size_t, c_uint32, c_void_p
 from typing import Optional, Sequence, Tuple
 
 import numpy as np
@@ -18,13 +19,15 @@ from . import build as _build
 
 OK, EINVAL, EUNSUPPORTED, ECUDA, ETIMEOUT, EWORKSPACE, EDEVICE = 0, -1, -2, -3, -4, -5, -6
 F32, BF16 = 0, 1
+I32, I64 = 2, 3
+NORM_LAYER, NORM_RMS = 0, 1
 OUT_FIRST_STAGE, OUT_COORDS, OUT_CODES = 0, 1, 2
 SCORE_CODES, SCORE_PAPER, SCORE_FP = 0, 1, 2
 TOPK_MAX = 256
 SRHT_MAX_M = 32768
-K_ROTATE, K_CONTRACT, K_PROJECT, K_PACK, K_SCORE, K_SIMT = range(6)
+K_ROTATE, K_CONTRACT, K_PROJECT, K_PACK, K_SCORE, K_SIMT, K_EMBED, K_NORM, K_LOSS = range(9)
 KERNEL_KINDS = {K_ROTATE: "rotate", K_CONTRACT: "contract", K_PROJECT: "project", K_PACK: "pack",
-                K_SCORE: "score", K_SIMT: "simt_f32"}
+                K_SCORE: "score", K_SIMT: "simt_f32", K_EMBED: "embed", K_NORM: "norm", K_LOSS: "loss"}
 
 _ERRNAMES = {EINVAL: "EINVAL", EUNSUPPORTED: "EUNSUPPORTED", ECUDA: "ECUDA",
              ETIMEOUT: "ETIMEOUT", EWORKSPACE: "EWORKSPACE", EDEVICE: "EDEVICE"}
@@ -118,6 +121,24 @@ EXPORTS = {
     "eogp_score_topk": (c_int, [c_void_p, c_int, c_void_p, c_int, c_int, c_void_p, c_int, c_int,
                                 c_void_p, c_int, c_void_p, c_int, c_int, c_int, c_void_p, c_int,
                                 c_void_p, c_int, c_void_p, c_size_t, c_void_p]),
+    "eogp_embed": (c_int, [c_void_p, c_int, c_longlong, c_void_p, c_int, c_int, c_int, c_longlong, c_float,
+                           c_void_p, c_longlong, c_void_p, c_int, c_int, c_void_p, c_longlong, c_longlong,
+                           c_void_p]),
+    "eogp_embed_grad_workspace_size": (c_int, [c_int, c_int, c_int, c_int, POINTER(c_size_t)]),
+    "eogp_embed_grad": (c_int, [c_void_p, c_int, c_longlong, c_void_p, c_int, c_longlong, c_longlong, c_void_p,
+                                c_int, c_int, c_int, c_int, c_float, c_void_p, c_int, c_longlong, c_int,
+                                c_void_p, c_size_t, c_void_p]),
+    "eogp_norm": (c_int, [c_int, c_void_p, c_int, c_longlong, c_longlong, c_void_p, c_void_p, c_int, c_float,
+                          c_void_p, c_int, c_int, c_int, c_void_p, c_longlong, c_longlong, c_void_p, c_void_p,
+                          c_void_p]),
+    "eogp_norm_grad_workspace_size": (c_int, [c_int, c_int, c_int, c_int, POINTER(c_size_t)]),
+    "eogp_norm_grad": (c_int, [c_int, c_void_p, c_longlong, c_longlong, c_void_p, c_int, c_longlong, c_longlong,
+                               c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_int, c_int, c_void_p,
+                               c_longlong, c_longlong, c_void_p, c_void_p, c_longlong, c_int, c_int, c_void_p,
+                               c_size_t, c_void_p]),
+    "eogp_cross_entropy": (c_int, [c_void_p, c_int, c_longlong, c_longlong, c_void_p, c_int, c_longlong, c_void_p,
+                                   c_longlong, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p,
+                                   c_longlong, c_longlong, c_void_p]),
 }
 
 _LIB = None
@@ -762,3 +783,247 @@ def fit_pca_from_moment(C, n_total: int, k: int, pt_dtype: int = F32, stream=Non
     _check(lib().eogp_fit_pca_from_moment(_ptr(C), m, C.stride(0), int(n_total), int(k), _ptr(Pt), Pt.stride(0),
                                           int(pt_dtype), _ptr(eig), _ptr(ws), ws.numel(), _stream(stream)))
     return Pt, eig
+
+
+# -------------------------------------------------------------- model ends
+def _btn(t, name: str):
+    """(B, T, n, example stride, token stride) of rows [B, T, n] or [T, n]."""
+    if t.dim() == 3:
+        B, T, n = t.shape
+        bs, ld, inner = t.stride()
+    elif t.dim() == 2:
+        B, (T, n) = 1, t.shape
+        bs, (ld, inner) = 0, t.stride()
+    else:
+        raise ValueError(f"{name} must be [B, T, n] or [T, n]")
+    if inner != 1 and n > 1 and B * T > 0:
+        raise ValueError(f"{name} must have unit stride along its last dimension")
+    return B, T, n, bs, ld
+
+
+def _index_code(t) -> int:
+    import torch
+    if t.dtype == torch.int64:
+        return I64
+    if t.dtype == torch.int32:
+        return I32
+    raise ValueError(f"unsupported dtype {t.dtype} for token numbers (int32 or int64)")
+
+
+def _bt(t, name: str):
+    """(B, T, example stride) of token numbers [B, T] or [T]."""
+    if t.dim() == 2:
+        B, T = t.shape
+        bs, inner = t.stride()
+    elif t.dim() == 1:
+        B, T = 1, t.shape[0]
+        bs, inner = 0, t.stride(0)
+    else:
+        raise ValueError(f"{name} must be [B, T] or [T]")
+    if inner != 1 and T > 1 and B > 0:
+        raise ValueError(f"{name} must have unit stride along its last dimension")
+    return B, T, bs
+
+
+def _like(t, name: str, shape, dtype):
+    """Require a tensor of this shape and type; returns t."""
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def _on_device(*tensors):
+    """All tensors (None allowed) on one CUDA device: its kernels read them by address."""
+    dev = None
+    for t in tensors:
+        if t is not None:
+            if not t.is_cuda or (dev is not None and t.device != dev):
+                raise ValueError("all tensors must be on the same CUDA device")
+            dev = t.device
+    return dev
+
+
+_NO_CONTEXT = contextlib.nullcontext()
+
+
+def _pool(stream):
+    """Context in which new tensors belong to the stream of the call: memory from another stream's pool may still
+    be in use there, and would go back to it while this stream works on it."""
+    import torch
+    if stream is None:
+        return _NO_CONTEXT
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+
+
+def _lengths(lengths, B: int):
+    import torch
+    if lengths is not None:
+        _dense(_like(lengths, "lengths", (B,), torch.int32), "lengths")
+    return _ptr(lengths)
+
+
+def embed(tokens, table, scale: float = 1.0, pos=None, lengths=None, out=None, stream=None):
+    """eogp_embed: scale * table[tokens] (+ pos rows 0..T-1) for tokens [B, T] or [T], table [V, d],
+    pos [>= T, d]. Returns out [B, T, d] (or [T, d]); rows of padding (t >= lengths[b]) are 0."""
+    import torch
+    dev = _on_device(tokens, table, pos, lengths, out)
+    B, T, tbs = _bt(tokens, "tokens")
+    if table.dim() != 2:
+        raise ValueError("table must be [V, d]")
+    _rows(table, "table")
+    V, d = table.shape
+    if pos is not None:
+        _rows(pos, "pos")
+        if pos.dim() != 2 or pos.dtype != table.dtype or pos.shape[1] != d or pos.shape[0] < T:
+            raise ValueError(f"pos must be [>= {T}, {d}] of {table.dtype}")
+    if out is None:
+        with _pool(stream):
+            out = torch.empty((*tokens.shape, d), dtype=table.dtype, device=dev)
+    _like(out, "out", (*tokens.shape, d), table.dtype)
+    _, _, _, obs, old = _btn(out, "out")
+    _check(lib().eogp_embed(tokens.data_ptr(), _index_code(tokens), tbs, table.data_ptr(), _dtype_code(table), V, d,
+                            table.stride(0), float(scale), _ptr(pos), 0 if pos is None else pos.stride(0),
+                            _lengths(lengths, B), B, T, out.data_ptr(), obs, old, _stream(stream)))
+    return out
+
+
+def embed_grad(tokens, dout, V: int, scale: float = 1.0, lengths=None, dtable=None, dtype=None,
+               accumulate: bool = False, ws=None, stream=None):
+    """eogp_embed_grad: dtable [V, d] (+)= scale * the sum of dout's rows of each token. dtable may be given,
+    else it is a new tensor of `dtype` (default float32). Gradient of `pos` in embed: tokens 0..T-1, V = its rows."""
+    import torch
+    dev = _on_device(tokens, dout, lengths, dtable, ws)
+    B, T, tbs = _bt(tokens, "tokens")
+    if tuple(dout.shape[:-1]) != tuple(tokens.shape):
+        raise ValueError("dout must be [*tokens.shape, d]")
+    _, _, d, dbs, dld = _btn(dout, "dout")
+    if dtable is None:
+        if accumulate:
+            raise ValueError("accumulate needs dtable")
+        with _pool(stream):
+            dtable = torch.empty((int(V), d), dtype=dtype or torch.float32, device=dev)
+    _like(dtable, "dtable", (int(V), d), dtype or dtable.dtype)
+    _rows(dtable, "dtable")
+    L = lib()
+    need = c_size_t()
+    _check(L.eogp_embed_grad_workspace_size(int(V), d, B, T, ctypes.byref(need)))
+    if ws is None:
+        with _pool(stream):
+            ws = workspace(need.value, dev)
+    _check(L.eogp_embed_grad(tokens.data_ptr(), _index_code(tokens), tbs, dout.data_ptr(), _dtype_code(dout), dbs, dld,
+                             _lengths(lengths, B), B, T, int(V), d, float(scale), dtable.data_ptr(),
+                             _dtype_code(dtable), dtable.stride(0), 1 if accumulate else 0, ws.data_ptr(), ws.numel(),
+                             _stream(stream)))
+    return dtable
+
+
+def _norm_params(weight, bias, d: int):
+    """param_dtype of weight / bias [d] (either may be None)."""
+    code = F32
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        if t is not None:
+            if tuple(t.shape) != (d,):
+                raise ValueError(f"{name} must have shape ({d},), got {tuple(t.shape)}")
+            _dense(t, name)
+            code = _dtype_code(t)
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise ValueError("weight and bias must have one dtype")
+    return code
+
+
+def norm(x, weight=None, bias=None, kind: int = NORM_LAYER, eps: float = 1e-5, lengths=None, out=None,
+         stream=None):
+    """eogp_norm on rows x [B, T, d] or [T, d]. Returns (y, mean, rstd); mean is None for NORM_RMS. Rows of
+    padding (t >= lengths[b]) are 0. `out` may be x."""
+    import torch
+    dev = _on_device(x, weight, bias, lengths, out)
+    B, T, d, xbs, xld = _btn(x, "x")
+    code = _norm_params(weight, bias, d)
+    with _pool(stream):
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev) if kind == NORM_LAYER else None
+        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev)
+    _like(out, "out", x.shape, x.dtype)
+    _, _, _, ybs, yld = _btn(out, "out")
+    _check(lib().eogp_norm(int(kind), x.data_ptr(), _dtype_code(x), xbs, xld, _ptr(weight), _ptr(bias), code,
+                           float(eps), _lengths(lengths, B), B, T, d, out.data_ptr(), ybs, yld, _ptr(mean),
+                           rstd.data_ptr(), _stream(stream)))
+    return out, mean, rstd
+
+
+def norm_grad(dy, x, mean, rstd, weight=None, kind: int = NORM_LAYER, lengths=None, per_example: bool = False,
+              want_dx: bool = True, want_dweight: bool = True, want_dbias: bool = True, dx=None, dweight=None,
+              dbias=None, accumulate: bool = False, ws=None, stream=None):
+    """eogp_norm_grad from norm's mean and rstd. Returns (dx, dweight, dbias), None where not wanted. dweight and
+    dbias are fp32 [d], or [B, d] with per_example; given tensors are written, or added to with accumulate."""
+    import torch
+    dev = _on_device(dy, x, mean, rstd, weight, lengths, dx, dweight, dbias, ws)
+    B, T, d, xbs, xld = _btn(x, "x")
+    _like(dy, "dy", x.shape, x.dtype)
+    _, _, _, dybs, dyld = _btn(dy, "dy")
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        if t is not None:
+            _dense(_like(t, name, x.shape[:-1], torch.float32), name)
+    code = _norm_params(weight, None, d)
+    shape = (B, d) if per_example else (d,)
+    if accumulate and ((want_dweight and dweight is None) or (want_dbias and dbias is None)):
+        raise ValueError("accumulate needs dweight and dbias")
+    L = lib()
+    with _pool(stream):
+        if dx is None and want_dx:
+            dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        if dweight is None and want_dweight:
+            dweight = torch.empty(shape, dtype=torch.float32, device=dev)
+        if dbias is None and want_dbias:
+            dbias = torch.empty(shape, dtype=torch.float32, device=dev)
+        if ws is None and (dweight is not None or dbias is not None):
+            need = c_size_t()
+            _check(L.eogp_norm_grad_workspace_size(B, T, d, 1 if per_example else 0, ctypes.byref(need)))
+            ws = workspace(need.value, dev)
+    dxbs = dxld = 0
+    if dx is not None:
+        _like(dx, "dx", x.shape, x.dtype)
+        _, _, _, dxbs, dxld = _btn(dx, "dx")
+    ldp = d
+    for t, name in ((dweight, "dweight"), (dbias, "dbias")):
+        if t is not None:
+            _rows(_like(t, name, shape, torch.float32), name)
+            ldp = t.stride(0) if per_example else d
+    if dweight is not None and dbias is not None and per_example and dweight.stride(0) != dbias.stride(0):
+        raise ValueError("dweight and dbias must have the same row stride")
+    _check(L.eogp_norm_grad(int(kind), dy.data_ptr(), dybs, dyld, x.data_ptr(), _dtype_code(x), xbs, xld, _ptr(mean),
+                            _ptr(rstd), _ptr(weight), code, _lengths(lengths, B), B, T, d, _ptr(dx), dxbs, dxld,
+                            _ptr(dweight), _ptr(dbias), ldp, 1 if per_example else 0, 1 if accumulate else 0, _ptr(ws),
+                            0 if ws is None else ws.numel(), _stream(stream)))
+    return dx, dweight, dbias
+
+
+def cross_entropy(logits, targets, weights=None, lengths=None, ignore_index: int = -100, want_grad: bool = True,
+                  dlogits=None, stream=None):
+    """eogp_cross_entropy on logits [B, T, V] or [T, V] with targets [B, T] or [T]. Returns (loss, lse, dlogits):
+    fp32 per position, and the gradient of the sum of the losses (None without want_grad). `dlogits` may be logits."""
+    import torch
+    dev = _on_device(logits, targets, weights, lengths, dlogits)
+    B, T, V, lbs, lld = _btn(logits, "logits")
+    if tuple(targets.shape) != tuple(logits.shape[:-1]):
+        raise ValueError("targets must have the shape of logits without its last dimension")
+    _, _, tbs = _bt(targets, "targets")
+    if weights is not None:
+        _dense(_like(weights, "weights", targets.shape, torch.float32), "weights")
+    with _pool(stream):
+        loss = torch.empty(targets.shape, dtype=torch.float32, device=dev)
+        lse = torch.empty(targets.shape, dtype=torch.float32, device=dev)
+        if dlogits is None and want_grad:
+            dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    gbs = gld = 0
+    if dlogits is not None:
+        _like(dlogits, "dlogits", logits.shape, logits.dtype)
+        _, _, _, gbs, gld = _btn(dlogits, "dlogits")
+    _check(lib().eogp_cross_entropy(logits.data_ptr(), _dtype_code(logits), lbs, lld, targets.data_ptr(),
+                                    _index_code(targets), tbs, _ptr(weights), int(ignore_index), _lengths(lengths, B),
+                                    B, T, V, loss.data_ptr(), lse.data_ptr(), _ptr(dlogits), gbs, gld,
+                                    _stream(stream)))
+    return loss, lse, dlogits
