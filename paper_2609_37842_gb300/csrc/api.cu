@@ -1583,8 +1583,8 @@ extern "C" int eogp_norm(int kind, const void* x, int dtype, long long x_bs, lon
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   ProfScope ps(EOGP_K_NORM, st);
   CUDA_TRY(launch_norm(kind == EOGP_NORM_RMS, RowSet{B, T, lengths}, RowView{x, x_bs, x_ld}, dtype == EOGP_BF16,
-                       weight, bias, param_dtype == EOGP_BF16, eps, d, RowView{y, y_bs, y_ld}, mean, rstd, sm_count(),
-                       st));
+                       weight, bias, param_dtype == EOGP_BF16, eps, d, RowView{y, y_bs, y_ld}, mean, rstd,
+                       sm_count(), st));
   return EOGP_OK;
 }
 
@@ -1593,7 +1593,7 @@ extern "C" int eogp_norm_grad_workspace_size(int B, int T, int d, int per_exampl
   if (!bytes) return set_error(EOGP_EINVAL, "bytes is NULL");
   if (int rc = check_rows(B, T)) return rc;
   if (d < 1) return set_error(EOGP_EINVAL, "d must be >= 1");
-  *bytes = norm_grad_ws_bytes(B, T, d, per_example != 0, sm_count());
+  *bytes = norm_grad_ws_bytes(B, T, d, sm_count());
   return EOGP_OK;
 }
 
@@ -1623,12 +1623,14 @@ extern "C" int eogp_norm_grad(int kind, const void* dy, long long dy_bs, long lo
     return set_error(EOGP_EWORKSPACE, "workspace of %zu bytes needed", need);
   if (sums && need && (reinterpret_cast<uintptr_t>(ws) & 255))
     return set_error(EOGP_EINVAL, "workspace must be 256-byte aligned");
+  unsigned* status = status_word();
+  if (!status) return set_error(EOGP_ECUDA, "device status word unavailable");
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   ProfScope ps(EOGP_K_NORM, st);
   const NormGrad g{kind == EOGP_NORM_RMS, dtype == EOGP_BF16, param_dtype == EOGP_BF16, per_example != 0,
                    accumulate != 0, RowSet{B, T, lengths}, d, RowView{dy, dy_bs, dy_ld}, RowView{x, x_bs, x_ld},
                    RowView{dx, dx_bs, dx_ld}, mean, rstd, weight, dweight, dbias, ld_dparam};
-  CUDA_TRY(launch_norm_grad(g, ws, sm_count(), st));
+  CUDA_TRY(launch_norm_grad(g, ws, status, sm_count(), st));
   return EOGP_OK;
 }
 

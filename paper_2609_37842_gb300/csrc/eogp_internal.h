@@ -259,8 +259,8 @@ struct NormGrad {
   float *dweight, *dbias;  // either NULL: not wanted
   long long ld_dparam;
 };
-size_t norm_grad_ws_bytes(int B, int T, int d, bool per_example, int num_sms);
-cudaError_t launch_norm_grad(const NormGrad& g, void* ws, int num_sms, cudaStream_t st);
+size_t norm_grad_ws_bytes(int B, int T, int d, int num_sms);
+cudaError_t launch_norm_grad(const NormGrad& g, void* ws, unsigned* status, int num_sms, cudaStream_t st);
 
 // k_loss.cu
 struct LossArgs {

@@ -6,6 +6,13 @@
 //   dw = sum over tokens of dy xh,  db = sum over tokens of dy.
 // Statistics and sums are fp32; the variance is the mean of squared differences
 // from the mean, not a difference of moments. HBM-bound: a few flop per byte.
+//
+// A row is worked on by a team: a warp, a quarter of one, or a whole block, each
+// thread holding vectors of the row in registers, so x (and dy) are read once.
+// Rows that 16-byte accesses do not fit are loaded two or one elements at a time;
+// rows too wide for registers take several passes.
+#include <algorithm>
+
 #include "rows_dev.cuh"
 
 using namespace eogp;
@@ -14,7 +21,424 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+constexpr int kWarpTeams = 4;     // warp teams of a block
+constexpr int kMaxWarps = 16;     // of a block team
 
+// Threads of a team: 32, or the block (TEAM = 0).
+template <int TEAM>
+__device__ __forceinline__ int team_lane() {
+  return TEAM ? threadIdx.x & (TEAM - 1) : threadIdx.x;
+}
+template <int TEAM>
+__device__ __forceinline__ int team_threads() {
+  return TEAM ? TEAM : blockDim.x;
+}
+template <int TEAM>
+__device__ __forceinline__ void team_sync() {
+  if constexpr (TEAM)
+    __syncwarp();
+  else
+    __syncthreads();
+}
+
+// Sum over the team, the same in every thread and in a fixed order. Block teams
+// synchronise once, so `part` must not be the one of the call before.
+template <int TEAM, int K>
+__device__ __forceinline__ void team_sum(float (&v)[K], float (*part)[kMaxWarps]) {
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+#pragma unroll
+    for (int o = (TEAM ? TEAM : 32) / 2; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+  }
+  if constexpr (TEAM == 0) {
+    const int nw = blockDim.x >> 5;
+    if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) part[k][threadIdx.x >> 5] = v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float s = 0.f;
+      for (int w = 0; w < nw; ++w) s += part[k][w];
+      v[k] = s;
+    }
+  }
+}
+
+// A team's ring of row stages in shared memory: `arrays` rows of row_bytes per
+// stage, one mbarrier each. Thread 0 of the team fills; every thread waits for
+// every stage in turn, and a team barrier separates the reads of a stage from its
+// next filling, so no thread is ever a whole phase away from a barrier it waits on.
+struct Ring {
+  uint8_t* data;
+  uint64_t* full;
+  int stages, stage_bytes, slot, phase;
+  bool dead;  // a wait ran out: the status word is set, results no longer matter
+};
+
+__device__ __forceinline__ void ring_wait(Ring& q, unsigned* status) {
+  if (q.dead || mbar_wait(&q.full[q.slot], q.phase, status)) return;
+  q.dead = true;
+  // No more is filled; what is on its way arrives (again waited for with a limit)
+  // before the block gives up its memory.
+  for (int k = 1; k < q.stages; ++k) {
+    const int s = q.slot + k;
+    mbar_wait(&q.full[s % q.stages], q.phase ^ (s >= q.stages), status, EOGP_WAIT_CYCLES / 16);
+  }
+}
+__device__ __forceinline__ void ring_next(Ring& q) {
+  if (++q.slot == q.stages) {
+    q.slot = 0;
+    q.phase ^= 1;
+  }
+}
+
+// -------------------------------------------------------------------- forward
+struct NormArgs {
+  RowSet rs;
+  int M;
+  RowView x;
+  const void *w, *bias;
+  bool pbf;
+  float eps;
+  int d;
+  RowView y;
+  float *mean, *rstd;
+};
+
+// A team holds a row as raw words in registers: all its loads are in flight at
+// once, the passes for the mean, the variance and the result read registers, and
+// other teams' loads cover the sums. Weights come from L1. At most 64 registers a
+// thread, so that 1,024 threads share a multiprocessor: with 16 vectors a thread
+// (164 registers) a warp waits for its sums with too few others to cover it (4096
+// channels, bf16: 201 us against 185 us for 8 vectors a thread and two warps).
+// Measured, 0.5 GB in and out: 145 us (1.0 of the copy rate) in fp32, 159 us (0.93)
+// for 2048 bf16 channels, 171 us (0.86) for 4096.
+template <typename T, int N, int NV, int TEAM, bool RMS>
+__global__ void __launch_bounds__(TEAM ? 128 : 512, TEAM ? 8 : 2) k_norm(const NormArgs a) {
+  __shared__ float part[2][1][kMaxWarps];
+  constexpr int teams = TEAM ? 128 / (TEAM ? TEAM : 1) : 1;
+  const int lane = team_lane<TEAM>(), tt = team_threads<TEAM>();
+  const int r0 = blockIdx.x * teams + (TEAM ? threadIdx.x / (TEAM ? TEAM : 1) : 0);
+  const bool on = r0 < a.M;  // teams smaller than a warp stay for its shuffles
+  if (TEAM != 8 && !on) return;
+  const int r = on ? r0 : 0;
+  int b, t;
+  locate(a.rs, r, b, t);
+  const bool kept = on && row_kept(a.rs, b, t);
+  if (TEAM != 8 && !kept) {
+    T* yr = row_out<T>(a.y, b, t);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (j * tt + lane) * N;
+      if (c < a.d) st_vals<T, N>(yr + c, fill<N>(0.f));
+    }
+    if (lane == 0) {
+      if (a.mean) a.mean[r] = 0.f;
+      if (a.rstd) a.rstd[r] = 0.f;
+    }
+    return;
+  }
+  Raw<T, N> raw[NV];
+  const T* xr = row_of<T>(a.x, b, t);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (j * tt + lane) * N;
+    raw[j] = Raw<T, N>{};
+    if (c < a.d && kept) raw[j] = ld_raw<T, N>(xr + c);
+  }
+  const float inv_d = 1.0f / a.d;
+  float mu = 0.f;
+  if (!RMS) {
+    float2 s = pair(0.f);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const Vals<N> v = unpack<T, N>(raw[j]);
+#pragma unroll
+      for (int i = 0; i < Vals<N>::P; ++i) s = add2(s, v.p[i]);
+    }
+    float m[1] = {s.x + s.y};
+    team_sum<TEAM>(m, part[0]);
+    mu = m[0] * inv_d;
+  }
+  float2 q = pair(0.f);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    if ((j * tt + lane) * N < a.d) {
+      const Vals<N> v = unpack<T, N>(raw[j]);
+#pragma unroll
+      for (int i = 0; i < Vals<N>::P; ++i) {
+        float2 e = add2(v.p[i], pair(-mu));
+        if (N == 1) e.y = 0.f;
+        q = fma2(e, e, q);
+      }
+    }
+  }
+  float var[1] = {q.x + q.y};
+  team_sum<TEAM>(var, part[1]);
+  const float rs_ = kept ? 1.0f / sqrtf(fmaf(var[0], inv_d, a.eps)) : 0.f;
+  if (!on) return;
+  T* yr = row_out<T>(a.y, b, t);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (j * tt + lane) * N;
+    if (c < a.d) {
+      const Vals<N> v = unpack<T, N>(raw[j]), w = ld_param<N>(a.w, a.pbf, c, 1.f),
+                    bi = ld_param<N>(a.bias, a.pbf, c, 0.f);
+      Vals<N> o = fill<N>(0.f);
+      if (kept) {
+#pragma unroll
+        for (int i = 0; i < Vals<N>::P; ++i) {
+          float2 e = v.p[i];
+          if (!RMS) e = add2(e, pair(-mu));
+          o.p[i] = fma2(mul2(e, pair(rs_)), w.p[i], bi.p[i]);
+        }
+      }
+      st_vals<T, N>(yr + c, o);
+    }
+  }
+  if (lane == 0) {
+    if (a.mean) a.mean[r] = mu;
+    if (a.rstd) a.rstd[r] = rs_;
+  }
+}
+
+// ------------------------------------------------------------------- gradient
+// Rows are numbered over groups (an example each, or the whole batch) of `rpg`
+// rows, and split evenly over the blocks, `per` consecutive rows each: a block's
+// rows cover whole groups and at most two pieces of groups that other blocks
+// share. Sums of a whole group are final; those of a piece go to the block's
+// slot 0 (the group began in an earlier block) or 1, [2][d] floats each, and
+// k_norm_grad_join adds a group's pieces in order.
+struct GradArgs {
+  NormGrad g;
+  int M, rpg, per;
+  float* slots;
+  int stages;
+  unsigned* status;
+};
+
+__device__ __forceinline__ void put_sums(const NormGrad& g, int e, int c, float sw, float sb) {
+  const size_t at = static_cast<size_t>(e) * g.ld_dparam + c;
+  if (g.dweight) g.dweight[at] = g.accumulate ? g.dweight[at] + sw : sw;
+  if (g.dbias) g.dbias[at] = g.accumulate ? g.dbias[at] + sb : sb;
+}
+
+template <typename T, int N, int NV, int TEAM, bool RMS, bool RING>
+__global__ void __launch_bounds__(TEAM ? 32 * kWarpTeams : 512, TEAM ? 3 : 1) k_norm_grad(const GradArgs a) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ uint64_t bars[RING ? kWarpTeams * 8 : 1];
+  __shared__ float part[2][2][kMaxWarps];
+  const NormGrad& g = a.g;
+  const int lane = team_lane<TEAM>(), tt = team_threads<TEAM>();
+  const int team = TEAM ? threadIdx.x / 32 : 0;
+  constexpr int teams = TEAM ? kWarpTeams : 1;
+  const int d = g.d;
+  const uint32_t row_bytes = static_cast<uint32_t>(d) * sizeof(T);
+  const long long first = static_cast<long long>(blockIdx.x) * a.per;
+  const int hi = static_cast<int>(min(static_cast<long long>(a.M), first + a.per)), lo = static_cast<int>(first);
+  // Warp teams add their sums up here, a team after the other.
+  float2* join = reinterpret_cast<float2*>(smem);
+  uint8_t* ring0 = smem + (TEAM ? (static_cast<size_t>(d) * 8 + 127) / 128 * 128 : 0);
+  Ring q;
+  if constexpr (RING) {
+    q = Ring{ring0 + static_cast<size_t>(team) * a.stages * 2 * row_bytes, bars + team * 8, a.stages,
+             static_cast<int>(2 * row_bytes), 0, 0, false};
+    if (lane == 0) {
+      for (int s = 0; s < a.stages; ++s) mbar_init(&q.full[s], 1);
+      fence_barrier_init();
+    }
+    team_sync<TEAM>();
+  }
+  auto issue = [&](int row, int s) {
+    int b, t;
+    locate(g.rs, row, b, t);
+    if (row_kept(g.rs, b, t)) {
+      mbar_arrive_expect_tx(&q.full[s], 2 * row_bytes);
+      uint8_t* to = q.data + static_cast<size_t>(s) * q.stage_bytes;
+      bulk_load(to, row_of<T>(g.x, b, t), row_bytes, &q.full[s]);
+      bulk_load(to + row_bytes, row_of<T>(g.dy, b, t), row_bytes, &q.full[s]);
+    } else {
+      mbar_arrive(&q.full[s]);
+    }
+  };
+  if (RING && lane == 0)
+    for (int s = 0; s < a.stages && lo + team + s * teams < hi; ++s) issue(lo + team + s * teams, s);
+  Vals<N> w[NV], dw[NV], db[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (j * tt + lane) * N;
+    w[j] = c < d ? ld_param<N>(g.weight, g.param_bf16, c, 1.f) : fill<N>(0.f);
+  }
+  const float inv_d = 1.0f / d;
+  const bool sums = g.dweight || g.dbias;
+  int r = lo + team, parity = 0;
+  float mu_next = 0.f, rs_next = 0.f;
+  auto stats = [&](int row) {
+    if (row < hi) {
+      mu_next = RMS ? 0.f : __ldg(g.mean + row);
+      rs_next = __ldg(g.rstd + row);
+    }
+  };
+  stats(r);
+  for (int p0 = lo; p0 < hi;) {
+    const int e = p0 / a.rpg;
+    const int p1 = static_cast<int>(min(static_cast<long long>(hi), (e + 1LL) * a.rpg));  // end of the piece
+#pragma unroll
+    for (int j = 0; j < NV; ++j) dw[j] = db[j] = fill<N>(0.f);
+    for (; r < p1; r += teams, parity ^= 1) {
+      int b, t;
+      locate(g.rs, r, b, t);
+      const bool kept = row_kept(g.rs, b, t);
+      const float mu = mu_next, rs_ = rs_next;
+      stats(r + teams);
+      Vals<N> xh[NV], gy[NV];
+      float sum[2] = {0.f, 0.f};
+      if constexpr (RING) ring_wait(q, a.status);
+      if (kept) {
+        float2 s1 = pair(0.f), s2 = pair(0.f);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          const int c = (j * tt + lane) * N;
+          Raw<T, N> rx{}, ry{};
+          if (c < d) {
+            if constexpr (RING) {
+              const uint8_t* at = q.data + static_cast<size_t>(q.slot) * q.stage_bytes + c * sizeof(T);
+              rx.w = *reinterpret_cast<const uint4*>(at);
+              ry.w = *reinterpret_cast<const uint4*>(at + row_bytes);
+            } else {
+              rx = ld_raw<T, N>(row_of<T>(g.x, b, t) + c);
+              ry = ld_raw<T, N>(row_of<T>(g.dy, b, t) + c);
+            }
+          }
+          xh[j] = unpack<T, N>(rx);
+          gy[j] = unpack<T, N>(ry);
+#pragma unroll
+          for (int i = 0; i < Vals<N>::P; ++i) {
+            const float2 dy = gy[j].p[i];
+            float2 h = xh[j].p[i];
+            if (!RMS) h = add2(h, pair(-mu));
+            h = mul2(h, pair(rs_));
+            dw[j].p[i] = fma2(dy, h, dw[j].p[i]);
+            db[j].p[i] = add2(db[j].p[i], dy);
+            const float2 gv = mul2(dy, w[j].p[i]);
+            if (!RMS) s1 = add2(s1, gv);
+            s2 = fma2(gv, h, s2);
+            xh[j].p[i] = h;
+            gy[j].p[i] = gv;
+          }
+        }
+        sum[0] = s1.x + s1.y;
+        sum[1] = s2.x + s2.y;
+      }
+      if (kept && g.dx.p)
+        team_sum<TEAM>(sum, part[parity]);
+      else
+        team_sync<TEAM>();
+      if constexpr (RING) {
+        // The sums (or the barrier) come after every thread's reads of the stage.
+        if constexpr (TEAM != 0) __syncwarp();
+        const long long ahead = r + static_cast<long long>(a.stages) * teams;
+        if (lane == 0 && ahead < hi && !q.dead) issue(static_cast<int>(ahead), q.slot);
+        ring_next(q);
+      }
+      if (g.dx.p) {
+        T* o = row_out<T>(g.dx, b, t);
+        const float2 c0 = pair(RMS ? 0.f : -rs_ * sum[0] * inv_d), c1 = pair(-rs_ * sum[1] * inv_d);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          const int c = (j * tt + lane) * N;
+          if (c < d) {
+            Vals<N> v = fill<N>(0.f);
+            if (kept) {
+#pragma unroll
+              for (int i = 0; i < Vals<N>::P; ++i) {
+                v.p[i] = RMS ? mul2(gy[j].p[i], pair(rs_)) : fma2(gy[j].p[i], pair(rs_), c0);
+                v.p[i] = fma2(xh[j].p[i], c1, v.p[i]);
+              }
+            }
+            st_vals<T, N>(o + c, v);
+          }
+        }
+      }
+    }
+    if (sums) {
+      const bool begins = static_cast<long long>(e) * a.rpg >= lo, ends = (e + 1LL) * a.rpg <= hi;
+      float* slot = a.slots + (static_cast<size_t>(blockIdx.x) * 2 + (begins ? 1 : 0)) * 2 * d;
+      auto put = [&](int c, float sw, float sb) {
+        if (begins && ends) {
+          put_sums(g, e, c, sw, sb);
+        } else {
+          slot[c] = sw;
+          slot[d + c] = sb;
+        }
+      };
+      if constexpr (TEAM == 0) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const int c = (j * tt + lane) * N + i;
+            if (c < d) put(c, i & 1 ? dw[j].p[i / 2].y : dw[j].p[i / 2].x, i & 1 ? db[j].p[i / 2].y : db[j].p[i / 2].x);
+          }
+      } else {
+        for (int k = 0; k < teams; ++k) {
+          if (team == k) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+              for (int i = 0; i < N; ++i) {
+                const int c = (j * tt + lane) * N + i;
+                if (c < d) {
+                  float2 v = make_float2(i & 1 ? dw[j].p[i / 2].y : dw[j].p[i / 2].x,
+                                         i & 1 ? db[j].p[i / 2].y : db[j].p[i / 2].x);
+                  if (k > 0) v = add2(join[c], v);
+                  join[c] = v;
+                }
+              }
+          }
+          __syncthreads();
+        }
+        for (int c = threadIdx.x; c < d; c += blockDim.x) put(c, join[c].x, join[c].y);
+        __syncthreads();
+      }
+    }
+    p0 = p1;
+  }
+}
+
+// Adds the pieces of the groups that several blocks share, in block order: each
+// of 16 slices of a block sums a contiguous run of pieces for 32 channels, the
+// slices are added in order. Groups of no rows (no block) get 0.
+constexpr int kJoinSlices = 16;
+
+__global__ void __launch_bounds__(32 * kJoinSlices) k_norm_grad_join(const GradArgs a, int groups) {
+  __shared__ float2 acc[kJoinSlices][32];
+  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, d = a.g.d, c = blockIdx.x * 32 + lane;
+  for (int e = blockIdx.y; e < groups; e += gridDim.y) {
+    const long long r0 = static_cast<long long>(e) * a.rpg, r1 = r0 + a.rpg;
+    const int b0 = a.rpg ? static_cast<int>(r0 / a.per) : 0, b1 = a.rpg ? static_cast<int>((r1 - 1) / a.per) + 1 : 0;
+    if (b1 - b0 == 1) continue;  // one block had it whole
+    const int each = (b1 - b0 + kJoinSlices - 1) / kJoinSlices;
+    float2 s = make_float2(0.f, 0.f);
+    if (c < d)
+#pragma unroll 4
+      for (int k = b0 + slice * each; k < min(b1, b0 + (slice + 1) * each); ++k) {
+        const float* slot = a.slots + (static_cast<size_t>(k) * 2 + (r0 >= static_cast<long long>(k) * a.per)) * 2 * d;
+        s = add2(s, make_float2(slot[c], slot[d + c]));
+      }
+    acc[slice][lane] = s;
+    __syncthreads();
+    if (slice == 0 && c < d) {
+      for (int k = 1; k < kJoinSlices; ++k) s = add2(s, acc[k][lane]);
+      put_sums(a.g, e, c, s.x, s.y);
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------- rows too wide for registers
 // One block per row, three passes over the row (the later ones from cache).
 template <typename T, bool RMS>
 __global__ void __launch_bounds__(kThreads) k_norm_rows(RowSet rs, RowView x, const void* w, const void* bias,
@@ -82,53 +506,207 @@ __global__ void __launch_bounds__(kThreads) k_norm_dx_rows(NormGrad g) {
   }
 }
 
-// dw, db: one thread per channel sums a run of rows; partial sums of run p of
-// group e go to part[(e * n_parts + p) * 2 + {0, 1}][d].
+// dw, db: one thread per channel sums the rows of a block's run, with the pieces
+// and slots of k_norm_grad.
 template <typename T, bool RMS>
-__global__ void __launch_bounds__(kThreads) k_norm_dparam_rows(NormGrad g, int rows_per_group, int rows_per_part,
-                                                               int n_parts, float* part) {
-  const int c = blockIdx.x * kThreads + threadIdx.x, p = blockIdx.y;
+__global__ void __launch_bounds__(kThreads) k_norm_dparam_rows(const GradArgs a) {
+  const NormGrad& g = a.g;
+  const int c = blockIdx.y * kThreads + threadIdx.x;
   if (c >= g.d) return;
-  const int groups = g.per_example ? g.rs.B : 1;
-  for (int e = blockIdx.z; e < groups; e += gridDim.z) {
-    const int end = min(rows_per_group, (p + 1) * rows_per_part);
+  const long long first = static_cast<long long>(blockIdx.x) * a.per;
+  const int hi = static_cast<int>(min(static_cast<long long>(a.M), first + a.per)), lo = static_cast<int>(first);
+  for (int p0 = lo; p0 < hi;) {
+    const int e = p0 / a.rpg;
+    const int p1 = static_cast<int>(min(static_cast<long long>(hi), (e + 1LL) * a.rpg));
     float sw = 0.f, sb = 0.f;
-    for (int i = p * rows_per_part; i < end; ++i) {
-      const int r = e * rows_per_group + i, b = r / g.rs.T, t = r - b * g.rs.T;
+    for (int r = p0; r < p1; ++r) {
+      int b, t;
+      locate(g.rs, r, b, t);
       if (!row_kept(g.rs, b, t)) continue;
       const float dy = to_f32(row_of<T>(g.dy, b, t)[c]);
       const float xh = (to_f32(row_of<T>(g.x, b, t)[c]) - (RMS ? 0.f : g.mean[r])) * g.rstd[r];
       sw = fmaf(dy, xh, sw);
       sb += dy;
     }
-    float* o = part + (static_cast<size_t>(e) * n_parts + p) * 2 * g.d;
-    o[c] = sw;
-    o[g.d + c] = sb;
-  }
-}
-
-// Adds a group's n_parts partial sums in order.
-__global__ void __launch_bounds__(kThreads) k_norm_dparam_join(NormGrad g, int n_parts, const float* part) {
-  const int c = blockIdx.x * kThreads + threadIdx.x;
-  if (c >= g.d) return;
-  const int groups = g.per_example ? g.rs.B : 1;
-  for (int e = blockIdx.y; e < groups; e += gridDim.y) {
-    float sw = 0.f, sb = 0.f;
-    const float* o = part + static_cast<size_t>(e) * n_parts * 2 * g.d;
-    for (int p = 0; p < n_parts; ++p, o += 2 * g.d) {
-      sw += o[c];
-      sb += o[g.d + c];
+    const bool begins = static_cast<long long>(e) * a.rpg >= lo, ends = (e + 1LL) * a.rpg <= hi;
+    if (begins && ends) {
+      put_sums(g, e, c, sw, sb);
+    } else {
+      float* slot = a.slots + (static_cast<size_t>(blockIdx.x) * 2 + (begins ? 1 : 0)) * 2 * g.d;
+      slot[c] = sw;
+      slot[g.d + c] = sb;
     }
-    const size_t at = static_cast<size_t>(e) * g.ld_dparam + c;
-    if (g.dweight) g.dweight[at] = g.accumulate ? g.dweight[at] + sw : sw;
-    if (g.dbias) g.dbias[at] = g.accumulate ? g.dbias[at] + sb : sb;
+    p0 = p1;
   }
 }
 
-// Runs of rows whose weight-gradient sums are formed apart.
-int grad_parts(int rows_per_group, int groups, int num_sms) {
-  const int want = std::max(1, 4 * num_sms / std::max(1, groups));
-  return std::max(1, std::min(want, (rows_per_group + 63) / 64));
+// ------------------------------------------------------------------ launching
+// How a row of d elements is worked on: NV vectors of n elements a thread by a warp
+// (team 32) or a block of `threads`; n = 0: too wide.
+struct Shape {
+  int n, nv, team, threads;
+};
+
+// `vec`: elements per access the arrays allow; es: element bytes; cap: most
+// elements a thread of a warp team may hold. Measured on 402 MB of 768-wide bf16
+// rows (gradient): see the kernels' notes.
+Shape team_shape(int d, int vec, int es, int warp_cap) {
+  const int full = 16 / es;
+  if (vec == full) {
+    const int nv = (d + vec - 1) / vec;
+    if (nv <= 32 * (warp_cap / vec)) return Shape{vec, (nv + 31) / 32, 32, 32 * kWarpTeams};
+    const int per = 16 / vec;  // 16 elements a thread
+    const int th = ((nv + per - 1) / per + 31) / 32 * 32;
+    if (th <= 512) return Shape{vec, per, 0, th};
+    return Shape{0, 0, 0, 0};
+  }
+  const int n = vec >= 2 ? 2 : 1, per = 16 / n, nv = (d + n - 1) / n;
+  const int th = ((nv + per - 1) / per + 31) / 32 * 32;
+  if (th <= 512) return Shape{n, per, 0, th};
+  return Shape{0, 0, 0, 0};
+}
+
+// Shared memory that the blocks of a multiprocessor share: 228 KB less 1 KB and the
+// static arrays of each.
+constexpr size_t kSmemPerSm = 220 * 1024;
+
+// Blocks of `threads` that a multiprocessor's registers and threads hold, at most
+// `most`: persistent blocks beyond the resident ones would run as a second wave.
+template <typename F>
+int resident(F k, int threads, int most) {
+  cudaFuncAttributes at;
+  if (cudaFuncGetAttributes(&at, k) != cudaSuccess || at.numRegs < 1) return 1;
+  const int per_block = (at.numRegs + 7) / 8 * 8 * ((threads + 127) / 128 * 128);
+  return std::max(1, std::min({most, 65536 / per_block, 2048 / threads}));
+}
+
+template <typename F>
+cudaError_t allow_smem(F k, size_t bytes) {
+  if (bytes <= 40 * 1024) return cudaSuccess;  // with the static part, below the 48 KB that need no asking
+  return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+}
+
+// Examples as one run of rows where no lengths and no strides tell them apart.
+template <typename... V>
+RowSet flatten(const RowSet& rs, const V&... v) {
+  if (!rs.lengths && (flat(v, rs) && ...)) return RowSet{1, static_cast<int>(rs.rows()), nullptr};
+  return rs;
+}
+
+// Most elements of a row that a thread of a warp team holds.
+template <typename T>
+constexpr int kWarpCap = sizeof(T) == 2 ? 32 : 24;
+
+int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
+
+template <typename T, int N, int NV, int TEAM>
+cudaError_t norm_team(bool rms, const NormArgs& a, int threads, cudaStream_t st) {
+  auto k = rms ? k_norm<T, N, NV, TEAM, true> : k_norm<T, N, NV, TEAM, false>;
+  k<<<ceil_div(a.M, TEAM ? 128 / (TEAM ? TEAM : 1) : 1), threads, 0, st>>>(a);
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t norm_launch(bool rms, const NormArgs& a, int num_sms, cudaStream_t st) {
+  constexpr int F = 16 / sizeof(T);
+  const int es = sizeof(T);
+  int vec = std::min(row_vec(a.x, a.rs, a.d, es), row_vec(a.y, a.rs, a.d, es));
+  const RowSet one{1, 1, nullptr};
+  const int pes = a.pbf ? 2 : 4;
+  const int pvec = std::min(row_vec(a.w, 0, 0, one, 8, pes), row_vec(a.bias, 0, 0, one, 8, pes));
+  if (vec > 1 && pvec < 2) vec = 1;
+  if (vec == F && pvec < 16 / pes) vec = 2;
+  const int nv = ceil_div(a.d, vec);
+  if (vec == F) {
+    // Few rows: their latency counts, so a row gets a block of two vectors a thread
+    // (one row of 4096 bf16: 2.3 us against 5.6 us for 16 vectors a thread).
+    if (nv > 64 && nv <= 1024 && a.M <= 4 * num_sms) return norm_team<T, F, 2, 0>(rms, a, ceil_div(nv, 64) * 32, st);
+    if (nv <= 8) return norm_team<T, F, 1, 8>(rms, a, 128, st);
+    if (nv <= 16) return norm_team<T, F, 2, 8>(rms, a, 128, st);
+    if (nv <= 32) return norm_team<T, F, 4, 8>(rms, a, 128, st);
+    if (nv <= 64) return norm_team<T, F, 2, 32>(rms, a, 128, st);
+    if (nv <= 96) return norm_team<T, F, 3, 32>(rms, a, 128, st);
+    if (nv <= 128) return norm_team<T, F, 4, 32>(rms, a, 128, st);
+    if (nv <= 192) return norm_team<T, F, 6, 32>(rms, a, 128, st);
+    if (nv <= 256) return norm_team<T, F, 8, 32>(rms, a, 128, st);
+    // A block team of as few warps as hold the row at 8 vectors a thread.
+    const int warps = ceil_div(nv, 8 * 32), th = warps * 32;
+    if (warps <= kMaxWarps) {
+      const int per = ceil_div(nv, th);
+      if (per <= 5) return norm_team<T, F, 5, 0>(rms, a, th, st);
+      if (per == 6) return norm_team<T, F, 6, 0>(rms, a, th, st);
+      if (per == 7) return norm_team<T, F, 7, 0>(rms, a, th, st);
+      return norm_team<T, F, 8, 0>(rms, a, th, st);
+    }
+  } else if (vec == 2) {
+    if (nv <= 256) return norm_team<T, 2, 8, 32>(rms, a, 128, st);
+    if (nv <= 512) return norm_team<T, 2, 16, 32>(rms, a, 128, st);
+    const int th = ceil_div(nv, 16 * 32) * 32;
+    if (th <= 512) return norm_team<T, 2, 16, 0>(rms, a, th, st);
+  } else {
+    if (nv <= 256) return norm_team<T, 1, 8, 32>(rms, a, 128, st);
+    const int th = ceil_div(nv, 16 * 32) * 32;
+    if (th <= 512) return norm_team<T, 1, 16, 0>(rms, a, th, st);
+  }
+  auto k = rms ? k_norm_rows<T, true> : k_norm_rows<T, false>;
+  k<<<a.M, kThreads, 0, st>>>(a.rs, a.x, a.w, a.bias, a.pbf, a.eps, a.d, a.y, a.mean, a.rstd);
+  return cudaGetLastError();
+}
+
+// Rows of a block of the gradient: blocks for `occ` a multiprocessor, and at least
+// 8 rows each so that joining their sums stays small beside forming them.
+int grad_rows(long long M, int num_sms, int occ) {
+  return std::max(8, ceil_div(M, static_cast<long long>(num_sms) * occ));
+}
+constexpr int kGradOcc = 8;  // most blocks a multiprocessor is given
+
+template <typename T, int N, int NV, int TEAM, bool RING>
+cudaError_t grad_team(GradArgs& a, int threads, int num_sms, cudaStream_t st) {
+  auto k = a.g.rms ? k_norm_grad<T, N, NV, TEAM, true, RING> : k_norm_grad<T, N, NV, TEAM, false, RING>;
+  const int teams = TEAM ? kWarpTeams : 1;
+  const int occ = resident(k, threads, kGradOcc);
+  const size_t stage = static_cast<size_t>(teams) * 2 * a.g.d * sizeof(T);
+  const size_t extra = TEAM ? (static_cast<size_t>(a.g.d) * 8 + 127) / 128 * 128 : 0;
+  a.stages = RING ? std::max(2, std::min<int>(8, static_cast<int>((kSmemPerSm / occ - extra) / stage))) : 0;
+  const size_t smem = extra + a.stages * stage;
+  if (cudaError_t e = allow_smem(k, smem); e != cudaSuccess) return e;
+  a.per = grad_rows(a.M, num_sms, occ);
+  k<<<ceil_div(a.M, a.per), threads, smem, st>>>(a);
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t grad_launch(GradArgs& a, int num_sms, cudaStream_t st) {
+  constexpr int F = 16 / sizeof(T);
+  const NormGrad& g = a.g;
+  const int es = sizeof(T), pes = g.param_bf16 ? 2 : 4;
+  int vec = std::min(row_vec(g.x, g.rs, g.d, es), row_vec(g.dy, g.rs, g.d, es));
+  if (g.dx.p) vec = std::min(vec, row_vec(g.dx, g.rs, g.d, es));
+  const int pvec = row_vec(g.weight, 0, 0, RowSet{1, 1, nullptr}, 8, pes);
+  if (vec > 1 && pvec < 2) vec = 1;
+  if (vec == F && pvec < 16 / pes) vec = 2;
+  const Shape s = team_shape(g.d, vec, es, kWarpCap<T>);
+  if (s.n == F && s.team == 32) {
+    if (s.nv == 1) return grad_team<T, F, 1, 32, true>(a, s.threads, num_sms, st);
+    if (s.nv == 2) return grad_team<T, F, 2, 32, true>(a, s.threads, num_sms, st);
+    if (s.nv == 3) return grad_team<T, F, 3, 32, true>(a, s.threads, num_sms, st);
+    if (s.nv == 4) return grad_team<T, F, 4, 32, true>(a, s.threads, num_sms, st);
+    if constexpr (sizeof(T) == 4) return grad_team<T, F, 6, 32, true>(a, s.threads, num_sms, st);
+  }
+  if (s.n == F) return grad_team<T, F, 16 / F, 0, true>(a, s.threads, num_sms, st);
+  if (s.n == 2) return grad_team<T, 2, 8, 0, false>(a, s.threads, num_sms, st);
+  if (s.n == 1) return grad_team<T, 1, 16, 0, false>(a, s.threads, num_sms, st);
+  // The sums read dy and x before dx may be written over them.
+  a.per = grad_rows(a.M, num_sms, kGradOcc);
+  if (g.dweight || g.dbias) {
+    auto k = g.rms ? k_norm_dparam_rows<T, true> : k_norm_dparam_rows<T, false>;
+    k<<<dim3(ceil_div(a.M, a.per), ceil_div(g.d, kThreads)), kThreads, 0, st>>>(a);
+  }
+  if (g.dx.p) {
+    auto k = g.rms ? k_norm_dx_rows<T, true> : k_norm_dx_rows<T, false>;
+    k<<<a.M, kThreads, 0, st>>>(g);
+  }
+  return cudaGetLastError();
 }
 
 }  // namespace
@@ -136,37 +714,27 @@ int grad_parts(int rows_per_group, int groups, int num_sms) {
 cudaError_t launch_norm(bool rms, RowSet rs, RowView x, bool bf16_, const void* weight, const void* bias,
                         bool param_bf16, float eps, int d, RowView y, float* mean, float* rstd, int num_sms,
                         cudaStream_t st) {
-  const int M = static_cast<int>(rs.rows());
-  auto k = bf16_ ? (rms ? k_norm_rows<bf16, true> : k_norm_rows<bf16, false>)
-                 : (rms ? k_norm_rows<float, true> : k_norm_rows<float, false>);
-  k<<<M, kThreads, 0, st>>>(rs, x, weight, bias, param_bf16, eps, d, y, mean, rstd);
-  return cudaGetLastError();
+  const NormArgs a{flatten(rs, x, y), static_cast<int>(rs.rows()), x, weight, bias, param_bf16, eps, d, y, mean, rstd};
+  return bf16_ ? norm_launch<bf16>(rms, a, num_sms, st) : norm_launch<float>(rms, a, num_sms, st);
 }
 
-size_t norm_grad_ws_bytes(int B, int T, int d, bool per_example, int num_sms) {
-  const int groups = per_example ? B : 1, rows = per_example ? T : B * T;
-  return static_cast<size_t>(groups) * grad_parts(rows, groups, num_sms) * 2 * d * 4;
+size_t norm_grad_ws_bytes(int B, int T, int d, int num_sms) {
+  const long long M = static_cast<long long>(B) * T;
+  if (M == 0) return 0;
+  return static_cast<size_t>(ceil_div(M, grad_rows(M, num_sms, kGradOcc))) * 4 * d * 4;
 }
 
-cudaError_t launch_norm_grad(const NormGrad& g, void* ws, int num_sms, cudaStream_t st) {
-  const int M = static_cast<int>(g.rs.rows());
-  if (g.dweight || g.dbias) {
-    const int groups = g.per_example ? g.rs.B : 1, rows = g.per_example ? g.rs.T : M;
-    if (groups > 0) {
-      const int parts = grad_parts(rows, groups, num_sms);
-      const int cols = (g.d + kThreads - 1) / kThreads;
-      auto k = g.bf16 ? (g.rms ? k_norm_dparam_rows<bf16, true> : k_norm_dparam_rows<bf16, false>)
-                      : (g.rms ? k_norm_dparam_rows<float, true> : k_norm_dparam_rows<float, false>);
-      k<<<dim3(cols, parts, std::min(groups, 65535)), kThreads, 0, st>>>(g, rows, (rows + parts - 1) / parts, parts,
-                                                                        static_cast<float*>(ws));
-      k_norm_dparam_join<<<dim3(cols, std::min(groups, 65535)), kThreads, 0, st>>>(g, parts,
-                                                                                  static_cast<const float*>(ws));
-    }
+cudaError_t launch_norm_grad(const NormGrad& g, void* ws, unsigned* status, int num_sms, cudaStream_t st) {
+  const int M = static_cast<int>(g.rs.rows()), groups = g.per_example ? g.rs.B : 1;
+  const bool sums = (g.dweight || g.dbias) && groups > 0;
+  if (!sums && (!g.dx.p || M == 0)) return cudaSuccess;
+  GradArgs a{g, M, g.per_example ? g.rs.T : M, 1, static_cast<float*>(ws), 0, status};
+  a.g.rs = g.dx.p ? flatten(g.rs, g.x, g.dy, g.dx) : flatten(g.rs, g.x, g.dy);
+  if (M > 0) {
+    const cudaError_t e = g.bf16 ? grad_launch<bf16>(a, num_sms, st) : grad_launch<float>(a, num_sms, st);
+    if (e != cudaSuccess) return e;
+    if (!sums || a.per % a.rpg == 0 || M <= a.per) return cudaSuccess;  // no group is shared by blocks
   }
-  if (g.dx.p && M > 0) {
-    auto k = g.bf16 ? (g.rms ? k_norm_dx_rows<bf16, true> : k_norm_dx_rows<bf16, false>)
-                    : (g.rms ? k_norm_dx_rows<float, true> : k_norm_dx_rows<float, false>);
-    k<<<M, kThreads, 0, st>>>(g);
-  }
+  k_norm_grad_join<<<dim3(ceil_div(g.d, 32), std::min(groups, 65535)), 32 * kJoinSlices, 0, st>>>(a, groups);
   return cudaGetLastError();
 }

@@ -39,6 +39,12 @@ __device__ __forceinline__ long long token_at(const TokenView& v, int b, int t) 
   return v.i64 ? static_cast<const long long*>(v.p)[b * v.bs + t] : static_cast<const int*>(v.p)[b * v.bs + t];
 }
 
+// Example and token of row r; one example needs no division.
+__device__ __forceinline__ void locate(const RowSet& rs, int r, int& b, int& t) {
+  b = rs.B == 1 ? 0 : r / rs.T;
+  t = r - b * rs.T;
+}
+
 __device__ __forceinline__ bool row_kept(const RowSet& rs, int b, int t) {
   return !rs.lengths || t < rs.lengths[b];
 }
@@ -62,4 +68,153 @@ __device__ __forceinline__ float block_sum(float v, float* part) {
   return s;
 }
 
+// N contiguous elements as raw words: 16 bytes, two elements, or one.
+template <typename T, int N>
+struct Raw {
+  uint4 w;
+  static_assert(sizeof(T) * N == 16, "a vector is 16 bytes");
+};
+template <>
+struct Raw<bf16, 2> {
+  uint32_t w;
+};
+template <>
+struct Raw<float, 2> {
+  uint2 w;
+};
+template <typename T>
+struct Raw<T, 1> {
+  T w;
+};
+
+// Streaming load (global data that is read once).
+template <typename T, int N>
+__device__ __forceinline__ Raw<T, N> ld_raw(const T* p) {
+  Raw<T, N> r;
+  if constexpr (N == 1)
+    r.w = *p;
+  else
+    r.w = __ldcs(reinterpret_cast<const decltype(r.w)*>(p));
+  return r;
+}
+
+// The N values as fp32 pairs (N = 1: the first of a pair), for the paired fp32
+// instructions.
+template <int N>
+struct Vals {
+  static constexpr int P = (N + 1) / 2;
+  float2 p[P];
+};
+
+template <typename T, int N>
+__device__ __forceinline__ Vals<N> unpack(const Raw<T, N>& r) {
+  Vals<N> v;
+  if constexpr (N == 1) {
+    v.p[0] = make_float2(to_f32(r.w), 0.f);
+  } else if constexpr (sizeof(T) == 4) {
+    v.p[0] = make_float2(__uint_as_float(r.w.x), __uint_as_float(r.w.y));
+    if constexpr (N == 4) v.p[1] = make_float2(__uint_as_float(r.w.z), __uint_as_float(r.w.w));
+  } else {
+    uint32_t u[N / 2];
+    if constexpr (N == 2) {
+      u[0] = r.w;
+    } else {
+      u[0] = r.w.x;
+      u[1] = r.w.y;
+      u[2] = r.w.z;
+      u[3] = r.w.w;
+    }
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i)
+      v.p[i] = make_float2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xffff0000u));
+  }
+  return v;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float2 v) {
+  const __nv_bfloat162 p = __floats2bfloat162_rn(v.x, v.y);
+  return *reinterpret_cast<const uint32_t*>(&p);
+}
+
+// Streaming store, rounded once to T.
+template <typename T, int N>
+__device__ __forceinline__ void st_vals(T* p, const Vals<N>& v) {
+  if constexpr (N == 1) {
+    *p = from_f32<T>(v.p[0].x);
+  } else if constexpr (sizeof(T) == 4) {
+    if constexpr (N == 4)
+      __stcs(reinterpret_cast<float4*>(p), make_float4(v.p[0].x, v.p[0].y, v.p[1].x, v.p[1].y));
+    else
+      __stcs(reinterpret_cast<float2*>(p), v.p[0]);
+  } else if constexpr (N == 2) {
+    __stcs(reinterpret_cast<unsigned*>(p), pack_bf16(v.p[0]));
+  } else {
+    __stcs(reinterpret_cast<uint4*>(p),
+           make_uint4(pack_bf16(v.p[0]), pack_bf16(v.p[1]), pack_bf16(v.p[2]), pack_bf16(v.p[3])));
+  }
+}
+
+template <int N>
+__device__ __forceinline__ Vals<N> fill(float x) {
+  Vals<N> v;
+#pragma unroll
+  for (int i = 0; i < Vals<N>::P; ++i) v.p[i] = make_float2(x, N == 1 ? 0.f : x);
+  return v;
+}
+
+// N weights or biases from channel c on, of either type; `none` where p is NULL
+// (N = 2: p and c aligned to two
+// elements; N > 2: p to 16 bytes).
+template <int N>
+__device__ __forceinline__ Vals<N> ld_param(const void* p, bool is_bf16, int c, float none) {
+  Vals<N> v;
+  if (!p) {
+    v = fill<N>(none);
+  } else if constexpr (N == 1) {
+    v.p[0] = make_float2(param_at(p, is_bf16, c, none), 0.f);
+  } else if (is_bf16) {
+    const bf16* q = static_cast<const bf16*>(p) + c;
+    if constexpr (N == 8) return unpack<bf16, 8>(Raw<bf16, 8>{__ldg(reinterpret_cast<const uint4*>(q))});
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      const uint32_t u = __ldg(reinterpret_cast<const unsigned*>(q) + i);
+      v.p[i] = make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+    }
+  } else {
+    const float* q = static_cast<const float*>(p) + c;
+    if constexpr (N >= 4) {
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) {
+        const float4 f = __ldg(reinterpret_cast<const float4*>(q) + i);
+        v.p[2 * i] = make_float2(f.x, f.y);
+        v.p[2 * i + 1] = make_float2(f.z, f.w);
+      }
+    } else {
+      v.p[0] = __ldg(reinterpret_cast<const float2*>(q));
+    }
+  }
+  return v;
+}
+
+__device__ __forceinline__ float2 pair(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) { return __fadd2_rn(a, b); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+
 }  // namespace eogp
+
+// Elements per access (16 bytes, two elements or one) that base, strides and width
+// of rows of es-byte elements allow.
+inline int row_vec(const void* p, long long bs, long long ld, const RowSet& rs, long long n, int es) {
+  for (int v = 16 / es; v > 1; v = v > 2 ? 2 : 1)
+    if (reinterpret_cast<uintptr_t>(p) % (v * es) == 0 && n % v == 0 && (rs.B == 1 || bs % v == 0) &&
+        (rs.T == 1 || ld % v == 0))
+      return v;
+  return 1;
+}
+inline int row_vec(const RowView& v, const RowSet& rs, long long n, int es) {
+  return row_vec(v.p, v.bs, v.ld, rs, n, es);
+}
+// Whether example strides continue the token strides, so that B examples of T
+// tokens are one run of rows.
+inline bool flat(const RowView& v, const RowSet& rs) { return rs.B == 1 || v.bs == v.ld * rs.T; }
