@@ -1559,7 +1559,7 @@ extern "C" int eogp_embed_grad(const void* tokens, int index_type, long long tok
   ProfScope ps(EOGP_K_EMBED, st);
   CUDA_TRY(launch_embed_grad(RowSet{B, T, lengths}, TokenView{tokens, index_type == EOGP_I64, tokens_bs},
                              RowView{dout, dout_bs, dout_ld}, dtype == EOGP_BF16, V, d, scale, dtable,
-                             grad_dtype == EOGP_BF16, ld_dtable, accumulate != 0, ws, status, sm_count(), st));
+                             grad_dtype == EOGP_BF16, ld_dtable, accumulate != 0, ws, status, st));
   return EOGP_OK;
 }
 

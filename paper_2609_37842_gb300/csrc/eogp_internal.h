@@ -243,7 +243,7 @@ cudaError_t launch_embed(RowSet rs, TokenView tok, const void* table, bool bf16,
 size_t embed_grad_ws_bytes(int V, int d, long long M);
 cudaError_t launch_embed_grad(RowSet rs, TokenView tok, RowView dout, bool bf16, int V, int d, float scale,
                               void* dtable, bool grad_bf16, long long ld_dtable, bool accumulate, void* ws,
-                              unsigned* status, int num_sms, cudaStream_t st);
+                              unsigned* status, cudaStream_t st);
 
 // k_norm.cu
 cudaError_t launch_norm(bool rms, RowSet rs, RowView x, bool bf16, const void* weight, const void* bias,

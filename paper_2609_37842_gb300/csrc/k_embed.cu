@@ -13,46 +13,79 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// One block per row.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) k_embed_rows(RowSet rs, TokenView tok, const T* __restrict__ table, int V,
-                                                         int d, long long ld_table, float scale,
-                                                         const T* __restrict__ pos, long long ld_pos, RowView out,
-                                                         unsigned* status) {
-  const int r = blockIdx.x, b = r / rs.T, t = r - b * rs.T;
-  T* o = row_out<T>(out, b, t);
-  bool kept = row_kept(rs, b, t);
-  long long v = 0;
-  if (kept) {
-    v = token_at(tok, b, t);
-    if (v < 0 || v >= V) {
-      if (threadIdx.x == 0) flag_status(status, EOGP_ST_DEVICE);
-      kept = false;
+// A team of TL threads copies NV vectors of N elements a thread of each of R rows
+// (wider rows are cut into slices of TL * NV vectors): the R token numbers are
+// waited for together, then R * NV table reads a thread are in flight.
+template <typename T, int N, int TL, int NV, int R>
+__global__ void __launch_bounds__(kThreads) k_embed(RowSet rs, TokenView tok, const T* __restrict__ table, int V, int d,
+                                                    long long ld_table, float scale, const T* __restrict__ pos,
+                                                    long long ld_pos, RowView out, int M, int slices,
+                                                    unsigned* status) {
+  constexpr int teams = kThreads / TL;
+  const long long team = static_cast<long long>(blockIdx.x) * teams + threadIdx.x / TL;
+  const long long rows = slices == 1 ? team : team / slices;
+  const int lane = threadIdx.x & (TL - 1), c0 = (static_cast<int>(team - rows * slices) * TL * NV + lane) * N;
+  int b[R], t[R];
+  int v[R];
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    const long long r = rows * R + k;
+    b[k] = -1;
+    v[k] = -1;
+    if (r < M) {
+      locate(rs, static_cast<int>(r), b[k], t[k]);
+      if (row_kept(rs, b[k], t[k])) {
+        const long long id = token_at(tok, b[k], t[k]);
+        if (id >= 0 && id < V)
+          v[k] = static_cast<int>(id);
+        else if (c0 == 0)
+          flag_status(status, EOGP_ST_DEVICE);
+      }
     }
   }
-  const T* e = table + v * ld_table;
-  for (int c = threadIdx.x; c < d; c += kThreads) {
-    float x = 0.f;
-    if (kept) {
-      x = scale * to_f32(e[c]);
-      if (pos) x += to_f32(pos[t * ld_pos + c]);
+  Raw<T, N> e[R][NV];
+#pragma unroll
+  for (int k = 0; k < R; ++k)
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = c0 + j * TL * N;
+      e[k][j] = Raw<T, N>{};
+      if (v[k] >= 0 && c < d) e[k][j] = ld_keep<T, N>(table + v[k] * ld_table + c);
     }
-    o[c] = from_f32<T>(x);
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    if (b[k] < 0) continue;
+    T* o = row_out<T>(out, b[k], t[k]);
+    const T* q = pos && v[k] >= 0 ? pos + t[k] * ld_pos : nullptr;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = c0 + j * TL * N;
+      if (c >= d) continue;
+      Vals<N> x = unpack<T, N>(e[k][j]), y = fill<N>(0.f);
+      if (q) y = unpack<T, N>(ld_keep<T, N>(q + c));
+#pragma unroll
+      for (int i = 0; i < Vals<N>::P; ++i) x.p[i] = fma2(x.p[i], pair(scale), y.p[i]);
+      st_vals<T, N>(o + c, x);
+    }
   }
 }
 
 // ---------------------------------------------------------------- radix sort
 // Stable sort of the positions r = 0..M-1 by key, the key being the token, or V
-// for positions that take no part. One pass per digit of `bits` bits: each block
-// counts the digits of its contiguous range of elements, then places them; the
-// elements of one warp's step are ranked with a warp match, the warps and steps
-// in order by counters in shared memory.
+// for positions that take no part. A pass places the positions by one digit of
+// the key: each block counts the digits of its contiguous range, then (next
+// launch) places its range tile by tile. Within a tile a warp owns 512 consecutive
+// positions; 32 at a time they are ranked among equal digits by a warp match and
+// the warp's own counters in shared memory, and the warps' counters are added up
+// once a tile. Up to one tile of positions is sorted by one block in one launch.
 constexpr int kMaxBins = 512;
-constexpr int kSortThreads = 256;
-constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kItems = 16;
+constexpr int kTile = kThreads * kItems;
+constexpr int kSortWarps = kThreads / 32;
+constexpr int kMaxSortBlocks = 128;
 
 struct SortPlan {
-  int passes, bits, bins, blocks, per_block;  // per_block: elements of a block's range
+  int passes, bits, bins, blocks, per_block;  // per_block: positions of a block's range
 };
 
 SortPlan sort_plan(int V, long long M) {
@@ -62,57 +95,142 @@ SortPlan sort_plan(int V, long long M) {
   p.passes = (key_bits + 8) / 9;
   p.bits = (key_bits + p.passes - 1) / p.passes;
   p.bins = 1 << p.bits;
-  const long long step = kSortThreads;
-  long long per = (M + 127) / 128;
-  per = std::max(step * 4, (per + step - 1) / step * step);
-  p.per_block = static_cast<int>(per);
-  p.blocks = static_cast<int>((M + per - 1) / per);
+  const long long tiles = (M + kTile - 1) / kTile;
+  const long long each = (tiles + kMaxSortBlocks - 1) / kMaxSortBlocks;
+  p.per_block = static_cast<int>(each * kTile);
+  p.blocks = static_cast<int>((tiles + each - 1) / each);
   return p;
 }
 
-__global__ void __launch_bounds__(kSortThreads) k_token_keys(RowSet rs, TokenView tok, int V, int M, int* key, int* idx,
-                                                             unsigned* status) {
-  const int r = blockIdx.x * kSortThreads + threadIdx.x;
-  if (r >= M) return;
-  const int b = r / rs.T, t = r - b * rs.T;
-  int k = V;
-  if (row_kept(rs, b, t)) {
-    const long long v = token_at(tok, b, t);
-    if (v >= 0 && v < V)
-      k = static_cast<int>(v);
-    else
-      flag_status(status, EOGP_ST_DEVICE);
+// Zeroing of dtable's rows of absent tokens, by blocks of their own beside those of
+// another job in the same launch: the stores fill the time that the sort waits.
+struct ZeroArgs {
+  uint8_t* table;
+  size_t stride, row_bytes;
+  int unit;                 // bytes of a store: 16, or an element's
+  const uint8_t* present;   // tokens that occur, or NULL: every row is zeroed
+  int v0, v1, rows, blocks;  // rows [v0, v1), `rows` of them a block
+};
+
+__device__ void zero_rows(const ZeroArgs& z, int block) {
+  const int lane = threadIdx.x & 31;
+  for (int i = threadIdx.x >> 5; i < z.rows; i += kThreads / 32) {
+    const long long v = z.v0 + static_cast<long long>(block) * z.rows + i;
+    if (v >= z.v1 || (z.present && z.present[v])) continue;
+    uint8_t* o = z.table + v * z.stride;
+    if (z.unit == 16) {
+      for (size_t k = lane * 16; k < z.row_bytes; k += 512)
+        __stcs(reinterpret_cast<uint4*>(o + k), make_uint4(0, 0, 0, 0));
+    } else if (z.unit == 4) {
+      for (size_t k = lane * 4; k < z.row_bytes; k += 128) *reinterpret_cast<uint32_t*>(o + k) = 0;
+    } else {
+      for (size_t k = lane * 2; k < z.row_bytes; k += 64) *reinterpret_cast<uint16_t*>(o + k) = 0;
+    }
   }
-  key[r] = k;
-  idx[r] = r;
 }
 
-// hist[block][digit] = elements of the block's range with that digit.
-__global__ void __launch_bounds__(kSortThreads) k_sort_count(const int* __restrict__ key, int M, int shift, int bins,
-                                                             int per_block, int* __restrict__ hist) {
+__device__ __forceinline__ int token_key(const RowSet& rs, const TokenView& tok, int V, int r, unsigned* status) {
+  int b, t;
+  locate(rs, r, b, t);
+  if (!row_kept(rs, b, t)) return V;
+  const long long v = token_at(tok, b, t);
+  if (v >= 0 && v < V) return static_cast<int>(v);
+  flag_status(status, EOGP_ST_DEVICE);
+  return V;
+}
+
+// Keys, the tokens that occur, and hist[block][digit] of the lowest digit.
+__global__ void __launch_bounds__(kThreads) k_sort_keys(RowSet rs, TokenView tok, int V, int M, int bins, int per_block,
+                                                        int* __restrict__ key, uint8_t* __restrict__ present,
+                                                        int* __restrict__ hist, unsigned* status) {
   __shared__ int cnt[kMaxBins];
-  for (int d = threadIdx.x; d < bins; d += kSortThreads) cnt[d] = 0;
+  for (int d = threadIdx.x; d < bins; d += kThreads) cnt[d] = 0;
   __syncthreads();
-  const long long lo = static_cast<long long>(blockIdx.x) * per_block;
-  const int hi = static_cast<int>(min(static_cast<long long>(M), lo + per_block));
-  for (int i = static_cast<int>(lo) + threadIdx.x; i < hi; i += kSortThreads)
-    atomicAdd(&cnt[(key[i] >> shift) & (bins - 1)], 1);
+  const int lo = blockIdx.x * per_block, hi = min(M, lo + per_block);
+  for (int i = lo + threadIdx.x; i < hi; i += kThreads) {
+    const int k = token_key(rs, tok, V, i, status);
+    key[i] = k;
+    if (k < V) present[k] = 1;
+    atomicAdd(&cnt[k & (bins - 1)], 1);
+  }
   __syncthreads();
-  for (int d = threadIdx.x; d < bins; d += kSortThreads) hist[blockIdx.x * bins + d] = cnt[d];
+  for (int d = threadIdx.x; d < bins; d += kThreads) hist[blockIdx.x * bins + d] = cnt[d];
 }
 
-// Places the block's elements: element -> (elements with a smaller digit) +
-// (elements of earlier blocks with the same digit) + (its rank in the block).
-__global__ void __launch_bounds__(kSortThreads) k_sort_place(const int* __restrict__ key, const int* __restrict__ idx,
-                                                             int M, int shift, int bins, int per_block, int blocks,
-                                                             const int* __restrict__ hist, int* __restrict__ key_out,
-                                                             int* __restrict__ idx_out) {
-  __shared__ int base[kMaxBins];
-  __shared__ int total[kMaxBins];
+// hist[block][digit] of another digit.
+__global__ void __launch_bounds__(kThreads) k_sort_count(const int* __restrict__ key, int M, int shift, int bins,
+                                                         int per_block, int blocks, int* __restrict__ hist,
+                                                         const ZeroArgs z) {
+  if (blockIdx.x >= blocks) return zero_rows(z, blockIdx.x - blocks);
+  __shared__ int cnt[kMaxBins];
+  for (int d = threadIdx.x; d < bins; d += kThreads) cnt[d] = 0;
+  __syncthreads();
+  const int lo = blockIdx.x * per_block, hi = min(M, lo + per_block);
+  for (int i = lo + threadIdx.x; i < hi; i += kThreads) atomicAdd(&cnt[(key[i] >> shift) & (bins - 1)], 1);
+  __syncthreads();
+  for (int d = threadIdx.x; d < bins; d += kThreads) hist[blockIdx.x * bins + d] = cnt[d];
+}
+
+// Exclusive sum of total[0..bins) added into base, by the first warp.
+__device__ __forceinline__ void scan_bins(const int* total, int* base, int bins) {
+  const int lane = threadIdx.x;
+  int carry = 0;
+  for (int d0 = 0; d0 < bins; d0 += 32) {
+    const int d = d0 + lane, v = d < bins ? total[d] : 0;
+    int s = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, s, o);
+      if (lane >= o) s += u;
+    }
+    if (d < bins) base[d] += carry + s - v;
+    carry += __shfl_sync(0xffffffffu, s, 31);
+  }
+}
+
+// Ranks of a tile: on return position dst of item s of this thread is
+// base[digit] + wcnt[warp][digit] + off[s]. dg < 0: no item. Uses two barriers.
+__device__ __forceinline__ void rank_tile(const int (&dg)[kItems], int (&off)[kItems], int (*wcnt)[kMaxBins],
+                                          int* tile_total, int bins) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  for (int d = lane; d < bins; d += 32) wcnt[warp][d] = 0;
+  __syncwarp();
+#pragma unroll
+  for (int s = 0; s < kItems; ++s) {
+    const unsigned same = __match_any_sync(0xffffffffu, dg[s]);
+    const int rank = __popc(same & ((1u << lane) - 1u));
+    off[s] = dg[s] >= 0 ? wcnt[warp][dg[s]] + rank : 0;
+    __syncwarp();
+    if (dg[s] >= 0 && rank == 0) wcnt[warp][dg[s]] += __popc(same);
+    __syncwarp();
+  }
+  __syncthreads();
+  for (int d = tid; d < bins; d += kThreads) {
+    int run = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) {
+      const int n = wcnt[w][d];
+      wcnt[w][d] = run;
+      run += n;
+    }
+    tile_total[d] = run;
+  }
+  __syncthreads();
+}
+
+// Places the block's range: position -> (positions with a smaller digit) + (earlier
+// blocks' with the same) + (its rank in the block). idx NULL: the positions themselves.
+__global__ void __launch_bounds__(kThreads) k_sort_place(const int* __restrict__ key, const int* __restrict__ idx,
+                                                         int M, int shift, int bins, int per_block, int blocks,
+                                                         const int* __restrict__ hist, int* __restrict__ key_out,
+                                                         int* __restrict__ idx_out, const ZeroArgs z) {
+  if (blockIdx.x >= blocks) return zero_rows(z, blockIdx.x - blocks);
+  __shared__ int base[kMaxBins], total[kMaxBins];
   __shared__ int wcnt[kSortWarps][kMaxBins];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  for (int d = tid; d < bins; d += kSortThreads) {
+  for (int d = tid; d < bins; d += kThreads) {
     int before = 0, all = 0;
+#pragma unroll 16
     for (int k = 0; k < blocks; ++k) {
       const int h = hist[k * bins + d];
       if (k < static_cast<int>(blockIdx.x)) before += h;
@@ -122,139 +240,438 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_place(const int* __restri
     total[d] = all;
   }
   __syncthreads();
-  if (warp == 0) {  // exclusive sum of the totals, 32 digits at a time
-    int carry = 0;
-    for (int d0 = 0; d0 < bins; d0 += 32) {
-      const int d = d0 + lane, v = d < bins ? total[d] : 0;
-      int s = v;
+  if (warp == 0) scan_bins(total, base, bins);
+  const int lo = blockIdx.x * per_block, hi = min(M, lo + per_block);
+  for (int t0 = lo; t0 < hi; t0 += kTile) {
+    int k[kItems], p[kItems], dg[kItems], off[kItems];
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, s, o);
-        if (lane >= o) s += u;
+    for (int s = 0; s < kItems; ++s) {
+      const int i = t0 + warp * (32 * kItems) + s * 32 + lane;
+      k[s] = i < hi ? key[i] : 0;
+      p[s] = i < hi ? (idx ? idx[i] : i) : 0;
+      dg[s] = i < hi ? (k[s] >> shift) & (bins - 1) : -1;
+    }
+    rank_tile(dg, off, wcnt, total, bins);
+#pragma unroll
+    for (int s = 0; s < kItems; ++s) {
+      if (dg[s] < 0) continue;
+      const int at = base[dg[s]] + wcnt[warp][dg[s]] + off[s];
+      key_out[at] = k[s];
+      idx_out[at] = p[s];
+    }
+    __syncthreads();
+    for (int d = tid; d < bins; d += kThreads) base[d] += total[d];
+    __syncthreads();
+  }
+}
+
+// M <= kTile: keys and every pass in block 0; the other blocks zero dtable.
+__global__ void __launch_bounds__(kThreads) k_sort_one(RowSet rs, TokenView tok, int V, int M, int passes, int bits,
+                                                       int* __restrict__ key_out, int* __restrict__ idx_out,
+                                                       const ZeroArgs z, unsigned* status) {
+  if (blockIdx.x > 0) return zero_rows(z, blockIdx.x - 1);
+  __shared__ int base[kMaxBins], total[kMaxBins];
+  __shared__ int wcnt[kSortWarps][kMaxBins];
+  __shared__ int skey[kTile];
+  __shared__ unsigned short sidx[kTile];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, bins = 1 << bits;
+  int k[kItems], p[kItems], dg[kItems], off[kItems];
+#pragma unroll
+  for (int s = 0; s < kItems; ++s) {
+    const int i = warp * (32 * kItems) + s * 32 + lane;
+    k[s] = i < M ? token_key(rs, tok, V, i, status) : 0;
+    p[s] = i;
+  }
+  for (int pass = 0; pass < passes; ++pass) {
+#pragma unroll
+    for (int s = 0; s < kItems; ++s) {
+      const int i = warp * (32 * kItems) + s * 32 + lane;
+      if (pass > 0 && i < M) {
+        k[s] = skey[i];
+        p[s] = sidx[i];
       }
-      if (d < bins) base[d] += carry + s - v;
-      carry += __shfl_sync(0xffffffffu, s, 31);
+      dg[s] = i < M ? (k[s] >> (pass * bits)) & (bins - 1) : -1;
     }
-  }
-  const long long lo = static_cast<long long>(blockIdx.x) * per_block;
-  const int hi = static_cast<int>(min(static_cast<long long>(M), lo + per_block));
-  for (int i0 = static_cast<int>(lo); i0 < hi; i0 += kSortThreads) {
-    for (int d = lane; d < bins; d += 32) wcnt[warp][d] = 0;
-    __syncwarp();
-    const int i = i0 + tid;
-    const bool on = i < hi;
-    const int k = on ? key[i] : 0, p = on ? idx[i] : 0;
-    const int dg = on ? (k >> shift) & (bins - 1) : -1;
-    const unsigned same = __match_any_sync(0xffffffffu, dg);
-    const int rank = __popc(same & ((1u << lane) - 1u));
-    if (on && rank == 0) wcnt[warp][dg] = __popc(same);
+    for (int d = tid; d < bins; d += kThreads) base[d] = 0;
+    rank_tile(dg, off, wcnt, total, bins);
+    if (warp == 0) scan_bins(total, base, bins);
     __syncthreads();
-    if (on) {
-      int at = base[dg] + rank;
-      for (int w = 0; w < warp; ++w) at += wcnt[w][dg];
-      key_out[at] = k;
-      idx_out[at] = p;
-    }
-    __syncthreads();
-    for (int d = tid; d < bins; d += kSortThreads) {
-      int s = 0;
-      for (int w = 0; w < kSortWarps; ++w) s += wcnt[w][d];
-      base[d] += s;
+#pragma unroll
+    for (int s = 0; s < kItems; ++s) {
+      if (dg[s] < 0) continue;
+      const int at = base[dg[s]] + wcnt[warp][dg[s]] + off[s];
+      if (pass == passes - 1) {
+        key_out[at] = k[s];
+        idx_out[at] = p[s];
+      } else {
+        skey[at] = k[s];
+        sidx[at] = static_cast<unsigned short>(p[s]);
+      }
     }
     __syncthreads();
   }
 }
 
-__device__ __forceinline__ int lower_bound(const int* __restrict__ key, int n, int v) {
-  int lo = 0, hi = n;
-  while (lo < hi) {
-    const int mid = lo + (hi - lo) / 2;
-    if (key[mid] < v)
-      lo = mid + 1;
+// -------------------------------------------------------------- sums of runs
+// The sorted positions are cut into chunks of `chunk`, `teams` chunks a block. A
+// thread sums one vector of N channels over one chunk, run after run. A run inside
+// a chunk is a finished row of dtable; the pieces of one that several chunks share
+// are added in order, those of a block in shared memory, those of several blocks by
+// k_embed_join from the blocks' slots: 0 for a run that began in an earlier block,
+// 1 for one that goes on in the next, d floats each.
+struct SumArgs {
+  RowSet rs;  // B = 1 where dout's rows follow each other
+  RowView dout;
+  const int *key, *idx;
+  int M, V, d, nv, chunk, ct, teams, tiles, groups;  // ct vectors a column tile; tiles x groups blocks
+  float scale;
+  void* dtable;
+  long long ld;
+  bool accumulate;
+  float* slots;
+};
+
+template <typename G, int N>
+__device__ __forceinline__ void st_run(G* o, Vals<N> s, float scale, bool accumulate) {
+#pragma unroll
+  for (int i = 0; i < Vals<N>::P; ++i) s.p[i] = mul2(s.p[i], pair(scale));
+  if (accumulate) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float v = to_f32(o[i]) + (i & 1 ? s.p[i / 2].y : s.p[i / 2].x);
+      (i & 1 ? s.p[i / 2].y : s.p[i / 2].x) = v;
+    }
+  }
+  st_wide<G, N>(o, s);
+}
+
+constexpr int kChunk = 64;                           // most positions of a chunk
+constexpr int kGroup = kThreads / 8 * kChunk;        // of a block (column tiles of 8 vectors)
+
+template <typename T, typename G, int N>
+__global__ void __launch_bounds__(kThreads, 3) k_embed_sum(const SumArgs a) {
+  __shared__ int skey[kGroup + 2];  // skey[1 + i]: key of the block's position i, with its neighbours
+  __shared__ int sidx[kGroup];
+  __shared__ __align__(16) float piece[kThreads * 2 * N];
+  const int tid = threadIdx.x, grp = blockIdx.x / a.tiles, tile = blockIdx.x - grp * a.tiles;
+  const int per_block = a.teams * a.chunk;
+  const int g0 = grp * per_block, n = min(a.M - g0, per_block);
+  for (int i = tid; i < n + 2; i += kThreads) {
+    const int at = g0 + i - 1;
+    skey[i] = at >= 0 && at < a.M ? a.key[at] : -1;
+  }
+  for (int i = tid; i < n; i += kThreads) sidx[i] = a.idx[g0 + i];
+  __syncthreads();
+  const int team = tid / a.ct, j = tile * a.ct + (tid - team * a.ct);
+  const bool on = j < a.nv;
+  G* const table = static_cast<G*>(a.dtable) + j * N;
+  const int lo = min(n, team * a.chunk), hi = min(n, lo + a.chunk);
+  float* const mine = piece + tid * 2 * N;
+  if (on && lo < hi) {
+    int run = skey[1 + lo];
+    bool begins = run != skey[lo];
+    Vals<N> s = fill<N>(0.f);
+    constexpr int kAhead = 8;
+    for (int i0 = lo; i0 < hi; i0 += kAhead) {
+      Raw<T, N> raw[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        raw[u] = Raw<T, N>{};
+        if (i0 + u < hi && skey[1 + i0 + u] != a.V) {
+          int b, t;
+          locate(a.rs, sidx[i0 + u], b, t);
+          raw[u] = ld_raw<T, N>(row_of<T>(a.dout, b, t) + j * N);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (i0 + u < hi) {
+          const int k = skey[1 + i0 + u];
+          if (k != run) {  // `run` ends inside the chunk
+            if (begins)
+              st_run<G, N>(table + run * a.ld, s, a.scale, a.accumulate);
+            else
+              st_floats<N>(mine, s);
+            run = k;
+            begins = true;
+            s = fill<N>(0.f);
+          }
+          const Vals<N> v = unpack<T, N>(raw[u]);
+#pragma unroll
+          for (int i = 0; i < Vals<N>::P; ++i) s.p[i] = add2(s.p[i], v.p[i]);
+        }
+      }
+    }
+    if (!begins)
+      st_floats<N>(mine, s);
+    else if (skey[1 + hi] == run)
+      st_floats<N>(mine + N, s);
+    else if (run != a.V)
+      st_run<G, N>(table + run * a.ld, s, a.scale, a.accumulate);
+  }
+  __syncthreads();
+  // The first team's threads go through the chunks' shared runs in order.
+  if (team > 0 || !on) return;
+  Vals<N> s = fill<N>(0.f);
+  bool inside = false;  // the run being added began in this block
+  for (int k = 0; k * a.chunk < n; ++k) {
+    const int l = k * a.chunk, h = min(n, l + a.chunk);
+    const float* pk = piece + (k * a.ct + tid) * 2 * N;
+    const int first = skey[1 + l], last = skey[h];
+    if (first == skey[l]) {
+      if (first != a.V) {
+        const Vals<N> v = ld_floats<N>(pk);
+#pragma unroll
+        for (int i = 0; i < Vals<N>::P; ++i) s.p[i] = add2(s.p[i], v.p[i]);
+        if (first != last || skey[1 + h] != first) {  // it ends in this chunk
+          if (inside)
+            st_run<G, N>(table + first * a.ld, s, a.scale, a.accumulate);
+          else
+            st_floats<N>(a.slots + (static_cast<size_t>(grp) * 2 * a.nv + j) * N, s);
+          s = fill<N>(0.f);
+        }
+      }
+      if (first == last) continue;
+    }
+    if (last != a.V && skey[1 + h] == last) {  // it begins in this chunk and goes on
+      s = ld_floats<N>(pk + N);
+      inside = true;
+    }
+  }
+  if (n > 0 && skey[n] != a.V && skey[1 + n] == skey[n])
+    st_floats<N>(a.slots + ((static_cast<size_t>(grp) * 2 + (inside ? 1 : 0)) * a.nv + j) * N, s);
+}
+
+// Runs over several blocks: the threads of the block in which a run begins add its
+// slots in order.
+template <typename G, int N>
+__global__ void __launch_bounds__(kThreads) k_embed_join(const SumArgs a) {
+  const long long id = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
+  const int c = static_cast<int>(id / a.nv), j = static_cast<int>(id - static_cast<long long>(c) * a.nv);
+  const int per_block = a.teams * a.chunk;
+  if (c >= a.groups - 1) return;
+  const int lo = c * per_block, hi = lo + per_block;
+  const int run = a.key[hi - 1];
+  if (run == a.V || a.key[hi] != run || (lo > 0 && a.key[lo - 1] == run)) return;
+  int end = hi + 1, far = a.M;  // first position after the run
+  while (end < far) {
+    const int mid = end + (far - end) / 2;
+    if (a.key[mid] == run)
+      end = mid + 1;
     else
-      hi = mid;
+      far = mid;
   }
-  return lo;
-}
-
-// One block per table row: its run of the sorted positions, summed in order.
-template <typename T, typename G>
-__global__ void __launch_bounds__(kThreads) k_embed_sum_rows(RowSet rs, RowView dout, const int* __restrict__ key,
-                                                             const int* __restrict__ idx, int M, int V, int d,
-                                                             float scale, G* __restrict__ dtable, long long ld,
-                                                             bool accumulate) {
-  const int v = blockIdx.x;
-  const int lo = lower_bound(key, M, v), hi = lower_bound(key, M, v + 1);
-  if (accumulate && lo == hi) return;
-  G* o = dtable + v * ld;
-  for (int c = threadIdx.x; c < d; c += kThreads) {
-    float s = 0.f;
-    for (int i = lo; i < hi; ++i) {
-      const int r = idx[i], b = r / rs.T, t = r - b * rs.T;
-      s += to_f32(row_of<T>(dout, b, t)[c]);
-    }
-    s *= scale;
-    o[c] = from_f32<G>(accumulate ? to_f32(o[c]) + s : s);
+  const int last = (end - 1) / per_block;
+  const size_t stride = static_cast<size_t>(a.nv) * N;
+  Vals<N> s = ld_floats<N>(a.slots + (static_cast<size_t>(c) * 2 + 1) * stride + j * N);
+#pragma unroll 8
+  for (int k = c + 1; k <= last; ++k) {
+    const Vals<N> v = ld_floats<N>(a.slots + static_cast<size_t>(k) * 2 * stride + j * N);
+#pragma unroll
+    for (int i = 0; i < Vals<N>::P; ++i) s.p[i] = add2(s.p[i], v.p[i]);
   }
+  st_run<G, N>(static_cast<G*>(a.dtable) + run * a.ld + j * N, s, a.scale, a.accumulate);
 }
 
 size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
 
 }  // namespace
 
-cudaError_t launch_embed(RowSet rs, TokenView tok, const void* table, bool bf16_, int V, int d, long long ld_table,
-                         float scale, const void* pos, long long ld_pos, RowView out, unsigned* status,
-                         cudaStream_t st) {
-  const int M = static_cast<int>(rs.rows());
-  if (bf16_)
-    k_embed_rows<bf16><<<M, kThreads, 0, st>>>(rs, tok, static_cast<const bf16*>(table), V, d, ld_table, scale,
-                                              static_cast<const bf16*>(pos), ld_pos, out, status);
-  else
-    k_embed_rows<float><<<M, kThreads, 0, st>>>(rs, tok, static_cast<const float*>(table), V, d, ld_table, scale,
-                                               static_cast<const float*>(pos), ld_pos, out, status);
+namespace {
+
+struct EmbedArgs {
+  RowSet rs;
+  TokenView tok;
+  const void* table;
+  int V, d;
+  long long ld_table;
+  float scale;
+  const void* pos;
+  long long ld_pos;
+  RowView out;
+  unsigned* status;
+};
+
+template <typename T, int N, int TL, int NV, int R>
+cudaError_t embed_team(const EmbedArgs& a, cudaStream_t st) {
+  const long long M = a.rs.rows(), nv = a.d / N, slices = (nv + TL * NV - 1) / (TL * NV);
+  const long long teams = (M + R - 1) / R * slices, blocks = (teams + kThreads / TL - 1) / (kThreads / TL);
+  if (blocks > 0x7FFFFFFFLL) return cudaErrorInvalidConfiguration;  // more than any memory holds
+  k_embed<T, N, TL, NV, R><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(
+      a.rs, a.tok, static_cast<const T*>(a.table), a.V, a.d, a.ld_table, a.scale, static_cast<const T*>(a.pos), a.ld_pos,
+      a.out, static_cast<int>(M), static_cast<int>(slices), a.status);
   return cudaGetLastError();
 }
 
-size_t embed_grad_ws_bytes(int V, int d, long long M) {
-  if (M == 0) return 0;
-  const SortPlan p = sort_plan(V, M);
-  return 4 * al256(M * 4) + al256(static_cast<size_t>(p.blocks) * p.bins * 4);
+template <typename T>
+cudaError_t embed_any(const EmbedArgs& a, cudaStream_t st) {
+  constexpr int F = 16 / sizeof(T);
+  const int es = sizeof(T);
+  int vec = std::min(row_vec(a.out, a.rs, a.d, es), row_vec(a.table, 0, a.ld_table, RowSet{1, a.V, nullptr}, a.d, es));
+  if (a.pos) vec = std::min(vec, row_vec(a.pos, 0, a.ld_pos, RowSet{1, a.rs.T, nullptr}, a.d, es));
+  const int nv = a.d / vec;
+  if (vec == F) {
+    if (nv <= 8) return embed_team<T, F, 8, 1, 4>(a, st);
+    if (nv <= 16) return embed_team<T, F, 8, 2, 4>(a, st);
+    if (nv <= 32) return embed_team<T, F, 32, 1, 4>(a, st);
+    if (nv <= 64) return embed_team<T, F, 32, 2, 2>(a, st);
+    if (nv <= 96) return embed_team<T, F, 32, 3, 2>(a, st);
+    return embed_team<T, F, 32, 4, 1>(a, st);
+  }
+  if (vec == 2) return embed_team<T, 2, 32, 8, 1>(a, st);
+  return embed_team<T, 1, 32, 8, 1>(a, st);
 }
+
+}  // namespace
+
+cudaError_t launch_embed(RowSet rs, TokenView tok, const void* table, bool bf16_, int V, int d, long long ld_table,
+                         float scale, const void* pos, long long ld_pos, RowView out, unsigned* status,
+                         cudaStream_t st) {
+  const EmbedArgs a{rs, tok, table, V, d, ld_table, scale, pos, ld_pos, out, status};
+  return bf16_ ? embed_any<bf16>(a, st) : embed_any<float>(a, st);
+}
+
+namespace {
+
+// Positions of a chunk: 64, fewer where that leaves less than 131,072 threads.
+int chunk_of(long long M, int nv) {
+  int c = kChunk;
+  while (c > 8 && M * nv / c < 131072) c >>= 1;
+  return c;
+}
+// Vectors of a column tile.
+int tile_of(int nv) { return nv <= 8 ? 8 : nv <= 16 ? 16 : 32; }
+
+template <typename T, typename G, int N>
+cudaError_t embed_sum(SumArgs a, cudaStream_t st) {
+  a.nv = a.d / N;
+  a.chunk = chunk_of(a.M, a.nv);
+  a.ct = tile_of(a.nv);
+  a.teams = kThreads / a.ct;
+  a.tiles = (a.nv + a.ct - 1) / a.ct;
+  a.groups = (a.M + a.teams * a.chunk - 1) / (a.teams * a.chunk);
+  const long long blocks = static_cast<long long>(a.tiles) * a.groups;
+  if (blocks > 0x7FFFFFFFLL) return cudaErrorInvalidConfiguration;
+  k_embed_sum<T, G, N><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(a);
+  if (a.groups > 1) {
+    const long long join = (static_cast<long long>(a.groups) * a.nv + kThreads - 1) / kThreads;
+    k_embed_join<G, N><<<static_cast<unsigned>(join), kThreads, 0, st>>>(a);
+  }
+  return cudaGetLastError();
+}
+
+template <typename T, typename G>
+cudaError_t embed_sum_vec(const SumArgs& a, cudaStream_t st) {
+  constexpr int F = 16 / sizeof(T);
+  // Elements per access of dout, and whether dtable takes as many at once.
+  int vec = row_vec(a.dout, a.rs, a.d, sizeof(T));
+  const int gb = std::min<int>(16, vec * sizeof(G));
+  if (reinterpret_cast<uintptr_t>(a.dtable) % gb || (a.V > 1 && a.ld * static_cast<long long>(sizeof(G)) % gb)) vec = 1;
+  if (vec == F) return embed_sum<T, G, F>(a, st);
+  if (vec == 2) return embed_sum<T, G, 2>(a, st);
+  return embed_sum<T, G, 1>(a, st);
+}
+
+struct EmbedWs {
+  size_t key, idx, key2, idx2, hist, present, slots, total;
+};
+
+EmbedWs embed_ws(int V, int d, long long M) {
+  EmbedWs w{};
+  if (M == 0) return w;
+  const SortPlan p = sort_plan(V, M);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at += al256(bytes);
+    return o;
+  };
+  w.key = take(M * 4);
+  w.idx = take(M * 4);
+  if (M > kTile) {
+    w.key2 = take(M * 4);
+    w.idx2 = take(M * 4);
+    w.hist = take(static_cast<size_t>(p.blocks) * p.bins * 4);
+    w.present = take(V);
+  }
+  // Enough for every access width: the most groups of positions any of them makes.
+  size_t slots = 0;
+  for (int n = 1; n <= 8; n *= 2) {
+    const int nv = (d + n - 1) / n;
+    const long long per = static_cast<long long>(kThreads / tile_of(nv)) * chunk_of(M, nv);
+    slots = std::max(slots, static_cast<size_t>((M + per - 1) / per) * 2 * nv * n * 4);
+  }
+  w.slots = take(slots);
+  w.total = at;
+  return w;
+}
+
+}  // namespace
+
+size_t embed_grad_ws_bytes(int V, int d, long long M) { return embed_ws(V, d, M).total; }
 
 cudaError_t launch_embed_grad(RowSet rs, TokenView tok, RowView dout, bool bf16_, int V, int d, float scale,
                               void* dtable, bool grad_bf16, long long ld_dtable, bool accumulate, void* ws,
-                              unsigned* status, int num_sms, cudaStream_t st) {
-  const int M = static_cast<int>(rs.rows());
-  int *key = nullptr, *idx = nullptr;
-  if (M > 0) {
-    const SortPlan p = sort_plan(V, M);
-    uint8_t* w = static_cast<uint8_t*>(ws);
-    const size_t a = al256(static_cast<size_t>(M) * 4);
-    key = reinterpret_cast<int*>(w);
-    idx = reinterpret_cast<int*>(w + a);
-    int* key2 = reinterpret_cast<int*>(w + 2 * a);
-    int* idx2 = reinterpret_cast<int*>(w + 3 * a);
-    int* hist = reinterpret_cast<int*>(w + 4 * a);
-    k_token_keys<<<(M + kSortThreads - 1) / kSortThreads, kSortThreads, 0, st>>>(rs, tok, V, M, key, idx, status);
+                              unsigned* status, cudaStream_t st) {
+  const int M = static_cast<int>(rs.rows()), es = grad_bf16 ? 2 : 4;
+  if (M == 0 && accumulate) return cudaSuccess;
+  const SortPlan p = sort_plan(V, M);
+  const EmbedWs w = embed_ws(V, d, M);
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  auto ints = [&](size_t at) { return reinterpret_cast<int*>(base + at); };
+
+  ZeroArgs z{};
+  z.table = static_cast<uint8_t*>(dtable);
+  z.row_bytes = static_cast<size_t>(d) * es;
+  z.stride = V > 1 ? static_cast<size_t>(ld_dtable) * es : z.row_bytes;
+  z.unit = reinterpret_cast<uintptr_t>(dtable) % 16 == 0 && z.stride % 16 == 0 && z.row_bytes % 16 == 0 ? 16 : es;
+  z.rows = static_cast<int>(std::max<size_t>(8, 32768 / z.row_bytes));
+  // Part i of n of the rows.
+  auto zero_part = [&](int i, int n) {
+    z.v0 = static_cast<int>(static_cast<long long>(V) * i / n);
+    z.v1 = static_cast<int>(static_cast<long long>(V) * (i + 1) / n);
+    z.blocks = accumulate ? 0 : (z.v1 - z.v0 + z.rows - 1) / z.rows;
+    return z;
+  };
+
+  int *key = ints(w.key), *idx = ints(w.idx);
+  if (M <= kTile) {
+    zero_part(0, 1);
+    k_sort_one<<<1 + z.blocks, kThreads, 0, st>>>(rs, tok, V, M, p.passes, p.bits, key, idx, z, status);
+  } else {
+    int *key2 = ints(w.key2), *idx2 = ints(w.idx2), *hist = ints(w.hist);
+    uint8_t* present = base + w.present;
+    if (cudaError_t e = cudaMemsetAsync(present, 0, V, st); e != cudaSuccess) return e;
+    k_sort_keys<<<p.blocks, kThreads, 0, st>>>(rs, tok, V, M, p.bins, p.per_block, key, present, hist, status);
+    z.present = present;
+    const int parts = 2 * p.passes - 1;
     for (int s = 0; s < p.passes; ++s) {
-      k_sort_count<<<p.blocks, kSortThreads, 0, st>>>(key, M, s * p.bits, p.bins, p.per_block, hist);
-      k_sort_place<<<p.blocks, kSortThreads, 0, st>>>(key, idx, M, s * p.bits, p.bins, p.per_block, p.blocks, hist,
-                                                      key2, idx2);
+      if (s > 0) {
+        zero_part(2 * s - 1, parts);
+        k_sort_count<<<p.blocks + z.blocks, kThreads, 0, st>>>(key, M, s * p.bits, p.bins, p.per_block, p.blocks, hist,
+                                                               z);
+      }
+      zero_part(2 * s, parts);
+      k_sort_place<<<p.blocks + z.blocks, kThreads, 0, st>>>(key, s ? idx : nullptr, M, s * p.bits, p.bins, p.per_block,
+                                                             p.blocks, hist, key2, idx2, z);
       std::swap(key, key2);
       std::swap(idx, idx2);
     }
   }
-  if (bf16_ && grad_bf16)
-    k_embed_sum_rows<bf16, bf16><<<V, kThreads, 0, st>>>(rs, dout, key, idx, M, V, d, scale, static_cast<bf16*>(dtable),
-                                                        ld_dtable, accumulate);
-  else if (bf16_)
-    k_embed_sum_rows<bf16, float><<<V, kThreads, 0, st>>>(rs, dout, key, idx, M, V, d, scale,
-                                                         static_cast<float*>(dtable), ld_dtable, accumulate);
-  else if (grad_bf16)
-    k_embed_sum_rows<float, bf16><<<V, kThreads, 0, st>>>(rs, dout, key, idx, M, V, d, scale,
-                                                         static_cast<bf16*>(dtable), ld_dtable, accumulate);
-  else
-    k_embed_sum_rows<float, float><<<V, kThreads, 0, st>>>(rs, dout, key, idx, M, V, d, scale,
-                                                          static_cast<float*>(dtable), ld_dtable, accumulate);
-  return cudaGetLastError();
+  if (M == 0) return cudaGetLastError();
+  SumArgs a{};
+  a.rs = flat(dout, rs) ? RowSet{1, M, nullptr} : RowSet{rs.B, rs.T, nullptr};
+  a.dout = dout;
+  a.key = key;
+  a.idx = idx;
+  a.M = M;
+  a.V = V;
+  a.d = d;
+  a.scale = scale;
+  a.dtable = dtable;
+  a.ld = ld_dtable;
+  a.accumulate = accumulate;
+  a.slots = reinterpret_cast<float*>(base + w.slots);
+  if (bf16_) return grad_bf16 ? embed_sum_vec<bf16, bf16>(a, st) : embed_sum_vec<bf16, float>(a, st);
+  return grad_bf16 ? embed_sum_vec<float, bf16>(a, st) : embed_sum_vec<float, float>(a, st);
 }

@@ -98,6 +98,17 @@ __device__ __forceinline__ Raw<T, N> ld_raw(const T* p) {
   return r;
 }
 
+// The same for data that other blocks read again, through the read-only path.
+template <typename T, int N>
+__device__ __forceinline__ Raw<T, N> ld_keep(const T* p) {
+  Raw<T, N> r;
+  if constexpr (N == 1)
+    r.w = *p;
+  else
+    r.w = __ldg(reinterpret_cast<const decltype(r.w)*>(p));
+  return r;
+}
+
 // The N values as fp32 pairs (N = 1: the first of a pair), for the paired fp32
 // instructions.
 template <int N>
@@ -151,6 +162,50 @@ __device__ __forceinline__ void st_vals(T* p, const Vals<N>& v) {
   } else {
     __stcs(reinterpret_cast<uint4*>(p),
            make_uint4(pack_bf16(v.p[0]), pack_bf16(v.p[1]), pack_bf16(v.p[2]), pack_bf16(v.p[3])));
+  }
+}
+
+// The same for a type whose N elements may take two accesses, or half of one.
+template <typename G, int N>
+__device__ __forceinline__ void st_wide(G* p, const Vals<N>& v) {
+  if constexpr (sizeof(G) * N == 32) {
+    __stcs(reinterpret_cast<float4*>(p), make_float4(v.p[0].x, v.p[0].y, v.p[1].x, v.p[1].y));
+    __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v.p[2].x, v.p[2].y, v.p[3].x, v.p[3].y));
+  } else if constexpr (sizeof(G) == 2 && N == 4) {
+    __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack_bf16(v.p[0]), pack_bf16(v.p[1])));
+  } else {
+    st_vals<G, N>(p, v);
+  }
+}
+
+// N floats, aligned to min(N, 4) of them (N = 1: the first of a pair).
+template <int N>
+__device__ __forceinline__ Vals<N> ld_floats(const float* p) {
+  Vals<N> v;
+  if constexpr (N == 1) {
+    v.p[0] = make_float2(*p, 0.f);
+  } else if constexpr (N == 2) {
+    v.p[0] = *reinterpret_cast<const float2*>(p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const float4 f = *(reinterpret_cast<const float4*>(p) + i);
+      v.p[2 * i] = make_float2(f.x, f.y);
+      v.p[2 * i + 1] = make_float2(f.z, f.w);
+    }
+  }
+  return v;
+}
+template <int N>
+__device__ __forceinline__ void st_floats(float* p, const Vals<N>& v) {
+  if constexpr (N == 1) {
+    *p = v.p[0].x;
+  } else if constexpr (N == 2) {
+    *reinterpret_cast<float2*>(p) = v.p[0];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i)
+      *(reinterpret_cast<float4*>(p) + i) = make_float4(v.p[2 * i].x, v.p[2 * i].y, v.p[2 * i + 1].x, v.p[2 * i + 1].y);
   }
 }
 
