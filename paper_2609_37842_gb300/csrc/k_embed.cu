@@ -74,15 +74,17 @@ __global__ void __launch_bounds__(kThreads) k_embed(RowSet rs, TokenView tok, co
 // Stable sort of the positions r = 0..M-1 by key, the key being the token, or V
 // for positions that take no part. A pass places the positions by one digit of
 // the key: each block counts the digits of its contiguous range, then (next
-// launch) places its range tile by tile. Within a tile a warp owns 512 consecutive
+// launch) places its range tile by tile. Within a tile a warp owns 256 consecutive
 // positions; 32 at a time they are ranked among equal digits by a warp match and
 // the warp's own counters in shared memory, and the warps' counters are added up
 // once a tile. Up to one tile of positions is sorted by one block in one launch.
 constexpr int kMaxBins = 512;
-constexpr int kItems = 16;
-constexpr int kTile = kThreads * kItems;
-constexpr int kSortWarps = kThreads / 32;
-constexpr int kMaxSortBlocks = 128;
+constexpr int kItems = 8;
+constexpr int kSortThreads = 512;
+constexpr int kTile = kSortThreads * kItems;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kMaxSortBlocks = 256;
+constexpr int kMarked = 1024;
 
 struct SortPlan {
   int passes, bits, bins, blocks, per_block;  // per_block: positions of a block's range
@@ -114,7 +116,7 @@ struct ZeroArgs {
 
 __device__ void zero_rows(const ZeroArgs& z, int block) {
   const int lane = threadIdx.x & 31;
-  for (int i = threadIdx.x >> 5; i < z.rows; i += kThreads / 32) {
+  for (int i = threadIdx.x >> 5; i < z.rows; i += kSortWarps) {
     const long long v = z.v0 + static_cast<long long>(block) * z.rows + i;
     if (v >= z.v1 || (z.present && z.present[v])) continue;
     uint8_t* o = z.table + v * z.stride;
@@ -129,46 +131,95 @@ __device__ void zero_rows(const ZeroArgs& z, int block) {
   }
 }
 
-__device__ __forceinline__ int token_key(const RowSet& rs, const TokenView& tok, int V, int r, unsigned* status) {
-  int b, t;
-  locate(rs, r, b, t);
-  if (!row_kept(rs, b, t)) return V;
-  const long long v = token_at(tok, b, t);
-  if (v >= 0 && v < V) return static_cast<int>(v);
-  flag_status(status, EOGP_ST_DEVICE);
-  return V;
+// Keys of positions at0 + s * step (those below hi, else -1), all their
+// loads in flight at once.
+template <bool I64, int K>
+__device__ __forceinline__ void token_keys(const RowSet& rs, const TokenView& tok, int V, int at0, int step, int hi,
+                                           int (&k)[K], unsigned* status) {
+  long long id[K];
+#pragma unroll
+  for (int s = 0; s < K; ++s) {
+    const int i = at0 + s * step;
+    int b, t;
+    locate(rs, i < hi ? i : 0, b, t);
+    id[s] = V;
+    if (i < hi && row_kept(rs, b, t)) {
+      if constexpr (I64)
+        id[s] = static_cast<const long long*>(tok.p)[b * tok.bs + t];
+      else
+        id[s] = static_cast<const int*>(tok.p)[b * tok.bs + t];
+      if (id[s] == V) id[s] = -1;  // V itself is no token
+    }
+  }
+  bool bad = false;
+#pragma unroll
+  for (int s = 0; s < K; ++s) {
+    const bool out = id[s] < 0 || id[s] > V;
+    bad |= out;
+    k[s] = at0 + s * step < hi ? (out ? V : static_cast<int>(id[s])) : -1;
+  }
+  if (bad) flag_status(status, EOGP_ST_DEVICE);
 }
 
-// Keys, the tokens that occur, and hist[block][digit] of the lowest digit.
+// Counting takes kCount positions a block, several blocks adding to the counts of
+// one range (whole numbers: the order does not matter).
+constexpr int kCount = kThreads * kItems / 2;
+
+// Keys, the tokens that occur, and hist[range][digit] of the lowest digit. present
+// and hist start at 0.
+template <bool I64>
 __global__ void __launch_bounds__(kThreads) k_sort_keys(RowSet rs, TokenView tok, int V, int M, int bins, int per_block,
                                                         int* __restrict__ key, uint8_t* __restrict__ present,
                                                         int* __restrict__ hist, unsigned* status) {
   __shared__ int cnt[kMaxBins];
+  // Tokens that this block has marked lately: a frequent token's mark would
+  // otherwise be stored at one address by every position that holds it.
+  __shared__ int marked[kMarked];
   for (int d = threadIdx.x; d < bins; d += kThreads) cnt[d] = 0;
+  for (int d = threadIdx.x; d < kMarked; d += kThreads) marked[d] = -1;
   __syncthreads();
-  const int lo = blockIdx.x * per_block, hi = min(M, lo + per_block);
-  for (int i = lo + threadIdx.x; i < hi; i += kThreads) {
-    const int k = token_key(rs, tok, V, i, status);
-    key[i] = k;
-    if (k < V) present[k] = 1;
-    atomicAdd(&cnt[k & (bins - 1)], 1);
+  const int lo = blockIdx.x * kCount;
+  int k[kCount / kThreads];
+  token_keys<I64>(rs, tok, V, lo + threadIdx.x, kThreads, M, k, status);
+#pragma unroll
+  for (int s = 0; s < kCount / kThreads; ++s) {
+    if (k[s] < 0) continue;
+    key[lo + threadIdx.x + s * kThreads] = k[s];
+    volatile int* const seen = &marked[k[s] & (kMarked - 1)];
+    if (k[s] < V && *seen != k[s]) {
+      *seen = k[s];
+      present[k[s]] = 1;
+    }
+    atomicAdd(&cnt[k[s] & (bins - 1)], 1);
   }
   __syncthreads();
-  for (int d = threadIdx.x; d < bins; d += kThreads) hist[blockIdx.x * bins + d] = cnt[d];
+  int* const to = hist + lo / per_block * bins;
+  for (int d = threadIdx.x; d < bins; d += kThreads)
+    if (cnt[d]) atomicAdd(&to[d], cnt[d]);
 }
 
-// hist[block][digit] of another digit.
-__global__ void __launch_bounds__(kThreads) k_sort_count(const int* __restrict__ key, int M, int shift, int bins,
-                                                         int per_block, int blocks, int* __restrict__ hist,
-                                                         const ZeroArgs z) {
+// hist[range][digit] of another digit.
+__global__ void __launch_bounds__(kSortThreads) k_sort_count(const int* __restrict__ key, int M, int shift, int bins,
+                                                             int per_block, int blocks, int* __restrict__ hist,
+                                                             const ZeroArgs z) {
   if (blockIdx.x >= blocks) return zero_rows(z, blockIdx.x - blocks);
   __shared__ int cnt[kMaxBins];
-  for (int d = threadIdx.x; d < bins; d += kThreads) cnt[d] = 0;
+  for (int d = threadIdx.x; d < bins; d += kSortThreads) cnt[d] = 0;
   __syncthreads();
-  const int lo = blockIdx.x * per_block, hi = min(M, lo + per_block);
-  for (int i = lo + threadIdx.x; i < hi; i += kThreads) atomicAdd(&cnt[(key[i] >> shift) & (bins - 1)], 1);
+  const int lo = blockIdx.x * kCount;
+  int k[kCount / kSortThreads];
+#pragma unroll
+  for (int s = 0; s < kCount / kSortThreads; ++s) {
+    const int i = lo + threadIdx.x + s * kSortThreads;
+    k[s] = i < M ? key[i] : -1;
+  }
+#pragma unroll
+  for (int s = 0; s < kCount / kSortThreads; ++s)
+    if (k[s] >= 0) atomicAdd(&cnt[(k[s] >> shift) & (bins - 1)], 1);
   __syncthreads();
-  for (int d = threadIdx.x; d < bins; d += kThreads) hist[blockIdx.x * bins + d] = cnt[d];
+  int* const to = hist + lo / per_block * bins;
+  for (int d = threadIdx.x; d < bins; d += kSortThreads)
+    if (cnt[d]) atomicAdd(&to[d], cnt[d]);
 }
 
 // Exclusive sum of total[0..bins) added into base, by the first warp.
@@ -190,7 +241,7 @@ __device__ __forceinline__ void scan_bins(const int* total, int* base, int bins)
 
 // Ranks of a tile: on return position dst of item s of this thread is
 // base[digit] + wcnt[warp][digit] + off[s]. dg < 0: no item. Uses two barriers.
-__device__ __forceinline__ void rank_tile(const int (&dg)[kItems], int (&off)[kItems], int (*wcnt)[kMaxBins],
+__device__ __forceinline__ void rank_tile(const int (&dg)[kItems], int (&off)[kItems], unsigned short (*wcnt)[kMaxBins],
                                           int* tile_total, int bins) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   for (int d = lane; d < bins; d += 32) wcnt[warp][d] = 0;
@@ -201,16 +252,16 @@ __device__ __forceinline__ void rank_tile(const int (&dg)[kItems], int (&off)[kI
     const int rank = __popc(same & ((1u << lane) - 1u));
     off[s] = dg[s] >= 0 ? wcnt[warp][dg[s]] + rank : 0;
     __syncwarp();
-    if (dg[s] >= 0 && rank == 0) wcnt[warp][dg[s]] += __popc(same);
+    if (dg[s] >= 0 && rank == 0) wcnt[warp][dg[s]] = static_cast<unsigned short>(off[s] + __popc(same));
     __syncwarp();
   }
   __syncthreads();
-  for (int d = tid; d < bins; d += kThreads) {
+  for (int d = tid; d < bins; d += kSortThreads) {
     int run = 0;
 #pragma unroll
     for (int w = 0; w < kSortWarps; ++w) {
       const int n = wcnt[w][d];
-      wcnt[w][d] = run;
+      wcnt[w][d] = static_cast<unsigned short>(run);
       run += n;
     }
     tile_total[d] = run;
@@ -220,17 +271,17 @@ __device__ __forceinline__ void rank_tile(const int (&dg)[kItems], int (&off)[kI
 
 // Places the block's range: position -> (positions with a smaller digit) + (earlier
 // blocks' with the same) + (its rank in the block). idx NULL: the positions themselves.
-__global__ void __launch_bounds__(kThreads) k_sort_place(const int* __restrict__ key, const int* __restrict__ idx,
+__global__ void __launch_bounds__(kSortThreads) k_sort_place(const int* __restrict__ key, const int* __restrict__ idx,
                                                          int M, int shift, int bins, int per_block, int blocks,
                                                          const int* __restrict__ hist, int* __restrict__ key_out,
                                                          int* __restrict__ idx_out, const ZeroArgs z) {
   if (blockIdx.x >= blocks) return zero_rows(z, blockIdx.x - blocks);
   __shared__ int base[kMaxBins], total[kMaxBins];
-  __shared__ int wcnt[kSortWarps][kMaxBins];
+  __shared__ unsigned short wcnt[kSortWarps][kMaxBins];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  for (int d = tid; d < bins; d += kThreads) {
+  for (int d = tid; d < bins; d += kSortThreads) {
     int before = 0, all = 0;
-#pragma unroll 16
+#pragma unroll 32
     for (int k = 0; k < blocks; ++k) {
       const int h = hist[k * bins + d];
       if (k < static_cast<int>(blockIdx.x)) before += h;
@@ -260,28 +311,26 @@ __global__ void __launch_bounds__(kThreads) k_sort_place(const int* __restrict__
       idx_out[at] = p[s];
     }
     __syncthreads();
-    for (int d = tid; d < bins; d += kThreads) base[d] += total[d];
+    for (int d = tid; d < bins; d += kSortThreads) base[d] += total[d];
     __syncthreads();
   }
 }
 
 // M <= kTile: keys and every pass in block 0; the other blocks zero dtable.
-__global__ void __launch_bounds__(kThreads) k_sort_one(RowSet rs, TokenView tok, int V, int M, int passes, int bits,
+template <bool I64>
+__global__ void __launch_bounds__(kSortThreads) k_sort_one(RowSet rs, TokenView tok, int V, int M, int passes, int bits,
                                                        int* __restrict__ key_out, int* __restrict__ idx_out,
                                                        const ZeroArgs z, unsigned* status) {
   if (blockIdx.x > 0) return zero_rows(z, blockIdx.x - 1);
   __shared__ int base[kMaxBins], total[kMaxBins];
-  __shared__ int wcnt[kSortWarps][kMaxBins];
+  __shared__ unsigned short wcnt[kSortWarps][kMaxBins];
   __shared__ int skey[kTile];
   __shared__ unsigned short sidx[kTile];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, bins = 1 << bits;
   int k[kItems], p[kItems], dg[kItems], off[kItems];
+  token_keys<I64, kItems>(rs, tok, V, warp * (32 * kItems) + lane, 32, M, k, status);
 #pragma unroll
-  for (int s = 0; s < kItems; ++s) {
-    const int i = warp * (32 * kItems) + s * 32 + lane;
-    k[s] = i < M ? token_key(rs, tok, V, i, status) : 0;
-    p[s] = i;
-  }
+  for (int s = 0; s < kItems; ++s) p[s] = warp * (32 * kItems) + s * 32 + lane;
   for (int pass = 0; pass < passes; ++pass) {
 #pragma unroll
     for (int s = 0; s < kItems; ++s) {
@@ -292,7 +341,7 @@ __global__ void __launch_bounds__(kThreads) k_sort_one(RowSet rs, TokenView tok,
       }
       dg[s] = i < M ? (k[s] >> (pass * bits)) & (bins - 1) : -1;
     }
-    for (int d = tid; d < bins; d += kThreads) base[d] = 0;
+    for (int d = tid; d < bins; d += kSortThreads) base[d] = 0;
     rank_tile(dg, off, wcnt, total, bins);
     if (warp == 0) scan_bins(total, base, bins);
     __syncthreads();
@@ -345,132 +394,174 @@ __device__ __forceinline__ void st_run(G* o, Vals<N> s, float scale, bool accumu
   st_wide<G, N>(o, s);
 }
 
-constexpr int kChunk = 64;                           // most positions of a chunk
-constexpr int kGroup = kThreads / 8 * kChunk;        // of a block (column tiles of 8 vectors)
+constexpr int kAhead = 8;                            // rows a thread has asked for and not added yet
+constexpr int kChunk = 32;                           // most positions of a chunk
+
+// Shared memory of a block: the rows in flight (later the pieces), then the rows'
+// offsets and keys.
+template <typename T, int N>
+constexpr int kFlightBytes = kThreads * (kAhead * N * int(sizeof(T)) > 8 * N ? kAhead * N * int(sizeof(T)) : 8 * N);
 
 template <typename T, typename G, int N>
-__global__ void __launch_bounds__(kThreads, 3) k_embed_sum(const SumArgs a) {
-  __shared__ int skey[kGroup + 2];  // skey[1 + i]: key of the block's position i, with its neighbours
-  __shared__ int sidx[kGroup];
-  __shared__ __align__(16) float piece[kThreads * 2 * N];
+__global__ void __launch_bounds__(kThreads, 4) k_embed_sum(const SumArgs a) {
+  extern __shared__ __align__(16) uint8_t smem[];
   const int tid = threadIdx.x, grp = blockIdx.x / a.tiles, tile = blockIdx.x - grp * a.tiles;
   const int per_block = a.teams * a.chunk;
-  const int g0 = grp * per_block, n = min(a.M - g0, per_block);
-  for (int i = tid; i < n + 2; i += kThreads) {
-    const int at = g0 + i - 1;
-    skey[i] = at >= 0 && at < a.M ? a.key[at] : -1;
+  // row[i]: the row of the block's position i; skey[1 + i]: its key, skey[0] the
+  // one before.
+  const T** const row = reinterpret_cast<const T**>(smem + kFlightBytes<T, N>);
+  int* const skey = reinterpret_cast<int*>(row + per_block);
+  __shared__ int snext, sn;  // key after the block's last position, -1 at the end; positions that are tokens
+  const int g0 = grp * per_block, n0 = min(a.M - g0, per_block);
+  if (a.key[g0] == a.V) return;  // sorted: none from here on
+  if (tid == 0) {
+    skey[0] = g0 > 0 ? a.key[g0 - 1] : -1;
+    snext = g0 + n0 < a.M ? a.key[g0 + n0] : -1;
+    sn = n0;
   }
-  for (int i = tid; i < n; i += kThreads) sidx[i] = a.idx[g0 + i];
   __syncthreads();
+  for (int i = tid; i < n0; i += kThreads) {
+    const int k = a.key[g0 + i], r = a.idx[g0 + i];
+    skey[1 + i] = k;
+    if (k == a.V) atomicMin(&sn, i);
+    int b, t;
+    locate(a.rs, r, b, t);
+    row[i] = row_of<T>(a.dout, b, t);
+  }
+  __syncthreads();
+  const int n = sn;
   const int team = tid / a.ct, j = tile * a.ct + (tid - team * a.ct);
   const bool on = j < a.nv;
   G* const table = static_cast<G*>(a.dtable) + j * N;
-  const int lo = min(n, team * a.chunk), hi = min(n, lo + a.chunk);
-  float* const mine = piece + tid * 2 * N;
+  // Key of position i of the block, i <= n.
+  auto key_at = [&](int i) { return i < n0 ? skey[1 + i] : snext; };
+  const int lo = team * a.chunk, hi = min(n, lo + a.chunk);
+  Vals<N> s = fill<N>(0.f), head = fill<N>(0.f);  // of the run in hand; of one begun earlier that ended here
+  bool begins = true;
   if (on && lo < hi) {
     int run = skey[1 + lo];
-    bool begins = run != skey[lo];
-    Vals<N> s = fill<N>(0.f);
-    constexpr int kAhead = 8;
+    begins = run != skey[lo];
+    // Rows arrive in this thread's own places of shared memory, kAhead - 1 of them
+    // on their way, so nothing but the thread waits for them.
+    Raw<T, N>* const flight = reinterpret_cast<Raw<T, N>*>(smem) + tid;
+#pragma unroll
+    for (int u = 0; u < kAhead - 1; ++u) {
+      if (lo + u < hi) copy_async<T, N>(flight + u * kThreads, row[lo + u] + j * N);
+      commit_async();
+    }
     for (int i0 = lo; i0 < hi; i0 += kAhead) {
-      Raw<T, N> raw[kAhead];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        raw[u] = Raw<T, N>{};
-        if (i0 + u < hi && skey[1 + i0 + u] != a.V) {
-          int b, t;
-          locate(a.rs, sidx[i0 + u], b, t);
-          raw[u] = ld_raw<T, N>(row_of<T>(a.dout, b, t) + j * N);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        if (i0 + u < hi) {
-          const int k = skey[1 + i0 + u];
+        const int i = i0 + u, next = i + kAhead - 1;
+        if (next < hi) copy_async<T, N>(flight + (u + kAhead - 1) % kAhead * kThreads, row[next] + j * N);
+        commit_async();
+        if (i < hi) {
+          wait_async<kAhead - 1>();
+          const Vals<N> v = unpack<T, N>(flight[u * kThreads]);
+          const int k = skey[1 + i];
           if (k != run) {  // `run` ends inside the chunk
             if (begins)
               st_run<G, N>(table + run * a.ld, s, a.scale, a.accumulate);
             else
-              st_floats<N>(mine, s);
+              head = s;
             run = k;
             begins = true;
             s = fill<N>(0.f);
           }
-          const Vals<N> v = unpack<T, N>(raw[u]);
 #pragma unroll
-          for (int i = 0; i < Vals<N>::P; ++i) s.p[i] = add2(s.p[i], v.p[i]);
+          for (int p = 0; p < Vals<N>::P; ++p) s.p[p] = add2(s.p[p], v.p[p]);
         }
       }
     }
-    if (!begins)
-      st_floats<N>(mine, s);
-    else if (skey[1 + hi] == run)
-      st_floats<N>(mine + N, s);
-    else if (run != a.V)
-      st_run<G, N>(table + run * a.ld, s, a.scale, a.accumulate);
+    if (begins && key_at(hi) != run) st_run<G, N>(table + run * a.ld, s, a.scale, a.accumulate);
+  }
+  // The pieces of shared runs go where the positions were: [0] of a run begun
+  // earlier, [1] of one that goes on. The first team's threads add them in order.
+  __syncthreads();
+  float* const piece = reinterpret_cast<float*>(smem);
+  if (on && lo < hi) {
+    const bool whole = skey[1 + lo] == skey[hi];  // one run
+    if (skey[1 + lo] == skey[lo]) st_floats<N>(piece + tid * 2 * N, whole ? s : head);
+    if (begins) st_floats<N>(piece + tid * 2 * N + N, s);
   }
   __syncthreads();
-  // The first team's threads go through the chunks' shared runs in order.
   if (team > 0 || !on) return;
-  Vals<N> s = fill<N>(0.f);
+  s = fill<N>(0.f);
   bool inside = false;  // the run being added began in this block
   for (int k = 0; k * a.chunk < n; ++k) {
     const int l = k * a.chunk, h = min(n, l + a.chunk);
     const float* pk = piece + (k * a.ct + tid) * 2 * N;
     const int first = skey[1 + l], last = skey[h];
     if (first == skey[l]) {
-      if (first != a.V) {
-        const Vals<N> v = ld_floats<N>(pk);
+      const Vals<N> v = ld_floats<N>(pk);
 #pragma unroll
-        for (int i = 0; i < Vals<N>::P; ++i) s.p[i] = add2(s.p[i], v.p[i]);
-        if (first != last || skey[1 + h] != first) {  // it ends in this chunk
-          if (inside)
-            st_run<G, N>(table + first * a.ld, s, a.scale, a.accumulate);
-          else
-            st_floats<N>(a.slots + (static_cast<size_t>(grp) * 2 * a.nv + j) * N, s);
-          s = fill<N>(0.f);
-        }
+      for (int i = 0; i < Vals<N>::P; ++i) s.p[i] = add2(s.p[i], v.p[i]);
+      if (first != last || key_at(h) != first) {  // it ends in this chunk
+        if (inside)
+          st_run<G, N>(table + first * a.ld, s, a.scale, a.accumulate);
+        else
+          st_floats<N>(a.slots + (static_cast<size_t>(grp) * 2 * a.nv + j) * N, s);
+        s = fill<N>(0.f);
       }
       if (first == last) continue;
     }
-    if (last != a.V && skey[1 + h] == last) {  // it begins in this chunk and goes on
+    if (key_at(h) == last) {  // it begins in this chunk and goes on
       s = ld_floats<N>(pk + N);
       inside = true;
     }
   }
-  if (n > 0 && skey[n] != a.V && skey[1 + n] == skey[n])
+  if (key_at(n) == skey[n])
     st_floats<N>(a.slots + ((static_cast<size_t>(grp) * 2 + (inside ? 1 : 0)) * a.nv + j) * N, s);
 }
 
-// Runs over several blocks: the threads of the block in which a run begins add its
-// slots in order.
+// Runs over several blocks, each added by a warp for 4 vectors: lane = slice * 4 +
+// vector, slice s of 8 taking every eighth of the run's blocks in order, the slices
+// then joined in a tree.
 template <typename G, int N>
 __global__ void __launch_bounds__(kThreads) k_embed_join(const SumArgs a) {
-  const long long id = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
-  const int c = static_cast<int>(id / a.nv), j = static_cast<int>(id - static_cast<long long>(c) * a.nv);
+  const int lane = threadIdx.x & 31, slice = lane >> 2, quads = (a.nv + 3) / 4;
+  const long long warp = static_cast<long long>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
+  const int c = static_cast<int>(warp / quads), j = static_cast<int>(warp - static_cast<long long>(c) * quads) * 4 + (lane & 3);
   const int per_block = a.teams * a.chunk;
   if (c >= a.groups - 1) return;
   const int lo = c * per_block, hi = lo + per_block;
   const int run = a.key[hi - 1];
   if (run == a.V || a.key[hi] != run || (lo > 0 && a.key[lo - 1] == run)) return;
-  int end = hi + 1, far = a.M;  // first position after the run
-  while (end < far) {
-    const int mid = end + (far - end) / 2;
-    if (a.key[mid] == run)
-      end = mid + 1;
-    else
-      far = mid;
-  }
-  const int last = (end - 1) / per_block;
   const size_t stride = static_cast<size_t>(a.nv) * N;
-  Vals<N> s = ld_floats<N>(a.slots + (static_cast<size_t>(c) * 2 + 1) * stride + j * N);
-#pragma unroll 8
-  for (int k = c + 1; k <= last; ++k) {
-    const Vals<N> v = ld_floats<N>(a.slots + static_cast<size_t>(k) * 2 * stride + j * N);
+  const float* slot = a.slots + static_cast<size_t>(min(j, a.nv - 1)) * N;
+  Vals<N> s = fill<N>(0.f);
+  if (slice == 0) s = ld_floats<N>(slot + (static_cast<size_t>(c) * 2 + 1) * stride);
+  // Block k has a piece if the run goes on at its first position.
+  constexpr int kAhead = 4;
+  bool more = true;
+  for (int k0 = c + 1 + slice; more; k0 += 8 * kAhead) {
+    Vals<N> v[kAhead];
+    bool has[kAhead];
 #pragma unroll
-    for (int i = 0; i < Vals<N>::P; ++i) s.p[i] = add2(s.p[i], v.p[i]);
+    for (int u = 0; u < kAhead; ++u) {
+      const int k = min(k0 + 8 * u, a.groups - 1);
+      has[u] = k0 + 8 * u < a.groups && a.key[k * per_block] == run;
+      v[u] = ld_floats<N>(slot + static_cast<size_t>(k) * 2 * stride);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      more = more && has[u];
+      if (more) {
+#pragma unroll
+        for (int i = 0; i < Vals<N>::P; ++i) s.p[i] = add2(s.p[i], v[u].p[i]);
+      }
+    }
   }
-  st_run<G, N>(static_cast<G*>(a.dtable) + run * a.ld + j * N, s, a.scale, a.accumulate);
+  __syncwarp();
+#pragma unroll
+  for (int o = 16; o >= 4; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < Vals<N>::P; ++i) {
+      s.p[i].x += __shfl_xor_sync(0xffffffffu, s.p[i].x, o);
+      s.p[i].y += __shfl_xor_sync(0xffffffffu, s.p[i].y, o);
+    }
+  if (slice == 0 && j < a.nv)
+    st_run<G, N>(static_cast<G*>(a.dtable) + run * a.ld + j * N, s, a.scale, a.accumulate);
 }
 
 size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -533,7 +624,7 @@ cudaError_t launch_embed(RowSet rs, TokenView tok, const void* table, bool bf16_
 
 namespace {
 
-// Positions of a chunk: 64, fewer where that leaves less than 131,072 threads.
+// Positions of a chunk: 32, fewer where that leaves less than 131,072 threads.
 int chunk_of(long long M, int nv) {
   int c = kChunk;
   while (c > 8 && M * nv / c < 131072) c >>= 1;
@@ -552,9 +643,15 @@ cudaError_t embed_sum(SumArgs a, cudaStream_t st) {
   a.groups = (a.M + a.teams * a.chunk - 1) / (a.teams * a.chunk);
   const long long blocks = static_cast<long long>(a.tiles) * a.groups;
   if (blocks > 0x7FFFFFFFLL) return cudaErrorInvalidConfiguration;
-  k_embed_sum<T, G, N><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(a);
+  const int smem = kFlightBytes<T, N> + a.teams * a.chunk * 12 + 16;
+  if (smem > 40 * 1024) {
+    const cudaError_t e =
+        cudaFuncSetAttribute(k_embed_sum<T, G, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+  }
+  k_embed_sum<T, G, N><<<static_cast<unsigned>(blocks), kThreads, smem, st>>>(a);
   if (a.groups > 1) {
-    const long long join = (static_cast<long long>(a.groups) * a.nv + kThreads - 1) / kThreads;
+    const long long join = (static_cast<long long>(a.groups) * ((a.nv + 3) / 4) + kThreads / 32 - 1) / (kThreads / 32);
     k_embed_join<G, N><<<static_cast<unsigned>(join), kThreads, 0, st>>>(a);
   }
   return cudaGetLastError();
@@ -591,7 +688,7 @@ EmbedWs embed_ws(int V, int d, long long M) {
   if (M > kTile) {
     w.key2 = take(M * 4);
     w.idx2 = take(M * 4);
-    w.hist = take(static_cast<size_t>(p.blocks) * p.bins * 4);
+    w.hist = take(static_cast<size_t>(p.passes) * p.blocks * p.bins * 4);
     w.present = take(V);
   }
   // Enough for every access width: the most groups of positions any of them makes.
@@ -625,7 +722,7 @@ cudaError_t launch_embed_grad(RowSet rs, TokenView tok, RowView dout, bool bf16_
   z.row_bytes = static_cast<size_t>(d) * es;
   z.stride = V > 1 ? static_cast<size_t>(ld_dtable) * es : z.row_bytes;
   z.unit = reinterpret_cast<uintptr_t>(dtable) % 16 == 0 && z.stride % 16 == 0 && z.row_bytes % 16 == 0 ? 16 : es;
-  z.rows = static_cast<int>(std::max<size_t>(8, 32768 / z.row_bytes));
+  z.rows = static_cast<int>(std::max<size_t>(kSortWarps, 65536 / z.row_bytes));
   // Part i of n of the rows.
   auto zero_part = [&](int i, int n) {
     z.v0 = static_cast<int>(static_cast<long long>(V) * i / n);
@@ -637,22 +734,27 @@ cudaError_t launch_embed_grad(RowSet rs, TokenView tok, RowView dout, bool bf16_
   int *key = ints(w.key), *idx = ints(w.idx);
   if (M <= kTile) {
     zero_part(0, 1);
-    k_sort_one<<<1 + z.blocks, kThreads, 0, st>>>(rs, tok, V, M, p.passes, p.bits, key, idx, z, status);
+    auto k = tok.i64 ? k_sort_one<true> : k_sort_one<false>;
+    k<<<1 + z.blocks, kSortThreads, 0, st>>>(rs, tok, V, M, p.passes, p.bits, key, idx, z, status);
   } else {
     int *key2 = ints(w.key2), *idx2 = ints(w.idx2), *hist = ints(w.hist);
     uint8_t* present = base + w.present;
-    if (cudaError_t e = cudaMemsetAsync(present, 0, V, st); e != cudaSuccess) return e;
-    k_sort_keys<<<p.blocks, kThreads, 0, st>>>(rs, tok, V, M, p.bins, p.per_block, key, present, hist, status);
+    const int count_blocks = (M + kCount - 1) / kCount;
+    // Marks and the counts of every digit, which lie together.
+    if (cudaError_t e = cudaMemsetAsync(base + w.hist, 0, w.slots - w.hist, st); e != cudaSuccess) return e;
+    auto k = tok.i64 ? k_sort_keys<true> : k_sort_keys<false>;
+    k<<<count_blocks, kThreads, 0, st>>>(rs, tok, V, M, p.bins, p.per_block, key, present, hist, status);
     z.present = present;
     const int parts = 2 * p.passes - 1;
     for (int s = 0; s < p.passes; ++s) {
       if (s > 0) {
         zero_part(2 * s - 1, parts);
-        k_sort_count<<<p.blocks + z.blocks, kThreads, 0, st>>>(key, M, s * p.bits, p.bins, p.per_block, p.blocks, hist,
-                                                               z);
+        hist += static_cast<size_t>(p.blocks) * p.bins;
+        k_sort_count<<<count_blocks + z.blocks, kSortThreads, 0, st>>>(key, M, s * p.bits, p.bins, p.per_block,
+                                                                       count_blocks, hist, z);
       }
       zero_part(2 * s, parts);
-      k_sort_place<<<p.blocks + z.blocks, kThreads, 0, st>>>(key, s ? idx : nullptr, M, s * p.bits, p.bins, p.per_block,
+      k_sort_place<<<p.blocks + z.blocks, kSortThreads, 0, st>>>(key, s ? idx : nullptr, M, s * p.bits, p.bins, p.per_block,
                                                              p.blocks, hist, key2, idx2, z);
       std::swap(key, key2);
       std::swap(idx, idx2);

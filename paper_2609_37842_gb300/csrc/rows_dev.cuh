@@ -109,6 +109,24 @@ __device__ __forceinline__ Raw<T, N> ld_keep(const T* p) {
   return r;
 }
 
+// Asynchronous copy of N elements into shared memory; of two bytes, which have no
+// such copy, a plain one.
+template <typename T, int N>
+__device__ __forceinline__ void copy_async(Raw<T, N>* dst, const T* src) {
+  constexpr int B = N * sizeof(T);
+  if constexpr (B == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+  else if constexpr (B >= 4)
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(dst)), "l"(src), "n"(B) : "memory");
+  else
+    dst->w = *src;
+}
+__device__ __forceinline__ void commit_async() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void wait_async() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+}
+
 // The N values as fp32 pairs (N = 1: the first of a pair), for the paired fp32
 // instructions.
 template <int N>
