@@ -557,8 +557,8 @@ int eogp_score_topk(const void* train, int ld_train, const float* train_scales, 
  * convenience with no counterpart in it.
  *
  * Conventions of these calls:
- *  - B examples of T tokens, B * T <= 2^30. Rows of width n (d or V) are
- *    contiguous; row (b, t) of an array starts at element b * bs + t * ld of its
+ *  - B examples of T tokens, B * T <= 2^30 (as V and d). Rows of width n (d
+ *    or V) are contiguous; row (b, t) of an array starts at element b * bs + t * ld of its
  *    base ("_bs" and "_ld" arguments, in elements, long long; any offset that
  *    fits 63 bits). Inputs may use any strides >= 0 (0 repeats a row); outputs
  *    must not overlap themselves: ld >= n and bs >= (T - 1) ld + n, or

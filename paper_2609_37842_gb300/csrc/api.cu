@@ -1497,6 +1497,13 @@ int check_rows(int B, int T) {
   return EOGP_OK;
 }
 
+// Table rows, classes or channels.
+int check_extent(int n, const char* name) {
+  if (n < 1) return set_error(EOGP_EINVAL, "%s must be >= 1", name);
+  if (n > (1 << 30)) return set_error(EOGP_EUNSUPPORTED, "%s must be <= 2^30", name);
+  return EOGP_OK;
+}
+
 }  // namespace
 
 extern "C" int eogp_embed(const void* tokens, int index_type, long long tokens_bs, const void* table, int dtype,
@@ -1507,7 +1514,8 @@ extern "C" int eogp_embed(const void* tokens, int index_type, long long tokens_b
   if (int rc = check_rows(B, T)) return rc;
   if (!index_type_ok(index_type)) return set_error(EOGP_EINVAL, "bad index_type");
   if (!elem_type(dtype)) return set_error(EOGP_EINVAL, "bad dtype");
-  if (V < 1 || d < 1) return set_error(EOGP_EINVAL, "V and d must be >= 1");
+  if (int rc = check_extent(V, "V")) return rc;
+  if (int rc = check_extent(d, "d")) return rc;
   if (B == 0 || T == 0) return EOGP_OK;
   if (!tokens || !table || !out) return set_error(EOGP_EINVAL, "NULL argument");
   if (!aligned_to(tokens, index_type) || !aligned_to(table, dtype) || !aligned_to(pos, dtype) ||
@@ -1529,7 +1537,8 @@ extern "C" int eogp_embed_grad_workspace_size(int V, int d, int B, int T, size_t
   clear_error();
   if (!bytes) return set_error(EOGP_EINVAL, "bytes is NULL");
   if (int rc = check_rows(B, T)) return rc;
-  if (V < 1 || d < 1) return set_error(EOGP_EINVAL, "V and d must be >= 1");
+  if (int rc = check_extent(V, "V")) return rc;
+  if (int rc = check_extent(d, "d")) return rc;
   *bytes = embed_grad_ws_bytes(V, d, static_cast<long long>(B) * T);
   return EOGP_OK;
 }
@@ -1570,7 +1579,7 @@ extern "C" int eogp_norm(int kind, const void* x, int dtype, long long x_bs, lon
   if (int rc = check_rows(B, T)) return rc;
   if (kind != EOGP_NORM_LAYER && kind != EOGP_NORM_RMS) return set_error(EOGP_EINVAL, "bad norm kind");
   if (!elem_type(dtype) || !elem_type(param_dtype)) return set_error(EOGP_EINVAL, "bad dtype");
-  if (d < 1) return set_error(EOGP_EINVAL, "d must be >= 1");
+  if (int rc = check_extent(d, "d")) return rc;
   if (!(eps >= 0.f) || !std::isfinite(eps)) return set_error(EOGP_EINVAL, "eps must be finite and >= 0");
   if (B == 0 || T == 0) return EOGP_OK;
   if (!x || !y) return set_error(EOGP_EINVAL, "NULL argument");
@@ -1592,7 +1601,7 @@ extern "C" int eogp_norm_grad_workspace_size(int B, int T, int d, int per_exampl
   clear_error();
   if (!bytes) return set_error(EOGP_EINVAL, "bytes is NULL");
   if (int rc = check_rows(B, T)) return rc;
-  if (d < 1) return set_error(EOGP_EINVAL, "d must be >= 1");
+  if (int rc = check_extent(d, "d")) return rc;
   *bytes = norm_grad_ws_bytes(B, T, d, sm_count());
   return EOGP_OK;
 }
@@ -1643,7 +1652,7 @@ extern "C" int eogp_cross_entropy(const void* logits, int dtype, long long logit
   if (int rc = check_rows(B, T)) return rc;
   if (!elem_type(dtype)) return set_error(EOGP_EINVAL, "bad dtype");
   if (!index_type_ok(index_type)) return set_error(EOGP_EINVAL, "bad index_type");
-  if (V < 1) return set_error(EOGP_EINVAL, "V must be >= 1");
+  if (int rc = check_extent(V, "V")) return rc;
   if (B == 0 || T == 0) return EOGP_OK;
   if (!logits || !targets || !loss) return set_error(EOGP_EINVAL, "NULL argument");
   if (!aligned_to(logits, dtype) || !aligned_to(dlogits, dtype) || !aligned_to(targets, index_type) ||

@@ -123,6 +123,14 @@ __device__ __forceinline__ void cluster_sync_all() {
                    : "memory");
 }
 
+// The two halves of it apart.
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 // Registers the expected TMA bytes on a (possibly remote) barrier; relaxed: the
 // data itself is tracked by the transaction count, nothing else needs ordering.
 __device__ __forceinline__ void mbar_arrive_expect_tx_cluster(uint32_t cl_addr, uint32_t bytes) {

@@ -165,6 +165,18 @@ __device__ __forceinline__ uint32_t pack_bf16(float2 v) {
   return *reinterpret_cast<const uint32_t*>(&p);
 }
 
+// The values rounded to T, as raw words of 16 bytes.
+template <typename T, int N>
+__device__ __forceinline__ Raw<T, N> pack_raw(const Vals<N>& v) {
+  Raw<T, N> r;
+  if constexpr (sizeof(T) == 4)
+    r.w = make_uint4(__float_as_uint(v.p[0].x), __float_as_uint(v.p[0].y), __float_as_uint(v.p[1].x),
+                     __float_as_uint(v.p[1].y));
+  else
+    r.w = make_uint4(pack_bf16(v.p[0]), pack_bf16(v.p[1]), pack_bf16(v.p[2]), pack_bf16(v.p[3]));
+  return r;
+}
+
 // Streaming store, rounded once to T.
 template <typename T, int N>
 __device__ __forceinline__ void st_vals(T* p, const Vals<N>& v) {
