@@ -786,14 +786,17 @@ def fit_pca_from_moment(C, n_total: int, k: int, pt_dtype: int = F32, stream=Non
 
 
 # -------------------------------------------------------------- model ends
-def _btn(t, name: str):
+# Small calls cost as much on the host as on the device: these functions look at a
+# tensor once, and only check what the caller gave.
+def _rows_of(t, name: str):
     """(B, T, n, example stride, token stride) of rows [B, T, n] or [T, n]."""
-    if t.dim() == 3:
-        B, T, n = t.shape
-        bs, ld, inner = t.stride()
-    elif t.dim() == 2:
-        B, (T, n) = 1, t.shape
-        bs, (ld, inner) = 0, t.stride()
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 3:
+        B, T, n = shape
+        bs, ld, inner = stride
+    elif len(shape) == 2:
+        (T, n), B = shape, 1
+        bs, (ld, inner) = 0, stride
     else:
         raise ValueError(f"{name} must be [B, T, n] or [T, n]")
     if inner != 1 and n > 1 and B * T > 0:
@@ -801,48 +804,71 @@ def _btn(t, name: str):
     return B, T, n, bs, ld
 
 
-def _index_code(t) -> int:
-    import torch
-    if t.dtype == torch.int64:
-        return I64
-    if t.dtype == torch.int32:
-        return I32
-    raise ValueError(f"unsupported dtype {t.dtype} for token numbers (int32 or int64)")
-
-
-def _bt(t, name: str):
-    """(B, T, example stride) of token numbers [B, T] or [T]."""
-    if t.dim() == 2:
-        B, T = t.shape
-        bs, inner = t.stride()
-    elif t.dim() == 1:
-        B, T = 1, t.shape[0]
-        bs, inner = 0, t.stride(0)
+def _tokens_of(t, name: str):
+    """(B, T, example stride, type code) of token numbers [B, T] or [T]."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 2:
+        B, T = shape
+        bs, inner = stride
+    elif len(shape) == 1:
+        B, T, bs, inner = 1, shape[0], 0, stride[0]
     else:
         raise ValueError(f"{name} must be [B, T] or [T]")
     if inner != 1 and T > 1 and B > 0:
         raise ValueError(f"{name} must have unit stride along its last dimension")
-    return B, T, bs
+    code = _type_codes().get(t.dtype)
+    if code != I64 and code != I32:
+        raise ValueError(f"unsupported dtype {t.dtype} for token numbers (int32 or int64)")
+    return B, T, bs, code
+
+
+_CODES = {}
+
+
+def _type_codes():
+    """Type codes by torch dtype (torch is imported with the first call)."""
+    if not _CODES:
+        import torch
+        _CODES.update({torch.float32: F32, torch.bfloat16: BF16, torch.int32: I32, torch.int64: I64})
+    return _CODES
+
+
+def _float_code(t, name: str) -> int:
+    code = _type_codes().get(t.dtype)
+    if code != F32 and code != BF16:
+        raise ValueError(f"{name} has unsupported dtype {t.dtype} (float32 or bfloat16)")
+    return code
 
 
 def _like(t, name: str, shape, dtype):
     """Require a tensor of this shape and type; returns t."""
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     return t
 
 
-def _on_device(*tensors):
-    """All tensors (None allowed) on one CUDA device: its kernels read them by address."""
+def _device_of(*tensors):
+    """The CUDA device that all tensors (None allowed) are on: kernels read them by address."""
     dev = None
     for t in tensors:
         if t is not None:
-            if not t.is_cuda or (dev is not None and t.device != dev):
+            d = t.device
+            if dev is None:
+                if d.type != "cuda":
+                    raise ValueError("all tensors must be on the same CUDA device")
+                dev = d
+            elif d != dev:
                 raise ValueError("all tensors must be on the same CUDA device")
-            dev = t.device
     return dev
+
+
+def _stream_on(stream, dev) -> int:
+    import torch
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev.index)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 _NO_CONTEXT = contextlib.nullcontext()
@@ -857,35 +883,41 @@ def _pool(stream):
     return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
 
 
-def _lengths(lengths, B: int):
+def _lengths_ptr(lengths, B: int):
     import torch
-    if lengths is not None:
-        _dense(_like(lengths, "lengths", (B,), torch.int32), "lengths")
-    return _ptr(lengths)
+    if lengths is None:
+        return None
+    return _dense(_like(lengths, "lengths", (B,), torch.int32), "lengths").data_ptr()
 
 
 def embed(tokens, table, scale: float = 1.0, pos=None, lengths=None, out=None, stream=None):
     """eogp_embed: scale * table[tokens] (+ pos rows 0..T-1) for tokens [B, T] or [T], table [V, d],
     pos [>= T, d]. Returns out [B, T, d] (or [T, d]); rows of padding (t >= lengths[b]) are 0."""
     import torch
-    dev = _on_device(tokens, table, pos, lengths, out)
-    B, T, tbs = _bt(tokens, "tokens")
+    dev = _device_of(tokens, table, pos, lengths, out)
+    B, T, tbs, icode = _tokens_of(tokens, "tokens")
+    code = _float_code(table, "table")
     if table.dim() != 2:
         raise ValueError("table must be [V, d]")
-    _rows(table, "table")
     V, d = table.shape
+    ldt, inner = table.stride()
+    if inner != 1 and d > 1:
+        raise ValueError("table must have unit stride along its last dimension")
+    ldp = 0
     if pos is not None:
-        _rows(pos, "pos")
         if pos.dim() != 2 or pos.dtype != table.dtype or pos.shape[1] != d or pos.shape[0] < T:
             raise ValueError(f"pos must be [>= {T}, {d}] of {table.dtype}")
+        ldp = _rows(pos, "pos").stride(0)
+    shape = (*tokens.shape, d)
     if out is None:
         with _pool(stream):
-            out = torch.empty((*tokens.shape, d), dtype=table.dtype, device=dev)
-    _like(out, "out", (*tokens.shape, d), table.dtype)
-    _, _, _, obs, old = _btn(out, "out")
-    _check(lib().eogp_embed(tokens.data_ptr(), _index_code(tokens), tbs, table.data_ptr(), _dtype_code(table), V, d,
-                            table.stride(0), float(scale), _ptr(pos), 0 if pos is None else pos.stride(0),
-                            _lengths(lengths, B), B, T, out.data_ptr(), obs, old, _stream(stream)))
+            out = torch.empty(shape, dtype=table.dtype, device=dev)
+        obs, old = T * d, d
+    else:
+        _, _, _, obs, old = _rows_of(_like(out, "out", shape, table.dtype), "out")
+    L = lib()
+    _check(L.eogp_embed(tokens.data_ptr(), icode, tbs, table.data_ptr(), code, V, d, ldt, scale, _ptr(pos), ldp,
+                        _lengths_ptr(lengths, B), B, T, out.data_ptr(), obs, old, _stream_on(stream, dev)))
     return out
 
 
@@ -894,28 +926,27 @@ def embed_grad(tokens, dout, V: int, scale: float = 1.0, lengths=None, dtable=No
     """eogp_embed_grad: dtable [V, d] (+)= scale * the sum of dout's rows of each token. dtable may be given,
     else it is a new tensor of `dtype` (default float32). Gradient of `pos` in embed: tokens 0..T-1, V = its rows."""
     import torch
-    dev = _on_device(tokens, dout, lengths, dtable, ws)
-    B, T, tbs = _bt(tokens, "tokens")
-    if tuple(dout.shape[:-1]) != tuple(tokens.shape):
+    dev = _device_of(tokens, dout, lengths, dtable, ws)
+    B, T, tbs, icode = _tokens_of(tokens, "tokens")
+    code = _float_code(dout, "dout")
+    if dout.shape[:-1] != tokens.shape:
         raise ValueError("dout must be [*tokens.shape, d]")
-    _, _, d, dbs, dld = _btn(dout, "dout")
-    if dtable is None:
-        if accumulate:
-            raise ValueError("accumulate needs dtable")
-        with _pool(stream):
-            dtable = torch.empty((int(V), d), dtype=dtype or torch.float32, device=dev)
-    _like(dtable, "dtable", (int(V), d), dtype or dtable.dtype)
-    _rows(dtable, "dtable")
+    _, _, d, dbs, dld = _rows_of(dout, "dout")
     L = lib()
     need = c_size_t()
-    _check(L.eogp_embed_grad_workspace_size(int(V), d, B, T, ctypes.byref(need)))
-    if ws is None:
-        with _pool(stream):
+    _check(L.eogp_embed_grad_workspace_size(V, d, B, T, need))
+    with _pool(stream):
+        if dtable is None:
+            if accumulate:
+                raise ValueError("accumulate needs dtable")
+            dtable = torch.empty((V, d), dtype=dtype or torch.float32, device=dev)
+        else:
+            _rows(_like(dtable, "dtable", (V, d), dtype or dtable.dtype), "dtable")
+        if ws is None:
             ws = workspace(need.value, dev)
-    _check(L.eogp_embed_grad(tokens.data_ptr(), _index_code(tokens), tbs, dout.data_ptr(), _dtype_code(dout), dbs, dld,
-                             _lengths(lengths, B), B, T, int(V), d, float(scale), dtable.data_ptr(),
-                             _dtype_code(dtable), dtable.stride(0), 1 if accumulate else 0, ws.data_ptr(), ws.numel(),
-                             _stream(stream)))
+    _check(L.eogp_embed_grad(tokens.data_ptr(), icode, tbs, dout.data_ptr(), code, dbs, dld, _lengths_ptr(lengths, B),
+                             B, T, V, d, scale, dtable.data_ptr(), _float_code(dtable, "dtable"), dtable.stride(0),
+                             1 if accumulate else 0, ws.data_ptr(), ws.numel(), _stream_on(stream, dev)))
     return dtable
 
 
@@ -924,10 +955,10 @@ def _norm_params(weight, bias, d: int):
     code = F32
     for t, name in ((weight, "weight"), (bias, "bias")):
         if t is not None:
-            if tuple(t.shape) != (d,):
+            if t.shape != (d,):
                 raise ValueError(f"{name} must have shape ({d},), got {tuple(t.shape)}")
             _dense(t, name)
-            code = _dtype_code(t)
+            code = _float_code(t, name)
     if weight is not None and bias is not None and weight.dtype != bias.dtype:
         raise ValueError("weight and bias must have one dtype")
     return code
@@ -938,20 +969,23 @@ def norm(x, weight=None, bias=None, kind: int = NORM_LAYER, eps: float = 1e-5, l
     """eogp_norm on rows x [B, T, d] or [T, d]. Returns (y, mean, rstd); mean is None for NORM_RMS. Rows of
     padding (t >= lengths[b]) are 0. `out` may be x."""
     import torch
-    dev = _on_device(x, weight, bias, lengths, out)
-    B, T, d, xbs, xld = _btn(x, "x")
-    code = _norm_params(weight, bias, d)
+    dev = _device_of(x, weight, bias, lengths, out)
+    B, T, d, xbs, xld = _rows_of(x, "x")
+    code = _float_code(x, "x")
+    pcode = _norm_params(weight, bias, d)
+    shape = x.shape
     with _pool(stream):
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev) if kind == NORM_LAYER else None
-        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev)
-    _like(out, "out", x.shape, x.dtype)
-    _, _, _, ybs, yld = _btn(out, "out")
-    _check(lib().eogp_norm(int(kind), x.data_ptr(), _dtype_code(x), xbs, xld, _ptr(weight), _ptr(bias), code,
-                           float(eps), _lengths(lengths, B), B, T, d, out.data_ptr(), ybs, yld, _ptr(mean),
-                           rstd.data_ptr(), _stream(stream)))
-    return out, mean, rstd
+        y = torch.empty(shape, dtype=x.dtype, device=dev) if out is None else out
+        rstd = torch.empty(shape[:-1], dtype=torch.float32, device=dev)
+        mean = torch.empty(shape[:-1], dtype=torch.float32, device=dev) if kind == NORM_LAYER else None
+    if out is None:
+        ybs, yld = T * d, d
+    else:
+        _, _, _, ybs, yld = _rows_of(_like(out, "out", shape, x.dtype), "out")
+    _check(lib().eogp_norm(kind, x.data_ptr(), code, xbs, xld, _ptr(weight), _ptr(bias), pcode, eps,
+                           _lengths_ptr(lengths, B), B, T, d, y.data_ptr(), ybs, yld, _ptr(mean), rstd.data_ptr(),
+                           _stream_on(stream, dev)))
+    return y, mean, rstd
 
 
 def norm_grad(dy, x, mean, rstd, weight=None, kind: int = NORM_LAYER, lengths=None, per_example: bool = False,
@@ -960,44 +994,51 @@ def norm_grad(dy, x, mean, rstd, weight=None, kind: int = NORM_LAYER, lengths=No
     """eogp_norm_grad from norm's mean and rstd. Returns (dx, dweight, dbias), None where not wanted. dweight and
     dbias are fp32 [d], or [B, d] with per_example; given tensors are written, or added to with accumulate."""
     import torch
-    dev = _on_device(dy, x, mean, rstd, weight, lengths, dx, dweight, dbias, ws)
-    B, T, d, xbs, xld = _btn(x, "x")
-    _like(dy, "dy", x.shape, x.dtype)
-    _, _, _, dybs, dyld = _btn(dy, "dy")
-    for t, name in ((mean, "mean"), (rstd, "rstd")):
-        if t is not None:
-            _dense(_like(t, name, x.shape[:-1], torch.float32), name)
-    code = _norm_params(weight, None, d)
-    shape = (B, d) if per_example else (d,)
+    dev = _device_of(dy, x, mean, rstd, weight, lengths, dx, dweight, dbias, ws)
+    B, T, d, xbs, xld = _rows_of(x, "x")
+    code = _float_code(x, "x")
+    _, _, _, dybs, dyld = _rows_of(_like(dy, "dy", x.shape, x.dtype), "dy")
+    shape = x.shape
+    if mean is not None:
+        _dense(_like(mean, "mean", shape[:-1], torch.float32), "mean")
+    _dense(_like(rstd, "rstd", shape[:-1], torch.float32), "rstd")
+    pcode = _norm_params(weight, None, d)
     if accumulate and ((want_dweight and dweight is None) or (want_dbias and dbias is None)):
         raise ValueError("accumulate needs dweight and dbias")
-    L = lib()
-    with _pool(stream):
-        if dx is None and want_dx:
-            dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        if dweight is None and want_dweight:
-            dweight = torch.empty(shape, dtype=torch.float32, device=dev)
-        if dbias is None and want_dbias:
-            dbias = torch.empty(shape, dtype=torch.float32, device=dev)
-        if ws is None and (dweight is not None or dbias is not None):
-            need = c_size_t()
-            _check(L.eogp_norm_grad_workspace_size(B, T, d, 1 if per_example else 0, ctypes.byref(need)))
-            ws = workspace(need.value, dev)
-    dxbs = dxld = 0
-    if dx is not None:
-        _like(dx, "dx", x.shape, x.dtype)
-        _, _, _, dxbs, dxld = _btn(dx, "dx")
+    pshape = (B, d) if per_example else (d,)
     ldp = d
     for t, name in ((dweight, "dweight"), (dbias, "dbias")):
         if t is not None:
-            _rows(_like(t, name, shape, torch.float32), name)
-            ldp = t.stride(0) if per_example else d
-    if dweight is not None and dbias is not None and per_example and dweight.stride(0) != dbias.stride(0):
-        raise ValueError("dweight and dbias must have the same row stride")
-    _check(L.eogp_norm_grad(int(kind), dy.data_ptr(), dybs, dyld, x.data_ptr(), _dtype_code(x), xbs, xld, _ptr(mean),
-                            _ptr(rstd), _ptr(weight), code, _lengths(lengths, B), B, T, d, _ptr(dx), dxbs, dxld,
-                            _ptr(dweight), _ptr(dbias), ldp, 1 if per_example else 0, 1 if accumulate else 0, _ptr(ws),
-                            0 if ws is None else ws.numel(), _stream(stream)))
+            _rows(_like(t, name, pshape, torch.float32), name)
+            if per_example:
+                ldp = t.stride(0)
+    given = (dweight is not None) + (dbias is not None)
+    if per_example and B > 1 and given:
+        if given == 2 and dweight.stride(0) != dbias.stride(0):
+            raise ValueError("dweight and dbias must have the same row stride")
+        if given == 1 and ldp != d and (want_dweight if dweight is None else want_dbias):
+            raise ValueError("give both dweight and dbias, or none, or rows that follow each other")
+    L = lib()
+    with _pool(stream):
+        if dx is not None:
+            _, _, _, dxbs, dxld = _rows_of(_like(dx, "dx", shape, x.dtype), "dx")
+        elif want_dx:
+            dx = torch.empty(shape, dtype=x.dtype, device=dev)
+            dxbs, dxld = T * d, d
+        else:
+            dxbs = dxld = 0
+        if dweight is None and want_dweight:
+            dweight = torch.empty(pshape, dtype=torch.float32, device=dev)
+        if dbias is None and want_dbias:
+            dbias = torch.empty(pshape, dtype=torch.float32, device=dev)
+        if ws is None and (dweight is not None or dbias is not None):
+            need = c_size_t()
+            _check(L.eogp_norm_grad_workspace_size(B, T, d, 1 if per_example else 0, need))
+            ws = workspace(need.value, dev)
+    _check(L.eogp_norm_grad(kind, dy.data_ptr(), dybs, dyld, x.data_ptr(), code, xbs, xld, _ptr(mean), rstd.data_ptr(),
+                            _ptr(weight), pcode, _lengths_ptr(lengths, B), B, T, d, _ptr(dx), dxbs, dxld, _ptr(dweight),
+                            _ptr(dbias), ldp, 1 if per_example else 0, 1 if accumulate else 0, _ptr(ws),
+                            0 if ws is None else ws.numel(), _stream_on(stream, dev)))
     return dx, dweight, dbias
 
 
@@ -1006,24 +1047,25 @@ def cross_entropy(logits, targets, weights=None, lengths=None, ignore_index: int
     """eogp_cross_entropy on logits [B, T, V] or [T, V] with targets [B, T] or [T]. Returns (loss, lse, dlogits):
     fp32 per position, and the gradient of the sum of the losses (None without want_grad). `dlogits` may be logits."""
     import torch
-    dev = _on_device(logits, targets, weights, lengths, dlogits)
-    B, T, V, lbs, lld = _btn(logits, "logits")
-    if tuple(targets.shape) != tuple(logits.shape[:-1]):
+    dev = _device_of(logits, targets, weights, lengths, dlogits)
+    B, T, V, lbs, lld = _rows_of(logits, "logits")
+    code = _float_code(logits, "logits")
+    shape = targets.shape
+    if shape != logits.shape[:-1]:
         raise ValueError("targets must have the shape of logits without its last dimension")
-    _, _, tbs = _bt(targets, "targets")
+    _, _, tbs, icode = _tokens_of(targets, "targets")
     if weights is not None:
-        _dense(_like(weights, "weights", targets.shape, torch.float32), "weights")
-    with _pool(stream):
-        loss = torch.empty(targets.shape, dtype=torch.float32, device=dev)
-        lse = torch.empty(targets.shape, dtype=torch.float32, device=dev)
-        if dlogits is None and want_grad:
-            dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+        _dense(_like(weights, "weights", shape, torch.float32), "weights")
     gbs = gld = 0
     if dlogits is not None:
-        _like(dlogits, "dlogits", logits.shape, logits.dtype)
-        _, _, _, gbs, gld = _btn(dlogits, "dlogits")
-    _check(lib().eogp_cross_entropy(logits.data_ptr(), _dtype_code(logits), lbs, lld, targets.data_ptr(),
-                                    _index_code(targets), tbs, _ptr(weights), int(ignore_index), _lengths(lengths, B),
-                                    B, T, V, loss.data_ptr(), lse.data_ptr(), _ptr(dlogits), gbs, gld,
-                                    _stream(stream)))
+        _, _, _, gbs, gld = _rows_of(_like(dlogits, "dlogits", logits.shape, logits.dtype), "dlogits")
+    with _pool(stream):
+        loss = torch.empty(shape, dtype=torch.float32, device=dev)
+        lse = torch.empty(shape, dtype=torch.float32, device=dev)
+        if dlogits is None and want_grad:
+            dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+            gbs, gld = T * V, V
+    _check(lib().eogp_cross_entropy(logits.data_ptr(), code, lbs, lld, targets.data_ptr(), icode, tbs, _ptr(weights),
+                                    ignore_index, _lengths_ptr(lengths, B), B, T, V, loss.data_ptr(), lse.data_ptr(),
+                                    _ptr(dlogits), gbs, gld, _stream_on(stream, dev)))
     return loss, lse, dlogits
