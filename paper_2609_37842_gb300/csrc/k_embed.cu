@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(kThreads) k_embed(RowSet rs, TokenView tok, co
       Vals<N> x = unpack<T, N>(e[k][j]), y = fill<N>(0.f);
       if (q) y = unpack<T, N>(ld_keep<T, N>(q + c));
 #pragma unroll
-      for (int i = 0; i < Vals<N>::P; ++i) x.p[i] = fma2(x.p[i], pair(scale), y.p[i]);
+      for (int i = 0; i < Vals<N>::P; ++i) x.p[i] = fma2(x.p[i], Vals<N>::all(scale), y.p[i]);
       st_vals<T, N>(o + c, x);
     }
   }
@@ -383,12 +383,11 @@ struct SumArgs {
 template <typename G, int N>
 __device__ __forceinline__ void st_run(G* o, Vals<N> s, float scale, bool accumulate) {
 #pragma unroll
-  for (int i = 0; i < Vals<N>::P; ++i) s.p[i] = mul2(s.p[i], pair(scale));
+  for (int i = 0; i < Vals<N>::P; ++i) s.p[i] = mul2(s.p[i], Vals<N>::all(scale));
   if (accumulate) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float v = to_f32(o[i]) + (i & 1 ? s.p[i / 2].y : s.p[i / 2].x);
-      (i & 1 ? s.p[i / 2].y : s.p[i / 2].x) = v;
+      s.set(i, to_f32(o[i]) + s.get(i));
     }
   }
   st_wide<G, N>(o, s);
@@ -556,10 +555,7 @@ __global__ void __launch_bounds__(kThreads) k_embed_join(const SumArgs a) {
 #pragma unroll
   for (int o = 16; o >= 4; o >>= 1)
 #pragma unroll
-    for (int i = 0; i < Vals<N>::P; ++i) {
-      s.p[i].x += __shfl_xor_sync(0xffffffffu, s.p[i].x, o);
-      s.p[i].y += __shfl_xor_sync(0xffffffffu, s.p[i].y, o);
-    }
+    for (int i = 0; i < N; ++i) s.set(i, s.get(i) + __shfl_xor_sync(0xffffffffu, s.get(i), o));
   if (slice == 0 && j < a.nv)
     st_run<G, N>(static_cast<G*>(a.dtable) + run * a.ld + j * N, s, a.scale, a.accumulate);
 }

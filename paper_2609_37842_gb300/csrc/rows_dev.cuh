@@ -127,19 +127,31 @@ __device__ __forceinline__ void wait_async() {
   asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
 }
 
-// The N values as fp32 pairs (N = 1: the first of a pair), for the paired fp32
-// instructions.
+// The N values in fp32: pairs, for the paired instructions, or a single one.
 template <int N>
 struct Vals {
-  static constexpr int P = (N + 1) / 2;
-  float2 p[P];
+  using E = float2;
+  static constexpr int P = N / 2;
+  E p[P];
+  __device__ __forceinline__ float get(int i) const { return i & 1 ? p[i / 2].y : p[i / 2].x; }
+  __device__ __forceinline__ void set(int i, float x) { (i & 1 ? p[i / 2].y : p[i / 2].x) = x; }
+  static __device__ __forceinline__ E all(float x) { return make_float2(x, x); }
+};
+template <>
+struct Vals<1> {
+  using E = float;
+  static constexpr int P = 1;
+  E p[P];
+  __device__ __forceinline__ float get(int) const { return p[0]; }
+  __device__ __forceinline__ void set(int, float x) { p[0] = x; }
+  static __device__ __forceinline__ E all(float x) { return x; }
 };
 
 template <typename T, int N>
 __device__ __forceinline__ Vals<N> unpack(const Raw<T, N>& r) {
   Vals<N> v;
   if constexpr (N == 1) {
-    v.p[0] = make_float2(to_f32(r.w), 0.f);
+    v.p[0] = to_f32(r.w);
   } else if constexpr (sizeof(T) == 4) {
     v.p[0] = make_float2(__uint_as_float(r.w.x), __uint_as_float(r.w.y));
     if constexpr (N == 4) v.p[1] = make_float2(__uint_as_float(r.w.z), __uint_as_float(r.w.w));
@@ -181,7 +193,7 @@ __device__ __forceinline__ Raw<T, N> pack_raw(const Vals<N>& v) {
 template <typename T, int N>
 __device__ __forceinline__ void st_vals(T* p, const Vals<N>& v) {
   if constexpr (N == 1) {
-    *p = from_f32<T>(v.p[0].x);
+    *p = from_f32<T>(v.p[0]);
   } else if constexpr (sizeof(T) == 4) {
     if constexpr (N == 4)
       __stcs(reinterpret_cast<float4*>(p), make_float4(v.p[0].x, v.p[0].y, v.p[1].x, v.p[1].y));
@@ -208,12 +220,12 @@ __device__ __forceinline__ void st_wide(G* p, const Vals<N>& v) {
   }
 }
 
-// N floats, aligned to min(N, 4) of them (N = 1: the first of a pair).
+// N floats, aligned to min(N, 4) of them.
 template <int N>
 __device__ __forceinline__ Vals<N> ld_floats(const float* p) {
   Vals<N> v;
   if constexpr (N == 1) {
-    v.p[0] = make_float2(*p, 0.f);
+    v.p[0] = *p;
   } else if constexpr (N == 2) {
     v.p[0] = *reinterpret_cast<const float2*>(p);
   } else {
@@ -229,7 +241,7 @@ __device__ __forceinline__ Vals<N> ld_floats(const float* p) {
 template <int N>
 __device__ __forceinline__ void st_floats(float* p, const Vals<N>& v) {
   if constexpr (N == 1) {
-    *p = v.p[0].x;
+    *p = v.p[0];
   } else if constexpr (N == 2) {
     *reinterpret_cast<float2*>(p) = v.p[0];
   } else {
@@ -243,7 +255,7 @@ template <int N>
 __device__ __forceinline__ Vals<N> fill(float x) {
   Vals<N> v;
 #pragma unroll
-  for (int i = 0; i < Vals<N>::P; ++i) v.p[i] = make_float2(x, N == 1 ? 0.f : x);
+  for (int i = 0; i < Vals<N>::P; ++i) v.p[i] = Vals<N>::all(x);
   return v;
 }
 
@@ -256,14 +268,17 @@ __device__ __forceinline__ Vals<N> ld_param(const void* p, bool is_bf16, int c, 
   if (!p) {
     v = fill<N>(none);
   } else if constexpr (N == 1) {
-    v.p[0] = make_float2(param_at(p, is_bf16, c, none), 0.f);
+    v.p[0] = param_at(p, is_bf16, c, none);
   } else if (is_bf16) {
     const bf16* q = static_cast<const bf16*>(p) + c;
-    if constexpr (N == 8) return unpack<bf16, 8>(Raw<bf16, 8>{__ldg(reinterpret_cast<const uint4*>(q))});
+    if constexpr (N == 8) {
+      v = unpack<bf16, 8>(Raw<bf16, 8>{__ldg(reinterpret_cast<const uint4*>(q))});
+    } else {
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-      const uint32_t u = __ldg(reinterpret_cast<const unsigned*>(q) + i);
-      v.p[i] = make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+      for (int i = 0; i < N / 2; ++i) {
+        const uint32_t u = __ldg(reinterpret_cast<const unsigned*>(q) + i);
+        v.p[i] = make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+      }
     }
   } else {
     const float* q = static_cast<const float*>(p) + c;
@@ -285,6 +300,11 @@ __device__ __forceinline__ float2 pair(float x) { return make_float2(x, x); }
 __device__ __forceinline__ float2 add2(float2 a, float2 b) { return __fadd2_rn(a, b); }
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ float sum2(float2 a) { return a.x + a.y; }
+__device__ __forceinline__ float add2(float a, float b) { return a + b; }
+__device__ __forceinline__ float mul2(float a, float b) { return a * b; }
+__device__ __forceinline__ float fma2(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ float sum2(float a) { return a; }
 
 }  // namespace eogp
 
