@@ -23,6 +23,7 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kWarpTeams = 4;     // warp teams of a block
 constexpr int kMaxWarps = 16;     // of a block team
+constexpr int kOwnStages = 3;     // rows ahead where threads copy their own elements
 
 // Threads of a team: 32, or the block (TEAM = 0).
 template <int TEAM>
@@ -270,11 +271,11 @@ __device__ __forceinline__ float2 block_sum2(float2 v, float2* part) {
 // (waits, sums, addresses) is as much as the work on ten elements, so it has up to 32.
 // Measured, bytes against the copy rate: 0.89 for 768 and 1024 channels of bf16, 0.87
 // (layer) and 0.94 (RMS) for 4096, 0.92 for 2048 and 4096 of fp32.
-template <typename T, int N, int NV, int TEAM, bool RMS, bool RING, bool WREG, int MAXT, int MINB>
+template <typename T, int N, int NV, int TEAM, bool RMS, bool BULK, bool WREG, int MAXT, int MINB>
 __global__ void __launch_bounds__(MAXT, MINB) k_norm_grad(const GradArgs a) {
   using V = Vals<N>;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ uint64_t bars[RING ? kWarpTeams * 8 : 1];
+  __shared__ uint64_t bars[BULK ? kWarpTeams * 8 : 1];
   __shared__ float2 part[2][kMaxWarps];
   const NormGrad& g = a.g;
   const RowSet rs = g.rs;
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(MAXT, MINB) k_norm_grad(const GradArgs a) {
       ws[c] = c < d ? param_at(g.weight, g.param_bf16, c, 1.f) : 0.f;
   }
   Ring q{};
-  if constexpr (RING) {
+  if constexpr (BULK) {
     q = Ring{ring0 + static_cast<size_t>(team) * a.stages * 2 * row_bytes, bars + team * 8, a.stages,
              static_cast<int>(2 * row_bytes), 0, 0, false};
     if (lane == 0) {
@@ -313,18 +314,39 @@ __global__ void __launch_bounds__(MAXT, MINB) k_norm_grad(const GradArgs a) {
   __syncthreads();
   RowAt p = row_at(rs, min(lo + team, a.M - 1));
   p.r = lo + team;
-  RowAt ahead = p;  // next row to be copied (thread 0)
+  int at[NV];  // first channel of vector j, within the row
+#pragma unroll
+  for (int j = 0; j < NV; ++j) at[j] = min((j * tt + lane) * N, d - N);
+  RowAt ahead = p;  // next row to be copied (BULK: by thread 0)
+  // Places of a thread's vectors when it copies them itself: of its own, so that it
+  // needs no other thread's copies.
+  T* const own = reinterpret_cast<T*>(ring0) + lane * N;
   auto issue = [&](int s) {
     to_kept(rs, ahead, teams, hi);
     if (ahead.r >= hi) return;
+    if constexpr (!BULK) {
+      const T* const xr = row_of<T>(g.x, ahead.b, ahead.t);
+      const T* const dyr = row_of<T>(g.dy, ahead.b, ahead.t);
+      T* const to = own + static_cast<size_t>(s) * 2 * width;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        copy_async<T, N>(reinterpret_cast<Raw<T, N>*>(to + j * tt * N), xr + at[j]);
+        copy_async<T, N>(reinterpret_cast<Raw<T, N>*>(to + width + j * tt * N), dyr + at[j]);
+      }
+      advance(rs, ahead, teams);
+      return;
+    }
     mbar_arrive_expect_tx(&q.full[s], 2 * row_bytes);
     uint8_t* to = q.data + static_cast<size_t>(s) * q.stage_bytes;
     bulk_load(to, row_of<T>(g.x, ahead.b, ahead.t), row_bytes, &q.full[s]);
     bulk_load(to + row_bytes, row_of<T>(g.dy, ahead.b, ahead.t), row_bytes, &q.full[s]);
     advance(rs, ahead, teams);
   };
-  if (RING && lane == 0)
-    for (int s = 0; s < a.stages; ++s) issue(s);
+  if (!BULK || lane == 0)
+    for (int s = 0; s < (BULK ? a.stages : kOwnStages); ++s) {
+      issue(s);
+      if (!BULK) commit_async();
+    }
   // Moves on to the next kept row, writing the rows of padding before it.
   auto skip = [&] {
     if (!rs.lengths) return;
@@ -337,9 +359,6 @@ __global__ void __launch_bounds__(MAXT, MINB) k_norm_grad(const GradArgs a) {
     }
   };
   skip();
-  int at[NV];  // first channel of vector j, within the row
-#pragma unroll
-  for (int j = 0; j < NV; ++j) at[j] = min((j * tt + lane) * N, d - N);
   const float* const wl = ws + lane * N;
   V dw[NV], db[NV];
   const float inv_d = 1.0f / d;
@@ -362,24 +381,20 @@ __global__ void __launch_bounds__(MAXT, MINB) k_norm_grad(const GradArgs a) {
       const float mu = mu_next, rstd = rs_next;
       T* const o = g.dx.p ? row_out<T>(g.dx, p.b, p.t) : nullptr;
       const T *xr, *dyr;
-      if constexpr (RING) {
+      if constexpr (BULK) {
         ring_wait(q, a.status);
         xr = reinterpret_cast<const T*>(q.data + static_cast<size_t>(q.slot) * q.stage_bytes);
         dyr = xr + d;
       } else {
-        xr = row_of<T>(g.x, p.b, p.t);
-        dyr = row_of<T>(g.dy, p.b, p.t);
+        wait_async<kOwnStages - 1>();
+        xr = own + static_cast<size_t>(q.slot) * 2 * width;
+        dyr = xr + width;
       }
       advance(rs, p, teams);
       skip();
       stats(p.r);
       auto load = [&](const T* from, int j) {
-        Raw<T, N> r;
-        if constexpr (RING)
-          r.w = *reinterpret_cast<const uint4*>(from + at[j]);
-        else
-          r = ld_raw<T, N>(from + at[j]);
-        return unpack<T, N>(r);
+        return unpack<T, N>(*reinterpret_cast<const Raw<T, N>*>(from + (BULK ? at[j] : j * tt * N)));
       };
       auto weight = [&](int j) {
         if constexpr (WREG)
@@ -410,8 +425,8 @@ __global__ void __launch_bounds__(MAXT, MINB) k_norm_grad(const GradArgs a) {
         if (o) sum = make_float2(warp_sum(sum.x), warp_sum(sum.y));
         team_sync<TEAM>();
       }
-      if constexpr (RING) {
-        asm volatile("" ::: "memory");  // the row is read again, not kept
+      asm volatile("" ::: "memory");  // the row is read again, not kept
+      if constexpr (BULK) {
         if (lane == 0 && back >= 0 && !q.dead) issue(back);
         back = q.slot;
         ring_next(q);
@@ -429,6 +444,11 @@ __global__ void __launch_bounds__(MAXT, MINB) k_norm_grad(const GradArgs a) {
           }
           if ((j * tt + lane) * N < d) st_vals<T, N>(o + at[j], dy);
         }
+      }
+      if constexpr (!BULK) {
+        issue(q.slot);
+        commit_async();
+        if (++q.slot == kOwnStages) q.slot = 0;
       }
       parity ^= 1;
     }
@@ -629,8 +649,8 @@ Shape grad_shape(int d, int vec, int es, int warp_nv, int block_nv) {
     const int th = ceil_div(nv, 32 * block_nv) * 32;
     return th <= 512 ? Shape{vec, block_nv, 0, th} : Shape{0, 0, 0, 0};
   }
-  const int per = vec == 2 ? 8 : 16, th = ceil_div(nv, 32 * per) * 32;
-  return th <= 512 ? Shape{vec, per, 0, th} : Shape{0, 0, 0, 0};
+  const int th = ceil_div(nv, 32 * 8) * 32;
+  return th <= 512 ? Shape{vec, 8, 0, th} : Shape{0, 0, 0, 0};
 }
 
 // Shared memory that the blocks of a multiprocessor share: 228 KB less 1 KB and the
@@ -643,8 +663,9 @@ template <typename F>
 int resident(F k, int threads, int most) {
   cudaFuncAttributes at;
   if (cudaFuncGetAttributes(&at, k) != cudaSuccess || at.numRegs < 1) return 1;
-  const int per_block = (at.numRegs + 7) / 8 * 8 * ((threads + 127) / 128 * 128);
-  return std::max(1, std::min({most, 65536 / per_block, 2048 / threads}));
+  // Each of the four parts of a multiprocessor gives its warps 16,384 registers.
+  const int warps = 4 * (16384 / ((at.numRegs + 7) / 8 * 8 * 32));
+  return std::max(1, std::min({most, warps / (threads / 32), 2048 / threads}));
 }
 
 template <typename F>
@@ -715,24 +736,26 @@ cudaError_t norm_launch(bool rms, const NormArgs& a, int num_sms, cudaStream_t s
 }
 
 // Rows of a block of the gradient: blocks for `occ` a multiprocessor, and at least
-// 8 rows each so that joining their sums stays small beside forming them.
+// 4 rows each so that joining their sums stays small beside forming them.
 int grad_rows(long long M, int num_sms, int occ) {
-  return std::max(8, ceil_div(M, static_cast<long long>(num_sms) * occ));
+  return std::max(4, ceil_div(M, static_cast<long long>(num_sms) * occ));
 }
 constexpr int kGradOcc = 8;  // most blocks a multiprocessor is given
 
-template <typename T, int N, int NV, int TEAM, bool RING, bool WREG, int MAXT, int MINB>
+template <typename T, int N, int NV, int TEAM, bool BULK, bool WREG, int MAXT, int MINB>
 cudaError_t grad_team(GradArgs& a, int threads, int num_sms, cudaStream_t st) {
-  auto k = a.g.rms ? k_norm_grad<T, N, NV, TEAM, true, RING, WREG, MAXT, MINB>
-                   : k_norm_grad<T, N, NV, TEAM, false, RING, WREG, MAXT, MINB>;
+  auto k = a.g.rms ? k_norm_grad<T, N, NV, TEAM, true, BULK, WREG, MAXT, MINB>
+                   : k_norm_grad<T, N, NV, TEAM, false, BULK, WREG, MAXT, MINB>;
   const int teams = TEAM ? kWarpTeams : 1;
-  const size_t stage = static_cast<size_t>(teams) * 2 * a.g.d * sizeof(T);
-  const size_t extra = static_cast<size_t>(NV) * (TEAM ? 32 : threads) * N * ((WREG ? 0 : 4) + (TEAM ? 8 : 0));
+  const size_t width = static_cast<size_t>(NV) * (TEAM ? 32 : threads) * N;
+  const size_t stage = static_cast<size_t>(teams) * 2 * (BULK ? a.g.d : width) * sizeof(T);
+  const size_t extra = width * ((WREG ? 0 : 4) + (TEAM ? 8 : 0));
   // Fewer blocks where the rings would have less than two or three rows each.
-  constexpr int kMinStages = sizeof(T) == 2 ? 3 : 2;
-  int occ = resident(k, threads, kGradOcc);
-  if (RING) occ = std::max(1, std::min(occ, static_cast<int>(kSmemPerSm / (extra + kMinStages * stage))));
-  a.stages = RING ? std::max(2, std::min<int>(8, static_cast<int>((kSmemPerSm / occ - extra) / stage))) : 0;
+  constexpr int kMinStages = !BULK ? kOwnStages : sizeof(T) == 2 ? 3 : 2;
+  const int occ = std::max(1, std::min(resident(k, threads, kGradOcc),
+                                       static_cast<int>(kSmemPerSm / (extra + kMinStages * stage))));
+  a.stages = !BULK ? kOwnStages
+                   : std::max(2, std::min<int>(8, static_cast<int>((kSmemPerSm / occ - extra) / stage)));
   const size_t smem = extra + a.stages * stage;
   if (cudaError_t e = allow_smem(k, smem); e != cudaSuccess) return e;
   a.per = grad_rows(a.M, num_sms, occ);
@@ -761,7 +784,7 @@ cudaError_t grad_launch(GradArgs& a, int num_sms, cudaStream_t st) {
     if (s.nv == 2) return grad_team<T, F, 2, 32, true, WREG, 128, 4>(a, s.threads, num_sms, st);
     if (s.nv == 3) return grad_team<T, F, 3, 32, true, WREG, 128, 4>(a, s.threads, num_sms, st);
     if (s.nv == 4) return grad_team<T, F, 4, 32, true, WREG, 128, 4>(a, s.threads, num_sms, st);
-    if constexpr (WNV > 4) return grad_team<T, F, WNV, 32, true, WREG, 128, 4>(a, s.threads, num_sms, st);
+    if constexpr (WNV > 4) return grad_team<T, F, WNV, 32, true, WREG, 128, 3>(a, s.threads, num_sms, st);
   }
   if (s.n == F && s.team == 0 && own_type) {
     // bf16, 32 elements a thread: few blocks of many registers, except where a row is
@@ -770,7 +793,7 @@ cudaError_t grad_launch(GradArgs& a, int num_sms, cudaStream_t st) {
     if constexpr (sizeof(T) == 2) {
       if (s.threads <= 64) return grad_team<T, F, BNV, 0, true, true, 64, 8>(a, s.threads, num_sms, st);
       if (s.threads <= 128) return grad_team<T, F, BNV, 0, true, true, 128, 2>(a, s.threads, num_sms, st);
-      if (s.threads <= 192) return grad_team<T, F, BNV, 0, true, true, 192, 2>(a, s.threads, num_sms, st);
+      if (s.threads <= 192) return grad_team<T, F, BNV, 0, true, true, 256, 2>(a, s.threads, num_sms, st);
       if (s.threads <= 256) return grad_team<T, F, BNV, 0, true, true, 256, 1>(a, s.threads, num_sms, st);
     } else {
       if (s.threads <= 128) return grad_team<T, F, BNV, 0, true, true, 128, 6>(a, s.threads, num_sms, st);
@@ -781,7 +804,7 @@ cudaError_t grad_launch(GradArgs& a, int num_sms, cudaStream_t st) {
   if (s.n == F && s.team == 32) return grad_team<T, F, WNV, 32, true, false, 128, 4>(a, s.threads, num_sms, st);
   if (s.n == F) return grad_team<T, F, BNV, 0, true, false, 512, 1>(a, s.threads, num_sms, st);
   if (s.n == 2) return grad_team<T, 2, 8, 0, false, false, 512, 1>(a, s.threads, num_sms, st);
-  if (s.n == 1) return grad_team<T, 1, 16, 0, false, false, 512, 1>(a, s.threads, num_sms, st);
+  if (s.n == 1) return grad_team<T, 1, 8, 0, false, false, 512, 1>(a, s.threads, num_sms, st);
   // The sums read dy and x before dx may be written over them.
   a.per = grad_rows(a.M, num_sms, kGradOcc);
   if (g.dweight || g.dbias) {
