@@ -7,7 +7,7 @@
 // Statistics and sums are fp32; the variance is the mean of squared differences
 // from the mean, not a difference of moments. HBM-bound: a few flop per byte.
 //
-// A row is worked on by a team: a warp, a quarter of one, or a whole block, each
+// A row is worked on by a team: a warp, a part of one, or a whole block, each
 // thread holding vectors of the row in registers, so x (and dy) are read once.
 // Rows that 16-byte accesses do not fit are loaded two or one elements at a time;
 // rows too wide for registers take several passes.
@@ -249,6 +249,17 @@ __device__ __forceinline__ void to_kept(const RowSet& rs, RowAt& p, int step, in
   while (p.r < hi && p.t >= rs.lengths[p.b]) advance(rs, p, (rs.T - p.t + step - 1) / step * step);
 }
 
+// Sum over the team's lanes of a warp (for a block team: of the warp); other teams
+// of the warp may be elsewhere.
+template <int TEAM>
+__device__ __forceinline__ float lane_sum(float v) {
+  constexpr int L = TEAM ? TEAM : 32;
+  const unsigned mask = L == 32 ? 0xffffffffu : ((1u << (L & 31)) - 1u) << (threadIdx.x & 31 & ~(L - 1));
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(mask, v, o);
+  return v;
+}
+
 // Two sums over the block, the same in every thread and in a fixed order.
 __device__ __forceinline__ float2 block_sum2(float2 v, float2* part) {
   v.x = warp_sum(v.x);
@@ -280,8 +291,8 @@ __global__ void __launch_bounds__(MAXT, MINB) k_norm_grad(const GradArgs a) {
   const NormGrad& g = a.g;
   const RowSet rs = g.rs;
   const int lane = team_lane<TEAM>(), tt = team_threads<TEAM>();
-  const int team = TEAM ? threadIdx.x / 32 : 0;
-  constexpr int teams = TEAM ? kWarpTeams : 1;
+  constexpr int teams = TEAM ? 32 * kWarpTeams / (TEAM ? TEAM : 1) : 1;
+  const int team = TEAM ? threadIdx.x / (TEAM ? TEAM : 1) : 0;
   const int d = g.d, width = NV * tt * N;
   const uint32_t row_bytes = static_cast<uint32_t>(d) * sizeof(T);
   const long long first = static_cast<long long>(blockIdx.x) * a.per;
@@ -320,7 +331,7 @@ __global__ void __launch_bounds__(MAXT, MINB) k_norm_grad(const GradArgs a) {
   RowAt ahead = p;  // next row to be copied (BULK: by thread 0)
   // Places of a thread's vectors when it copies them itself: of its own, so that it
   // needs no other thread's copies.
-  T* const own = reinterpret_cast<T*>(ring0) + lane * N;
+  T* const own = reinterpret_cast<T*>(ring0) + static_cast<size_t>(team) * kOwnStages * 2 * width + lane * N;
   auto issue = [&](int s) {
     to_kept(rs, ahead, teams, hi);
     if (ahead.r >= hi) return;
@@ -421,10 +432,10 @@ __global__ void __launch_bounds__(MAXT, MINB) k_norm_grad(const GradArgs a) {
       float2 sum = make_float2(sum2(s1), sum2(s2));
       if (o && TEAM == 0) {
         sum = block_sum2(sum, part[parity]);
-      } else {
-        if (o) sum = make_float2(warp_sum(sum.x), warp_sum(sum.y));
-        team_sync<TEAM>();
+      } else if (o) {
+        sum = make_float2(lane_sum<TEAM>(sum.x), lane_sum<TEAM>(sum.y));
       }
+      if (BULK && !(o && TEAM == 0)) team_sync<TEAM>();
       asm volatile("" ::: "memory");  // the row is read again, not kept
       if constexpr (BULK) {
         if (lane == 0 && back >= 0 && !q.dead) issue(back);
@@ -746,8 +757,8 @@ template <typename T, int N, int NV, int TEAM, bool BULK, bool WREG, int MAXT, i
 cudaError_t grad_team(GradArgs& a, int threads, int num_sms, cudaStream_t st) {
   auto k = a.g.rms ? k_norm_grad<T, N, NV, TEAM, true, BULK, WREG, MAXT, MINB>
                    : k_norm_grad<T, N, NV, TEAM, false, BULK, WREG, MAXT, MINB>;
-  const int teams = TEAM ? kWarpTeams : 1;
-  const size_t width = static_cast<size_t>(NV) * (TEAM ? 32 : threads) * N;
+  const int teams = TEAM ? 32 * kWarpTeams / (TEAM ? TEAM : 1) : 1;
+  const size_t width = static_cast<size_t>(NV) * (TEAM ? TEAM : threads) * N;
   const size_t stage = static_cast<size_t>(teams) * 2 * (BULK ? a.g.d : width) * sizeof(T);
   const size_t extra = width * ((WREG ? 0 : 4) + (TEAM ? 8 : 0));
   // Fewer blocks where the rings would have less than two or three rows each.
@@ -779,9 +790,15 @@ cudaError_t grad_launch(GradArgs& a, int num_sms, cudaStream_t st) {
   constexpr bool WREG = sizeof(T) == 4;
   const bool own_type = g.param_bf16 == (sizeof(T) == 2);
   const Shape s = grad_shape(g.d, vec, es, WNV, BNV);
+  // Narrow rows, several to a warp, whose lanes copy their own vectors.
+  if (s.n == F && s.team == 32) {
+    const int nv = g.d / F;
+    if (nv <= 8) return grad_team<T, F, 1, 8, false, false, 128, 4>(a, 128, num_sms, st);
+    if (nv <= 16) return grad_team<T, F, 2, 8, false, false, 128, 4>(a, 128, num_sms, st);
+    if (nv <= 32) return grad_team<T, F, 4, 8, false, false, 128, 3>(a, 128, num_sms, st);
+    if (nv <= 64) return grad_team<T, F, 4, 16, false, false, 128, 3>(a, 128, num_sms, st);
+  }
   if (s.n == F && s.team == 32 && (own_type || !WREG)) {
-    if (s.nv == 1) return grad_team<T, F, 1, 32, true, WREG, 128, 4>(a, s.threads, num_sms, st);
-    if (s.nv == 2) return grad_team<T, F, 2, 32, true, WREG, 128, 4>(a, s.threads, num_sms, st);
     if (s.nv == 3) return grad_team<T, F, 3, 32, true, WREG, 128, 4>(a, s.threads, num_sms, st);
     if (s.nv == 4) return grad_team<T, F, 4, 32, true, WREG, 128, 4>(a, s.threads, num_sms, st);
     if constexpr (WNV > 4) return grad_team<T, F, WNV, 32, true, WREG, 128, 3>(a, s.threads, num_sms, st);
