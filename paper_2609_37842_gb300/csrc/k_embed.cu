@@ -385,10 +385,9 @@ __device__ __forceinline__ void st_run(G* o, Vals<N> s, float scale, bool accumu
 #pragma unroll
   for (int i = 0; i < Vals<N>::P; ++i) s.p[i] = mul2(s.p[i], Vals<N>::all(scale));
   if (accumulate) {
+    const Vals<N> old = ld_wide<G, N>(o);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      s.set(i, to_f32(o[i]) + s.get(i));
-    }
+    for (int i = 0; i < Vals<N>::P; ++i) s.p[i] = add2(old.p[i], s.p[i]);
   }
   st_wide<G, N>(o, s);
 }

@@ -251,6 +251,22 @@ __device__ __forceinline__ void st_floats(float* p, const Vals<N>& v) {
   }
 }
 
+// N elements of G, as st_wide writes them.
+template <typename G, int N>
+__device__ __forceinline__ Vals<N> ld_wide(const G* p) {
+  if constexpr (sizeof(G) == 4) {
+    return ld_floats<N>(p);
+  } else if constexpr (N == 4) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    Vals<4> v;
+    v.p[0] = make_float2(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u));
+    v.p[1] = make_float2(__uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
+    return v;
+  } else {
+    return unpack<G, N>(*reinterpret_cast<const Raw<G, N>*>(p));
+  }
+}
+
 template <int N>
 __device__ __forceinline__ Vals<N> fill(float x) {
   Vals<N> v;
