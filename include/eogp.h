@@ -566,8 +566,9 @@ int eogp_score_topk(const void* train, int ld_train, const float* train_scales, 
  *  - Token numbers (tokens, targets) are EOGP_I32 or EOGP_I64, row b at element
  *    b * bs, contiguous over t.
  *  - lengths: device int32 [B] or NULL. Positions t >= lengths[b] are padding, as
- *    in eogp_layer_desc: nothing of theirs is read, their output rows are 0, and
- *    they add nothing to any sum.
+ *    in eogp_layer_desc: their rows are not read (their token numbers and weights
+ *    may be, and may hold anything), their output rows are 0, and they add
+ *    nothing to any sum.
  *  - EOGP_F32 or EOGP_BF16 arrays, aligned to their element; sums, statistics
  *    and exponentials are formed in fp32, each result rounded once to its type.
  *    16-byte aligned bases and strides run fastest; nothing else needs them.

@@ -189,6 +189,34 @@ def test_norm_grad(kind, dt, pt, rows, d):
                 check(dx, dx_w, tol, "dx")
 
 
+@pytest.mark.parametrize("per", [False, True])
+@pytest.mark.parametrize("d,dt", [(64, BF), (768, BF), (770, F32), (4096, BF), (2048, F32)])
+@pytest.mark.parametrize("T,lengths", [(64, [0, 0, 0]), (100, [0] * 40), (64, [0] * 20 + [1] + [0] * 20),
+                                       (3000, [0, 0, 3000, 0]), (5000, [1]), (5000, [4999]), (300, [300, 0] * 30),
+                                       (90, [90] * 50 + [0] * 50), (200, [0] * 50 + [200] * 50 + [1])])
+def test_norm_grad_uneven_lengths(T, lengths, d, dt, per):
+    """Rows are shared out by the work of the lengths: none at all, a few, all in one place; with and without dx."""
+    g = gen(T + d)
+    B = len(lengths)
+    ln = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    keep = kept(B, T, ln)[..., None]
+    x, dy = whole(g, (B, T, d), dt, 7), whole(g, (B, T, d), dt, 4)
+    x.masked_fill_(~keep, float("nan"))
+    dy.masked_fill_(~keep, float("nan"))
+    rstd = torch.ones((B, T), device=DEV)
+    X, DY = torch.where(keep, x.double(), 0.0), torch.where(keep, dy.double(), 0.0)
+    over = (1,) if per else (0, 1)
+    args = dict(kind=E.NORM_RMS, lengths=ln, per_example=per)
+    for want_dx in (True, False):
+        dx, dw, db = E.norm_grad(dy, x, None, rstd, None, want_dx=want_dx, **args)
+        assert torch.equal(dw.double(), (DY * X).sum(over)) and torch.equal(db.double(), DY.sum(over))
+        if want_dx:
+            full = dx
+            assert not torch.where(keep, 0.0, dx.double()).any() and torch.isfinite(dx).all()
+    only = E.norm_grad(dy, x, None, rstd, None, want_dweight=False, want_dbias=False, **args)[0]
+    assert torch.equal(only, full)
+
+
 # -------------------------------------------------------------------- loss
 @pytest.mark.parametrize("dt", [F32, BF])
 @pytest.mark.parametrize("rows,V", [(40_000, 40), (40_000, 1000), (40_000, 1025), (30_000, 2100), (20_000, 4099),
