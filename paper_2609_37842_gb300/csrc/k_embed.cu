@@ -104,6 +104,12 @@ SortPlan sort_plan(int V, long long M) {
   return p;
 }
 
+// A token's mark. Neighbours lie apart: the frequent tokens of many vocabularies are
+// neighbours, and stores to one sector wait for each other (keys and marks of 262,144
+// positions: 17 us with neighbours together, 10 us so).
+__host__ __device__ __forceinline__ int mark_stride(int V) { return (V + 31) / 32; }
+__device__ __forceinline__ int mark_of(int v, int V) { return (v & 31) * mark_stride(V) + (v >> 5); }
+
 // Zeroing of dtable's rows of absent tokens, by blocks of their own beside those of
 // another job in the same launch: the stores fill the time that the sort waits.
 struct ZeroArgs {
@@ -111,14 +117,14 @@ struct ZeroArgs {
   size_t stride, row_bytes;
   int unit;                 // bytes of a store: 16, or an element's
   const uint8_t* present;   // tokens that occur, or NULL: every row is zeroed
-  int v0, v1, rows, blocks;  // rows [v0, v1), `rows` of them a block
+  int V, v0, v1, rows, blocks;  // rows [v0, v1), `rows` of them a block
 };
 
 __device__ void zero_rows(const ZeroArgs& z, int block) {
   const int lane = threadIdx.x & 31;
   for (int i = threadIdx.x >> 5; i < z.rows; i += kSortWarps) {
     const long long v = z.v0 + static_cast<long long>(block) * z.rows + i;
-    if (v >= z.v1 || (z.present && z.present[v])) continue;
+    if (v >= z.v1 || (z.present && z.present[mark_of(static_cast<int>(v), z.V)])) continue;
     uint8_t* o = z.table + v * z.stride;
     if (z.unit == 16) {
       for (size_t k = lane * 16; k < z.row_bytes; k += 512)
@@ -188,7 +194,7 @@ __global__ void __launch_bounds__(kThreads) k_sort_keys(RowSet rs, TokenView tok
     volatile int* const seen = &marked[k[s] & (kMarked - 1)];
     if (k[s] < V && *seen != k[s]) {
       *seen = k[s];
-      present[k[s]] = 1;
+      present[mark_of(k[s], V)] = 1;
     }
     atomicAdd(&cnt[k[s] & (bins - 1)], 1);
   }
@@ -279,6 +285,17 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_place(const int* __restri
   __shared__ int base[kMaxBins], total[kMaxBins];
   __shared__ unsigned short wcnt[kSortWarps][kMaxBins];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int lo = blockIdx.x * per_block, hi = min(M, lo + per_block);
+  int k[kItems], p[kItems];
+  auto load = [&](int t0) {
+#pragma unroll
+    for (int s = 0; s < kItems; ++s) {
+      const int i = t0 + warp * (32 * kItems) + s * 32 + lane;
+      k[s] = i < hi ? key[i] : 0;
+      p[s] = i < hi ? (idx ? idx[i] : i) : 0;
+    }
+  };
+  load(lo);  // on their way beside the counts
   for (int d = tid; d < bins; d += kSortThreads) {
     int before = 0, all = 0;
 #pragma unroll 32
@@ -292,16 +309,11 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_place(const int* __restri
   }
   __syncthreads();
   if (warp == 0) scan_bins(total, base, bins);
-  const int lo = blockIdx.x * per_block, hi = min(M, lo + per_block);
   for (int t0 = lo; t0 < hi; t0 += kTile) {
-    int k[kItems], p[kItems], dg[kItems], off[kItems];
+    int dg[kItems], off[kItems];
 #pragma unroll
-    for (int s = 0; s < kItems; ++s) {
-      const int i = t0 + warp * (32 * kItems) + s * 32 + lane;
-      k[s] = i < hi ? key[i] : 0;
-      p[s] = i < hi ? (idx ? idx[i] : i) : 0;
-      dg[s] = i < hi ? (k[s] >> shift) & (bins - 1) : -1;
-    }
+    for (int s = 0; s < kItems; ++s)
+      dg[s] = t0 + warp * (32 * kItems) + s * 32 + lane < hi ? (k[s] >> shift) & (bins - 1) : -1;
     rank_tile(dg, off, wcnt, total, bins);
 #pragma unroll
     for (int s = 0; s < kItems; ++s) {
@@ -310,6 +322,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_place(const int* __restri
       key_out[at] = k[s];
       idx_out[at] = p[s];
     }
+    load(min(t0 + kTile, hi));
     __syncthreads();
     for (int d = tid; d < bins; d += kSortThreads) base[d] += total[d];
     __syncthreads();
@@ -684,7 +697,7 @@ EmbedWs embed_ws(int V, int d, long long M) {
     w.key2 = take(M * 4);
     w.idx2 = take(M * 4);
     w.hist = take(static_cast<size_t>(p.passes) * p.blocks * p.bins * 4);
-    w.present = take(V);
+    w.present = take(32 * static_cast<size_t>(mark_stride(V)));
   }
   // Enough for every access width: the most groups of positions any of them makes.
   size_t slots = 0;
@@ -713,6 +726,7 @@ cudaError_t launch_embed_grad(RowSet rs, TokenView tok, RowView dout, bool bf16_
   auto ints = [&](size_t at) { return reinterpret_cast<int*>(base + at); };
 
   ZeroArgs z{};
+  z.V = V;
   z.table = static_cast<uint8_t*>(dtable);
   z.row_bytes = static_cast<size_t>(d) * es;
   z.stride = V > 1 ? static_cast<size_t>(ld_dtable) * es : z.row_bytes;
