@@ -856,8 +856,9 @@ cudaError_t grad_team(GradArgs& a, int threads, int num_sms, cudaStream_t st) {
   const size_t smem = extra + a.stages * stage;
   if (cudaError_t e = allow_smem(k, smem); e != cudaSuccess) return e;
   a.per = grad_rows(a.M, num_sms, occ);
-  // Rows of padding are less work than others: 512 examples of 512 x 768 bf16, from 1
-  // token to all kept, 200 us in blocks of equally many rows and 170 us of equal work.
+  // Rows of padding are less work than others: 512 examples of 512 x 768 bf16, a
+  // quarter to all tokens kept, 200 us in blocks of equally many rows and 170 us of
+  // equal work.
   // Every block reads all lengths for its share, so examples of fewer than 64 tokens,
   // whose lengths would be a tenth of the traffic, are cut by rows.
   a.by_work = a.g.rs.lengths && a.g.rs.T >= 64;
