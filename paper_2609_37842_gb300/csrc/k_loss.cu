@@ -6,8 +6,12 @@
 // The sum is formed in one pass with a running maximum, in powers of two: with
 // c = m log2(e) for the maximum m so far, s = sum 2^(x log2(e) - c), one fused
 // multiply-add and one exponential a logit; sums of different references are joined
-// by 2^(c - c'). Rows whose maximum is infinite or beyond 1e29, where c would lose
-// the logits or overflow, take a plain path (slow_row).
+// by 2^(c - c'). c is rounded to fp32 and x log2(e) is not, so 2^(x log2(e) - c) at
+// x = m is off from 1 by up to half a unit in c's last place in the exponent: nothing up
+// to kNearLogit, but 2^64 and more from 1e9 on. Rows whose maximum is beyond that, or
+// infinite, take a plain path that forms x - m first (slow_row); logits below
+// -kNearLogit are held against that bound's reference, so that those met before a row's
+// larger ones add what they are worth, which is nothing, and no infinity.
 //
 // k_loss: a row lies in the shared memory of a CTA, or in slices in that of the CTAs
 // of a cluster. A thread copies its vectors to its own places and reads them there
@@ -32,7 +36,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kFarLogit = 1e29f;
+constexpr float kNearLogit = 1048576.f;  // c's last place is 1/8 at most: the exponent's error is 1/16
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;
@@ -44,7 +48,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
 struct __align__(8) MaxSum {
   float m, s;
 };
-__device__ __forceinline__ float ref(float m) { return fmaxf(m * kLog2e, -kFarLogit); }
+// The reference c, rounded: sums are joined right only if every use has the same value,
+// so the product is kept from being fused with what follows.
+__device__ __forceinline__ float ref(float m) { return fmaxf(__fmul_rn(m, kLog2e), -kNearLogit * kLog2e); }
 // Over a warp: the maximum first, then one rescaling a lane and a plain sum.
 __device__ __forceinline__ MaxSum warp_join(MaxSum v) {
   float m = v.m;
@@ -69,7 +75,7 @@ __device__ __forceinline__ void raise(MaxSum& v, float m) {
   }
 }
 // Whether the reference of this maximum does for a row.
-__device__ __forceinline__ bool near(float m) { return fabsf(m) <= kFarLogit; }
+__device__ __forceinline__ bool near(float m) { return fabsf(m) <= kNearLogit; }
 
 // Which row r is, whether it takes part, its target and weight.
 struct RowJob {

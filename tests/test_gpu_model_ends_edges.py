@@ -1,0 +1,67 @@
+"""GPU checks of the model-end operators where values, sizes or aliasing are at their
+edges, against float64 restatements of the formulas (tolerances: test_gpu_model_ends)."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2609_37842_gb300 import eogp as E  # noqa: E402
+from test_gpu_model_ends import (BF, DEV, F32, TYPES, U, _lib, _status, chain, check, f64, loss_ref,  # noqa: E402,F401
+                                 out_u, rnd)
+
+
+# -------------------------------------------------------------------- loss
+# Rows that a warp, a block, a cluster and the two-pass kernel work on, in both types.
+LOSS_WIDTHS = [64, 1003, 8192, 50_001, 140_000, 1_000_003]
+
+
+def check_loss(x, tgt, **args):
+    """Loss, lse and gradient of rows x [T, V] of one type against loss_ref, and the call without gradient."""
+    T = x.shape[0]
+    tk = torch.from_numpy(tgt).to(DEV)
+    loss, lse, g = E.cross_entropy(x, tk, **args)
+    want = loss_ref(f64(x)[None], tgt[None], np.ones((1, T)), np.ones((1, T), bool))
+    loss_w, lse_w, g_w, el, es, eg = (a[0] for a in want)
+    check(loss, loss_w, el, "loss")
+    check(lse, lse_w, es, "lse")
+    check(g, g_w, out_u(x.dtype) * np.abs(g_w) + eg, "dlogits")
+    alone = E.cross_entropy(x, tk, want_grad=False, **args)
+    check(alone[0], loss_w, el, "loss alone")
+    check(alone[1], lse_w, es, "lse alone")
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("V", LOSS_WIDTHS)
+def test_cross_entropy_far_rows(dt, V):
+    """Rows of equal and of mixed logits far from 0: finite logits give finite losses, whatever they are."""
+    far = [s * m for m in (1e6, 2.0 ** 20, 2.0 ** 20 + 1, 1e9, 1e10, 1.1e10, 1e12, 1e20, 0.9e29, 3e29)
+           for s in (1, -1)]
+    rng = np.random.default_rng(V)
+    for q in far:
+        x = np.full((2, V), q, np.float64)
+        # in steps of the type's spacing there, some of which are less than 1
+        x[1] += rng.integers(-4, 5, V) * abs(q) * 2 * out_u(dt)
+        check_loss(torch.from_numpy(x.astype(np.float32)).to(DEV).to(dt), np.array([3, V - 1]))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("V", LOSS_WIDTHS)
+def test_cross_entropy_far_masks(dt, V):
+    """Masks of finite values in front of, behind and between ordinary logits, single survivors, and logits that
+    rise from far below: a thread, a warp or a block may meet the masked ones first, or nothing else."""
+    rng = np.random.default_rng(V + 1)
+    for mask in (-3e4, -1e9, -1e10, -1.1e10, -1e12, -1e20, -0.9e29, -1e30):
+        x = rng.standard_normal((6, V)) * 2
+        x[0, :V // 2] = mask
+        x[1, V // 2:] = mask
+        x[2, rng.random(V) < 0.9] = mask
+        x[2, V - 1] = 0.3
+        x[3, :] = mask
+        x[3, V - 2] = 0.3              # the target alone is left
+        x[4, :-1] = mask               # a far row but for one logit of ordinary size
+        x[5] = np.linspace(mask, 0, V)
+        tgt = np.array([V - 2, 1, V - 1, V - 2, V - 1, V - 1])
+        check_loss(torch.from_numpy(x.astype(np.float32)).to(DEV).to(dt), tgt)
+    x = np.stack([np.linspace(-3e6, 0, V), np.linspace(-3e6, -1.2e6, V), np.linspace(0, 3e6, V)])
+    check_loss(torch.from_numpy(x.astype(np.float32)).to(DEV).to(dt), np.array([V - 1, V - 1, V - 2]))
