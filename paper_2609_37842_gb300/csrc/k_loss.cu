@@ -317,6 +317,7 @@ __global__ void __launch_bounds__(128) k_loss_warp(const LossArgs a, int M, unsi
     }
   }
   if (!g) return;
+  __syncwarp();  // lane 0 has read the target's logit, which another lane may now write the gradient over
   const RowVecs<T> out(g, a.V);
   const float inv = j.w / s;
   const int target = static_cast<int>(j.target);

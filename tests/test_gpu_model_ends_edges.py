@@ -65,3 +65,21 @@ def test_cross_entropy_far_masks(dt, V):
         check_loss(torch.from_numpy(x.astype(np.float32)).to(DEV).to(dt), tgt)
     x = np.stack([np.linspace(-3e6, 0, V), np.linspace(-3e6, -1.2e6, V), np.linspace(0, 3e6, V)])
     check_loss(torch.from_numpy(x.astype(np.float32)).to(DEV).to(dt), np.array([V - 1, V - 1, V - 2]))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("V", [1, 7, 64, 97, 515, 1000, 1024, 2000, 2048, 5000, 50_001, 140_000])
+def test_cross_entropy_over_its_logits(dt, V):
+    """Loss and lse, not the gradient alone, have the same bits where the gradient is written over the logits, with
+    targets in every place of a row: the target's logit is read before anything is written over it."""
+    T = min(8192, max(64, (1 << 25) // V))
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(V)
+    x = torch.empty((T, V), dtype=dt, device=DEV).normal_(generator=gen).mul_(3)
+    tgt = torch.arange(T, device=DEV) * 7 % V
+    want = E.cross_entropy(x, tgt)
+    for _ in range(3):
+        xx = x.clone()
+        got = E.cross_entropy(xx, tgt, dlogits=xx)
+        assert got[2] is xx
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
