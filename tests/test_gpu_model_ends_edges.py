@@ -83,3 +83,37 @@ def test_cross_entropy_over_its_logits(dt, V):
         got = E.cross_entropy(xx, tgt, dlogits=xx)
         assert got[2] is xx
         assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+# ----------------------------------------------------------- normalisation
+@pytest.mark.parametrize("kind", [E.NORM_LAYER, E.NORM_RMS])
+@pytest.mark.parametrize("d", [33, 64, 256, 768, 770, 2048, 4095, 20_000])
+def test_norm_grad_of_rows_with_an_offset(kind, d):
+    """dx where the rows' mean is many times their spread and dy follows the rows: its error is that of centred rows.
+
+    mean and rstd are inputs, so the formula holds for them as given. With e = x - mean (off by u |e|), xh = e rstd
+    and g = dy w: mean(g) and mean(g xh) are off by (c + 4) u of the mean magnitudes, c the chain of the sums, and
+    the terms g, mean(g) and xh mean(g xh), in whatever grouping, by a few u each."""
+    rng = np.random.default_rng(d)
+    rows = np.array([0.0, 3.0, 30.0, 300.0, 3000.0])
+    T = len(rows)
+    x = (rng.standard_normal((1, T, d)) + rows[None, :, None]).astype(np.float32)
+    x64 = x.astype(np.float64)
+    mu64 = x64.mean(-1) if kind == E.NORM_LAYER else np.zeros((1, T))
+    mu = mu64.astype(np.float32)
+    rs = (1 / np.sqrt(((x64 - mu64[..., None]) ** 2).mean(-1) + 1e-5)).astype(np.float32)
+    xh = (x64 - mu[..., None].astype(np.float64)) * rs[..., None].astype(np.float64)
+    w = (1 + 0.1 * rng.standard_normal(d)).astype(np.float32)
+    dy = (xh + 0.3 * rng.standard_normal((1, T, d))).astype(np.float32)
+    g = dy.astype(np.float64) * w
+    r = rs[..., None].astype(np.float64)
+    m1 = g.mean(-1, keepdims=True) if kind == E.NORM_LAYER else np.zeros((1, T, 1))
+    m2 = (g * xh).mean(-1, keepdims=True)
+    want = r * (g - m1 - xh * m2)
+    c = chain(d) + (d / 256 if d > 16_384 else 0)      # the widest rows: one block, an element a thread
+    e1 = np.abs(g).mean(-1, keepdims=True) if kind == E.NORM_LAYER else 0.0
+    tol = r * U * ((c + 8) * (e1 + np.abs(xh) * np.abs(g * xh).mean(-1, keepdims=True)) +
+                   8 * (np.abs(g) + np.abs(m1) + np.abs(xh * m2)))
+    t = lambda a: torch.from_numpy(a).to(DEV)  # noqa: E731
+    dx, _, _ = E.norm_grad(t(dy), t(x), t(mu) if kind == E.NORM_LAYER else None, t(rs), t(w), kind=kind)
+    check(dx, want, tol, "dx")
