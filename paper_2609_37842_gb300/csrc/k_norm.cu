@@ -312,14 +312,18 @@ __device__ __forceinline__ void cut_rows(const RowSet& rs, bool dx, int k, int n
   __syncthreads();
 }
 
-// Sum over the team's lanes of a warp (for a block team: of the warp); other teams
-// of the warp may be elsewhere.
+// The team's lanes of a warp (for a block team: the warp); other teams of the warp may
+// be elsewhere.
+template <int TEAM>
+__device__ __forceinline__ unsigned lane_mask() {
+  constexpr int L = TEAM ? TEAM : 32;
+  return L == 32 ? 0xffffffffu : ((1u << (L & 31)) - 1u) << (threadIdx.x & 31 & ~(L - 1));
+}
+// Sum over them.
 template <int TEAM>
 __device__ __forceinline__ float lane_sum(float v) {
-  constexpr int L = TEAM ? TEAM : 32;
-  const unsigned mask = L == 32 ? 0xffffffffu : ((1u << (L & 31)) - 1u) << (threadIdx.x & 31 & ~(L - 1));
 #pragma unroll
-  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(mask, v, o);
+  for (int o = (TEAM ? TEAM : 32) / 2; o > 0; o >>= 1) v += __shfl_xor_sync(lane_mask<TEAM>(), v, o);
   return v;
 }
 
@@ -471,6 +475,9 @@ __global__ void __launch_bounds__(MAXT, MINB) k_norm_grad(const GradArgs a) {
         dyr = xr + d;
       } else {
         wait_async<kOwnStages - 1>();
+        // dx may be x or dy: lanes beyond a row have copied its last vector for
+        // themselves, which another lane writes over.
+        if (TEAM && d < width) __syncwarp(lane_mask<TEAM>());
         xr = own + static_cast<size_t>(q.slot) * 2 * width;
         dyr = xr + width;
       }

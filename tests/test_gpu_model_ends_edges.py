@@ -117,3 +117,23 @@ def test_norm_grad_of_rows_with_an_offset(kind, d):
     t = lambda a: torch.from_numpy(a).to(DEV)  # noqa: E731
     dx, _, _ = E.norm_grad(t(dy), t(x), t(mu) if kind == E.NORM_LAYER else None, t(rs), t(w), kind=kind)
     check(dx, want, tol, "dx")
+
+
+@pytest.mark.parametrize("kind", [E.NORM_LAYER, E.NORM_RMS])
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("d", [8, 24, 40, 72, 100, 136, 200, 264, 392, 520, 770, 776, 1003, 1544, 4104, 16_392, 20_000])
+def test_norm_grad_over_its_inputs(kind, dt, d):
+    """dx over dy and over x, in rows that leave lanes and threads of their last vector over: the bits of the others."""
+    T = min(4096, max(8, (1 << 22) // d))
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(d)
+    x, dy = (torch.empty((3, T, d), dtype=dt, device=DEV).normal_(generator=gen) for _ in range(2))
+    ln = torch.tensor([T, 1, T // 2], dtype=torch.int32, device=DEV)
+    w = torch.rand((d,), generator=gen, device=DEV).to(dt)
+    for lengths in (None, ln):
+        _, mean, rstd = E.norm(x, w, kind=kind, lengths=lengths)
+        want = E.norm_grad(dy, x, mean, rstd, w, kind=kind, lengths=lengths)
+        for over in ("dy", "x"):
+            a, b = dy.clone(), x.clone()
+            got = E.norm_grad(a, b, mean, rstd, w, kind=kind, lengths=lengths, dx=a if over == "dy" else b)
+            assert all(torch.equal(p, q) for p, q in zip(got, want)), over
