@@ -357,13 +357,18 @@ __device__ __forceinline__ void put_peer(const MaxSum* slot, const uint64_t* bar
 
 // A cluster works on `rows` consecutive rows. The next row's target and weight are
 // asked for at the start of a row, and its vectors follow each vector's last use
-// into the same places, which a thread shares with no other.
+// into the same places, which a thread shares with no other. The first warp waits for
+// the other CTAs' sums and tells the rest of its CTA, so that all threads go the same
+// way. Where a wait runs out, the CTA takes no further part, lets its copies arrive and
+// stays until no CTA of the cluster may store to it any more; the others' waits for it
+// run out in turn.
 template <typename T, bool GRAD>
 __global__ void __launch_bounds__(kSliceThreads, 4) k_loss(const LossArgs a, int M, int rows, int per, int cs,
                                                            unsigned* status) {
   constexpr int N = 16 / sizeof(T), K = 4;
-  extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ MaxSum part[kSliceThreads / 32], peers[2][kMaxCluster];
+  extern __shared__ __align__(128) uint8_t smem[];  // 16 bytes off 32 cost 8 % (8192 classes of bf16)
+  __shared__ MaxSum part[kSliceThreads / 32], peers[2][kMaxCluster], all;
+  __shared__ bool lost;
   __shared__ uint64_t bar[2];
   __shared__ float target_logit;
   const int tid = threadIdx.x, nt = blockDim.x, nw = nt >> 5;
@@ -449,10 +454,20 @@ __global__ void __launch_bounds__(kSliceThreads, 4) k_loss(const LossArgs a, int
         const int set = turn & 1;
         if (!met) cluster_wait();  // every CTA of the cluster runs, its mbarriers set
         met = true;
-        if (tid < cs) put_peer(&peers[set][rank], &bar[set], tid, v);
-        mbar_wait_cluster(&bar[set], (turn >> 1) & 1, status);
-        if (tid == 0) mbar_arrive_expect_tx(&bar[set], cs * sizeof(MaxSum));  // for the turn after next
-        v = join_all(peers[set], cs);
+        if (tid < 32) {
+          if (tid < cs) put_peer(&peers[set][rank], &bar[set], tid, v);
+          const bool came = __all_sync(0xffffffffu, mbar_wait_cluster(&bar[set], (turn >> 1) & 1, status));
+          if (tid == 0) {
+            lost = !came;
+            if (came) {
+              mbar_arrive_expect_tx(&bar[set], cs * sizeof(MaxSum));  // for the turn after next
+              all = join_all(peers[set], cs);
+            }
+          }
+        }
+        __syncthreads();
+        if (lost) break;
+        v = all;
         ++turn;
       }
       if (!near(v.m)) {  // in every CTA of the cluster
@@ -506,6 +521,12 @@ __global__ void __launch_bounds__(kSliceThreads, 4) k_loss(const LossArgs a, int
     xt = first && p.j.kept ? to_f32(p.x[p.j.target]) : 0.f;
   }
   if (!met) cluster_wait();
+  if (cs > 1 && met && lost) {
+    commit_async();
+    wait_async<0>();
+    cluster_arrive();
+    cluster_wait();  // for the threads of the cluster that have not ended
+  }
 }
 
 // -------------------------------------------------------------------- launching
