@@ -756,11 +756,7 @@ cudaError_t embed_sum(SumArgs a, cudaStream_t st) {
   const long long blocks = static_cast<long long>(a.tiles) * a.groups;
   if (blocks > 0x7FFFFFFFLL) return cudaErrorInvalidConfiguration;
   const int smem = kFlightBytes<T, N> + a.teams * a.chunk * 12 + 16;
-  if (smem > 40 * 1024) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(k_embed_sum<T, G, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
-  }
+  if (cudaError_t e = allow_smem(k_embed_sum<T, G, N>, smem); e != cudaSuccess) return e;
   k_embed_sum<T, G, N><<<static_cast<unsigned>(blocks), kThreads, smem, st>>>(a);
   if (a.groups > 1) {
     const long long join = (static_cast<long long>(a.groups) * ((a.nv + 3) / 4) + kThreads / 32 - 1) / (kThreads / 32);

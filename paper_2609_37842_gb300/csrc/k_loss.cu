@@ -578,10 +578,7 @@ cudaError_t loss_launch(LossArgs a, unsigned* status, int num_sms, cudaStream_t 
   const int threads = std::min(kSliceThreads, std::max(64, (per / each + 31) / 32 * 32));
   const int rows = loss_rows(M, cs, threads, num_sms);
   auto k = grad ? k_loss<T, true> : k_loss<T, false>;
-  if (smem > 40 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-    if (e != cudaSuccess) return e;
-  }
+  if (cudaError_t e = allow_smem(k, smem); e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>((M + rows - 1) / rows) * cs);
   cfg.blockDim = dim3(threads);

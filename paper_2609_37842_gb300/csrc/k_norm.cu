@@ -784,12 +784,6 @@ int resident(F k, int threads, int most) {
   return std::max(1, std::min({most, warps / (threads / 32), 2048 / threads}));
 }
 
-template <typename F>
-cudaError_t allow_smem(F k, size_t bytes) {
-  if (bytes <= 40 * 1024) return cudaSuccess;  // with the static part, below the 48 KB that need no asking
-  return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
-}
-
 // Examples as one run of rows where no lengths and no strides tell them apart.
 template <typename... V>
 RowSet flatten(const RowSet& rs, const V&... v) {

@@ -339,3 +339,16 @@ inline int row_vec(const RowView& v, const RowSet& rs, long long n, int es) {
 // Whether example strides continue the token strides, so that B examples of T
 // tokens are one run of rows.
 inline bool flat(const RowView& v, const RowSet& rs) { return rs.B == 1 || v.bs == v.ld * rs.T; }
+
+// Lets kernel k be launched with `bytes` of dynamic shared memory. The limit belongs to
+// the process: calls of several host threads share it, so every call sets the same
+// value, which none of them can need more than, and no thread takes from another what
+// it has asked for. (227 KB a block, less up to 3 KB of static arrays.)
+constexpr size_t kMostDynamicSmem = 224 * 1024;
+constexpr size_t kFreeDynamicSmem = 40 * 1024;  // with the static part, below the 48 KB that need no asking
+template <typename F>
+cudaError_t allow_smem(F k, size_t bytes) {
+  if (bytes <= kFreeDynamicSmem) return cudaSuccess;
+  if (bytes > kMostDynamicSmem) return cudaErrorInvalidValue;
+  return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMostDynamicSmem));
+}

@@ -137,3 +137,54 @@ def test_norm_grad_over_its_inputs(kind, dt, d):
             a, b = dy.clone(), x.clone()
             got = E.norm_grad(a, b, mean, rstd, w, kind=kind, lengths=lengths, dx=a if over == "dy" else b)
             assert all(torch.equal(p, q) for p, q in zip(got, want)), over
+
+
+# ----------------------------------------------------------- all operators
+def test_host_threads_with_calls_of_different_sizes():
+    """Calls of several host threads, each on a stream of its own, that launch one kernel with different amounts of
+    shared memory: none is refused, and all give what they give alone."""
+    import threading
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(1)
+    R, L = 200, E.lib()
+    jobs = []      # (call, its arguments but for the stream, outputs): nothing but the C calls in the threads' loops
+    for V in (12_500, 17_000, 22_000, 27_000):     # 50 to 108 KB a row of fp32
+        x = torch.randn((R, V), generator=gen, device=DEV)
+        tgt = torch.randint(0, V, (R,), generator=gen, device=DEV)
+        loss, g = torch.empty(R, device=DEV), torch.empty_like(x)
+        jobs.append((L.eogp_cross_entropy,
+                     (x.data_ptr(), E.F32, 0, V, tgt.data_ptr(), E.I64, 0, None, -100, None, 1, R, V, loss.data_ptr(),
+                      None, g.data_ptr(), 0, V), (loss, g), (x, tgt)))
+    for d in (260, 300, 340, 384):                 # 51 to 53 KB a block, of one kernel
+        x, dy = (torch.randn((R, d), generator=gen, device=DEV) for _ in range(2))
+        _, mean, rstd = E.norm(x)
+        dx = torch.empty_like(x)
+        jobs.append((L.eogp_norm_grad,
+                     (E.NORM_LAYER, dy.data_ptr(), 0, d, x.data_ptr(), E.F32, 0, d, mean.data_ptr(), rstd.data_ptr(),
+                      None, E.F32, None, 1, R, d, dx.data_ptr(), 0, d, None, None, 0, 0, 0, None, 0), (dx,),
+                     (x, dy, mean, rstd)))
+    torch.cuda.synchronize()
+    for call, args, outs, _ in jobs:
+        assert call(*args, None) == E.OK
+    torch.cuda.synchronize()
+    want = [[t.clone() for t in outs] for _, _, outs, _ in jobs]
+    torch.cuda.synchronize()
+    refused = []
+
+    def work(call, args):
+        stream = torch.cuda.Stream()
+        for _ in range(4000):
+            if call(*args, stream.cuda_stream) != E.OK:
+                refused.append(E.lib().eogp_last_error())
+                break
+        stream.synchronize()
+
+    threads = [threading.Thread(target=work, args=j[:2]) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not refused, refused
+    for j, expect in zip(jobs, want):
+        assert all(torch.equal(p, q) for p, q in zip(j[2], expect))
