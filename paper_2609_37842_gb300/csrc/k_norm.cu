@@ -714,13 +714,14 @@ __global__ void __launch_bounds__(kThreads) k_norm_dx_rows(NormGrad g) {
 }
 
 // dw, db: one thread per channel sums the rows of a block's run, with the pieces
-// and slots of k_norm_grad.
+// and slots of k_norm_grad. Channels along grid.x, which has room for any width; the runs,
+// at most kGradOcc a multiprocessor, along grid.y.
 template <typename T, bool RMS>
 __global__ void __launch_bounds__(kThreads) k_norm_dparam_rows(const GradArgs a) {
   const NormGrad& g = a.g;
-  const int c = blockIdx.y * kThreads + threadIdx.x;
+  const int c = blockIdx.x * kThreads + threadIdx.x;
   if (c >= g.d) return;
-  const long long first = static_cast<long long>(blockIdx.x) * a.per;
+  const long long first = static_cast<long long>(blockIdx.y) * a.per;
   const int hi = static_cast<int>(min(static_cast<long long>(a.M), first + a.per)), lo = static_cast<int>(first);
   for (int p0 = lo; p0 < hi;) {
     const int e = p0 / a.rpg;
@@ -739,7 +740,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_dparam_rows(const GradArgs a)
     if (begins && ends) {
       put_sums(g, e, c, sw, sb);
     } else {
-      float* slot = a.slots + (static_cast<size_t>(blockIdx.x) * 2 + (begins ? 1 : 0)) * 2 * g.d;
+      float* slot = a.slots + (static_cast<size_t>(blockIdx.y) * 2 + (begins ? 1 : 0)) * 2 * g.d;
       slot[c] = sw;
       slot[g.d + c] = sb;
     }
@@ -936,7 +937,9 @@ cudaError_t grad_launch(GradArgs& a, int num_sms, cudaStream_t st) {
   a.per = grad_rows(a.M, num_sms, kGradOcc);
   if (g.dweight || g.dbias) {
     auto k = g.rms ? k_norm_dparam_rows<T, true> : k_norm_dparam_rows<T, false>;
-    k<<<dim3(ceil_div(a.M, a.per), ceil_div(g.d, kThreads)), kThreads, 0, st>>>(a);
+    k<<<dim3(ceil_div(g.d, kThreads), ceil_div(a.M, a.per)), kThreads, 0, st>>>(a);
+    // dx may go over dy or x: not after sums that did not start.
+    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
   }
   if (g.dx.p) {
     auto k = g.rms ? k_norm_dx_rows<T, true> : k_norm_dx_rows<T, false>;

@@ -139,6 +139,32 @@ def test_norm_grad_over_its_inputs(kind, dt, d):
             assert all(torch.equal(p, q) for p, q in zip(got, want)), over
 
 
+def test_norm_grad_of_very_wide_rows():
+    """More channels than 65,535 blocks of threads: the weights' gradients and dx, in place of dy."""
+    if torch.cuda.mem_get_info()[0] < 8 << 30:
+        pytest.skip("needs 8 GB of device memory")
+    T, d = 2, 65_536 * 256 + 257
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(5)
+    x, dy = (torch.randn((1, T, d), generator=gen, device=DEV) for _ in range(2))
+    mean, rstd = x.mean(-1), 1 / x.std(-1)
+    xh = (x.double() - mean.double()[..., None]) * rstd.double()[..., None]
+    g = dy.double()
+    dw_w, db_w = (g * xh).sum((0, 1)), g.sum((0, 1))
+    dw_m, db_m = (g * xh).abs().sum((0, 1)), g.abs().sum((0, 1))
+    m1, m2 = g.mean(-1, keepdim=True), (g * xh).mean(-1, keepdim=True)
+    dx_w = rstd.double()[..., None] * (g - m1 - xh * m2)
+    # The means over channels: chains of d / 256 terms, whose errors of random sign add up to far less than the
+    # bound d / 256 u; it is 4e-3 of the mean magnitudes, which are below 1.
+    c = d / 256 + 32
+    dx_m = rstd.double()[..., None] * U * ((c + 8) * (1 + xh.abs()) + 8 * g.abs())
+    dx, dw, db = E.norm_grad(dy, x, mean, rstd, dx=dy)
+    assert dx is dy
+    assert bool(((dw.double() - dw_w).abs() <= 8 * U * dw_m).all())
+    assert bool(((db.double() - db_w).abs() <= 4 * U * db_m).all())
+    assert bool(((dx.double() - dx_w).abs() <= dx_m).all())
+
+
 # ----------------------------------------------------------- all operators
 def test_host_threads_with_calls_of_different_sizes():
     """Calls of several host threads, each on a stream of its own, that launch one kernel with different amounts of
