@@ -6,6 +6,7 @@
 #include <algorithm>
 
 #include "rows_dev.cuh"
+#include "sort_plan.h"
 
 using namespace eogp;
 
@@ -81,31 +82,11 @@ __global__ void __launch_bounds__(kThreads) k_embed(RowSet rs, TokenView tok, co
 // the warp's own counters in shared memory, and the warps' counters are added up
 // once a tile. Up to one tile of positions is sorted by one block, up to eight by a
 // cluster of blocks, in one launch.
-constexpr int kMaxBins = 512;
-constexpr int kItems = 8;
-constexpr int kSortThreads = 512;
-constexpr int kTile = kSortThreads * kItems;
+constexpr int kMaxBins = 1 << kMaxSortBits;
+constexpr int kItems = kSortItems;
+constexpr int kTile = kSortTile;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kMaxSortBlocks = 256;
 constexpr int kMarked = 1024;
-
-struct SortPlan {
-  int passes, bits, bins, blocks, per_block;  // per_block: positions of a block's range
-};
-
-SortPlan sort_plan(int V, long long M) {
-  SortPlan p;
-  int key_bits = 1;
-  while ((1ll << key_bits) <= V) ++key_bits;  // keys 0..V
-  p.passes = (key_bits + 8) / 9;
-  p.bits = (key_bits + p.passes - 1) / p.passes;
-  p.bins = 1 << p.bits;
-  const long long tiles = (M + kTile - 1) / kTile;
-  const long long each = (tiles + kMaxSortBlocks - 1) / kMaxSortBlocks;
-  p.per_block = static_cast<int>(each * kTile);
-  p.blocks = static_cast<int>((tiles + each - 1) / each);
-  return p;
-}
 
 // A token's mark. Neighbours lie apart: the frequent tokens of many vocabularies are
 // neighbours, and stores to one sector wait for each other (keys and marks of 262,144

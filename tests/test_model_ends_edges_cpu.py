@@ -1,6 +1,10 @@
 """Checks of the model-end operators' host side and sources that need no GPU."""
 import os
 import re
+import shutil
+import subprocess
+
+import pytest
 
 from paper_2609_37842_gb300 import build as B
 
@@ -18,3 +22,40 @@ def test_an_expired_wait_is_answered():
                     dropped = re.match(r"\s*mbar_wait(_cluster)?\(", line)
                     assert not dropped or "EOGP_WAIT_CYCLES /" in line, (name, line)
     assert waits
+
+
+SORT_PLAN_CHECK = r"""
+#include "sort_plan.h"
+#include <initializer_list>
+#include <cstdio>
+int main() {
+  const long long most = 1ll << 30;
+  for (int V : {1, 2, 511, 512, 513, 50000, 262143, 262144, 1 << 30})
+    for (long long M : {0ll, 1ll, 4095ll, 4096ll, 4097ll, 32768ll, 32769ll, 1048576ll, 1048577ll, most - 1, most}) {
+      const SortPlan p = sort_plan(V, M);
+      const bool keys = p.bits <= kMaxSortBits && p.bins == 1 << p.bits && (1ll << (p.passes * p.bits)) > V;
+      const bool all = p.blocks <= kMaxSortBlocks && static_cast<long long>(p.blocks) * p.per_block >= M;
+      const bool used = M == 0 ? p.blocks == 0 : static_cast<long long>(p.blocks - 1) * p.per_block < M;
+      if (!keys || !all || !used) {
+        std::printf("V %d M %lld: %d passes of %d bits, %d blocks of %d\n", V, M, p.passes, p.bits, p.blocks,
+                    p.per_block);
+        return 1;
+      }
+    }
+  return 0;
+}
+"""
+
+
+def test_sort_plan(tmp_path):
+    """The plan of the embedding gradient's sort, compiled without optimisation and with undefined arithmetic trapped:
+    it covers all positions and keys, and a batch without positions needs no block."""
+    gxx = shutil.which("g++")
+    if gxx is None:
+        pytest.skip("no g++")
+    src, exe = tmp_path / "plan.cpp", tmp_path / "plan"
+    src.write_text(SORT_PLAN_CHECK)
+    subprocess.run([gxx, "-std=c++17", "-O0", "-fsanitize=undefined", "-fsanitize-undefined-trap-on-error",
+                    "-I", B.CSRC, str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, (r.returncode, r.stdout)
