@@ -850,7 +850,9 @@ def _like(t, name: str, shape, dtype):
 
 
 def _device_of(*tensors):
-    """The CUDA device that all tensors (None allowed) are on: kernels read them by address."""
+    """The CUDA device that all tensors (None allowed) are on: kernels read them by address. It has to be the current
+    one, which the library launches on."""
+    import torch
     dev = None
     for t in tensors:
         if t is not None:
@@ -861,6 +863,8 @@ def _device_of(*tensors):
                 dev = d
             elif d != dev:
                 raise ValueError("all tensors must be on the same CUDA device")
+    if dev is not None and dev.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors' device {dev} must be the current CUDA device")
     return dev
 
 

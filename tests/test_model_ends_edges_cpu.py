@@ -3,10 +3,14 @@ import os
 import re
 import shutil
 import subprocess
+from types import SimpleNamespace
 
 import pytest
 
 from paper_2609_37842_gb300 import build as B
+from paper_2609_37842_gb300 import eogp as E
+
+torch = pytest.importorskip("torch")
 
 
 def test_an_expired_wait_is_answered():
@@ -59,3 +63,13 @@ def test_sort_plan(tmp_path):
                     "-I", B.CSRC, str(src), "-o", str(exe)], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0, (r.returncode, r.stdout)
+
+
+def test_tensors_of_a_device_that_is_not_current(monkeypatch):
+    """The library launches on the current device, whose kernels could not read another device's memory."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    t = SimpleNamespace(device=torch.device("cuda", 1))
+    for f in (lambda: E.norm(t), lambda: E.embed(t, t), lambda: E.embed_grad(t, t, 4), lambda: E.cross_entropy(t, t),
+              lambda: E.norm_grad(t, t, t, t)):
+        with pytest.raises(ValueError, match="current CUDA device"):
+            f()
