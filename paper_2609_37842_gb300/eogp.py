@@ -788,6 +788,14 @@ def fit_pca_from_moment(C, n_total: int, k: int, pt_dtype: int = F32, stream=Non
 # -------------------------------------------------------------- model ends
 # Small calls cost as much on the host as on the device: these functions look at a
 # tensor once, and only check what the caller gave.
+_INT_MAX = 2 ** 31 - 1
+
+
+def _too_large(name: str):
+    """For sizes that a C int does not hold: ctypes would pass their lowest 32 bits on."""
+    raise EOGPError(EUNSUPPORTED, f"{name}: sizes must be < 2^31")
+
+
 def _rows_of(t, name: str):
     """(B, T, n, example stride, token stride) of rows [B, T, n] or [T, n]."""
     shape, stride = t.shape, t.stride()
@@ -801,6 +809,8 @@ def _rows_of(t, name: str):
         raise ValueError(f"{name} must be [B, T, n] or [T, n]")
     if inner != 1 and n > 1 and B * T > 0:
         raise ValueError(f"{name} must have unit stride along its last dimension")
+    if B > _INT_MAX or T > _INT_MAX or n > _INT_MAX:
+        _too_large(name)
     return B, T, n, bs, ld
 
 
@@ -816,6 +826,8 @@ def _tokens_of(t, name: str):
         raise ValueError(f"{name} must be [B, T] or [T]")
     if inner != 1 and T > 1 and B > 0:
         raise ValueError(f"{name} must have unit stride along its last dimension")
+    if B > _INT_MAX or T > _INT_MAX:
+        _too_large(name)
     code = _type_codes().get(t.dtype)
     if code != I64 and code != I32:
         raise ValueError(f"unsupported dtype {t.dtype} for token numbers (int32 or int64)")
@@ -907,6 +919,8 @@ def embed(tokens, table, scale: float = 1.0, pos=None, lengths=None, out=None, s
     ldt, inner = table.stride()
     if inner != 1 and d > 1:
         raise ValueError("table must have unit stride along its last dimension")
+    if V > _INT_MAX or d > _INT_MAX:
+        _too_large("table")
     ldp = 0
     if pos is not None:
         if pos.dim() != 2 or pos.dtype != table.dtype or pos.shape[1] != d or pos.shape[0] < T:
@@ -936,6 +950,8 @@ def embed_grad(tokens, dout, V: int, scale: float = 1.0, lengths=None, dtable=No
     if dout.shape[:-1] != tokens.shape:
         raise ValueError("dout must be [*tokens.shape, d]")
     _, _, d, dbs, dld = _rows_of(dout, "dout")
+    if not -_INT_MAX <= V <= _INT_MAX:
+        _too_large("V")
     L = lib()
     need = c_size_t()
     _check(L.eogp_embed_grad_workspace_size(V, d, B, T, need))

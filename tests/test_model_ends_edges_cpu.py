@@ -13,6 +13,12 @@ from paper_2609_37842_gb300 import eogp as E
 torch = pytest.importorskip("torch")
 
 
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    B.build()
+    E.lib()
+
+
 def test_an_expired_wait_is_answered():
     """A bounded wait that runs out must change what the kernel does next: a CTA that went on would use stale data,
     and might leave while another still stores to its shared memory. Only the drain after an expired wait, which has
@@ -73,3 +79,21 @@ def test_tensors_of_a_device_that_is_not_current(monkeypatch):
               lambda: E.norm_grad(t, t, t, t)):
         with pytest.raises(ValueError, match="current CUDA device"):
             f()
+
+
+def test_sizes_beyond_a_c_int(monkeypatch):
+    """A call whose size a C int does not hold is refused, not made on the size's lowest 32 bits. The tensors are
+    views of a few elements."""
+    monkeypatch.setattr(E, "_device_of", lambda *t: torch.device("cpu"))
+    n = 2 ** 32 + 2
+    rows, tok = torch.zeros(1, 1, 8), torch.zeros((1, 1), dtype=torch.int64)
+    many, toks = rows.expand(n, 1, 8), tok.expand(n, 1)
+    stat = torch.zeros(1, 1).expand(n, 1)
+    small = torch.zeros(2, 1, 8)
+    for f in (lambda: E.norm(many, out=many), lambda: E.norm_grad(many, many, stat, stat),
+              lambda: E.embed(toks, torch.zeros(4, 8), out=many), lambda: E.embed(tok, torch.zeros(1, 8).expand(n, 8)),
+              lambda: E.embed_grad(toks, many, 4), lambda: E.embed_grad(tok.expand(2, 1), small, n),
+              lambda: E.cross_entropy(many, toks, dlogits=many)):
+        with pytest.raises(E.EOGPError) as e:
+            f()
+        assert e.value.code == E.EUNSUPPORTED
