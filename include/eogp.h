@@ -641,7 +641,7 @@ int eogp_norm_grad(int kind, const void* dy, long long dy_bs, long long dy_ld, c
  * target equals ignore_index, or when its weight is 0. Logits of -inf have
  * probability 0; rows without a finite logit, or with a NaN or +inf, give NaN.
  * Finite logits may have any size (masks of -1e9 or the type's lowest value, say);
- * rows whose largest one is beyond +-2^20 take a slower path.
+ * rows whose largest one is beyond +-2^27 take a slower path.
  * loss and lse fp32 [B x T], dense; lse and dlogits may be NULL; dlogits has the
  * type of logits and may be logits itself with the same strides. */
 int eogp_cross_entropy(const void* logits, int dtype, long long logits_bs, long long logits_ld,

@@ -7,11 +7,13 @@
 // c = m log2(e) for the maximum m so far, s = sum 2^(x log2(e) - c), one fused
 // multiply-add and one exponential a logit; sums of different references are joined
 // by 2^(c - c'). c is rounded to fp32 and x log2(e) is not, so 2^(x log2(e) - c) at
-// x = m is off from 1 by up to half a unit in c's last place in the exponent: nothing up
-// to kNearLogit, but 2^64 and more from 1e9 on. Rows whose maximum is beyond that, or
-// infinite, take a plain path that forms x - m first (slow_row); logits below
-// -kNearLogit are held against that bound's reference, so that those met before a row's
-// larger ones add what they are worth, which is nothing, and no infinity.
+// x = m is not 1 but off by up to half a unit in c's last place in the exponent: by 8 up
+// to kNearLogit, where it takes no digits that count, by 64 at 1e9, by more than a float
+// holds beyond. Rows whose maximum is beyond kNearLogit, or infinite, take a plain path
+// that forms x - m first (slow_row, one CTA: 1 GB of bf16 with gradient where every row
+// does, 2.9 ms for 50,000 classes and 9.8 ms for 100,096, instead of 0.33 ms); logits
+// below -kNearLogit are held against that bound's reference, so that those met before a
+// row's larger ones add what they are worth, which is nothing, and no infinity.
 //
 // k_loss: a row lies in the shared memory of a CTA, or in slices in that of the CTAs
 // of a cluster. A thread copies its vectors to its own places and reads them there
@@ -36,7 +38,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kNearLogit = 1048576.f;  // c's last place is 1/8 at most: the exponent's error is 1/16
+constexpr float kNearLogit = 134217728.f;  // 2^27: c's last place is 16 at most
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;

@@ -35,7 +35,7 @@ def check_loss(x, tgt, **args):
 @pytest.mark.parametrize("V", LOSS_WIDTHS)
 def test_cross_entropy_far_rows(dt, V):
     """Rows of equal and of mixed logits far from 0: finite logits give finite losses, whatever they are."""
-    far = [s * m for m in (1e6, 2.0 ** 20, 2.0 ** 20 + 1, 1e9, 1e10, 1.1e10, 1e12, 1e20, 0.9e29, 3e29)
+    far = [s * m for m in (1e6, 2.0 ** 20, 2.0 ** 20 + 1, 3e7, 1e8, 2.0 ** 27, 2.0 ** 27 + 16, 3e8, 1e9, 1e10, 1.1e10, 1e12, 1e20, 0.9e29, 3e29)
            for s in (1, -1)]
     rng = np.random.default_rng(V)
     for q in far:
@@ -51,7 +51,7 @@ def test_cross_entropy_far_masks(dt, V):
     """Masks of finite values in front of, behind and between ordinary logits, single survivors, and logits that
     rise from far below: a thread, a warp or a block may meet the masked ones first, or nothing else."""
     rng = np.random.default_rng(V + 1)
-    for mask in (-3e4, -1e9, -1e10, -1.1e10, -1e12, -1e20, -0.9e29, -1e30):
+    for mask in (-3e4, -1e8, -1e9, -1e10, -1.1e10, -1e12, -1e20, -0.9e29, -1e30):
         x = rng.standard_normal((6, V)) * 2
         x[0, :V // 2] = mask
         x[1, V // 2:] = mask
@@ -63,8 +63,9 @@ def test_cross_entropy_far_masks(dt, V):
         x[5] = np.linspace(mask, 0, V)
         tgt = np.array([V - 2, 1, V - 1, V - 2, V - 1, V - 1])
         check_loss(torch.from_numpy(x.astype(np.float32)).to(DEV).to(dt), tgt)
-    x = np.stack([np.linspace(-3e6, 0, V), np.linspace(-3e6, -1.2e6, V), np.linspace(0, 3e6, V)])
-    check_loss(torch.from_numpy(x.astype(np.float32)).to(DEV).to(dt), np.array([V - 1, V - 1, V - 2]))
+    for far in (3e6, 3e8):             # through every bound on the way
+        x = np.stack([np.linspace(-far, 0, V), np.linspace(-far, -0.47 * far, V), np.linspace(0, far, V)])
+        check_loss(torch.from_numpy(x.astype(np.float32)).to(DEV).to(dt), np.array([V - 1, V - 1, V - 2]))
 
 
 @pytest.mark.parametrize("dt", TYPES)
