@@ -590,8 +590,9 @@ int eogp_embed(const void* tokens, int index_type, long long tokens_bs, const vo
                int B, int T, void* out, long long out_bs, long long out_ld, eogp_stream_t stream);
 
 /* dtable[v] (+)= scale * sum of dout[b][t] over the positions with
- * tokens[b][t] = v, in ascending order of (b, t): positions are sorted by token
- * and each token's run of rows is summed, with no floating-point atomics. Every
+ * tokens[b][t] = v: positions are sorted by token and each token's run of rows is
+ * summed, chunk by chunk in ascending order of (b, t) and then the chunks' sums, in an
+ * order that the sizes and the tokens fix, with no floating-point atomics. Every
  * row of dtable [V x ld_dtable] (type `grad_dtype`) is written, 0 for tokens that
  * do not occur; with `accumulate` the sums are added instead and rows of other
  * tokens are left alone. dout has type `dtype`. */

@@ -117,8 +117,10 @@ struct NormArgs {
 // channels of bf16: 8 vectors a thread and two warps take 8 % less). USUAL: weight
 // (and, for layer norm, bias) given and of the rows' type; the choice at each vector
 // otherwise fills the issue slots (65,536 rows of 4096 bf16: 185 us with it, 161 us
-// without). Measured, 0.5 GB in and out: 145 us (1.0 of the copy rate) in fp32, 149 us
-// (0.99) for 768 to 8192 channels of bf16, 152 to 233 us for 64 to 512.
+// without). The limit makes ten of the bf16 kernels and one of fp32 spill, up to 96
+// bytes stored and 264 loaded again a thread (8 vectors, layer norm), from and to L1.
+// Measured, 0.5 GB in and out: 141 to 149 us (1.0 of the copy rate) in fp32 up to 16,384
+// channels, 149 us (0.99) for 768 to 8192 channels of bf16, 153 to 233 us for 64 to 512.
 template <typename T, int N, int NV, int TEAM, bool RMS, bool USUAL>
 __global__ void __launch_bounds__(TEAM ? 128 : 512, TEAM ? 8 : 2) k_norm(const NormArgs a) {
   __shared__ float part[2][1][kMaxWarps];
@@ -350,8 +352,10 @@ __device__ __forceinline__ float2 block_sum2(float2 v, float2* part) {
 // weights are (WREG, of the rows' type) or lie in shared memory in fp32, 0 beyond the
 // row, where threads read the row's last vector again. What a thread does once a row
 // (waits, sums, addresses) is as much as the work on ten elements, so it has up to 32.
-// Measured, bytes against the copy rate: 0.89 for 768 and 1024 channels of bf16, 0.87
-// (layer) and 0.94 (RMS) for 4096, 0.92 for 2048 and 4096 of fp32.
+// Measured, bytes against the copy rate: 0.89 for 768 and 1024 channels of bf16, 0.85
+// (layer) and 0.94 (RMS) for 4096, 0.92 for 2048 and 4096 of fp32; narrow rows 0.77 to
+// 0.87 in fp32 and 0.60 to 0.87 in bf16, whose kernels for 17 to 64 vectors spill up to
+// 104 bytes a thread.
 template <typename T, int N, int NV, int TEAM, bool RMS, bool BULK, bool WREG, int MAXT, int MINB>
 __global__ void __launch_bounds__(MAXT, MINB) k_norm_grad(const GradArgs a) {
   using V = Vals<N>;
@@ -646,7 +650,8 @@ __global__ void __launch_bounds__(SLICES == 1 ? kThreads : 32 * SLICES) k_norm_g
 }
 
 // ---------------------------------------------- rows too wide for registers
-// One block per row, three passes over the row (the later ones from cache).
+// One block per row, three passes over the row (the later ones from cache), an element
+// a load: 20,001 channels of bf16 0.28 of the copy rate.
 template <typename T, bool RMS>
 __global__ void __launch_bounds__(kThreads) k_norm_rows(RowSet rs, RowView x, const void* w, const void* bias,
                                                         bool pbf, float eps, int d, RowView y, float* mean,
@@ -685,7 +690,8 @@ __global__ void __launch_bounds__(kThreads) k_norm_rows(RowSet rs, RowView x, co
   }
 }
 
-// dx: one block per row, two passes over the row.
+// dx: one block per row, two passes over the row. With the sums below, which read x and
+// dy again: 12,288 and 16,384 channels of fp32 0.26 of the copy rate, 24,576 of bf16 0.19.
 template <typename T, bool RMS>
 __global__ void __launch_bounds__(kThreads) k_norm_dx_rows(NormGrad g) {
   __shared__ float part[2][kWarps];
