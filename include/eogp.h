@@ -97,8 +97,9 @@ int eogp_sync_status(eogp_stream_t stream);
 #define EOGP_K_SIMT     5 /* fp32 CUDA-core kernels of the EOGP_F32 path       */
 #define EOGP_K_EMBED    6 /* token embedding and its gradient (a call's launches counted as one) */
 #define EOGP_K_NORM     7 /* normalisation and its gradient (likewise)         */
-#define EOGP_K_LOSS     8 /* token loss and its gradient                       */
-#define EOGP_K_COUNT    9
+#define EOGP_K_LOSS     8 /* token loss and distillation, with their gradients  */
+#define EOGP_K_HEAD     9 /* token loss through the output matrix and its gradient (likewise) */
+#define EOGP_K_COUNT    10
 int eogp_profile_enable(int on);
 int eogp_profile_read(int kind, int* launches, double* total_ms, int reset);
 
@@ -548,7 +549,8 @@ int eogp_score_topk(const void* train, int ld_train, const float* train_scales, 
                     void* ws, size_t ws_bytes, eogp_stream_t stream);
 
 /* ========================================================================
- * Model ends: token embedding, normalisation and token loss, with gradients
+ * Model ends: token embedding, normalisation, token loss and distillation, with
+ * gradients
  *
  * What a program runs around the linear modules to get their activations a_t
  * and output gradients s_t: the embedding starts the forward pass, a
@@ -649,6 +651,63 @@ int eogp_cross_entropy(const void* logits, int dtype, long long logits_bs, long 
                        const void* targets, int index_type, long long targets_bs, const float* weights,
                        long long ignore_index, const int32_t* lengths, int B, int T, int V, float* loss, float* lse,
                        void* dlogits, long long dlogits_bs, long long dlogits_ld, eogp_stream_t stream);
+
+/* Token loss through the output matrix, without the logits of the whole batch:
+ *   z = scale * x W^T,  x = x[b][t] [d], W = weight [V x d],
+ *   lse[b][t]  = log sum_v exp(z_v),
+ *   loss[b][t] = w * (lse - z_target),   w and what is left out as in eogp_cross_entropy,
+ * and the gradient of sum loss[b][t]: with D = w * scale * (softmax(z) - e_target) per position,
+ *   dx[b][t]  = D W                      (type `dtype`, 0 where a position is left out),
+ *   dweight (+)= sum D^T x               (type `grad_dtype`, [V x ld_dweight]; every row is written,
+ *                                         with `accumulate` the sums are added instead).
+ * dx and dweight may each be NULL; dx may be x with the same strides. Positions left out cost
+ * nothing but their zeros: the others are gathered first. With a gradient, the logits of a piece
+ * of the positions at a time lie in the workspace, in fp32, of at most about 4 GB (more only where
+ * 256 positions take more); without one none are stored.
+ * EOGP_BF16: products of bf16 on the tensor cores, sums in fp32. D enters the products for dx, and
+ * for a dweight of EOGP_BF16, rounded to bf16, as dlogits of eogp_cross_entropy would; for one of
+ * EOGP_F32 it enters as two bf16 parts (about 2^-16 relative). EOGP_F32: products to fp32.
+ * A NaN or infinity in a counted position's x, or in weight, reaches all that it is multiplied
+ * with: that position's loss, and dx or dweight. */
+int eogp_head_loss_workspace_size(const void* weight, int dtype, long long ld_weight, int V, int d, int B, int T,
+                                  int want_dx, int want_dweight, int grad_dtype, size_t* bytes);
+int eogp_head_loss(const void* x, int dtype, long long x_bs, long long x_ld, const void* weight,
+                   long long ld_weight, float scale, const void* targets, int index_type, long long targets_bs,
+                   const float* weights, long long ignore_index, const int32_t* lengths, int B, int T, int d, int V,
+                   float* loss, float* lse, void* dx, long long dx_bs, long long dx_ld, void* dweight,
+                   int grad_dtype, long long ld_dweight, int accumulate, void* ws, size_t ws_bytes,
+                   eogp_stream_t stream);
+
+/* Distillation from a teacher's top logits, and the gradient of the sum of the losses. Each
+ * position has a list of K entries: a class (classes[b][t][k], index_type; a negative number: no
+ * entry) and the teacher's logit y of it (teacher[b][t][k], type teacher_dtype). With p = softmax(x / h),
+ * x = logits[b][t], h = temperature:
+ *   teacher_lse NULL: q_k = softmax(y / h) over the list,
+ *     loss[b][t] = w * sum_k q_k (log q_k - log p_k);
+ *   else q_k = exp(y_k / h - teacher_lse[b][t]), where teacher_lse (fp32 [B x T], dense) is the log of
+ *     the sum of exp(y / h) over all the teacher's classes (0 for lists of log-probabilities with
+ *     h = 1), and what the lists leave of both sides is one more class:
+ *     q_r = max(0, 1 - sum q_k), p_r = 1 - sum p_k over the listed classes, summed without them,
+ *     loss[b][t] = w * (sum_k q_k (log q_k - log p_k) + q_r (log q_r - log p_r));
+ *   lse[b][t] = log sum_v exp(x_v / h),
+ *   dlogits[b][t] = (w / h) * (p - q) at listed classes and (w / h) * p * (1 - q_r / p_r), without
+ *     teacher_lse (w / h) * p, at the others.
+ * Where a list holds all V classes there is no such class more. Terms of q = 0 are 0. Multiply the weights by h^2 for the usual scaling of softened targets.
+ * A class that is listed twice counts as one entry with the sum of both q in the gradient, and as two
+ * in the loss. A position is left out (loss, lse and gradient 0, its logits not read) when it is
+ * padding, when its weight is 0, or, without teacher_lse, when no entry has a logit above -inf; a class >= V
+ * sets EOGP_EDEVICE in the device status word and leaves its position out. Rows of logits without a finite one,
+ * or with a NaN or +inf, give NaN; a NaN or +inf in a list gives a loss that is not finite; finite logits
+ * may have any size.
+ * loss and lse fp32 [B x T], dense; lse and dlogits may be NULL; dlogits has the type of logits
+ * and may be logits itself with the same strides. Rows of lists have the strides classes_bs / _ld
+ * and teacher_bs / _ld, K <= EOGP_DISTILL_MAX. */
+#define EOGP_DISTILL_MAX 256
+int eogp_distill(const void* logits, int dtype, long long logits_bs, long long logits_ld, const void* classes,
+                 int index_type, long long classes_bs, long long classes_ld, const void* teacher,
+                 int teacher_dtype, long long teacher_bs, long long teacher_ld, const float* teacher_lse, int K,
+                 float temperature, const float* weights, const int32_t* lengths, int B, int T, int V, float* loss,
+                 float* lse, void* dlogits, long long dlogits_bs, long long dlogits_ld, eogp_stream_t stream);
 
 #ifdef __cplusplus
 }

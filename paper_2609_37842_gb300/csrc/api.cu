@@ -1672,3 +1672,104 @@ extern "C" int eogp_cross_entropy(const void* logits, int dtype, long long logit
   CUDA_TRY(launch_cross_entropy(a, dtype == EOGP_BF16, status, sm_count(), st));
   return EOGP_OK;
 }
+
+extern "C" int eogp_head_loss_workspace_size(const void* weight, int dtype, long long ld_weight, int V, int d, int B,
+                                             int T, int want_dx, int want_dweight, int grad_dtype, size_t* bytes) {
+  clear_error();
+  if (!bytes) return set_error(EOGP_EINVAL, "bytes is NULL");
+  if (int rc = check_rows(B, T)) return rc;
+  if (!elem_type(dtype) || (want_dweight && !elem_type(grad_dtype))) return set_error(EOGP_EINVAL, "bad dtype");
+  if (dtype == EOGP_F32 && want_dweight && grad_dtype != EOGP_F32)
+    return set_error(EOGP_EUNSUPPORTED, "the gradient of an fp32 weight is fp32");
+  if (int rc = check_extent(V, "V")) return rc;
+  if (int rc = check_extent(d, "d")) return rc;
+  if (ld_weight < 0) return set_error(EOGP_EINVAL, "negative stride");
+  HeadArgs a{};
+  a.rs = RowSet{B, T, nullptr};
+  a.weight = weight;
+  a.ld_weight = ld_weight;
+  a.bf16 = dtype == EOGP_BF16;
+  a.grad_bf16 = grad_dtype == EOGP_BF16;
+  a.d = d;
+  a.V = V;
+  a.dx.p = want_dx ? &a : nullptr;
+  a.dweight = want_dweight ? &a : nullptr;
+  *bytes = head_loss_ws_bytes(a);
+  return EOGP_OK;
+}
+
+extern "C" int eogp_head_loss(const void* x, int dtype, long long x_bs, long long x_ld, const void* weight,
+                              long long ld_weight, float scale, const void* targets, int index_type,
+                              long long targets_bs, const float* weights, long long ignore_index,
+                              const int32_t* lengths, int B, int T, int d, int V, float* loss, float* lse, void* dx,
+                              long long dx_bs, long long dx_ld, void* dweight, int grad_dtype, long long ld_dweight,
+                              int accumulate, void* ws, size_t ws_bytes, eogp_stream_t stream) {
+  clear_error();
+  size_t need = 0;
+  if (int rc = eogp_head_loss_workspace_size(weight, dtype, ld_weight, V, d, B, T, dx != nullptr, dweight != nullptr,
+                                             grad_dtype, &need))
+    return rc;
+  if (!index_type_ok(index_type)) return set_error(EOGP_EINVAL, "bad index_type");
+  if (!std::isfinite(scale)) return set_error(EOGP_EINVAL, "scale must be finite");
+  if (!dweight) grad_dtype = dtype;
+  const bool empty = B == 0 || T == 0;
+  if (empty && !dweight) return EOGP_OK;
+  if (!empty && (!x || !weight || !targets || !loss)) return set_error(EOGP_EINVAL, "NULL argument");
+  if (!aligned_to(x, dtype) || !aligned_to(weight, dtype) || !aligned_to(targets, index_type) ||
+      !aligned_to(weights, EOGP_F32) || !aligned_to(loss, EOGP_F32) || !aligned_to(lse, EOGP_F32) ||
+      !aligned_to(lengths, EOGP_I32) || !aligned_to(dx, dtype) || !aligned_to(dweight, grad_dtype))
+    return set_error(EOGP_EINVAL, "an array is not aligned to its elements");
+  if (targets_bs < 0 || !in_strides_ok(x_bs, x_ld)) return set_error(EOGP_EINVAL, "negative stride");
+  if (dx && !empty && !out_strides_ok(dx_bs, dx_ld, B, T, d)) return set_error(EOGP_EINVAL, "rows of dx overlap");
+  if (dweight && V > 1 && ld_dweight < d) return set_error(EOGP_EINVAL, "ld_dweight < d");
+  if (need && (!ws || ws_bytes < need)) return set_error(EOGP_EWORKSPACE, "workspace of %zu bytes needed", need);
+  if (need && (reinterpret_cast<uintptr_t>(ws) & 255))
+    return set_error(EOGP_EINVAL, "workspace must be 256-byte aligned");
+  unsigned* status = status_word();
+  if (!status) return set_error(EOGP_ECUDA, "device status word unavailable");
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  ProfScope ps(EOGP_K_HEAD, st);
+  const HeadArgs a{RowSet{B, T, lengths}, RowView{x, x_bs, x_ld}, RowView{dx, dx_bs, dx_ld}, weight, ld_weight,
+                   dtype == EOGP_BF16, grad_dtype == EOGP_BF16, accumulate != 0, scale,
+                   TokenView{targets, index_type == EOGP_I64, targets_bs}, weights, ignore_index, d, V, loss, lse,
+                   dweight, ld_dweight};
+  CUDA_TRY(launch_head_loss(a, ws, status, sm_count(), st));
+  return EOGP_OK;
+}
+
+extern "C" int eogp_distill(const void* logits, int dtype, long long logits_bs, long long logits_ld,
+                            const void* classes, int index_type, long long classes_bs, long long classes_ld,
+                            const void* teacher, int teacher_dtype, long long teacher_bs, long long teacher_ld,
+                            const float* teacher_lse, int K, float temperature, const float* weights,
+                            const int32_t* lengths, int B, int T, int V, float* loss, float* lse, void* dlogits,
+                            long long dlogits_bs, long long dlogits_ld, eogp_stream_t stream) {
+  clear_error();
+  if (int rc = check_rows(B, T)) return rc;
+  if (!elem_type(dtype) || !elem_type(teacher_dtype)) return set_error(EOGP_EINVAL, "bad dtype");
+  if (!index_type_ok(index_type)) return set_error(EOGP_EINVAL, "bad index_type");
+  if (int rc = check_extent(V, "V")) return rc;
+  if (K < 1 || K > EOGP_DISTILL_MAX) return set_error(EOGP_EINVAL, "K must be in [1, %d]", EOGP_DISTILL_MAX);
+  if (!std::isfinite(temperature) || !(temperature > 0.f) || !std::isfinite(1.f / temperature))
+    return set_error(EOGP_EINVAL, "temperature and its reciprocal must be finite and > 0");
+  if (B == 0 || T == 0) return EOGP_OK;
+  if (!logits || !classes || !teacher || !loss) return set_error(EOGP_EINVAL, "NULL argument");
+  if (!aligned_to(logits, dtype) || !aligned_to(dlogits, dtype) || !aligned_to(classes, index_type) ||
+      !aligned_to(teacher, teacher_dtype) || !aligned_to(teacher_lse, EOGP_F32) || !aligned_to(weights, EOGP_F32) ||
+      !aligned_to(loss, EOGP_F32) || !aligned_to(lse, EOGP_F32) || !aligned_to(lengths, EOGP_I32))
+    return set_error(EOGP_EINVAL, "an array is not aligned to its elements");
+  if (!in_strides_ok(logits_bs, logits_ld) || !in_strides_ok(classes_bs, classes_ld) ||
+      !in_strides_ok(teacher_bs, teacher_ld))
+    return set_error(EOGP_EINVAL, "negative stride");
+  if (dlogits && !out_strides_ok(dlogits_bs, dlogits_ld, B, T, V))
+    return set_error(EOGP_EINVAL, "rows of dlogits overlap");
+  unsigned* status = status_word();
+  if (!status) return set_error(EOGP_ECUDA, "device status word unavailable");
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  ProfScope ps(EOGP_K_LOSS, st);
+  const DistillArgs a{RowSet{B, T, lengths}, RowView{logits, logits_bs, logits_ld},
+                      RowView{dlogits, dlogits_bs, dlogits_ld}, RowView{classes, classes_bs, classes_ld},
+                      RowView{teacher, teacher_bs, teacher_ld}, index_type == EOGP_I64, teacher_dtype == EOGP_BF16,
+                      teacher_lse, weights, K, V, temperature, loss, lse};
+  CUDA_TRY(launch_distill(a, dtype == EOGP_BF16, status, sm_count(), st));
+  return EOGP_OK;
+}

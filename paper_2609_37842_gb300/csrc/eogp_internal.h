@@ -273,3 +273,35 @@ struct LossArgs {
   float *loss, *lse;
 };
 cudaError_t launch_cross_entropy(const LossArgs& a, bool bf16, unsigned* status, int num_sms, cudaStream_t st);
+
+// k_head.cu
+struct HeadArgs {
+  RowSet rs;
+  RowView x, dx;  // dx.p NULL: not wanted
+  const void* weight;
+  long long ld_weight;
+  bool bf16, grad_bf16, accumulate;
+  float scale;
+  TokenView targets;
+  const float* weights;
+  long long ignore;
+  int d, V;
+  float *loss, *lse;
+  void* dweight;  // NULL: not wanted
+  long long ld_dweight;
+};
+size_t head_loss_ws_bytes(const HeadArgs& a);
+cudaError_t launch_head_loss(const HeadArgs& a, void* ws, unsigned* status, int num_sms, cudaStream_t st);
+
+// k_distill.cu
+struct DistillArgs {
+  RowSet rs;
+  RowView logits, dlogits;  // dlogits.p NULL: not wanted
+  RowView classes, teacher;
+  bool classes_i64, teacher_bf16;
+  const float *teacher_lse, *weights;
+  int K, V;
+  float temperature;
+  float *loss, *lse;
+};
+cudaError_t launch_distill(const DistillArgs& a, bool bf16, unsigned* status, int num_sms, cudaStream_t st);

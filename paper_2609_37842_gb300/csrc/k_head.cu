@@ -1,0 +1,382 @@
+// Token loss through the output matrix and its gradient. Per counted position, with
+// z = scale x W^T over the V classes:
+//   lse = log sum_v exp(z_v),  loss = w (lse - z_target),
+//   D = w scale (exp(z - lse) - e_target),  dx = D W,  dW (+)= sum D^T x.
+//
+// The counted positions (inside their example's length, target not ignored, weight not
+// 0) are found first and their rows of x gathered, a piece of them at a time: what is
+// left out costs no products. The logits of one piece lie in the workspace in fp32 and
+// become D in place.
+#include <algorithm>
+
+#include "rows_dev.cuh"
+
+using namespace eogp;
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kFindThreads = 1024;
+constexpr int kFindBlocks = 1024;
+constexpr size_t kPieceBytes = size_t(4) << 30;  // logits of a piece
+
+size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
+long long up(long long x, long long a) { return (x + a - 1) / a * a; }
+
+// Where everything lies in the workspace.
+struct Plan {
+  int find_blocks, per_block;  // blocks of the search, positions of each
+  int piece, pieces;           // rows of a piece, most pieces
+  int ldz, ldx;                // row strides of the logits and of the gathered rows
+  size_t counts, idx, target, w, x, z, acc, total;
+};
+
+Plan plan_of(const HeadArgs& a) {
+  Plan p{};
+  const long long M = a.rs.rows();
+  if (M == 0) return p;
+  const long long tiles = (M + kFindThreads - 1) / kFindThreads;
+  const long long each = (tiles + kFindBlocks - 1) / kFindBlocks;
+  p.per_block = static_cast<int>(each * kFindThreads);
+  p.find_blocks = static_cast<int>((tiles + each - 1) / each);
+  p.ldz = static_cast<int>(up(a.V, 64));
+  p.ldx = static_cast<int>(up(a.d, 8));
+  const long long most = std::max<long long>(256, static_cast<long long>(kPieceBytes / (4ull * p.ldz)) / 256 * 256);
+  p.pieces = static_cast<int>((M + most - 1) / most);
+  p.piece = static_cast<int>(std::min(most, up((M + p.pieces - 1) / p.pieces, 256)));
+  const int es = a.bf16 ? 2 : 4;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at += al256(bytes);
+    return o;
+  };
+  p.counts = take((kFindBlocks + 1) * 4);
+  p.idx = take(M * 4);
+  p.target = take(M * 4);
+  p.w = take(M * 4);
+  p.x = take(static_cast<size_t>(p.piece) * p.ldx * es);
+  p.z = take(static_cast<size_t>(p.piece) * p.ldz * 4);
+  if (a.dweight && a.bf16 && a.grad_bf16 && p.pieces > 1) p.acc = take(static_cast<size_t>(a.V) * a.d * 4);
+  p.total = at;
+  return p;
+}
+
+// ------------------------------------------------------------ counted positions
+struct Job {
+  int target;
+  float w;
+  bool kept;
+};
+__device__ __forceinline__ Job job_of(const HeadArgs& a, int r, unsigned* status) {
+  int b, t;
+  locate(a.rs, r, b, t);
+  const int len = a.rs.lengths ? a.rs.lengths[b] : a.rs.T;
+  const long long target = token_at(a.targets, b, t);
+  const float w = a.weights ? a.weights[r] : 1.f;
+  bool kept = t < len && target != a.ignore && w != 0.f;
+  if (kept && (target < 0 || target >= a.V)) {
+    flag_status(status, EOGP_ST_DEVICE);
+    kept = false;
+  }
+  return Job{static_cast<int>(target), w, kept};
+}
+
+__global__ void __launch_bounds__(kFindThreads) k_head_count(const HeadArgs a, int M, int per, int* counts) {
+  const int r0 = blockIdx.x * per, r1 = min(M, r0 + per);
+  int n = 0;
+  for (int r = r0; r < r1; r += kFindThreads) {
+    const int i = r + threadIdx.x;
+    n += __syncthreads_count(i < r1 && job_of(a, i, nullptr).kept);
+  }
+  if (threadIdx.x == 0) counts[blockIdx.x] = n;
+}
+
+// idx[i], target[i], w[i] of counted position i, in ascending order of (b, t); their
+// number in counts[kFindBlocks]. Losses of the others are 0.
+__global__ void __launch_bounds__(kFindThreads) k_head_place(const HeadArgs a, int M, int per, int* counts, int* idx,
+                                                             int* target, float* w, unsigned* status) {
+  __shared__ int part[kFindThreads / 32], base;
+  const int tid = threadIdx.x, lane = tid & 31;
+  int before = 0;
+  if (gridDim.x > 1) {
+    before = tid < blockIdx.x ? counts[tid] : 0;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+    if (lane == 0) part[tid >> 5] = before;
+    __syncthreads();
+    before = 0;
+    for (int i = 0; i < kFindThreads / 32; ++i) before += part[i];
+    __syncthreads();
+  }
+  const int r0 = blockIdx.x * per, r1 = min(M, r0 + per);
+  for (int r = r0; r < r1; r += kFindThreads) {
+    const int i = r + tid;
+    Job j{0, 0.f, false};
+    if (i < r1) j = job_of(a, i, status);
+    const unsigned mask = __ballot_sync(0xffffffffu, j.kept);
+    if (lane == 0) part[tid >> 5] = __popc(mask);
+    __syncthreads();
+    int at = before + __popc(mask & ((1u << lane) - 1u)), all = 0;
+    for (int k = 0; k < kFindThreads / 32; ++k) {
+      if (k < tid >> 5) at += part[k];
+      all += part[k];
+    }
+    if (j.kept) {
+      idx[at] = i;
+      target[at] = j.target;
+      w[at] = j.w;
+    } else if (i < r1) {
+      a.loss[i] = 0.f;
+      if (a.lse) a.lse[i] = 0.f;
+    }
+    before += all;
+    __syncthreads();
+  }
+  if (blockIdx.x == gridDim.x - 1 && tid == 0) counts[kFindBlocks] = before;
+}
+
+// Zeros in the rows of dx that are left out.
+template <typename T>
+__global__ void __launch_bounds__(256) k_head_zero(const HeadArgs a, int M) {
+  const int lane = threadIdx.x & 31;
+  for (int r = blockIdx.x * 8 + (threadIdx.x >> 5); r < M; r += gridDim.x * 8) {
+    if (job_of(a, r, nullptr).kept) continue;
+    int b, t;
+    locate(a.rs, r, b, t);
+    T* const g = row_out<T>(a.dx, b, t);
+    for (int c = lane; c < a.d; c += 32) g[c] = from_f32<T>(0.f);
+  }
+}
+
+// Rows first .. of the counted positions, dense; zeros up to the next multiple of 64.
+template <typename T>
+__global__ void __launch_bounds__(256) k_head_gather(const HeadArgs a, const int* counts, const int* idx, int first,
+                                                     int piece, int ldx, T* out) {
+  const int n = min(piece, counts[kFindBlocks] - first), lane = threadIdx.x & 31;
+  const int n64 = (max(n, 0) + 63) & ~63;
+  for (int i = blockIdx.x * 8 + (threadIdx.x >> 5); i < n64; i += gridDim.x * 8) {
+    T* const o = out + static_cast<size_t>(i) * ldx;
+    const T* x = nullptr;
+    if (i < n) {
+      int b, t;
+      locate(a.rs, idx[first + i], b, t);
+      x = row_of<T>(a.x, b, t);
+    }
+    for (int c = lane; c < ldx; c += 32) o[c] = x && c < a.d ? x[c] : from_f32<T>(0.f);
+  }
+}
+
+// ------------------------------------------------------------------ loss and D
+// One block on a row of logits: loss and lse, then D over them.
+__global__ void __launch_bounds__(512) k_head_rows(const HeadArgs a, const int* counts, const int* idx,
+                                                   const int* targets, const float* ws, int first, int piece, float* z,
+                                                   int ldz, bool grad) {
+  __shared__ float part[2][16];
+  const int n = min(piece, counts[kFindBlocks] - first), tid = threadIdx.x, i = blockIdx.x;
+  if (i >= n) return;
+  float* const x = z + static_cast<size_t>(i) * ldz;
+  const int target = targets[first + i], r = idx[first + i];
+  const float w = ws[first + i];
+  float m = -3.402823466e38f;
+  for (int c = tid; c < a.V; c += 512) m = fmaxf(m, x[c]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if ((tid & 31) == 0) part[0][tid >> 5] = m;
+  __syncthreads();
+  m = part[0][0];
+  for (int k = 1; k < 16; ++k) m = fmaxf(m, part[0][k]);
+  float s = 0.f;
+  for (int c = tid; c < a.V; c += 512) s += exp2f((x[c] - m) * kLog2e);
+  s = block_sum<16>(s, part[1]);
+  if (tid == 0) {
+    const float ls = s > 0.f ? logf(s) : NAN;  // no finite logit: NaN
+    a.loss[r] = w * ((m - x[target]) + ls);
+    if (a.lse) a.lse[r] = m + ls;
+  }
+  if (!grad) return;
+  __syncthreads();
+  const float g = w * a.scale, inv = g / s;
+  for (int c = tid; c < ldz; c += 512)
+    x[c] = c < a.V ? exp2f((x[c] - m) * kLog2e) * inv - (c == target ? g : 0.f) : 0.f;
+}
+
+// ------------------------------------------------------------------ products
+// C[i][j] = alpha sum_k A(i, k) B(j, k) (+ add[i][j]), A(i, k) at A + i sai + k sak and
+// B likewise: 64 x 64 tiles, 4 x 4 outputs a thread, sums in fp32 in ascending order.
+template <typename TA, typename TB>
+struct Product {
+  const TA* A;
+  long long sai, sak;
+  const TB* B;
+  long long sbj, sbk;
+  int M, N, K;  // M or K: the piece's rows at most, then as many as there are
+  bool rows_m, rows_k;
+  float alpha;
+};
+
+// Where a product goes: rows of dx by position, or rows of an array, on top of what an
+// array of `add` holds.
+struct Out {
+  void* p;
+  long long ld;
+  bool bf16;
+  const void* add;  // NULL: nothing is added
+  long long ld_add;
+  bool add_bf16;
+};
+
+template <typename TA, typename TB>
+__global__ void __launch_bounds__(256) k_head_product(const Product<TA, TB> g, const HeadArgs a, const Out o,
+                                                      const int* counts, const int* idx, int first, bool to_dx) {
+  __shared__ float As[16][65], Bs[16][65];
+  const int n = max(0, counts[kFindBlocks] - first);
+  const int M = g.rows_m ? min(g.M, n) : g.M, K = g.rows_k ? min(g.K, n) : g.K;
+  const int nn = (g.N + 63) / 64;
+  const int m0 = static_cast<int>(blockIdx.x / nn) * 64, n0 = static_cast<int>(blockIdx.x % nn) * 64;
+  if (m0 >= M) return;
+  const int tid = threadIdx.x, ti = tid >> 4, tj = tid & 15;
+  float acc[4][4] = {};
+  for (int k0 = 0; k0 < K; k0 += 16) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      // neighbouring threads along whichever index is contiguous
+      const int q = tid + e * 256;
+      int i = g.sak == 1 ? q >> 4 : q & 63, k = g.sak == 1 ? q & 15 : q >> 6;
+      As[k][i] = m0 + i < M && k0 + k < K ? to_f32(g.A[(m0 + i) * g.sai + (k0 + k) * g.sak]) : 0.f;
+      i = g.sbk == 1 ? q >> 4 : q & 63, k = g.sbk == 1 ? q & 15 : q >> 6;
+      Bs[k][i] = n0 + i < g.N && k0 + k < K ? to_f32(g.B[(n0 + i) * g.sbj + (k0 + k) * g.sbk]) : 0.f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[u][v] = fmaf(As[k][ti + 16 * u], Bs[k][tj + 16 * v], acc[u][v]);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int i = m0 + ti + 16 * u;
+    if (i >= M) continue;
+    long long row = i * o.ld;
+    if (to_dx) {
+      int b, t;
+      locate(a.rs, idx[first + i], b, t);
+      row = b * a.dx.bs + t * a.dx.ld;
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const int j = n0 + tj + 16 * v;
+      if (j >= g.N) continue;
+      float x = g.alpha * acc[u][v];
+      if (o.add) {
+        const long long at = i * o.ld_add + j;
+        x += o.add_bf16 ? to_f32(static_cast<const bf16*>(o.add)[at]) : static_cast<const float*>(o.add)[at];
+      }
+      if (o.bf16)
+        static_cast<bf16*>(o.p)[row + j] = from_f32<bf16>(x);
+      else
+        static_cast<float*>(o.p)[row + j] = x;
+    }
+  }
+}
+
+template <typename TA, typename TB>
+cudaError_t product(const Product<TA, TB>& g, const HeadArgs& a, const Out& o, const int* counts, const int* idx,
+                    int first, bool to_dx, cudaStream_t st) {
+  const long long tiles = static_cast<long long>((g.M + 63) / 64) * ((g.N + 63) / 64);
+  if (tiles > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
+  k_head_product<TA, TB><<<static_cast<unsigned>(tiles), 256, 0, st>>>(g, a, o, counts, idx, first, to_dx);
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, cudaStream_t st) {
+  const Plan p = plan_of(a);
+  const int M = static_cast<int>(a.rs.rows());
+  int* const counts = reinterpret_cast<int*>(ws + p.counts);
+  int* const idx = reinterpret_cast<int*>(ws + p.idx);
+  int* const target = reinterpret_cast<int*>(ws + p.target);
+  float* const w = reinterpret_cast<float*>(ws + p.w);
+  T* const x = reinterpret_cast<T*>(ws + p.x);
+  float* const z = reinterpret_cast<float*>(ws + p.z);
+  const T* const W = static_cast<const T*>(a.weight);
+  if (p.find_blocks > 1) {
+    k_head_count<<<p.find_blocks, kFindThreads, 0, st>>>(a, M, p.per_block, counts);
+    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
+  }
+  k_head_place<<<p.find_blocks, kFindThreads, 0, st>>>(a, M, p.per_block, counts, idx, target, w, status);
+  if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
+  if (a.dx.p) {
+    k_head_zero<T><<<std::min((M + 7) / 8, num_sms * 8), 256, 0, st>>>(a, M);
+    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
+  }
+  const bool grad = a.dx.p || a.dweight;
+  for (int c = 0; c < p.pieces; ++c) {
+    const int first = c * p.piece;
+    k_head_gather<T><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, first, p.piece, p.ldx, x);
+    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
+    const Out logits{z, p.ldz, false, nullptr, 0, false};
+    if (cudaError_t e = product(Product<T, T>{x, p.ldx, 1, W, a.ld_weight, 1, p.piece, a.V, a.d, true, false, a.scale},
+                                a, logits, counts, idx, first, false, st);
+        e != cudaSuccess)
+      return e;
+    k_head_rows<<<p.piece, 512, 0, st>>>(a, counts, idx, target, w, first, p.piece, z, p.ldz, grad);
+    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
+    if (a.dx.p) {
+      const Out dx{const_cast<void*>(a.dx.p), 0, a.bf16, nullptr, 0, false};
+      if (cudaError_t e = product(Product<float, T>{z, p.ldz, 1, W, 1, a.ld_weight, p.piece, a.d, a.V, true, false,
+                                                    1.f},
+                                  a, dx, counts, idx, first, true, st);
+          e != cudaSuccess)
+        return e;
+    }
+    if (a.dweight) {
+      // Sums of several pieces stay in fp32: in dweight itself, or beside it until the last piece.
+      float* const acc = p.acc ? reinterpret_cast<float*>(ws + p.acc) : nullptr;
+      const bool last = c == p.pieces - 1;
+      Out o{a.dweight, a.ld_dweight, a.grad_bf16, nullptr, 0, false};
+      if (acc && !last) o = Out{acc, a.d, false, nullptr, 0, false};
+      if (c > 0) {
+        o.add = acc ? static_cast<void*>(acc) : a.dweight;
+        o.ld_add = acc ? a.d : a.ld_dweight;
+      } else if (a.accumulate) {
+        o.add = a.dweight;
+        o.ld_add = a.ld_dweight;
+        o.add_bf16 = a.grad_bf16;
+      }
+      if (cudaError_t e = product(Product<float, T>{z, 1, p.ldz, x, 1, p.ldx, a.V, a.d, p.piece, false, true, 1.f}, a,
+                                  o, counts, idx, first, false, st);
+          e != cudaSuccess)
+        return e;
+    }
+  }
+  return cudaSuccess;
+}
+
+// dweight of a batch without positions.
+template <typename T>
+__global__ void __launch_bounds__(256) k_head_clear(T* p, long long ld, int V, int d) {
+  for (long long r = blockIdx.x; r < V; r += gridDim.x)
+    for (int c = threadIdx.x; c < d; c += 256) p[r * ld + c] = from_f32<T>(0.f);
+}
+
+}  // namespace
+
+size_t head_loss_ws_bytes(const HeadArgs& a) { return plan_of(a).total; }
+
+cudaError_t launch_head_loss(const HeadArgs& a, void* ws, unsigned* status, int num_sms, cudaStream_t st) {
+  if (a.rs.rows() == 0) {
+    if (a.accumulate) return cudaSuccess;
+    const int blocks = std::min(a.V, num_sms * 8);
+    if (a.grad_bf16)
+      k_head_clear<bf16><<<blocks, 256, 0, st>>>(static_cast<bf16*>(a.dweight), a.ld_dweight, a.V, a.d);
+    else
+      k_head_clear<float><<<blocks, 256, 0, st>>>(static_cast<float*>(a.dweight), a.ld_dweight, a.V, a.d);
+    return cudaGetLastError();
+  }
+  return a.bf16 ? run<bf16>(a, static_cast<uint8_t*>(ws), status, num_sms, st)
+                : run<float>(a, static_cast<uint8_t*>(ws), status, num_sms, st);
+}

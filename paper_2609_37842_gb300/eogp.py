@@ -25,9 +25,11 @@ OUT_FIRST_STAGE, OUT_COORDS, OUT_CODES = 0, 1, 2
 SCORE_CODES, SCORE_PAPER, SCORE_FP = 0, 1, 2
 TOPK_MAX = 256
 SRHT_MAX_M = 32768
-K_ROTATE, K_CONTRACT, K_PROJECT, K_PACK, K_SCORE, K_SIMT, K_EMBED, K_NORM, K_LOSS = range(9)
+DISTILL_MAX = 256
+K_ROTATE, K_CONTRACT, K_PROJECT, K_PACK, K_SCORE, K_SIMT, K_EMBED, K_NORM, K_LOSS, K_HEAD = range(10)
 KERNEL_KINDS = {K_ROTATE: "rotate", K_CONTRACT: "contract", K_PROJECT: "project", K_PACK: "pack",
-                K_SCORE: "score", K_SIMT: "simt_f32", K_EMBED: "embed", K_NORM: "norm", K_LOSS: "loss"}
+                K_SCORE: "score", K_SIMT: "simt_f32", K_EMBED: "embed", K_NORM: "norm", K_LOSS: "loss",
+                K_HEAD: "head"}
 
 _ERRNAMES = {EINVAL: "EINVAL", EUNSUPPORTED: "EUNSUPPORTED", ECUDA: "ECUDA",
              ETIMEOUT: "ETIMEOUT", EWORKSPACE: "EWORKSPACE", EDEVICE: "EDEVICE"}
@@ -139,6 +141,15 @@ EXPORTS = {
     "eogp_cross_entropy": (c_int, [c_void_p, c_int, c_longlong, c_longlong, c_void_p, c_int, c_longlong, c_void_p,
                                    c_longlong, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p,
                                    c_longlong, c_longlong, c_void_p]),
+    "eogp_head_loss_workspace_size": (c_int, [c_void_p, c_int, c_longlong, c_int, c_int, c_int, c_int, c_int, c_int,
+                                              c_int, POINTER(c_size_t)]),
+    "eogp_head_loss": (c_int, [c_void_p, c_int, c_longlong, c_longlong, c_void_p, c_longlong, c_float, c_void_p, c_int,
+                               c_longlong, c_void_p, c_longlong, c_void_p, c_int, c_int, c_int, c_int, c_void_p,
+                               c_void_p, c_void_p, c_longlong, c_longlong, c_void_p, c_int, c_longlong, c_int,
+                               c_void_p, c_size_t, c_void_p]),
+    "eogp_distill": (c_int, [c_void_p, c_int, c_longlong, c_longlong, c_void_p, c_int, c_longlong, c_longlong,
+                             c_void_p, c_int, c_longlong, c_longlong, c_void_p, c_int, c_float, c_void_p, c_void_p,
+                             c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_longlong, c_longlong, c_void_p]),
 }
 
 _LIB = None
@@ -1088,4 +1099,98 @@ def cross_entropy(logits, targets, weights=None, lengths=None, ignore_index: int
     _check(lib().eogp_cross_entropy(logits.data_ptr(), code, lbs, lld, targets.data_ptr(), icode, tbs, _ptr(weights),
                                     ignore_index, _lengths_ptr(lengths, B), B, T, V, loss.data_ptr(), lse.data_ptr(),
                                     _ptr(dlogits), gbs, gld, _stream_on(stream, dev)))
+    return loss, lse, dlogits
+
+
+def head_loss(x, weight, targets, scale: float = 1.0, weights=None, lengths=None, ignore_index: int = -100,
+              want_dx: bool = True, want_dweight: bool = True, dx=None, dweight=None, dtype=None,
+              accumulate: bool = False, ws=None, stream=None):
+    """eogp_head_loss: token loss of the logits scale * x weight^T for x [B, T, d] or [T, d], weight [V, d] and targets
+    [B, T] or [T], without keeping the logits. Returns (loss, lse, dx, dweight): fp32 per position, and the gradients of
+    the sum of the losses (None where not wanted). `dx` may be x. dweight may be given, and added to with accumulate,
+    else it is a new tensor of `dtype` (default that of weight; float32 always possible)."""
+    import torch
+    dev = _device_of(x, weight, targets, weights, lengths, dx, dweight, ws)
+    B, T, d, xbs, xld = _rows_of(x, "x")
+    code = _float_code(x, "x")
+    shape = targets.shape
+    if shape != x.shape[:-1]:
+        raise ValueError("targets must have the shape of x without its last dimension")
+    _, _, tbs, icode = _tokens_of(targets, "targets")
+    if weight.dtype != x.dtype or weight.dim() != 2 or weight.shape[1] != d:
+        raise ValueError(f"weight must be [V, {d}] of {x.dtype}")
+    V = weight.shape[0]
+    ldw, inner = weight.stride()
+    if inner != 1 and d > 1:
+        raise ValueError("weight must have unit stride along its last dimension")
+    if V > _INT_MAX:
+        _too_large("weight")
+    if weights is not None:
+        _dense(_like(weights, "weights", shape, torch.float32), "weights")
+    dxbs = dxld = 0
+    if dx is not None:
+        _, _, _, dxbs, dxld = _rows_of(_like(dx, "dx", x.shape, x.dtype), "dx")
+    if dweight is not None:
+        _rows(_like(dweight, "dweight", (V, d), dtype or dweight.dtype), "dweight")
+    elif accumulate:
+        raise ValueError("accumulate needs dweight")
+    want_dx, want_dweight = want_dx or dx is not None, want_dweight or dweight is not None
+    L = lib()
+    with _pool(stream):
+        loss = torch.empty(shape, dtype=torch.float32, device=dev)
+        lse = torch.empty(shape, dtype=torch.float32, device=dev)
+        if dx is None and want_dx:
+            dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
+            dxbs, dxld = T * d, d
+        if dweight is None and want_dweight:
+            dweight = torch.empty((V, d), dtype=dtype or weight.dtype, device=dev)
+        gcode = code if dweight is None else _float_code(dweight, "dweight")
+        if ws is None:
+            need = c_size_t()
+            _check(L.eogp_head_loss_workspace_size(weight.data_ptr(), code, ldw, V, d, B, T, want_dx, want_dweight,
+                                                   gcode, need))
+            ws = workspace(need.value, dev)
+    _check(L.eogp_head_loss(x.data_ptr(), code, xbs, xld, weight.data_ptr(), ldw, scale, targets.data_ptr(), icode, tbs,
+                            _ptr(weights), ignore_index, _lengths_ptr(lengths, B), B, T, d, V, loss.data_ptr(),
+                            lse.data_ptr(), _ptr(dx), dxbs, dxld, _ptr(dweight), gcode,
+                            0 if dweight is None else dweight.stride(0), 1 if accumulate else 0, ws.data_ptr(),
+                            ws.numel(), _stream_on(stream, dev)))
+    return loss, lse, dx, dweight
+
+
+def distill(logits, classes, teacher, teacher_lse=None, temperature: float = 1.0, weights=None, lengths=None,
+            want_grad: bool = True, dlogits=None, stream=None):
+    """eogp_distill on logits [B, T, V] or [T, V] with the teacher's top logits: classes (int32 or int64, negative: no
+    entry) and teacher (float32 or bfloat16) [B, T, K] or [T, K], and teacher_lse [B, T] or [T], the log of the sum of
+    exp(y / temperature) over all the teacher's classes, or None to renormalise the lists. Returns (loss, lse, dlogits):
+    fp32 per position, and the gradient of the sum of the losses (None without want_grad). `dlogits` may be logits."""
+    import torch
+    dev = _device_of(logits, classes, teacher, teacher_lse, weights, lengths, dlogits)
+    B, T, V, lbs, lld = _rows_of(logits, "logits")
+    code = _float_code(logits, "logits")
+    shape = logits.shape[:-1]
+    _, _, K, cbs, cld = _rows_of(classes, "classes")
+    icode = _type_codes().get(classes.dtype)
+    if icode != I64 and icode != I32:
+        raise ValueError(f"unsupported dtype {classes.dtype} for classes (int32 or int64)")
+    _, _, _, ybs, yld = _rows_of(teacher, "teacher")
+    ycode = _float_code(teacher, "teacher")
+    if classes.shape[:-1] != shape or teacher.shape != classes.shape:
+        raise ValueError("classes and teacher must have one shape, that of logits with K in its last dimension")
+    for t, name in ((teacher_lse, "teacher_lse"), (weights, "weights")):
+        if t is not None:
+            _dense(_like(t, name, shape, torch.float32), name)
+    gbs = gld = 0
+    if dlogits is not None:
+        _, _, _, gbs, gld = _rows_of(_like(dlogits, "dlogits", logits.shape, logits.dtype), "dlogits")
+    with _pool(stream):
+        loss = torch.empty(shape, dtype=torch.float32, device=dev)
+        lse = torch.empty(shape, dtype=torch.float32, device=dev)
+        if dlogits is None and want_grad:
+            dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+            gbs, gld = T * V, V
+    _check(lib().eogp_distill(logits.data_ptr(), code, lbs, lld, classes.data_ptr(), icode, cbs, cld,
+                              teacher.data_ptr(), ycode, ybs, yld, _ptr(teacher_lse), K, temperature, _ptr(weights),
+                              _lengths_ptr(lengths, B), B, T, V, loss.data_ptr(), lse.data_ptr(), _ptr(dlogits), gbs,
+                              gld, _stream_on(stream, dev)))
     return loss, lse, dlogits
