@@ -305,3 +305,42 @@ struct DistillArgs {
   float *loss, *lse;
 };
 cudaError_t launch_distill(const DistillArgs& a, bool bf16, unsigned* status, int num_sms, cudaStream_t st);
+
+// k_head_tc.cu: the three products of a piece of the counted positions, on bf16 operands.
+// An operand of several parts has 64 columns of each in turn (parts * 64 columns a block).
+struct HeadTc {
+  const int* count;  // counted positions in all; the piece has those from `first` on, at most `piece`
+  int first, piece, d, V;
+  const void *A, *B;
+  uint64_t inner_a, rows_a, lda, inner_b, rows_b, ldb;  // elements as they lie
+  int parts_a, parts_b;
+  int pairs;           // products of parts that are summed,
+  uint32_t pair_list;  // four bits each: part of A | part of B << 2
+  int bn, splits;      // columns of a tile; slabs that the sum is split into
+  // logits: z (NULL: not kept) [piece x ldz], -inf beyond V; (maximum, sum) of each row's half tiles
+  // [2 * tiles][piece]; the target's logit
+  float scale;
+  float* z;
+  int ldz;
+  float2* part;
+  float* zt;
+  const int* target;
+  // dx, by position
+  RowSet rs;
+  const int* idx;
+  RowView dx;
+  // dW, on top of what `add` holds (NULL: nothing)
+  void* out;
+  long long ld_out;
+  const void* add;
+  long long ld_add;
+  bool add_bf16;
+  bool out_bf16, wide;  // type of dx or dW; whether its rows allow 32-byte stores
+  // of split sums: [splits][slab_rows][ld_slab]
+  float* slabs;
+  size_t slab_rows;
+  int ld_slab;
+};
+cudaError_t launch_head_logits(const HeadTc& h, unsigned* status, int num_sms, cudaStream_t st);
+cudaError_t launch_head_dx(const HeadTc& h, unsigned* status, int num_sms, cudaStream_t st);
+cudaError_t launch_head_dw(const HeadTc& h, unsigned* status, int num_sms, cudaStream_t st);

@@ -16,6 +16,7 @@ using namespace eogp;
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLowest = -3.402823466e38f;
 constexpr int kFindThreads = 1024;
 constexpr int kFindBlocks = 1024;
 constexpr size_t kPieceBytes = size_t(4) << 30;  // logits of a piece
@@ -23,25 +24,56 @@ constexpr size_t kPieceBytes = size_t(4) << 30;  // logits of a piece
 size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
 long long up(long long x, long long a) { return (x + a - 1) / a * a; }
 
-// Where everything lies in the workspace.
+// Where everything lies in the workspace, and how the products are cut. bf16 only: from `W` on.
 struct Plan {
   int find_blocks, per_block;  // blocks of the search, positions of each
   int piece, pieces;           // rows of a piece, most pieces
-  int ldz, ldx;                // row strides of the logits and of the gathered rows
-  size_t counts, idx, target, w, x, z, acc, total;
+  int ldz, ldx, ldw;           // row strides of the logits, of the gathered rows and of the matrix
+  int parts;                   // bf16 parts of D
+  int bn_z, bn_d;              // columns of a tile of the logits, of dx and dW
+  int splits_dx, splits_dw, ld_slab;
+  size_t counts, idx, target, w, x, z, acc, W, D, part, zt, row, slabs, total;
 };
+
+// Slabs of a sum of `steps` 64-deep steps for tiles that 76 pairs of multiprocessors take in turn:
+// the fewest rounds, where each costs its steps and about 8 more (filling the ring, ending the
+// tile), and a split the writing and reading of its slabs and a launch (in steps of 0.38 us).
+int splits_for(long long tiles, long long steps, long long rows, int d) {
+  int best = 1;
+  double least = 0;
+  for (int s = 1; s <= 32 && s <= steps; ++s) {
+    const double rounds = static_cast<double>((tiles * s + 75) / 76);
+    double cost = rounds * (static_cast<double>((steps + s - 1) / s) + 8);
+    if (s > 1) cost += 8 + 8.0 * s * rows * d / 6.8e12 / 0.38e-6;
+    if (s == 1 || cost < least) {
+      best = s;
+      least = cost;
+    }
+  }
+  return best;
+}
+
+bool w_fits(const HeadArgs& a) {
+  return reinterpret_cast<uintptr_t>(a.weight) % 16 == 0 &&
+         (a.V == 1 || (a.ld_weight % 8 == 0 && a.ld_weight >= a.d));
+}
 
 Plan plan_of(const HeadArgs& a) {
   Plan p{};
   const long long M = a.rs.rows();
   if (M == 0) return p;
+  const bool grad = a.dx.p || a.dweight;
   const long long tiles = (M + kFindThreads - 1) / kFindThreads;
   const long long each = (tiles + kFindBlocks - 1) / kFindBlocks;
   p.per_block = static_cast<int>(each * kFindThreads);
   p.find_blocks = static_cast<int>((tiles + each - 1) / each);
   p.ldz = static_cast<int>(up(a.V, 64));
   p.ldx = static_cast<int>(up(a.d, 8));
-  const long long most = std::max<long long>(256, static_cast<long long>(kPieceBytes / (4ull * p.ldz)) / 256 * 256);
+  p.parts = a.bf16 ? a.dweight && !a.grad_bf16 ? 2 : 1 : 0;
+  // A row of a piece: logits and D, or the gathered row and the sums of its half tiles.
+  const size_t row_bytes = grad || !a.bf16 ? static_cast<size_t>(p.ldz) * (4 + 2 * p.parts)
+                                           : static_cast<size_t>(p.ldx) * 2 + p.ldz / 64 * 16;
+  const long long most = std::max<long long>(256, static_cast<long long>(kPieceBytes / row_bytes) / 256 * 256);
   p.pieces = static_cast<int>((M + most - 1) / most);
   p.piece = static_cast<int>(std::min(most, up((M + p.pieces - 1) / p.pieces, 256)));
   const int es = a.bf16 ? 2 : 4;
@@ -56,8 +88,33 @@ Plan plan_of(const HeadArgs& a) {
   p.target = take(M * 4);
   p.w = take(M * 4);
   p.x = take(static_cast<size_t>(p.piece) * p.ldx * es);
-  p.z = take(static_cast<size_t>(p.piece) * p.ldz * 4);
+  if (grad || !a.bf16) p.z = take(static_cast<size_t>(p.piece) * p.ldz * 4);
   if (a.dweight && a.bf16 && a.grad_bf16 && p.pieces > 1) p.acc = take(static_cast<size_t>(a.V) * a.d * 4);
+  if (a.bf16) {
+    p.ldw = static_cast<int>(up(a.d, 8));
+    if (!w_fits(a)) p.W = take(static_cast<size_t>(a.V) * p.ldw * 2);
+    const long long mt = p.piece / 256;
+    p.bn_z = 256;
+    if (mt * ((a.V + 255) / 256) < 4 * 76)  // few tiles: those that share them out best
+      for (int bn = 128; bn >= 64; bn /= 2)
+        if ((mt * ((a.V + bn - 1) / bn) + 75) / 76 * bn < (mt * ((a.V + p.bn_z - 1) / p.bn_z) + 75) / 76 * p.bn_z)
+          p.bn_z = bn;
+    p.bn_d = up(a.d, 128) * 1.15 < up(a.d, 256) ? 128 : 256;
+    p.part = take(static_cast<size_t>((a.V + p.bn_z - 1) / p.bn_z) * 2 * p.piece * 8);
+    p.zt = take(static_cast<size_t>(p.piece) * 4);
+    p.row = take(static_cast<size_t>(p.piece) * 8);
+    if (grad) {
+      p.D = take(static_cast<size_t>(p.piece) * p.ldz * 2 * p.parts);
+      const long long nt = (a.d + p.bn_d - 1) / p.bn_d;
+      p.ld_slab = static_cast<int>(up(a.d, 8));
+      p.splits_dx = a.dx.p ? splits_for(mt * nt, (a.V + 63) / 64, p.piece, a.d) : 1;
+      p.splits_dw = a.dweight ? splits_for((a.V + 255ll) / 256 * nt, p.piece / 64 * p.parts, a.V, a.d) : 1;
+      size_t slabs = 0;
+      if (p.splits_dx > 1) slabs = static_cast<size_t>(p.splits_dx) * p.piece * p.ld_slab * 4;
+      if (p.splits_dw > 1) slabs = std::max(slabs, static_cast<size_t>(p.splits_dw) * a.V * p.ld_slab * 4);
+      if (slabs) p.slabs = take(slabs);
+    }
+  }
   p.total = at;
   return p;
 }
@@ -292,34 +349,265 @@ cudaError_t product(const Product<TA, TB>& g, const HeadArgs& a, const Out& o, c
   return cudaGetLastError();
 }
 
-template <typename T>
-cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, cudaStream_t st) {
+// ------------------------------------------------------- between the tensor products
+// The matrix with rows that TMA can read.
+__global__ void __launch_bounds__(256) k_head_matrix(const bf16* W, long long ld, int V, int d, bf16* out, int ldo) {
+  const int lane = threadIdx.x & 31;
+  for (long long r = blockIdx.x * 8 + (threadIdx.x >> 5); r < V; r += gridDim.x * 8)
+    for (int c = lane; c < d; c += 32) out[r * ldo + c] = W[r * ld + c];
+}
+
+// 32 rows a block: the (maximum, sum) pairs of a row's half tiles joined to its loss and lse,
+// and what D needs of them: maximum and w scale / sum.
+__global__ void __launch_bounds__(1024) k_head_join(const HeadArgs a, const int* counts, const int* idx, const float* ws,
+                                                    int first, int piece, const float2* parts, int n_parts,
+                                                    const float* zt, float2* row) {
+  __shared__ float2 all[32][33];
+  const int n = min(piece, counts[kFindBlocks] - first), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int i = blockIdx.x * 32 + lane;
+  if (blockIdx.x * 32 >= n) return;
+  float m = kLowest, s = 0.f;
+  if (i < n) {
+    for (int p = warp; p < n_parts; p += 32) {
+      const float2 v = parts[static_cast<size_t>(p) * piece + i];
+      const float top = fmaxf(m, v.x);
+      s = s * exp2f((m - top) * kLog2e) + v.y * exp2f((v.x - top) * kLog2e);
+      m = top;
+    }
+  }
+  all[warp][lane] = make_float2(m, s);
+  __syncthreads();
+  if (warp > 0 || i >= n) return;
+  for (int p = 1; p < 32; ++p) m = fmaxf(m, all[p][lane].x);
+  s = 0.f;
+  for (int p = 0; p < 32; ++p) s += all[p][lane].y * exp2f((all[p][lane].x - m) * kLog2e);
+  const float ls = s > 0.f ? logf(s) : NAN;  // no finite logit: NaN
+  const int r = idx[first + i];
+  const float w = ws[first + i];
+  a.loss[r] = w * ((m - zt[i]) + ls);
+  if (a.lse) a.lse[r] = m + ls;
+  if (row) row[i] = make_float2(m, w * a.scale / s);
+}
+
+// D in bf16 parts from the logits, eight columns a thread; zeros in the rows up to the next multiple of 64,
+// which the sum over rows runs over.
+template <int PARTS>
+__global__ void __launch_bounds__(256) k_head_d(const HeadArgs a, const int* counts, const int* targets,
+                                                const float* ws, int first, int piece, const float* z, int ldz,
+                                                const float2* row, bf16* D) {
+  const int n = min(piece, counts[kFindBlocks] - first), n64 = (max(n, 0) + 63) & ~63;
+  for (int i = blockIdx.x; i < n64; i += gridDim.x) {
+    bf16* const out = D + static_cast<size_t>(i) * ldz * PARTS;
+    const float* const x = z + static_cast<size_t>(i) * ldz;
+    const bool real = i < n;
+    const float2 mi = real ? row[i] : make_float2(0.f, 0.f);
+    const int target = real ? targets[first + i] : -1;
+    const float g = real ? ws[first + i] * a.scale : 0.f;
+    for (int c = threadIdx.x * 8; c < ldz; c += 256 * 8) {
+      Vals<8> v = fill<8>(0.f);
+      if (real) {
+        v = ld_floats<8>(x + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v.p[e].x = exp2f((v.p[e].x - mi.x) * kLog2e) * mi.y;
+          v.p[e].y = exp2f((v.p[e].y - mi.x) * kLog2e) * mi.y;
+        }
+        if (c + 8 > a.V) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (c + e >= a.V) v.set(e, 0.f);
+        }
+        if (static_cast<unsigned>(target - c) < 8u) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (target - c == e) v.set(e, v.get(e) - g);
+        }
+      }
+      bf16* o = out + (c >> 6) * 64 * PARTS + (c & 63);
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) {
+        const Raw<bf16, 8> r = pack_raw<bf16, 8>(v);
+        *reinterpret_cast<uint4*>(o + 64 * p) = r.w;
+        if (p + 1 < PARTS) {
+          const Vals<8> h = unpack<bf16, 8>(r);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v.p[e] = make_float2(v.p[e].x - h.p[e].x, v.p[e].y - h.p[e].y);
+        }
+      }
+    }
+  }
+}
+
+// The slabs of a split sum joined, in order: rows of dx by position, or rows of dW.
+__global__ void __launch_bounds__(256) k_head_slabs(const HeadTc h, int rows_most, bool to_dx) {
+  const int rows = to_dx ? min(h.piece, *h.count - h.first) : rows_most, lane = threadIdx.x & 31;
+  for (int i = blockIdx.x * 8 + (threadIdx.x >> 5); i < rows; i += gridDim.x * 8) {
+    long long at = i * h.ld_out;
+    void* out = h.out;
+    if (to_dx) {
+      int b, t;
+      locate(h.rs, h.idx[h.first + i], b, t);
+      at = b * h.dx.bs + t * h.dx.ld;
+      out = const_cast<void*>(h.dx.p);
+    }
+    for (int c = lane; c < h.d; c += 32) {
+      float v = 0.f;
+      for (int s = 0; s < h.splits; ++s) v += h.slabs[(s * h.slab_rows + i) * h.ld_slab + c];
+      if (h.add) {
+        const long long from = i * h.ld_add + c;
+        v += h.add_bf16 ? to_f32(static_cast<const bf16*>(h.add)[from]) : static_cast<const float*>(h.add)[from];
+      }
+      if (h.out_bf16)
+        static_cast<bf16*>(out)[at + c] = from_f32<bf16>(v);
+      else
+        static_cast<float*>(out)[at + c] = v;
+    }
+  }
+}
+
+// The counted positions of the batch.
+cudaError_t find(const HeadArgs& a, const Plan& p, uint8_t* ws, unsigned* status, cudaStream_t st) {
+  const int M = static_cast<int>(a.rs.rows());
+  int* const counts = reinterpret_cast<int*>(ws + p.counts);
+  if (p.find_blocks > 1) {
+    k_head_count<<<p.find_blocks, kFindThreads, 0, st>>>(a, M, p.per_block, counts);
+    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
+  }
+  k_head_place<<<p.find_blocks, kFindThreads, 0, st>>>(
+      a, M, p.per_block, counts, reinterpret_cast<int*>(ws + p.idx), reinterpret_cast<int*>(ws + p.target),
+      reinterpret_cast<float*>(ws + p.w), status);
+  return cudaGetLastError();
+}
+
+#define TRY(x)                                             \
+  do {                                                     \
+    if (cudaError_t e_ = (x); e_ != cudaSuccess) return e_; \
+  } while (0)
+
+// Whether rows of `es`-byte elements allow 32-byte stores at multiples of 32 columns.
+bool wide_rows(const void* p, long long bs, long long ld, int es) {
+  return reinterpret_cast<uintptr_t>(p) % 32 == 0 && bs * es % 32 == 0 && ld * es % 32 == 0;
+}
+
+cudaError_t run_bf16(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, cudaStream_t st) {
+  const Plan p = plan_of(a);
+  const int M = static_cast<int>(a.rs.rows());
+  const bool grad = a.dx.p || a.dweight;
+  int* const counts = reinterpret_cast<int*>(ws + p.counts);
+  int* const idx = reinterpret_cast<int*>(ws + p.idx);
+  int* const target = reinterpret_cast<int*>(ws + p.target);
+  float* const w = reinterpret_cast<float*>(ws + p.w);
+  bf16* const x = reinterpret_cast<bf16*>(ws + p.x);
+  bf16* const D = reinterpret_cast<bf16*>(ws + p.D);
+  float2* const row = reinterpret_cast<float2*>(ws + p.row);
+  const bf16* W = static_cast<const bf16*>(a.weight);
+  long long ldw = a.V == 1 ? p.ldw : a.ld_weight;
+  if (!w_fits(a)) {
+    bf16* const copy = reinterpret_cast<bf16*>(ws + p.W);
+    k_head_matrix<<<std::min((a.V + 7) / 8, num_sms * 8), 256, 0, st>>>(W, a.ld_weight, a.V, a.d, copy, p.ldw);
+    TRY(cudaGetLastError());
+    W = copy;
+    ldw = p.ldw;
+  }
+  TRY(find(a, p, ws, status, st));
+  if (a.dx.p) {
+    k_head_zero<bf16><<<std::min((M + 7) / 8, num_sms * 8), 256, 0, st>>>(a, M);
+    TRY(cudaGetLastError());
+  }
+  HeadTc h{};
+  h.count = counts + kFindBlocks;
+  h.piece = p.piece;
+  h.d = a.d;
+  h.V = a.V;
+  h.scale = a.scale;
+  h.z = grad ? reinterpret_cast<float*>(ws + p.z) : nullptr;
+  h.ldz = p.ldz;
+  h.part = reinterpret_cast<float2*>(ws + p.part);
+  h.zt = reinterpret_cast<float*>(ws + p.zt);
+  h.target = target;
+  h.rs = a.rs;
+  h.idx = idx;
+  h.parts_a = h.parts_b = h.pairs = 1;
+  h.ld_slab = p.ld_slab;
+  h.slabs = reinterpret_cast<float*>(ws + p.slabs);
+  const uint64_t ud = a.d, uv = a.V, rows = p.piece, dcols = static_cast<uint64_t>(p.ldz) * p.parts;
+  for (int c = 0; c < p.pieces; ++c) {
+    h.first = c * p.piece;
+    k_head_gather<bf16><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, h.first, p.piece, p.ldx, x);
+    TRY(cudaGetLastError());
+    HeadTc z = h;
+    z.A = x, z.inner_a = ud, z.rows_a = rows, z.lda = p.ldx;
+    z.B = W, z.inner_b = ud, z.rows_b = uv, z.ldb = ldw;
+    z.bn = p.bn_z, z.splits = 1;
+    TRY(launch_head_logits(z, status, num_sms, st));
+    k_head_join<<<(p.piece + 31) / 32, 1024, 0, st>>>(a, counts, idx, w, h.first, p.piece, h.part,
+                                                      (a.V + p.bn_z - 1) / p.bn_z * 2, h.zt, grad ? row : nullptr);
+    TRY(cudaGetLastError());
+    if (!grad) continue;
+    auto d = p.parts == 2 ? k_head_d<2> : k_head_d<1>;
+    d<<<std::min(p.piece, num_sms * 8), 256, 0, st>>>(a, counts, target, w, h.first, p.piece, h.z, p.ldz, row, D);
+    TRY(cudaGetLastError());
+    if (a.dx.p) {
+      HeadTc g = h;
+      g.A = D, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = p.parts;
+      g.B = W, g.inner_b = ud, g.rows_b = uv, g.ldb = ldw;
+      g.bn = p.bn_d, g.splits = p.splits_dx, g.slab_rows = p.piece;
+      g.dx = a.dx, g.out_bf16 = true, g.wide = wide_rows(a.dx.p, a.dx.bs, a.dx.ld, 2);
+      TRY(launch_head_dx(g, status, num_sms, st));
+      if (g.splits > 1) {
+        k_head_slabs<<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(g, p.piece, true);
+        TRY(cudaGetLastError());
+      }
+    }
+    if (a.dweight) {
+      HeadTc g = h;
+      g.A = D, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = p.parts;
+      g.B = x, g.inner_b = ud, g.rows_b = rows, g.ldb = p.ldx;
+      if (p.parts == 2) g.pairs = 2, g.pair_list = 0x10;  // D's parts with x
+      g.bn = p.bn_d, g.splits = p.splits_dw, g.slab_rows = a.V;
+      // Sums of several pieces stay in fp32: in dweight itself, or beside it until the last piece.
+      float* const acc = p.acc ? reinterpret_cast<float*>(ws + p.acc) : nullptr;
+      if (acc && c < p.pieces - 1)
+        g.out = acc, g.ld_out = a.d;
+      else
+        g.out = a.dweight, g.ld_out = a.ld_dweight, g.out_bf16 = a.grad_bf16;
+      if (c > 0)
+        g.add = acc ? static_cast<void*>(acc) : a.dweight, g.ld_add = acc ? a.d : a.ld_dweight;
+      else if (a.accumulate)
+        g.add = a.dweight, g.ld_add = a.ld_dweight, g.add_bf16 = a.grad_bf16;
+      g.wide = wide_rows(g.out, 0, g.ld_out, g.out_bf16 ? 2 : 4);
+      TRY(launch_head_dw(g, status, num_sms, st));
+      if (g.splits > 1) {
+        k_head_slabs<<<std::min((a.V + 7) / 8, num_sms * 8), 256, 0, st>>>(g, a.V, false);
+        TRY(cudaGetLastError());
+      }
+    }
+  }
+  return cudaSuccess;
+}
+
+cudaError_t run_f32(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, cudaStream_t st) {
   const Plan p = plan_of(a);
   const int M = static_cast<int>(a.rs.rows());
   int* const counts = reinterpret_cast<int*>(ws + p.counts);
   int* const idx = reinterpret_cast<int*>(ws + p.idx);
   int* const target = reinterpret_cast<int*>(ws + p.target);
   float* const w = reinterpret_cast<float*>(ws + p.w);
-  T* const x = reinterpret_cast<T*>(ws + p.x);
+  float* const x = reinterpret_cast<float*>(ws + p.x);
   float* const z = reinterpret_cast<float*>(ws + p.z);
-  const T* const W = static_cast<const T*>(a.weight);
-  if (p.find_blocks > 1) {
-    k_head_count<<<p.find_blocks, kFindThreads, 0, st>>>(a, M, p.per_block, counts);
-    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
-  }
-  k_head_place<<<p.find_blocks, kFindThreads, 0, st>>>(a, M, p.per_block, counts, idx, target, w, status);
-  if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
+  const float* const W = static_cast<const float*>(a.weight);
+  TRY(find(a, p, ws, status, st));
   if (a.dx.p) {
-    k_head_zero<T><<<std::min((M + 7) / 8, num_sms * 8), 256, 0, st>>>(a, M);
+    k_head_zero<float><<<std::min((M + 7) / 8, num_sms * 8), 256, 0, st>>>(a, M);
     if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
   }
   const bool grad = a.dx.p || a.dweight;
   for (int c = 0; c < p.pieces; ++c) {
     const int first = c * p.piece;
-    k_head_gather<T><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, first, p.piece, p.ldx, x);
+    k_head_gather<float><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, first, p.piece, p.ldx, x);
     if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
     const Out logits{z, p.ldz, false, nullptr, 0, false};
-    if (cudaError_t e = product(Product<T, T>{x, p.ldx, 1, W, a.ld_weight, 1, p.piece, a.V, a.d, true, false, a.scale},
+    if (cudaError_t e = product(Product<float, float>{x, p.ldx, 1, W, a.ld_weight, 1, p.piece, a.V, a.d, true, false, a.scale},
                                 a, logits, counts, idx, first, false, st);
         e != cudaSuccess)
       return e;
@@ -327,27 +615,19 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
     if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
     if (a.dx.p) {
       const Out dx{const_cast<void*>(a.dx.p), 0, a.bf16, nullptr, 0, false};
-      if (cudaError_t e = product(Product<float, T>{z, p.ldz, 1, W, 1, a.ld_weight, p.piece, a.d, a.V, true, false,
+      if (cudaError_t e = product(Product<float, float>{z, p.ldz, 1, W, 1, a.ld_weight, p.piece, a.d, a.V, true, false,
                                                     1.f},
                                   a, dx, counts, idx, first, true, st);
           e != cudaSuccess)
         return e;
     }
     if (a.dweight) {
-      // Sums of several pieces stay in fp32: in dweight itself, or beside it until the last piece.
-      float* const acc = p.acc ? reinterpret_cast<float*>(ws + p.acc) : nullptr;
-      const bool last = c == p.pieces - 1;
-      Out o{a.dweight, a.ld_dweight, a.grad_bf16, nullptr, 0, false};
-      if (acc && !last) o = Out{acc, a.d, false, nullptr, 0, false};
-      if (c > 0) {
-        o.add = acc ? static_cast<void*>(acc) : a.dweight;
-        o.ld_add = acc ? a.d : a.ld_dweight;
-      } else if (a.accumulate) {
+      Out o{a.dweight, a.ld_dweight, false, nullptr, 0, false};
+      if (c > 0 || a.accumulate) {
         o.add = a.dweight;
         o.ld_add = a.ld_dweight;
-        o.add_bf16 = a.grad_bf16;
       }
-      if (cudaError_t e = product(Product<float, T>{z, 1, p.ldz, x, 1, p.ldx, a.V, a.d, p.piece, false, true, 1.f}, a,
+      if (cudaError_t e = product(Product<float, float>{z, 1, p.ldz, x, 1, p.ldx, a.V, a.d, p.piece, false, true, 1.f}, a,
                                   o, counts, idx, first, false, st);
           e != cudaSuccess)
         return e;
@@ -377,6 +657,6 @@ cudaError_t launch_head_loss(const HeadArgs& a, void* ws, unsigned* status, int 
       k_head_clear<float><<<blocks, 256, 0, st>>>(static_cast<float*>(a.dweight), a.ld_dweight, a.V, a.d);
     return cudaGetLastError();
   }
-  return a.bf16 ? run<bf16>(a, static_cast<uint8_t*>(ws), status, num_sms, st)
-                : run<float>(a, static_cast<uint8_t*>(ws), status, num_sms, st);
+  return a.bf16 ? run_bf16(a, static_cast<uint8_t*>(ws), status, num_sms, st)
+                : run_f32(a, static_cast<uint8_t*>(ws), status, num_sms, st);
 }

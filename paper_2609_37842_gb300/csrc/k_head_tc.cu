@@ -1,0 +1,374 @@
+// The products of the token loss through the output matrix, on the tensor cores (see
+// k_head.cu for the formulas): z = scale x W^T with the sums of the loss, dx = D W and
+// dW = D^T x, all sums in fp32.
+//
+// k_head_tc: a pair of CTAs (tcgen05 cta_group::2) works on tiles of 256 x BN outputs, one
+// after the other. Each CTA loads its 128 rows of A and its half of B's columns, 64 steps of the
+// sum at a time, by TMA into a ring; the leader's MMA warp issues M = 256 instructions, whose
+// accumulators (two, in turn) lie in both CTAs' tensor memory; eight warps a CTA take a finished
+// one while the next is filled. An operand is read as it lies: K-major (x and W for the logits, D
+// for dx) or MN-major (W for dx, D and x for dW), so nothing is transposed.
+// An operand may come in several bf16 parts, blocks of 64 columns of each in turn; a sum then
+// runs over the products of parts that are listed.
+//
+// Warps (320 threads): 0 issues TMA, 1 owns tensor memory and issues MMAs, 2-9 end tiles.
+// Every wait is bounded; after one that ran out each role goes to the common end.
+#include <algorithm>
+
+#include "rows_dev.cuh"
+
+using namespace eogp;
+
+namespace {
+
+constexpr int kThreads = 320;
+constexpr int kStages = 6;
+constexpr uint32_t kABytes = 128u * 64u * 2u;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLowest = -3.402823466e38f;
+
+enum { kLogits = 0, kDx = 1, kDw = 2 };
+
+struct TcArgs {
+  HeadTc h;
+  int nN;  // tiles along N
+  unsigned* status;
+};
+
+// What a tile is about: its place, the steps of its sum, and which slab of a split sum it gives.
+struct Tile {
+  int m0, n0, split, i0, i1;
+};
+struct Shape {
+  int rows, M, mt, steps, per, tiles;
+};
+template <int MODE>
+__device__ __forceinline__ Shape shape_of(const TcArgs& g) {
+  Shape s;
+  s.rows = max(0, min(g.h.piece, *g.h.count - g.h.first));
+  s.M = MODE == kDw ? g.h.V : s.rows;
+  s.mt = (s.M + 255) / 256;
+  const int K = MODE == kLogits ? g.h.d : MODE == kDx ? g.h.V : s.rows;
+  s.steps = (K + 63) / 64 * g.h.pairs;
+  s.per = (s.steps + g.h.splits - 1) / g.h.splits;
+  s.tiles = s.mt * g.nN * g.h.splits;
+  return s;
+}
+template <int MODE>
+__device__ __forceinline__ Tile tile_of(const TcArgs& g, const Shape& s, int t) {
+  Tile r;
+  // Tiles that run together share what is read from far: the logits' W, and D for the others.
+  const int mn = s.mt * g.nN;
+  r.split = t / mn;
+  t -= r.split * mn;
+  const int m = MODE == kLogits ? t % s.mt : t / g.nN, n = MODE == kLogits ? t / s.mt : t % g.nN;
+  r.m0 = m * 256;
+  r.n0 = n * g.h.bn;
+  r.i0 = r.split * s.per;
+  r.i1 = min(s.steps, r.i0 + s.per);
+  return r;
+}
+
+// 32 outputs of one row from column c0 on, where the row's columns end at `n`; `wide`: 32-byte stores fit.
+__device__ __forceinline__ void put_f32(float* p, int left, bool wide, const float (&v)[32]) {
+  if (left >= 32 && wide) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      uint32_t w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[8 * q + e]);
+      st_global_v8(p + 8 * q, w);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+      if (e < left) p[e] = v[e];
+  }
+}
+__device__ __forceinline__ void put_bf16(bf16* p, int left, bool wide, const float (&v)[32]) {
+  if (left >= 32 && wide) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<uint4*>(p + 8 * q) =
+          make_uint4(pack_bf16(make_float2(v[8 * q], v[8 * q + 1])), pack_bf16(make_float2(v[8 * q + 2], v[8 * q + 3])),
+                     pack_bf16(make_float2(v[8 * q + 4], v[8 * q + 5])),
+                     pack_bf16(make_float2(v[8 * q + 6], v[8 * q + 7])));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+      if (e < left) p[e] = from_f32<bf16>(v[e]);
+  }
+}
+
+// A thread's columns c0 .. c1 of its row of the tile; `none`: the sum has no terms.
+template <int MODE>
+__device__ __forceinline__ void end_tile(const TcArgs& g, const Shape& s, const Tile& t, uint32_t tmem, int row, int c0,
+                                         int c1, int half, bool none) {
+  const HeadTc& h = g.h;
+  const bool mine = row < s.M;
+  float m = kLowest, sum = 0.f;
+  int target = -1;
+  bf16* out16 = nullptr;
+  float* out32 = nullptr;
+  const void* add = nullptr;
+  bool wide = true;
+  const int N = MODE == kLogits ? h.V : h.d;
+  if (MODE == kLogits) {
+    if (mine) target = h.target[h.first + row];
+    if (h.z) out32 = h.z + static_cast<size_t>(row) * h.ldz;
+  } else if (h.splits > 1) {
+    out32 = h.slabs + (static_cast<size_t>(t.split) * h.slab_rows + row) * h.ld_slab;
+  } else if (MODE == kDx) {
+    if (mine) {
+      int b, tt;
+      locate(h.rs, h.idx[h.first + row], b, tt);
+      if (h.out_bf16)
+        out16 = row_out<bf16>(h.dx, b, tt);
+      else
+        out32 = row_out<float>(h.dx, b, tt);
+    }
+    wide = h.wide;
+  } else {
+    const long long at = static_cast<long long>(row) * h.ld_out;
+    if (h.out_bf16)
+      out16 = static_cast<bf16*>(h.out) + at;
+    else
+      out32 = static_cast<float*>(h.out) + at;
+    wide = h.wide;
+  }
+  for (int c = c0; c < c1; c += 32) {
+    float v[32];
+    if (none) {
+#pragma unroll
+      for (int e = 0; e < 32; ++e) v[e] = 0.f;
+    } else {
+      tmem_ld32(tmem + c, v);
+    }
+    const int col = t.n0 + c, left = N - col;
+    if (!mine || left <= 0) continue;
+    if (MODE == kLogits) {
+      float top = kLowest;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        v[e] = e < left ? v[e] * h.scale : -INFINITY;
+        top = fmaxf(top, v[e]);
+      }
+      if (out32) put_f32(out32 + col, h.ldz - col, true, v);
+      if (static_cast<unsigned>(target - col) < 32u) {
+        float zt = 0.f;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) zt = target - col == e ? v[e] : zt;
+        h.zt[row] = zt;
+      }
+      if (top > m) {
+        sum *= exp2f((m - top) * kLog2e);
+        m = top;
+      }
+      float part = 0.f;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) part += exp2f((v[e] - m) * kLog2e);
+      sum += part;
+    } else {
+      if (MODE == kDw && h.splits == 1 && h.add) {
+        const long long at = static_cast<long long>(row) * h.ld_add + col;
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          if (e < left)
+            v[e] += h.add_bf16 ? to_f32(static_cast<const bf16*>(h.add)[at + e])
+                               : static_cast<const float*>(h.add)[at + e];
+      }
+      if (out16)
+        put_bf16(out16 + col, left, wide, v);
+      else
+        put_f32(out32 + col, left, wide, v);
+    }
+  }
+  if (MODE == kLogits && mine) h.part[static_cast<size_t>(t.n0 / h.bn * 2 + half) * h.piece + row] = make_float2(m, sum);
+}
+
+template <int MODE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    k_head_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const TcArgs g) {
+  constexpr bool kAmn = MODE == kDw, kBmn = MODE != kLogits;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = align1024(smem_raw);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int half = g.h.bn / 2;  // columns of B in this CTA
+  const uint32_t stage_bytes = kABytes + static_cast<uint32_t>(half) * 128u;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + static_cast<size_t>(kStages) * stage_bytes);
+  uint64_t* empty = full + kStages;
+  uint64_t* tfull = empty + kStages;
+  uint64_t* tempty = tfull + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
+  const uint32_t tcols = static_cast<uint32_t>(g.h.bn) * 2u;
+  const int cl = blockIdx.x >> 1, ncl = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    tma_prefetch_desc(&tmA);
+    tma_prefetch_desc(&tmB);
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full[s], 2);   // one expect_tx arrive from each CTA (the leader's copy is used)
+      mbar_init(&empty[s], 1);  // MMA completion, in both CTAs
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&tfull[b], 1);
+      mbar_init(&tempty[b], 16);  // 8 warps of 2 CTAs (the leader's copy is used)
+    }
+    fence_barrier_init();
+  }
+  if (warp == 1) tmem_alloc_pair(tmem_slot, tcols);
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const Shape sh = shape_of<MODE>(g);
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int rs = 0;
+      uint32_t rph = 0;
+      bool ok = true;
+      for (int t = cl; t < sh.tiles && ok; t += ncl) {
+        const Tile tl = tile_of<MODE>(g, sh, t);
+        const int am = tl.m0 + static_cast<int>(rank) * 128, bn = tl.n0 + static_cast<int>(rank) * half;
+        for (int i = tl.i0; i < tl.i1; ++i) {
+          const int s = rs;
+          const uint32_t ph = rph;
+          if (++rs == kStages) {
+            rs = 0;
+            rph ^= 1u;
+          }
+          if (!mbar_wait(&empty[s], ph ^ 1u, g.status)) {
+            ok = false;
+            break;
+          }
+          const int kb = i / g.h.pairs, c = (g.h.pair_list >> (4 * (i % g.h.pairs))) & 15;
+          const int pa = c & 3, pb = c >> 2;
+          const uint32_t st = smem_u32(smem + static_cast<size_t>(s) * stage_bytes);
+          const uint32_t fl = mapa_shared(smem_u32(&full[s]), 0);
+          mbar_arrive_expect_tx_cluster(fl, stage_bytes);
+          if (kAmn) {
+            tma_load_2d_pair(st, &tmA, (am / 64 * g.h.parts_a + pa) * 64, kb * 64, fl);
+            tma_load_2d_pair(st + 8192, &tmA, ((am / 64 + 1) * g.h.parts_a + pa) * 64, kb * 64, fl);
+          } else {
+            tma_load_2d_pair(st, &tmA, (kb * g.h.parts_a + pa) * 64, am, fl);
+          }
+          if (kBmn) {
+            for (int j = 0; j < half / 64; ++j)
+              tma_load_2d_pair(st + kABytes + j * 8192, &tmB, ((bn / 64 + j) * g.h.parts_b + pb) * 64, kb * 64, fl);
+          } else {
+            tma_load_2d_pair(st + kABytes, &tmB, (kb * g.h.parts_b + pb) * 64, bn, fl);
+          }
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      const uint32_t idesc = idesc_bf16_f32(256, g.h.bn, kAmn, kBmn);
+      // Step of 16 along the sum: 32 bytes of a K-major row, 16 rows of 128 bytes of MN-major ones.
+      constexpr uint64_t ka = kAmn ? 128 : 2, kb_ = kBmn ? 128 : 2;
+      int rs = 0, i = 0;
+      uint32_t rph = 0;
+      bool ok = true;
+      for (int t = cl; t < sh.tiles && ok; t += ncl) {
+        const Tile tl = tile_of<MODE>(g, sh, t);
+        if (tl.i0 >= tl.i1) continue;
+        const int buf = i & 1;
+        if (!mbar_wait(&tempty[buf], (static_cast<uint32_t>(i >> 1) & 1u) ^ 1u, g.status)) break;
+        ++i;
+        tc_fence_after();
+        const uint32_t d = tmem + buf * g.h.bn;
+        for (int k = tl.i0; k < tl.i1; ++k) {
+          const int s = rs;
+          const uint32_t ph = rph;
+          if (++rs == kStages) {
+            rs = 0;
+            rph ^= 1u;
+          }
+          if (!mbar_wait(&full[s], ph, g.status)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t st = smem_u32(smem + static_cast<size_t>(s) * stage_bytes);
+          const uint64_t a = kAmn ? sdesc_sw128(st, 8192, 1024) : sdesc_sw128(st, 16, 1024);
+          const uint64_t b = kBmn ? sdesc_sw128(st + kABytes, 8192, 1024) : sdesc_sw128(st + kABytes, 16, 1024);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            tc_mma_f16_pair(d, a + ka * kk, b + kb_ * kk, idesc, (k != tl.i0 || kk != 0) ? 1u : 0u);
+          tc_commit_pair_mc(&empty[s], 0x3);
+        }
+        tc_commit_pair_mc(&tfull[buf], 0x3);
+      }
+    }
+    __syncwarp();
+  } else {
+    const int q = warp & 3, side = (warp - 2) >> 2;
+    int i = 0;
+    for (int t = cl; t < sh.tiles; t += ncl) {
+      const Tile tl = tile_of<MODE>(g, sh, t);
+      const bool none = tl.i0 >= tl.i1;
+      const int buf = i & 1;
+      if (!none) {
+        uint32_t ok = 1;
+        if (lane == 0) ok = mbar_wait(&tfull[buf], static_cast<uint32_t>(i >> 1) & 1u, g.status) ? 1u : 0u;
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) break;
+        ++i;
+        tc_fence_after();
+      }
+      const int row = tl.m0 + static_cast<int>(rank) * 128 + q * 32 + lane;
+      end_tile<MODE>(g, sh, tl, tmem + buf * g.h.bn + (static_cast<uint32_t>(q * 32) << 16), row, side * half,
+                     side * half + half, side, none);
+      if (!none) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_relaxed_cluster(mapa_shared(smem_u32(&tempty[buf]), 0));
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();  // neither CTA leaves while its peer may still signal it
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc_pair(tmem, tcols);
+}
+
+int tmap(CUtensorMap* tm, const void* base, uint64_t inner, uint64_t rows, uint64_t ld, uint32_t box_rows) {
+  const uint64_t dims[2] = {inner, rows};
+  const uint64_t strides[1] = {ld * 2};
+  const uint32_t box[2] = {64, box_rows};
+  return make_tmap(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+template <int MODE>
+cudaError_t launch(const HeadTc& h, int most_m, int N, unsigned* status, int num_sms, cudaStream_t st) {
+  TcArgs g{h, (N + h.bn - 1) / h.bn, status};
+  CUtensorMap ta, tb;
+  const bool a_mn = MODE == kDw, b_mn = MODE != kLogits;
+  if (tmap(&ta, h.A, h.inner_a, h.rows_a, h.lda, a_mn ? 64 : 128) ||
+      tmap(&tb, h.B, h.inner_b, h.rows_b, h.ldb, b_mn ? 64 : h.bn / 2))
+    return cudaErrorInvalidValue;
+  const long long tiles = static_cast<long long>((most_m + 255) / 256) * g.nN * h.splits;
+  if (tiles > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
+  const size_t smem = 1024 + static_cast<size_t>(kStages) * (kABytes + h.bn / 2 * 128u) + (2 * kStages + 4) * 8 + 16;
+  if (cudaError_t e = allow_smem(k_head_tc<MODE>, smem); e != cudaSuccess) return e;
+  const unsigned grid = 2u * static_cast<unsigned>(std::min<long long>(tiles, num_sms / 2));
+  k_head_tc<MODE><<<grid, kThreads, smem, st>>>(ta, tb, g);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_head_logits(const HeadTc& h, unsigned* status, int num_sms, cudaStream_t st) {
+  return launch<kLogits>(h, h.piece, h.V, status, num_sms, st);
+}
+cudaError_t launch_head_dx(const HeadTc& h, unsigned* status, int num_sms, cudaStream_t st) {
+  return launch<kDx>(h, h.piece, h.d, status, num_sms, st);
+}
+cudaError_t launch_head_dw(const HeadTc& h, unsigned* status, int num_sms, cudaStream_t st) {
+  return launch<kDw>(h, h.V, h.d, status, num_sms, st);
+}
