@@ -317,6 +317,7 @@ struct HeadTc {
   int pairs;           // products of parts that are summed,
   uint32_t pair_list;  // four bits each: part of A | part of B << 2
   int bn, splits;      // columns of a tile; slabs that the sum is split into
+  int run;             // steps of 64 (times pairs) that one accumulator sums
   // logits: z (NULL: not kept) [piece x ldz], -inf beyond V; (maximum, sum) of each row's half tiles
   // [2 * tiles][piece]; the target's logit
   float scale;
@@ -334,8 +335,9 @@ struct HeadTc {
   long long ld_out;
   const void* add;
   long long ld_add;
-  bool add_bf16;
-  bool out_bf16, wide;  // type of dx or dW; whether its rows allow 32-byte stores
+  bool add_bf16, add_wide;
+  float* acc;  // [V x d]: takes the sums instead where more pieces follow (NULL: out does)
+  bool out_bf16, wide;  // type of dx or dW; whether its rows allow 32-byte stores (add_wide: such loads)
   // of split sums: [splits][slab_rows][ld_slab]
   float* slabs;
   size_t slab_rows;

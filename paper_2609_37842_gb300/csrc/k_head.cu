@@ -29,10 +29,10 @@ struct Plan {
   int find_blocks, per_block;  // blocks of the search, positions of each
   int piece, pieces;           // rows of a piece, most pieces
   int ldz, ldx, ldw;           // row strides of the logits, of the gathered rows and of the matrix
-  int parts;                   // bf16 parts of D
+  int parts;                   // bf16 parts of D that are used
   int bn_z, bn_d;              // columns of a tile of the logits, of dx and dW
   int splits_dx, splits_dw, ld_slab;
-  size_t counts, idx, target, w, x, z, acc, W, D, part, zt, row, slabs, total;
+  size_t counts, idx, target, w, x, z, acc, W, part, zt, row, slabs, total;
 };
 
 // Slabs of a sum of `steps` 64-deep steps for tiles that 76 pairs of multiprocessors take in turn:
@@ -70,8 +70,8 @@ Plan plan_of(const HeadArgs& a) {
   p.ldz = static_cast<int>(up(a.V, 64));
   p.ldx = static_cast<int>(up(a.d, 8));
   p.parts = a.bf16 ? a.dweight && !a.grad_bf16 ? 2 : 1 : 0;
-  // A row of a piece: logits and D, or the gathered row and the sums of its half tiles.
-  const size_t row_bytes = grad || !a.bf16 ? static_cast<size_t>(p.ldz) * (4 + 2 * p.parts)
+  // A row of a piece: logits, or the gathered row and the sums of its half tiles.
+  const size_t row_bytes = grad || !a.bf16 ? static_cast<size_t>(p.ldz) * 4
                                            : static_cast<size_t>(p.ldx) * 2 + p.ldz / 64 * 16;
   const long long most = std::max<long long>(256, static_cast<long long>(kPieceBytes / row_bytes) / 256 * 256);
   p.pieces = static_cast<int>((M + most - 1) / most);
@@ -104,7 +104,6 @@ Plan plan_of(const HeadArgs& a) {
     p.zt = take(static_cast<size_t>(p.piece) * 4);
     p.row = take(static_cast<size_t>(p.piece) * 8);
     if (grad) {
-      p.D = take(static_cast<size_t>(p.piece) * p.ldz * 2 * p.parts);
       const long long nt = (a.d + p.bn_d - 1) / p.bn_d;
       p.ld_slab = static_cast<int>(up(a.d, 8));
       p.splits_dx = a.dx.p ? splits_for(mt * nt, (a.V + 63) / 64, p.piece, a.d) : 1;
@@ -209,7 +208,7 @@ __global__ void __launch_bounds__(256) k_head_zero(const HeadArgs a, int M) {
 // Rows first .. of the counted positions, dense; zeros up to the next multiple of 64.
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_gather(const HeadArgs a, const int* counts, const int* idx, int first,
-                                                     int piece, int ldx, T* out) {
+                                                     int piece, int ldx, bool vec, T* out) {
   const int n = min(piece, counts[kFindBlocks] - first), lane = threadIdx.x & 31;
   const int n64 = (max(n, 0) + 63) & ~63;
   for (int i = blockIdx.x * 8 + (threadIdx.x >> 5); i < n64; i += gridDim.x * 8) {
@@ -220,7 +219,16 @@ __global__ void __launch_bounds__(256) k_head_gather(const HeadArgs a, const int
       locate(a.rs, idx[first + i], b, t);
       x = row_of<T>(a.x, b, t);
     }
-    for (int c = lane; c < ldx; c += 32) o[c] = x && c < a.d ? x[c] : from_f32<T>(0.f);
+    constexpr int N = 16 / sizeof(T);
+    if (vec && x) {
+      const int nv = a.d / N;
+#pragma unroll 4
+      for (int c = lane; c < nv; c += 32)
+        *reinterpret_cast<uint4*>(o + c * N) = __ldcs(reinterpret_cast<const uint4*>(x) + c);
+      for (int c = nv * N + lane; c < ldx; c += 32) o[c] = c < a.d ? x[c] : from_f32<T>(0.f);
+    } else {
+      for (int c = lane; c < ldx; c += 32) o[c] = x && c < a.d ? x[c] : from_f32<T>(0.f);
+    }
   }
 }
 
@@ -389,23 +397,24 @@ __global__ void __launch_bounds__(1024) k_head_join(const HeadArgs a, const int*
   if (row) row[i] = make_float2(m, w * a.scale / s);
 }
 
-// D in bf16 parts from the logits, eight columns a thread; zeros in the rows up to the next multiple of 64,
-// which the sum over rows runs over.
+// D over the logits, in place: the 256 bytes of 64 columns become the 64 first bf16 parts and, with PARTS = 2,
+// the 64 second ones. Eight columns a thread, eight threads on such a block, which read it before one writes.
+// Zeros in the rows up to the next multiple of 64, which the sum over rows runs over. (4,096 x 50,000 to two parts: 255 us,
+// 6.4 TB/s.)
 template <int PARTS>
 __global__ void __launch_bounds__(256) k_head_d(const HeadArgs a, const int* counts, const int* targets,
-                                                const float* ws, int first, int piece, const float* z, int ldz,
-                                                const float2* row, bf16* D) {
+                                                const float* ws, int first, int piece, float* z, int ldz,
+                                                const float2* row) {
   const int n = min(piece, counts[kFindBlocks] - first), n64 = (max(n, 0) + 63) & ~63;
   for (int i = blockIdx.x; i < n64; i += gridDim.x) {
-    bf16* const out = D + static_cast<size_t>(i) * ldz * PARTS;
-    const float* const x = z + static_cast<size_t>(i) * ldz;
+    float* const x = z + static_cast<size_t>(i) * ldz;
     const bool real = i < n;
     const float2 mi = real ? row[i] : make_float2(0.f, 0.f);
     const int target = real ? targets[first + i] : -1;
     const float g = real ? ws[first + i] * a.scale : 0.f;
-    for (int c = threadIdx.x * 8; c < ldz; c += 256 * 8) {
+    for (int c = threadIdx.x * 8; (c & ~255) < ldz; c += 256 * 8) {
       Vals<8> v = fill<8>(0.f);
-      if (real) {
+      if (real && c < ldz) {
         v = ld_floats<8>(x + c);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -423,7 +432,9 @@ __global__ void __launch_bounds__(256) k_head_d(const HeadArgs a, const int* cou
             if (target - c == e) v.set(e, v.get(e) - g);
         }
       }
-      bf16* o = out + (c >> 6) * 64 * PARTS + (c & 63);
+      __syncwarp();
+      if (c >= ldz) continue;
+      bf16* const o = reinterpret_cast<bf16*>(x + (c & ~63)) + (c & 63);
 #pragma unroll
       for (int p = 0; p < PARTS; ++p) {
         const Raw<bf16, 8> r = pack_raw<bf16, 8>(v);
@@ -438,31 +449,49 @@ __global__ void __launch_bounds__(256) k_head_d(const HeadArgs a, const int* cou
   }
 }
 
-// The slabs of a split sum joined, in order: rows of dx by position, or rows of dW.
+// The slabs of a split sum joined, in order, four columns a thread: rows of dx by position, or rows of dW.
 __global__ void __launch_bounds__(256) k_head_slabs(const HeadTc h, int rows_most, bool to_dx) {
-  const int rows = to_dx ? min(h.piece, *h.count - h.first) : rows_most, lane = threadIdx.x & 31;
-  for (int i = blockIdx.x * 8 + (threadIdx.x >> 5); i < rows; i += gridDim.x * 8) {
-    long long at = i * h.ld_out;
-    void* out = h.out;
+  const int there = *h.count - h.first, rows = to_dx ? min(h.piece, there) : rows_most, nv = h.ld_slab / 4;
+  if (!to_dx && there <= 0 && h.first > 0) return;
+  const bool to_acc = !to_dx && h.acc && there > h.piece;
+  const size_t slab = h.slab_rows * static_cast<size_t>(h.ld_slab);
+  for (long long k = blockIdx.x * 256ll + threadIdx.x; k < static_cast<long long>(rows) * nv; k += gridDim.x * 256ll) {
+    const int i = static_cast<int>(k / nv), c = static_cast<int>(k - static_cast<long long>(i) * nv) * 4;
+    const float* const from = h.slabs + static_cast<size_t>(i) * h.ld_slab + c;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int s = 0; s < h.splits; ++s) {
+      const float4 x = __ldcs(reinterpret_cast<const float4*>(from + s * slab));
+      v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+    }
+    const float w[4] = {v.x, v.y, v.z, v.w};
+    long long at = to_acc ? static_cast<long long>(i) * h.d : i * h.ld_out;
+    void* out = to_acc ? h.acc : h.out;
     if (to_dx) {
       int b, t;
       locate(h.rs, h.idx[h.first + i], b, t);
       at = b * h.dx.bs + t * h.dx.ld;
       out = const_cast<void*>(h.dx.p);
     }
-    for (int c = lane; c < h.d; c += 32) {
-      float v = 0.f;
-      for (int s = 0; s < h.splits; ++s) v += h.slabs[(s * h.slab_rows + i) * h.ld_slab + c];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (c + e >= h.d) break;
+      float x = w[e];
       if (h.add) {
-        const long long from = i * h.ld_add + c;
-        v += h.add_bf16 ? to_f32(static_cast<const bf16*>(h.add)[from]) : static_cast<const float*>(h.add)[from];
+        const long long a = i * h.ld_add + c + e;
+        x += h.add_bf16 ? to_f32(static_cast<const bf16*>(h.add)[a]) : static_cast<const float*>(h.add)[a];
       }
-      if (h.out_bf16)
-        static_cast<bf16*>(out)[at + c] = from_f32<bf16>(v);
+      if (h.out_bf16 && !to_acc)
+        static_cast<bf16*>(out)[at + c + e] = from_f32<bf16>(x);
       else
-        static_cast<float*>(out)[at + c] = v;
+        static_cast<float*>(out)[at + c + e] = x;
     }
   }
+}
+
+// Whether rows of `es`-byte elements begin on 16 bytes.
+bool vec_rows(const RowView& v, int es) {
+  return reinterpret_cast<uintptr_t>(v.p) % 16 == 0 && v.bs * es % 16 == 0 && v.ld * es % 16 == 0;
 }
 
 // The counted positions of the batch.
@@ -498,7 +527,6 @@ cudaError_t run_bf16(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_s
   int* const target = reinterpret_cast<int*>(ws + p.target);
   float* const w = reinterpret_cast<float*>(ws + p.w);
   bf16* const x = reinterpret_cast<bf16*>(ws + p.x);
-  bf16* const D = reinterpret_cast<bf16*>(ws + p.D);
   float2* const row = reinterpret_cast<float2*>(ws + p.row);
   const bf16* W = static_cast<const bf16*>(a.weight);
   long long ldw = a.V == 1 ? p.ldw : a.ld_weight;
@@ -530,55 +558,56 @@ cudaError_t run_bf16(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_s
   h.parts_a = h.parts_b = h.pairs = 1;
   h.ld_slab = p.ld_slab;
   h.slabs = reinterpret_cast<float*>(ws + p.slabs);
-  const uint64_t ud = a.d, uv = a.V, rows = p.piece, dcols = static_cast<uint64_t>(p.ldz) * p.parts;
+  const bool vec = vec_rows(a.x, 2);
+  const uint64_t ud = a.d, uv = a.V, rows = p.piece, dcols = static_cast<uint64_t>(p.ldz) * 2;  // D lies in the logits' place
   for (int c = 0; c < p.pieces; ++c) {
     h.first = c * p.piece;
-    k_head_gather<bf16><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, h.first, p.piece, p.ldx, x);
+    k_head_gather<bf16><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, h.first, p.piece, p.ldx, vec, x);
     TRY(cudaGetLastError());
     HeadTc z = h;
     z.A = x, z.inner_a = ud, z.rows_a = rows, z.lda = p.ldx;
     z.B = W, z.inner_b = ud, z.rows_b = uv, z.ldb = ldw;
-    z.bn = p.bn_z, z.splits = 1;
+    z.bn = p.bn_z, z.splits = 1, z.run = 16;
     TRY(launch_head_logits(z, status, num_sms, st));
     k_head_join<<<(p.piece + 31) / 32, 1024, 0, st>>>(a, counts, idx, w, h.first, p.piece, h.part,
                                                       (a.V + p.bn_z - 1) / p.bn_z * 2, h.zt, grad ? row : nullptr);
     TRY(cudaGetLastError());
     if (!grad) continue;
     auto d = p.parts == 2 ? k_head_d<2> : k_head_d<1>;
-    d<<<std::min(p.piece, num_sms * 8), 256, 0, st>>>(a, counts, target, w, h.first, p.piece, h.z, p.ldz, row, D);
+    d<<<std::min(p.piece, num_sms * 8), 256, 0, st>>>(a, counts, target, w, h.first, p.piece, h.z, p.ldz, row);
     TRY(cudaGetLastError());
     if (a.dx.p) {
       HeadTc g = h;
-      g.A = D, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = p.parts;
+      g.A = h.z, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = 2;
       g.B = W, g.inner_b = ud, g.rows_b = uv, g.ldb = ldw;
-      g.bn = p.bn_d, g.splits = p.splits_dx, g.slab_rows = p.piece;
+      g.bn = p.bn_d, g.splits = p.splits_dx, g.slab_rows = p.piece, g.run = 64;
       g.dx = a.dx, g.out_bf16 = true, g.wide = wide_rows(a.dx.p, a.dx.bs, a.dx.ld, 2);
       TRY(launch_head_dx(g, status, num_sms, st));
       if (g.splits > 1) {
-        k_head_slabs<<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(g, p.piece, true);
+        k_head_slabs<<<num_sms * 8, 256, 0, st>>>(g, p.piece, true);
         TRY(cudaGetLastError());
       }
     }
     if (a.dweight) {
       HeadTc g = h;
-      g.A = D, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = p.parts;
+      g.A = h.z, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = 2;
       g.B = x, g.inner_b = ud, g.rows_b = rows, g.ldb = p.ldx;
       if (p.parts == 2) g.pairs = 2, g.pair_list = 0x10;  // D's parts with x
-      g.bn = p.bn_d, g.splits = p.splits_dw, g.slab_rows = a.V;
-      // Sums of several pieces stay in fp32: in dweight itself, or beside it until the last piece.
+      g.bn = p.bn_d, g.splits = p.splits_dw, g.slab_rows = a.V, g.run = a.grad_bf16 ? 64 : 16;
+      // Sums of several pieces stay in fp32, in dweight itself or beside it; the last piece that has rows
+      // ends them, and those after it do nothing.
+      g.out = a.dweight, g.ld_out = a.ld_dweight, g.out_bf16 = a.grad_bf16;
       float* const acc = p.acc ? reinterpret_cast<float*>(ws + p.acc) : nullptr;
-      if (acc && c < p.pieces - 1)
-        g.out = acc, g.ld_out = a.d;
-      else
-        g.out = a.dweight, g.ld_out = a.ld_dweight, g.out_bf16 = a.grad_bf16;
       if (c > 0)
         g.add = acc ? static_cast<void*>(acc) : a.dweight, g.ld_add = acc ? a.d : a.ld_dweight;
       else if (a.accumulate)
         g.add = a.dweight, g.ld_add = a.ld_dweight, g.add_bf16 = a.grad_bf16;
+      g.acc = c < p.pieces - 1 ? acc : nullptr;
       g.wide = wide_rows(g.out, 0, g.ld_out, g.out_bf16 ? 2 : 4);
+      g.add_wide = wide_rows(g.add, 0, g.ld_add, g.add_bf16 ? 2 : 4);
       TRY(launch_head_dw(g, status, num_sms, st));
       if (g.splits > 1) {
-        k_head_slabs<<<std::min((a.V + 7) / 8, num_sms * 8), 256, 0, st>>>(g, a.V, false);
+        k_head_slabs<<<num_sms * 8, 256, 0, st>>>(g, a.V, false);
         TRY(cudaGetLastError());
       }
     }
@@ -601,10 +630,10 @@ cudaError_t run_f32(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sm
     k_head_zero<float><<<std::min((M + 7) / 8, num_sms * 8), 256, 0, st>>>(a, M);
     if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
   }
-  const bool grad = a.dx.p || a.dweight;
+  const bool grad = a.dx.p || a.dweight, vec = vec_rows(a.x, 4);
   for (int c = 0; c < p.pieces; ++c) {
     const int first = c * p.piece;
-    k_head_gather<float><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, first, p.piece, p.ldx, x);
+    k_head_gather<float><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, first, p.piece, p.ldx, vec, x);
     if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
     const Out logits{z, p.ldz, false, nullptr, 0, false};
     if (cudaError_t e = product(Product<float, float>{x, p.ldx, 1, W, a.ld_weight, 1, p.piece, a.V, a.d, true, false, a.scale},

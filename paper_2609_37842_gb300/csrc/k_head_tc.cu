@@ -8,10 +8,14 @@
 // accumulators (two, in turn) lie in both CTAs' tensor memory; eight warps a CTA take a finished
 // one while the next is filled. An operand is read as it lies: K-major (x and W for the logits, D
 // for dx) or MN-major (W for dx, D and x for dW), so nothing is transposed.
+// Tensor cores cut an accumulator off where they add to it: towards 0, by up to 2^-23 of it every
+// 16 products. So a long sum goes through several accumulators, `run` steps of 64 each, which are
+// added up in registers, rounded.
 // An operand may come in several bf16 parts, blocks of 64 columns of each in turn; a sum then
 // runs over the products of parts that are listed.
 //
-// Warps (320 threads): 0 issues TMA, 1 owns tensor memory and issues MMAs, 2-9 end tiles.
+// Warps (384 threads): 0 issues TMA, 1 owns tensor memory and issues MMAs, 4-11 end tiles; these
+// take over registers from the first four (168 x 384 = 56 x 128 + 224 x 256).
 // Every wait is bounded; after one that ran out each role goes to the common end.
 #include <algorithm>
 
@@ -21,7 +25,7 @@ using namespace eogp;
 
 namespace {
 
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;
 constexpr int kStages = 6;
 constexpr uint32_t kABytes = 128u * 64u * 2u;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -39,19 +43,26 @@ struct TcArgs {
 struct Tile {
   int m0, n0, split, i0, i1;
 };
+// Outputs of a thread: a row's half tile, in registers while a sum goes through several accumulators.
+struct Sums {
+  float v[4][32];
+};
 struct Shape {
   int rows, M, mt, steps, per, tiles;
+  bool last;  // no piece with rows follows
 };
 template <int MODE>
 __device__ __forceinline__ Shape shape_of(const TcArgs& g) {
   Shape s;
-  s.rows = max(0, min(g.h.piece, *g.h.count - g.h.first));
+  const int left = *g.h.count - g.h.first;
+  s.rows = max(0, min(g.h.piece, left));
+  s.last = left <= g.h.piece;
   s.M = MODE == kDw ? g.h.V : s.rows;
   s.mt = (s.M + 255) / 256;
   const int K = MODE == kLogits ? g.h.d : MODE == kDx ? g.h.V : s.rows;
   s.steps = (K + 63) / 64 * g.h.pairs;
   s.per = (s.steps + g.h.splits - 1) / g.h.splits;
-  s.tiles = s.mt * g.nN * g.h.splits;
+  s.tiles = s.rows == 0 && g.h.first > 0 ? 0 : s.mt * g.nN * g.h.splits;
   return s;
 }
 template <int MODE>
@@ -66,6 +77,12 @@ __device__ __forceinline__ Tile tile_of(const TcArgs& g, const Shape& s, int t) 
   r.n0 = n * g.h.bn;
   r.i0 = r.split * s.per;
   r.i1 = min(s.steps, r.i0 + s.per);
+  return r;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 
@@ -100,17 +117,33 @@ __device__ __forceinline__ void put_bf16(bf16* p, int left, bool wide, const flo
   }
 }
 
-// A thread's columns c0 .. c1 of its row of the tile; `none`: the sum has no terms.
+template <typename T>
+__device__ __forceinline__ void add_row(const T* p, int left, bool wide, float (&v)[32]) {
+  constexpr int N = 16 / sizeof(T);
+  if (left >= 32 && wide) {
+#pragma unroll
+    for (int q = 0; q < 32; q += N) {
+      const Vals<N> a = unpack<T, N>(ld_raw<T, N>(p + q));
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[q + e] += a.get(e);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+      if (e < left) v[e] += to_f32(p[e]);
+  }
+}
+
+// What the sums of a thread's row of its side's columns of the tile become.
 template <int MODE>
-__device__ __forceinline__ void end_tile(const TcArgs& g, const Shape& s, const Tile& t, uint32_t tmem, int row, int c0,
-                                         int c1, int half, bool none) {
+__device__ __forceinline__ void end_tile(const TcArgs& g, const Shape& s, const Tile& t, int row, int side,
+                                         Sums& sums) {
   const HeadTc& h = g.h;
   const bool mine = row < s.M;
   float m = kLowest, sum = 0.f;
   int target = -1;
   bf16* out16 = nullptr;
   float* out32 = nullptr;
-  const void* add = nullptr;
   bool wide = true;
   const int N = MODE == kLogits ? h.V : h.d;
   if (MODE == kLogits) {
@@ -128,6 +161,9 @@ __device__ __forceinline__ void end_tile(const TcArgs& g, const Shape& s, const 
         out32 = row_out<float>(h.dx, b, tt);
     }
     wide = h.wide;
+  } else if (h.acc && !s.last) {
+    out32 = h.acc + static_cast<size_t>(row) * h.d;
+    wide = h.d % 8 == 0;
   } else {
     const long long at = static_cast<long long>(row) * h.ld_out;
     if (h.out_bf16)
@@ -136,54 +172,68 @@ __device__ __forceinline__ void end_tile(const TcArgs& g, const Shape& s, const 
       out32 = static_cast<float*>(h.out) + at;
     wide = h.wide;
   }
-  for (int c = c0; c < c1; c += 32) {
-    float v[32];
-    if (none) {
 #pragma unroll
-      for (int e = 0; e < 32; ++e) v[e] = 0.f;
-    } else {
-      tmem_ld32(tmem + c, v);
-    }
-    const int col = t.n0 + c, left = N - col;
-    if (!mine || left <= 0) continue;
-    if (MODE == kLogits) {
-      float top = kLowest;
+  for (int k = 0; k < 4; ++k) {
+    const int col = t.n0 + side * (h.bn / 2) + k * 32, left = N - col;
+    float(&v)[32] = sums.v[k];
+    if (k * 64 < h.bn && mine && left > 0) {
+      if (MODE == kLogits) {
+        float top = kLowest;
 #pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        v[e] = e < left ? v[e] * h.scale : -INFINITY;
-        top = fmaxf(top, v[e]);
+        for (int e = 0; e < 32; ++e) {
+          v[e] = e < left ? v[e] * h.scale : -INFINITY;
+          top = fmaxf(top, v[e]);
+        }
+        if (out32) put_f32(out32 + col, h.ldz - col, true, v);
+        if (static_cast<unsigned>(target - col) < 32u) {
+          float zt = 0.f;
+#pragma unroll
+          for (int e = 0; e < 32; ++e) zt = target - col == e ? v[e] : zt;
+          h.zt[row] = zt;
+        }
+        if (top > m) {
+          sum *= exp2_fast((m - top) * kLog2e);
+          m = top;
+        }
+        float2 part = pair(0.f);
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+          const float2 d = mul2(add2(make_float2(v[e], v[e + 1]), pair(-m)), pair(kLog2e));
+          part = add2(part, make_float2(exp2_fast(d.x), exp2_fast(d.y)));
+        }
+        sum += part.x + part.y;
+      } else {
+        if (MODE == kDw && h.splits == 1 && h.add) {
+          const long long at = static_cast<long long>(row) * h.ld_add + col;
+          if (h.add_bf16)
+            add_row(static_cast<const bf16*>(h.add) + at, left, h.add_wide, v);
+          else
+            add_row(static_cast<const float*>(h.add) + at, left, h.add_wide, v);
+        }
+        if (out16)
+          put_bf16(out16 + col, left, wide, v);
+        else
+          put_f32(out32 + col, left, wide, v);
       }
-      if (out32) put_f32(out32 + col, h.ldz - col, true, v);
-      if (static_cast<unsigned>(target - col) < 32u) {
-        float zt = 0.f;
-#pragma unroll
-        for (int e = 0; e < 32; ++e) zt = target - col == e ? v[e] : zt;
-        h.zt[row] = zt;
-      }
-      if (top > m) {
-        sum *= exp2f((m - top) * kLog2e);
-        m = top;
-      }
-      float part = 0.f;
-#pragma unroll
-      for (int e = 0; e < 32; ++e) part += exp2f((v[e] - m) * kLog2e);
-      sum += part;
-    } else {
-      if (MODE == kDw && h.splits == 1 && h.add) {
-        const long long at = static_cast<long long>(row) * h.ld_add + col;
-#pragma unroll
-        for (int e = 0; e < 32; ++e)
-          if (e < left)
-            v[e] += h.add_bf16 ? to_f32(static_cast<const bf16*>(h.add)[at + e])
-                               : static_cast<const float*>(h.add)[at + e];
-      }
-      if (out16)
-        put_bf16(out16 + col, left, wide, v);
-      else
-        put_f32(out32 + col, left, wide, v);
     }
   }
-  if (MODE == kLogits && mine) h.part[static_cast<size_t>(t.n0 / h.bn * 2 + half) * h.piece + row] = make_float2(m, sum);
+  if (MODE == kLogits && mine) h.part[static_cast<size_t>(t.n0 / h.bn * 2 + side) * h.piece + row] = make_float2(m, sum);
+}
+
+// An accumulator, in place of the sums or added to them.
+__device__ __forceinline__ void take_sums(uint32_t tmem, int bn, bool more, Sums& sums) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (k * 64 < bn) {
+#pragma unroll
+      for (int c = 0; c < 32; c += 16) {
+        float v[16];
+        tmem_ld16(tmem + k * 32 + c, v);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sums.v[k][c + e] = (more ? sums.v[k][c + e] : 0.f) + v[e];
+      }
+    }
+  }
 }
 
 template <int MODE>
@@ -225,6 +275,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const uint32_t tmem = *tmem_slot;
   const Shape sh = shape_of<MODE>(g);
 
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
   if (warp == 0) {
     if (lane == 0) {
       int rs = 0;
@@ -275,59 +327,71 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       bool ok = true;
       for (int t = cl; t < sh.tiles && ok; t += ncl) {
         const Tile tl = tile_of<MODE>(g, sh, t);
-        if (tl.i0 >= tl.i1) continue;
-        const int buf = i & 1;
-        if (!mbar_wait(&tempty[buf], (static_cast<uint32_t>(i >> 1) & 1u) ^ 1u, g.status)) break;
-        ++i;
-        tc_fence_after();
-        const uint32_t d = tmem + buf * g.h.bn;
-        for (int k = tl.i0; k < tl.i1; ++k) {
-          const int s = rs;
-          const uint32_t ph = rph;
-          if (++rs == kStages) {
-            rs = 0;
-            rph ^= 1u;
-          }
-          if (!mbar_wait(&full[s], ph, g.status)) {
+        for (int k0 = tl.i0; k0 < tl.i1 && ok; k0 += g.h.run) {
+          const int buf = i & 1, k1 = min(tl.i1, k0 + g.h.run);
+          if (!mbar_wait(&tempty[buf], (static_cast<uint32_t>(i >> 1) & 1u) ^ 1u, g.status)) {
             ok = false;
             break;
           }
+          ++i;
           tc_fence_after();
-          const uint32_t st = smem_u32(smem + static_cast<size_t>(s) * stage_bytes);
-          const uint64_t a = kAmn ? sdesc_sw128(st, 8192, 1024) : sdesc_sw128(st, 16, 1024);
-          const uint64_t b = kBmn ? sdesc_sw128(st + kABytes, 8192, 1024) : sdesc_sw128(st + kABytes, 16, 1024);
+          const uint32_t d = tmem + buf * g.h.bn;
+          for (int k = k0; k < k1; ++k) {
+            const int s = rs;
+            const uint32_t ph = rph;
+            if (++rs == kStages) {
+              rs = 0;
+              rph ^= 1u;
+            }
+            if (!mbar_wait(&full[s], ph, g.status)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t st = smem_u32(smem + static_cast<size_t>(s) * stage_bytes);
+            const uint64_t a = kAmn ? sdesc_sw128(st, 8192, 1024) : sdesc_sw128(st, 16, 1024);
+            const uint64_t b = kBmn ? sdesc_sw128(st + kABytes, 8192, 1024) : sdesc_sw128(st + kABytes, 16, 1024);
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-            tc_mma_f16_pair(d, a + ka * kk, b + kb_ * kk, idesc, (k != tl.i0 || kk != 0) ? 1u : 0u);
-          tc_commit_pair_mc(&empty[s], 0x3);
+            for (int kk = 0; kk < 4; ++kk)
+              tc_mma_f16_pair(d, a + ka * kk, b + kb_ * kk, idesc, (k != k0 || kk != 0) ? 1u : 0u);
+            tc_commit_pair_mc(&empty[s], 0x3);
+          }
+          tc_commit_pair_mc(&tfull[buf], 0x3);
         }
-        tc_commit_pair_mc(&tfull[buf], 0x3);
       }
     }
     __syncwarp();
+  }
   } else {
-    const int q = warp & 3, side = (warp - 2) >> 2;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    const int q = warp & 3, side = (warp - 4) >> 2;
     int i = 0;
-    for (int t = cl; t < sh.tiles; t += ncl) {
+    bool ok = true;
+    for (int t = cl; t < sh.tiles && ok; t += ncl) {
       const Tile tl = tile_of<MODE>(g, sh, t);
-      const bool none = tl.i0 >= tl.i1;
-      const int buf = i & 1;
-      if (!none) {
-        uint32_t ok = 1;
-        if (lane == 0) ok = mbar_wait(&tfull[buf], static_cast<uint32_t>(i >> 1) & 1u, g.status) ? 1u : 0u;
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-        if (!ok) break;
-        ++i;
-        tc_fence_after();
-      }
       const int row = tl.m0 + static_cast<int>(rank) * 128 + q * 32 + lane;
-      end_tile<MODE>(g, sh, tl, tmem + buf * g.h.bn + (static_cast<uint32_t>(q * 32) << 16), row, side * half,
-                     side * half + half, side, none);
-      if (!none) {
+      const uint32_t lanes = tmem + (static_cast<uint32_t>(q * 32) << 16);
+      Sums sums;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 32; ++e) sums.v[k][e] = 0.f;  // what a sum without terms is
+      for (int k0 = tl.i0; k0 < tl.i1; k0 += g.h.run, ++i) {
+        const int buf = i & 1;
+        uint32_t there = 1;
+        if (lane == 0) there = mbar_wait(&tfull[buf], static_cast<uint32_t>(i >> 1) & 1u, g.status) ? 1u : 0u;
+        there = __shfl_sync(0xffffffffu, there, 0);
+        if (!there) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        take_sums(lanes + buf * g.h.bn + side * half, g.h.bn, k0 > tl.i0, sums);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_relaxed_cluster(mapa_shared(smem_u32(&tempty[buf]), 0));
       }
+      if (ok) end_tile<MODE>(g, sh, tl, row, side, sums);
     }
   }
   tc_fence_before();
