@@ -316,7 +316,7 @@ struct HeadTc {
   int parts_a, parts_b;
   int pairs;           // products of parts that are summed,
   uint32_t pair_list;  // four bits each: part of A | part of B << 2
-  int bn, splits;      // columns of a tile; slabs that the sum is split into
+  int bn;              // columns of a tile
   int run;             // steps of 64 (times pairs) that one accumulator sums
   // logits: z (NULL: not kept) [piece x ldz], -inf beyond V; (maximum, sum) of each row's half tiles
   // [2 * tiles][piece]; the target's logit
@@ -338,11 +338,12 @@ struct HeadTc {
   bool add_bf16, add_wide;
   float* acc;  // [V x d]: takes the sums instead where more pieces follow (NULL: out does)
   bool out_bf16, wide;  // type of dx or dW; whether its rows allow 32-byte stores (add_wide: such loads)
-  // of split sums: [splits][slab_rows][ld_slab]
+  // of split sums of dx or dW: [splits][rows][ld_slab], as many as fit (head_splits)
   float* slabs;
-  size_t slab_rows;
-  int ld_slab;
+  size_t slab_bytes;
+  int ld_slab, clusters;
+  int piece_rows, rows_box;  // most rows of this piece; rows of a K-major A that a CTA loads
 };
-cudaError_t launch_head_logits(const HeadTc& h, unsigned* status, int num_sms, cudaStream_t st);
-cudaError_t launch_head_dx(const HeadTc& h, unsigned* status, int num_sms, cudaStream_t st);
-cudaError_t launch_head_dw(const HeadTc& h, unsigned* status, int num_sms, cudaStream_t st);
+cudaError_t launch_head_logits(const HeadTc& h, unsigned* status, cudaStream_t st);
+cudaError_t launch_head_dx(const HeadTc& h, unsigned* status, cudaStream_t st);
+cudaError_t launch_head_dw(const HeadTc& h, unsigned* status, cudaStream_t st);

@@ -1,0 +1,28 @@
+// Device code that the kernels of the token loss through the output matrix share
+// (k_head.cu, k_head_tc.cu).
+#pragma once
+
+#include "rows_dev.cuh"
+
+namespace eogp {
+
+constexpr int kMostSplits = 32;
+
+// How many slabs the sums of `tiles` tiles of 256 rows are split into, `steps` 64-deep steps each, so that
+// the pairs of multiprocessors take about the same share, by a whole warp. Tiles are taken in rounds;
+// a round costs its steps and about 8 more (filling the ring, ending a tile), and a split the
+// writing and reading of its slabs and the launch that joins them, in steps of 0.38 us (3,977 rows
+// of 4096 columns, 1,563 steps: 2.40 ms unsplit in four rounds of 76, the last a third full).
+__device__ __forceinline__ int head_splits(const HeadTc& h, long long tiles, int steps, int rows) {
+  const int s = static_cast<int>(threadIdx.x & 31) + 1;
+  const unsigned long long slab = static_cast<unsigned long long>(rows) * h.ld_slab;
+  long long cost = (tiles * s + h.clusters - 1) / h.clusters * ((steps + s - 1) / s + 8);
+  if (s > 1) cost += 8 + static_cast<long long>(s * slab / 323000);
+  if (s > 1 && (s > steps || s * slab * 4 > h.slab_bytes)) cost = 0x7fffffffffffffffll;
+  unsigned long long best = static_cast<unsigned long long>(cost);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, o));
+  return __ffs(__ballot_sync(0xffffffffu, static_cast<unsigned long long>(cost) == best));
+}
+
+}  // namespace eogp

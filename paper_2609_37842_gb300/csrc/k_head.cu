@@ -9,7 +9,7 @@
 // become D in place.
 #include <algorithm>
 
-#include "rows_dev.cuh"
+#include "head_dev.cuh"
 
 using namespace eogp;
 
@@ -19,6 +19,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
 constexpr int kFindThreads = 1024;
 constexpr int kFindBlocks = 1024;
+constexpr int kFewRows = 1024;
+constexpr size_t kSlabBytes = size_t(512) << 20;
 constexpr size_t kPieceBytes = size_t(4) << 30;  // logits of a piece
 
 size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -31,27 +33,11 @@ struct Plan {
   int ldz, ldx, ldw;           // row strides of the logits, of the gathered rows and of the matrix
   int parts;                   // bf16 parts of D that are used
   int bn_z, bn_d;              // columns of a tile of the logits, of dx and dW
-  int splits_dx, splits_dw, ld_slab;
+  int ld_slab;
+  bool few;  // positions are found and gathered in one launch
+  size_t slab_bytes;
   size_t counts, idx, target, w, x, z, acc, W, part, zt, row, slabs, total;
 };
-
-// Slabs of a sum of `steps` 64-deep steps for tiles that 76 pairs of multiprocessors take in turn:
-// the fewest rounds, where each costs its steps and about 8 more (filling the ring, ending the
-// tile), and a split the writing and reading of its slabs and a launch (in steps of 0.38 us).
-int splits_for(long long tiles, long long steps, long long rows, int d) {
-  int best = 1;
-  double least = 0;
-  for (int s = 1; s <= 32 && s <= steps; ++s) {
-    const double rounds = static_cast<double>((tiles * s + 75) / 76);
-    double cost = rounds * (static_cast<double>((steps + s - 1) / s) + 8);
-    if (s > 1) cost += 8 + 8.0 * s * rows * d / 6.8e12 / 0.38e-6;
-    if (s == 1 || cost < least) {
-      best = s;
-      least = cost;
-    }
-  }
-  return best;
-}
 
 bool w_fits(const HeadArgs& a) {
   return reinterpret_cast<uintptr_t>(a.weight) % 16 == 0 &&
@@ -76,6 +62,7 @@ Plan plan_of(const HeadArgs& a) {
   const long long most = std::max<long long>(256, static_cast<long long>(kPieceBytes / row_bytes) / 256 * 256);
   p.pieces = static_cast<int>((M + most - 1) / most);
   p.piece = static_cast<int>(std::min(most, up((M + p.pieces - 1) / p.pieces, 256)));
+  p.few = p.pieces == 1 && M <= kFewRows;
   const int es = a.bf16 ? 2 : 4;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -93,25 +80,23 @@ Plan plan_of(const HeadArgs& a) {
   if (a.bf16) {
     p.ldw = static_cast<int>(up(a.d, 8));
     if (!w_fits(a)) p.W = take(static_cast<size_t>(a.V) * p.ldw * 2);
-    const long long mt = p.piece / 256;
+    // Columns of a tile of the logits: the widest, but for few tiles those that 76 pairs share out best.
+    const long long mt = (std::min<long long>(M, p.piece) + 255) / 256;
     p.bn_z = 256;
-    if (mt * ((a.V + 255) / 256) < 4 * 76)  // few tiles: those that share them out best
+    if (mt * ((a.V + 255) / 256) < 4 * 76)
       for (int bn = 128; bn >= 64; bn /= 2)
-        if ((mt * ((a.V + bn - 1) / bn) + 75) / 76 * bn < (mt * ((a.V + p.bn_z - 1) / p.bn_z) + 75) / 76 * p.bn_z)
+        if ((mt * ((a.V + bn - 1) / bn) + 75) / 76 * bn * 10 < (mt * ((a.V + p.bn_z - 1) / p.bn_z) + 75) / 76 * p.bn_z * 9)
           p.bn_z = bn;
     p.bn_d = up(a.d, 128) * 1.15 < up(a.d, 256) ? 128 : 256;
     p.part = take(static_cast<size_t>((a.V + p.bn_z - 1) / p.bn_z) * 2 * p.piece * 8);
     p.zt = take(static_cast<size_t>(p.piece) * 4);
     p.row = take(static_cast<size_t>(p.piece) * 8);
     if (grad) {
-      const long long nt = (a.d + p.bn_d - 1) / p.bn_d;
       p.ld_slab = static_cast<int>(up(a.d, 8));
-      p.splits_dx = a.dx.p ? splits_for(mt * nt, (a.V + 63) / 64, p.piece, a.d) : 1;
-      p.splits_dw = a.dweight ? splits_for((a.V + 255ll) / 256 * nt, p.piece / 64 * p.parts, a.V, a.d) : 1;
-      size_t slabs = 0;
-      if (p.splits_dx > 1) slabs = static_cast<size_t>(p.splits_dx) * p.piece * p.ld_slab * 4;
-      if (p.splits_dw > 1) slabs = std::max(slabs, static_cast<size_t>(p.splits_dw) * a.V * p.ld_slab * 4);
-      if (slabs) p.slabs = take(slabs);
+      // Room for split sums: as many as there may be, half a GB at most.
+      const size_t most_rows = std::max<size_t>(a.dx.p ? p.piece : 0, a.dweight ? a.V : 0);
+      p.slab_bytes = std::min<size_t>(kSlabBytes, most_rows * p.ld_slab * 4 * kMostSplits);
+      p.slabs = take(p.slab_bytes);
     }
   }
   p.total = at;
@@ -205,29 +190,80 @@ __global__ void __launch_bounds__(256) k_head_zero(const HeadArgs a, int M) {
   }
 }
 
+// Row i of the gathered ones by a warp: x (NULL: zeros), and zeros from d to ldx.
+template <typename T>
+__device__ __forceinline__ void put_row(const T* x, int d, int ldx, bool vec, T* o) {
+  constexpr int N = 16 / sizeof(T);
+  const int lane = threadIdx.x & 31, nv = vec && x ? d / N : 0;
+#pragma unroll 4
+  for (int c = lane; c < nv; c += 32)
+    *reinterpret_cast<uint4*>(o + c * N) = __ldcs(reinterpret_cast<const uint4*>(x) + c);
+  for (int c = nv * N + lane; c < ldx; c += 32) o[c] = x && c < d ? x[c] : from_f32<T>(0.f);
+}
+
 // Rows first .. of the counted positions, dense; zeros up to the next multiple of 64.
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_gather(const HeadArgs a, const int* counts, const int* idx, int first,
                                                      int piece, int ldx, bool vec, T* out) {
-  const int n = min(piece, counts[kFindBlocks] - first), lane = threadIdx.x & 31;
-  const int n64 = (max(n, 0) + 63) & ~63;
+  const int n = min(piece, counts[kFindBlocks] - first), n64 = (max(n, 0) + 63) & ~63;
   for (int i = blockIdx.x * 8 + (threadIdx.x >> 5); i < n64; i += gridDim.x * 8) {
-    T* const o = out + static_cast<size_t>(i) * ldx;
     const T* x = nullptr;
     if (i < n) {
       int b, t;
       locate(a.rs, idx[first + i], b, t);
       x = row_of<T>(a.x, b, t);
     }
-    constexpr int N = 16 / sizeof(T);
-    if (vec && x) {
-      const int nv = a.d / N;
-#pragma unroll 4
-      for (int c = lane; c < nv; c += 32)
-        *reinterpret_cast<uint4*>(o + c * N) = __ldcs(reinterpret_cast<const uint4*>(x) + c);
-      for (int c = nv * N + lane; c < ldx; c += 32) o[c] = c < a.d ? x[c] : from_f32<T>(0.f);
-    } else {
-      for (int c = lane; c < ldx; c += 32) o[c] = x && c < a.d ? x[c] : from_f32<T>(0.f);
+    put_row<T>(x, a.d, ldx, vec, out + static_cast<size_t>(i) * ldx);
+  }
+}
+
+// Up to kFewRows positions: the search, the gathering and the zeros in one launch. Every block looks at all of
+// them, and each of its warps then has one.
+template <typename T>
+__global__ void __launch_bounds__(256) k_head_few(const HeadArgs a, int M, int* counts, int* idx, int* target, float* w,
+                                                  int ldx, bool vec, T* out, unsigned* status) {
+  __shared__ unsigned kept[kFewRows / 32];
+  const int tid = threadIdx.x, lane = tid & 31, r = blockIdx.x * 8 + (tid >> 5);
+#pragma unroll
+  for (int k = 0; k < kFewRows / 256; ++k) {
+    const int i = tid + k * 256;
+    const unsigned mask = __ballot_sync(0xffffffffu, i < M && job_of(a, i, nullptr).kept);
+    if (lane == 0) kept[i >> 5] = mask;
+  }
+  __syncthreads();
+  int before = 0, n = 0;
+  for (int k = lane; k < kFewRows / 32; k += 32) {
+    const unsigned m = kept[k];
+    n += __popc(m);
+    before += __popc(k * 32 + 32 <= r ? m : k * 32 <= r ? m & ((1u << (r & 31)) - 1u) : 0u);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    n += __shfl_xor_sync(0xffffffffu, n, o);
+    before += __shfl_xor_sync(0xffffffffu, before, o);
+  }
+  if (r == 0 && lane == 0) counts[kFindBlocks] = n;
+  for (int i = n + r; i < ((n + 63) & ~63); i += gridDim.x * 8)
+    put_row<T>(nullptr, a.d, ldx, vec, out + static_cast<size_t>(i) * ldx);
+  if (r >= M) return;
+  const Job j = job_of(a, r, status);
+  int b, t;
+  locate(a.rs, r, b, t);
+  if (j.kept) {
+    if (lane == 0) {
+      idx[before] = r;
+      target[before] = j.target;
+      w[before] = j.w;
+    }
+    put_row<T>(row_of<T>(a.x, b, t), a.d, ldx, vec, out + static_cast<size_t>(before) * ldx);
+  } else {
+    if (lane == 0) {
+      a.loss[r] = 0.f;
+      if (a.lse) a.lse[r] = 0.f;
+    }
+    if (a.dx.p) {
+      T* const g = row_out<T>(a.dx, b, t);
+      for (int c = lane; c < a.d; c += 32) g[c] = from_f32<T>(0.f);
     }
   }
 }
@@ -376,11 +412,13 @@ __global__ void __launch_bounds__(1024) k_head_join(const HeadArgs a, const int*
   if (blockIdx.x * 32 >= n) return;
   float m = kLowest, s = 0.f;
   if (i < n) {
+    const float2* const v = parts + i;
+#pragma unroll 8
+    for (int p = warp; p < n_parts; p += 32) m = fmaxf(m, v[static_cast<size_t>(p) * piece].x);
+#pragma unroll 8
     for (int p = warp; p < n_parts; p += 32) {
-      const float2 v = parts[static_cast<size_t>(p) * piece + i];
-      const float top = fmaxf(m, v.x);
-      s = s * exp2f((m - top) * kLog2e) + v.y * exp2f((v.x - top) * kLog2e);
-      m = top;
+      const float2 x = v[static_cast<size_t>(p) * piece];
+      s += x.y * exp2f((x.x - m) * kLog2e);
     }
   }
   all[warp][lane] = make_float2(m, s);
@@ -450,17 +488,20 @@ __global__ void __launch_bounds__(256) k_head_d(const HeadArgs a, const int* cou
 }
 
 // The slabs of a split sum joined, in order, four columns a thread: rows of dx by position, or rows of dW.
-__global__ void __launch_bounds__(256) k_head_slabs(const HeadTc h, int rows_most, bool to_dx) {
-  const int there = *h.count - h.first, rows = to_dx ? min(h.piece, there) : rows_most, nv = h.ld_slab / 4;
-  if (!to_dx && there <= 0 && h.first > 0) return;
+__global__ void __launch_bounds__(256) k_head_slabs(const HeadTc h, bool to_dx) {
+  const int there = *h.count - h.first, some = max(0, min(h.piece, there)), rows = to_dx ? some : h.V;
+  if ((to_dx || h.first > 0) && some == 0) return;
+  const int steps = ((to_dx ? h.V : some) + 63) / 64 * h.pairs, nv = h.ld_slab / 4;
+  const int splits = head_splits(h, static_cast<long long>((rows + 255) / 256) * ((h.d + h.bn - 1) / h.bn), steps, rows);
+  if (splits == 1) return;
   const bool to_acc = !to_dx && h.acc && there > h.piece;
-  const size_t slab = h.slab_rows * static_cast<size_t>(h.ld_slab);
+  const size_t slab = static_cast<size_t>(rows) * h.ld_slab;
   for (long long k = blockIdx.x * 256ll + threadIdx.x; k < static_cast<long long>(rows) * nv; k += gridDim.x * 256ll) {
     const int i = static_cast<int>(k / nv), c = static_cast<int>(k - static_cast<long long>(i) * nv) * 4;
     const float* const from = h.slabs + static_cast<size_t>(i) * h.ld_slab + c;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
-    for (int s = 0; s < h.splits; ++s) {
+    for (int s = 0; s < splits; ++s) {
       const float4 x = __ldcs(reinterpret_cast<const float4*>(from + s * slab));
       v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
     }
@@ -494,24 +535,36 @@ bool vec_rows(const RowView& v, int es) {
   return reinterpret_cast<uintptr_t>(v.p) % 16 == 0 && v.bs * es % 16 == 0 && v.ld * es % 16 == 0;
 }
 
-// The counted positions of the batch.
-cudaError_t find(const HeadArgs& a, const Plan& p, uint8_t* ws, unsigned* status, cudaStream_t st) {
-  const int M = static_cast<int>(a.rs.rows());
-  int* const counts = reinterpret_cast<int*>(ws + p.counts);
-  if (p.find_blocks > 1) {
-    k_head_count<<<p.find_blocks, kFindThreads, 0, st>>>(a, M, p.per_block, counts);
-    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
-  }
-  k_head_place<<<p.find_blocks, kFindThreads, 0, st>>>(
-      a, M, p.per_block, counts, reinterpret_cast<int*>(ws + p.idx), reinterpret_cast<int*>(ws + p.target),
-      reinterpret_cast<float*>(ws + p.w), status);
-  return cudaGetLastError();
-}
-
 #define TRY(x)                                             \
   do {                                                     \
     if (cudaError_t e_ = (x); e_ != cudaSuccess) return e_; \
   } while (0)
+
+// The counted positions of the batch, zeros for the others, and, where there are few, their rows at `x`.
+template <typename T>
+cudaError_t find(const HeadArgs& a, const Plan& p, uint8_t* ws, T* x, bool vec, unsigned* status, int num_sms,
+                 cudaStream_t st) {
+  const int M = static_cast<int>(a.rs.rows());
+  int* const counts = reinterpret_cast<int*>(ws + p.counts);
+  int* const idx = reinterpret_cast<int*>(ws + p.idx);
+  int* const target = reinterpret_cast<int*>(ws + p.target);
+  float* const w = reinterpret_cast<float*>(ws + p.w);
+  if (p.few) {
+    k_head_few<T><<<(M + 7) / 8, 256, 0, st>>>(a, M, counts, idx, target, w, p.ldx, vec, x, status);
+    return cudaGetLastError();
+  }
+  if (p.find_blocks > 1) {
+    k_head_count<<<p.find_blocks, kFindThreads, 0, st>>>(a, M, p.per_block, counts);
+    TRY(cudaGetLastError());
+  }
+  k_head_place<<<p.find_blocks, kFindThreads, 0, st>>>(a, M, p.per_block, counts, idx, target, w, status);
+  TRY(cudaGetLastError());
+  if (a.dx.p) {
+    k_head_zero<T><<<std::min((M + 7) / 8, num_sms * 8), 256, 0, st>>>(a, M);
+    TRY(cudaGetLastError());
+  }
+  return cudaSuccess;
+}
 
 // Whether rows of `es`-byte elements allow 32-byte stores at multiples of 32 columns.
 bool wide_rows(const void* p, long long bs, long long ld, int es) {
@@ -537,11 +590,8 @@ cudaError_t run_bf16(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_s
     W = copy;
     ldw = p.ldw;
   }
-  TRY(find(a, p, ws, status, st));
-  if (a.dx.p) {
-    k_head_zero<bf16><<<std::min((M + 7) / 8, num_sms * 8), 256, 0, st>>>(a, M);
-    TRY(cudaGetLastError());
-  }
+  const bool vec = vec_rows(a.x, 2);
+  TRY(find(a, p, ws, x, vec, status, num_sms, st));
   HeadTc h{};
   h.count = counts + kFindBlocks;
   h.piece = p.piece;
@@ -558,17 +608,21 @@ cudaError_t run_bf16(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_s
   h.parts_a = h.parts_b = h.pairs = 1;
   h.ld_slab = p.ld_slab;
   h.slabs = reinterpret_cast<float*>(ws + p.slabs);
-  const bool vec = vec_rows(a.x, 2);
+  h.slab_bytes = p.slab_bytes;
+  h.clusters = num_sms / 2;
+  h.piece_rows = static_cast<int>(std::min<long long>(M, p.piece));
+  h.rows_box = static_cast<int>(std::min<long long>(128, up(h.piece_rows, 8)));
   const uint64_t ud = a.d, uv = a.V, rows = p.piece, dcols = static_cast<uint64_t>(p.ldz) * 2;  // D lies in the logits' place
   for (int c = 0; c < p.pieces; ++c) {
     h.first = c * p.piece;
-    k_head_gather<bf16><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, h.first, p.piece, p.ldx, vec, x);
+    if (!p.few)
+      k_head_gather<bf16><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, h.first, p.piece, p.ldx, vec, x);
     TRY(cudaGetLastError());
     HeadTc z = h;
     z.A = x, z.inner_a = ud, z.rows_a = rows, z.lda = p.ldx;
     z.B = W, z.inner_b = ud, z.rows_b = uv, z.ldb = ldw;
-    z.bn = p.bn_z, z.splits = 1, z.run = 16;
-    TRY(launch_head_logits(z, status, num_sms, st));
+    z.bn = p.bn_z, z.run = 16;
+    TRY(launch_head_logits(z, status, st));
     k_head_join<<<(p.piece + 31) / 32, 1024, 0, st>>>(a, counts, idx, w, h.first, p.piece, h.part,
                                                       (a.V + p.bn_z - 1) / p.bn_z * 2, h.zt, grad ? row : nullptr);
     TRY(cudaGetLastError());
@@ -580,20 +634,18 @@ cudaError_t run_bf16(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_s
       HeadTc g = h;
       g.A = h.z, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = 2;
       g.B = W, g.inner_b = ud, g.rows_b = uv, g.ldb = ldw;
-      g.bn = p.bn_d, g.splits = p.splits_dx, g.slab_rows = p.piece, g.run = 64;
+      g.bn = p.bn_d, g.run = 64;
       g.dx = a.dx, g.out_bf16 = true, g.wide = wide_rows(a.dx.p, a.dx.bs, a.dx.ld, 2);
-      TRY(launch_head_dx(g, status, num_sms, st));
-      if (g.splits > 1) {
-        k_head_slabs<<<num_sms * 8, 256, 0, st>>>(g, p.piece, true);
-        TRY(cudaGetLastError());
-      }
+      TRY(launch_head_dx(g, status, st));
+      k_head_slabs<<<num_sms * 8, 256, 0, st>>>(g, true);
+      TRY(cudaGetLastError());
     }
     if (a.dweight) {
       HeadTc g = h;
       g.A = h.z, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = 2;
       g.B = x, g.inner_b = ud, g.rows_b = rows, g.ldb = p.ldx;
       if (p.parts == 2) g.pairs = 2, g.pair_list = 0x10;  // D's parts with x
-      g.bn = p.bn_d, g.splits = p.splits_dw, g.slab_rows = a.V, g.run = a.grad_bf16 ? 64 : 16;
+      g.bn = p.bn_d, g.run = a.grad_bf16 ? 64 : 16;
       // Sums of several pieces stay in fp32, in dweight itself or beside it; the last piece that has rows
       // ends them, and those after it do nothing.
       g.out = a.dweight, g.ld_out = a.ld_dweight, g.out_bf16 = a.grad_bf16;
@@ -605,11 +657,9 @@ cudaError_t run_bf16(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_s
       g.acc = c < p.pieces - 1 ? acc : nullptr;
       g.wide = wide_rows(g.out, 0, g.ld_out, g.out_bf16 ? 2 : 4);
       g.add_wide = wide_rows(g.add, 0, g.ld_add, g.add_bf16 ? 2 : 4);
-      TRY(launch_head_dw(g, status, num_sms, st));
-      if (g.splits > 1) {
-        k_head_slabs<<<num_sms * 8, 256, 0, st>>>(g, a.V, false);
-        TRY(cudaGetLastError());
-      }
+      TRY(launch_head_dw(g, status, st));
+      k_head_slabs<<<num_sms * 8, 256, 0, st>>>(g, false);
+      TRY(cudaGetLastError());
     }
   }
   return cudaSuccess;
@@ -625,15 +675,12 @@ cudaError_t run_f32(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sm
   float* const x = reinterpret_cast<float*>(ws + p.x);
   float* const z = reinterpret_cast<float*>(ws + p.z);
   const float* const W = static_cast<const float*>(a.weight);
-  TRY(find(a, p, ws, status, st));
-  if (a.dx.p) {
-    k_head_zero<float><<<std::min((M + 7) / 8, num_sms * 8), 256, 0, st>>>(a, M);
-    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
-  }
   const bool grad = a.dx.p || a.dweight, vec = vec_rows(a.x, 4);
+  TRY(find(a, p, ws, x, vec, status, num_sms, st));
   for (int c = 0; c < p.pieces; ++c) {
     const int first = c * p.piece;
-    k_head_gather<float><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, first, p.piece, p.ldx, vec, x);
+    if (!p.few)
+      k_head_gather<float><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, first, p.piece, p.ldx, vec, x);
     if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
     const Out logits{z, p.ldz, false, nullptr, 0, false};
     if (cudaError_t e = product(Product<float, float>{x, p.ldx, 1, W, a.ld_weight, 1, p.piece, a.V, a.d, true, false, a.scale},

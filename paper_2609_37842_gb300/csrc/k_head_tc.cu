@@ -19,14 +19,15 @@
 // Every wait is bounded; after one that ran out each role goes to the common end.
 #include <algorithm>
 
-#include "rows_dev.cuh"
+#include "head_dev.cuh"
 
 using namespace eogp;
 
 namespace {
 
 constexpr int kThreads = 384;
-constexpr int kStages = 6;
+constexpr int kMostStages = 16;
+constexpr size_t kRingBytes = 6 * 32768;
 constexpr uint32_t kABytes = 128u * 64u * 2u;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
@@ -35,7 +36,8 @@ enum { kLogits = 0, kDx = 1, kDw = 2 };
 
 struct TcArgs {
   HeadTc h;
-  int nN;  // tiles along N
+  int nN;      // tiles along N
+  int stages;  // of the ring
   unsigned* status;
 };
 
@@ -48,9 +50,10 @@ struct Sums {
   float v[4][32];
 };
 struct Shape {
-  int rows, M, mt, steps, per, tiles;
+  int rows, M, mt, steps, splits, per, tiles;
   bool last;  // no piece with rows follows
 };
+// By whole warps.
 template <int MODE>
 __device__ __forceinline__ Shape shape_of(const TcArgs& g) {
   Shape s;
@@ -61,8 +64,9 @@ __device__ __forceinline__ Shape shape_of(const TcArgs& g) {
   s.mt = (s.M + 255) / 256;
   const int K = MODE == kLogits ? g.h.d : MODE == kDx ? g.h.V : s.rows;
   s.steps = (K + 63) / 64 * g.h.pairs;
-  s.per = (s.steps + g.h.splits - 1) / g.h.splits;
-  s.tiles = s.rows == 0 && g.h.first > 0 ? 0 : s.mt * g.nN * g.h.splits;
+  s.splits = MODE == kLogits ? 1 : head_splits(g.h, s.mt * g.nN, s.steps, s.M);
+  s.per = (s.steps + s.splits - 1) / s.splits;
+  s.tiles = s.rows == 0 && g.h.first > 0 ? 0 : s.mt * g.nN * s.splits;
   return s;
 }
 template <int MODE>
@@ -105,11 +109,12 @@ __device__ __forceinline__ void put_f32(float* p, int left, bool wide, const flo
 __device__ __forceinline__ void put_bf16(bf16* p, int left, bool wide, const float (&v)[32]) {
   if (left >= 32 && wide) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      *reinterpret_cast<uint4*>(p + 8 * q) =
-          make_uint4(pack_bf16(make_float2(v[8 * q], v[8 * q + 1])), pack_bf16(make_float2(v[8 * q + 2], v[8 * q + 3])),
-                     pack_bf16(make_float2(v[8 * q + 4], v[8 * q + 5])),
-                     pack_bf16(make_float2(v[8 * q + 6], v[8 * q + 7])));
+    for (int q = 0; q < 2; ++q) {
+      uint32_t w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = pack_bf16(make_float2(v[16 * q + 2 * e], v[16 * q + 2 * e + 1]));
+      st_global_v8(p + 16 * q, w);
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < 32; ++e)
@@ -149,8 +154,8 @@ __device__ __forceinline__ void end_tile(const TcArgs& g, const Shape& s, const 
   if (MODE == kLogits) {
     if (mine) target = h.target[h.first + row];
     if (h.z) out32 = h.z + static_cast<size_t>(row) * h.ldz;
-  } else if (h.splits > 1) {
-    out32 = h.slabs + (static_cast<size_t>(t.split) * h.slab_rows + row) * h.ld_slab;
+  } else if (s.splits > 1) {
+    out32 = h.slabs + (static_cast<size_t>(t.split) * s.M + row) * h.ld_slab;
   } else if (MODE == kDx) {
     if (mine) {
       int b, tt;
@@ -203,7 +208,7 @@ __device__ __forceinline__ void end_tile(const TcArgs& g, const Shape& s, const 
         }
         sum += part.x + part.y;
       } else {
-        if (MODE == kDw && h.splits == 1 && h.add) {
+        if (MODE == kDw && s.splits == 1 && h.add) {
           const long long at = static_cast<long long>(row) * h.ld_add + col;
           if (h.add_bf16)
             add_row(static_cast<const bf16*>(h.add) + at, left, h.add_wide, v);
@@ -246,9 +251,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const uint32_t rank = cluster_ctarank();
   const int half = g.h.bn / 2;  // columns of B in this CTA
   const uint32_t stage_bytes = kABytes + static_cast<uint32_t>(half) * 128u;
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + static_cast<size_t>(kStages) * stage_bytes);
-  uint64_t* empty = full + kStages;
-  uint64_t* tfull = empty + kStages;
+  const int stages = g.stages;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + static_cast<size_t>(stages) * stage_bytes);
+  uint64_t* empty = full + stages;
+  uint64_t* tfull = empty + stages;
   uint64_t* tempty = tfull + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
   const uint32_t tcols = static_cast<uint32_t>(g.h.bn) * 2u;
@@ -257,7 +263,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0) {
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < stages; ++s) {
       mbar_init(&full[s], 2);   // one expect_tx arrive from each CTA (the leader's copy is used)
       mbar_init(&empty[s], 1);  // MMA completion, in both CTAs
     }
@@ -279,6 +285,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
   if (warp == 0) {
     if (lane == 0) {
+      // Few rows: those of A that there are, and none of the second CTA's. What lies in the others' place
+      // only reaches outputs that are not taken.
+      const bool a_there = kAmn || static_cast<int>(rank) * 128 < g.h.piece_rows;
+      const uint32_t bytes = (kAmn ? kABytes : a_there ? g.h.rows_box * 128u : 0u) + static_cast<uint32_t>(half) * 128u;
       int rs = 0;
       uint32_t rph = 0;
       bool ok = true;
@@ -288,7 +298,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         for (int i = tl.i0; i < tl.i1; ++i) {
           const int s = rs;
           const uint32_t ph = rph;
-          if (++rs == kStages) {
+          if (++rs == stages) {
             rs = 0;
             rph ^= 1u;
           }
@@ -300,11 +310,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           const int pa = c & 3, pb = c >> 2;
           const uint32_t st = smem_u32(smem + static_cast<size_t>(s) * stage_bytes);
           const uint32_t fl = mapa_shared(smem_u32(&full[s]), 0);
-          mbar_arrive_expect_tx_cluster(fl, stage_bytes);
+          mbar_arrive_expect_tx_cluster(fl, bytes);
           if (kAmn) {
             tma_load_2d_pair(st, &tmA, (am / 64 * g.h.parts_a + pa) * 64, kb * 64, fl);
             tma_load_2d_pair(st + 8192, &tmA, ((am / 64 + 1) * g.h.parts_a + pa) * 64, kb * 64, fl);
-          } else {
+          } else if (a_there) {
             tma_load_2d_pair(st, &tmA, (kb * g.h.parts_a + pa) * 64, am, fl);
           }
           if (kBmn) {
@@ -339,7 +349,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           for (int k = k0; k < k1; ++k) {
             const int s = rs;
             const uint32_t ph = rph;
-            if (++rs == kStages) {
+            if (++rs == stages) {
               rs = 0;
               rph ^= 1u;
             }
@@ -409,30 +419,31 @@ int tmap(CUtensorMap* tm, const void* base, uint64_t inner, uint64_t rows, uint6
 }
 
 template <int MODE>
-cudaError_t launch(const HeadTc& h, int most_m, int N, unsigned* status, int num_sms, cudaStream_t st) {
-  TcArgs g{h, (N + h.bn - 1) / h.bn, status};
+cudaError_t launch(const HeadTc& h, int most_m, int N, unsigned* status, cudaStream_t st) {
+  const size_t stage = kABytes + h.bn / 2 * 128u;
+  TcArgs g{h, (N + h.bn - 1) / h.bn, static_cast<int>(std::min<size_t>(kMostStages, kRingBytes / stage)), status};
   CUtensorMap ta, tb;
   const bool a_mn = MODE == kDw, b_mn = MODE != kLogits;
-  if (tmap(&ta, h.A, h.inner_a, h.rows_a, h.lda, a_mn ? 64 : 128) ||
+  if (tmap(&ta, h.A, h.inner_a, h.rows_a, h.lda, a_mn ? 64 : h.rows_box) ||
       tmap(&tb, h.B, h.inner_b, h.rows_b, h.ldb, b_mn ? 64 : h.bn / 2))
     return cudaErrorInvalidValue;
-  const long long tiles = static_cast<long long>((most_m + 255) / 256) * g.nN * h.splits;
+  const long long tiles = static_cast<long long>((most_m + 255) / 256) * g.nN * (MODE == kLogits ? 1 : kMostSplits);
   if (tiles > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
-  const size_t smem = 1024 + static_cast<size_t>(kStages) * (kABytes + h.bn / 2 * 128u) + (2 * kStages + 4) * 8 + 16;
+  const size_t smem = 1024 + g.stages * stage + (2 * g.stages + 4) * 8 + 16;
   if (cudaError_t e = allow_smem(k_head_tc<MODE>, smem); e != cudaSuccess) return e;
-  const unsigned grid = 2u * static_cast<unsigned>(std::min<long long>(tiles, num_sms / 2));
+  const unsigned grid = 2u * static_cast<unsigned>(std::min<long long>(tiles, h.clusters));
   k_head_tc<MODE><<<grid, kThreads, smem, st>>>(ta, tb, g);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_head_logits(const HeadTc& h, unsigned* status, int num_sms, cudaStream_t st) {
-  return launch<kLogits>(h, h.piece, h.V, status, num_sms, st);
+cudaError_t launch_head_logits(const HeadTc& h, unsigned* status, cudaStream_t st) {
+  return launch<kLogits>(h, h.piece_rows, h.V, status, st);
 }
-cudaError_t launch_head_dx(const HeadTc& h, unsigned* status, int num_sms, cudaStream_t st) {
-  return launch<kDx>(h, h.piece, h.d, status, num_sms, st);
+cudaError_t launch_head_dx(const HeadTc& h, unsigned* status, cudaStream_t st) {
+  return launch<kDx>(h, h.piece_rows, h.d, status, st);
 }
-cudaError_t launch_head_dw(const HeadTc& h, unsigned* status, int num_sms, cudaStream_t st) {
-  return launch<kDw>(h, h.V, h.d, status, num_sms, st);
+cudaError_t launch_head_dw(const HeadTc& h, unsigned* status, cudaStream_t st) {
+  return launch<kDw>(h, h.V, h.d, status, st);
 }
