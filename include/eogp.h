@@ -694,9 +694,9 @@ int eogp_head_loss(const void* x, int dtype, long long x_bs, long long x_ld, con
  *     teacher_lse (w / h) * p, at the others.
  * Where a list holds all V classes there is no such class more. Terms of q = 0 are 0. Multiply the weights by h^2 for the usual scaling of softened targets.
  * A class that is listed twice counts as one entry with the sum of both q in the gradient, and as two
- * in the loss. A position is left out (loss, lse and gradient 0, its logits not read) when it is
- * padding, when its weight is 0, or, without teacher_lse, when no entry has a logit above -inf; a class >= V
- * sets EOGP_EDEVICE in the device status word and leaves its position out. Rows of logits without a finite one,
+ * in the loss. A position is left out (loss, lse and gradient 0, whatever its logits hold)
+ * when it is padding, when its weight is 0, or, without teacher_lse, when no entry has a logit above -inf; a class
+ * >= V sets EOGP_EDEVICE in the device status word and leaves its position out. Rows of logits without a finite one,
  * or with a NaN or +inf, give NaN; a NaN or +inf in a list gives a loss that is not finite; finite logits
  * may have any size.
  * loss and lse fp32 [B x T], dense; lse and dlogits may be NULL; dlogits has the type of logits
