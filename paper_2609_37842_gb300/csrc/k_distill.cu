@@ -35,7 +35,6 @@ struct __align__(16) List {
   int cls[kListMax];         // -1: no entry; -2: out of range
   float y[kListMax];         // the teacher's logit
   float x[kListMax];         // the student's
-  float q[kListMax], log_q[kListMax];
   float q_all[kListMax];     // sum of q of the entries of this class
   uint8_t first[kListMax];   // the first entry of its class
   unsigned seen[kSeen / 32]; // of slow_row: bit c % kSeen: a class like c is listed
@@ -82,59 +81,80 @@ __device__ __forceinline__ Entry entry_of(const DistillArgs& a, const Job& j, co
   return r;
 }
 
-// The teacher's side, by every warp for itself: the log-sum that logarithms of q are against, and the sum of q.
-struct Teacher {
-  float whole, sum;
+// What a list comes to by itself, by every warp alone: log q of an entry is (y - top) / h - whole; sum of q; the
+// largest of the student's logits m, and t = sum q (log q - (x - m) / h), so that the loss's sum over
+// the list is t + sum * (lse - m / h).
+struct Sums {
+  float top, whole, sum, m, t;
   bool bad, some;  // a class out of range; something to learn from
 };
-__device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, const List& l, const Job& j, float inv_h) {
+__device__ __forceinline__ float log_q_of(const Sums& t, float y, float inv_h) { return (y - t.top) * inv_h - t.whole; }
+__device__ __forceinline__ float term(float q, float log_q, float log_p) {
+  return q > 0.f || q != q ? q * (log_q - log_p) : 0.f;
+}
+__device__ __forceinline__ Sums sums_of(const DistillArgs& a, const List& l, const Job& j, float inv_h) {
   const int lane = threadIdx.x & 31;
-  Teacher t;
-  float m = -INFINITY;
+  Sums t;
+  float top = -INFINITY, m = kLowest;
   bool bad = false, any = false;
   for (int k = lane; k < a.K; k += 32) {
     const int c = l.cls[k];
     const float y = l.y[k];
     bad |= c == -2;
-    any |= c >= 0 && !(y == -INFINITY);
-    if (c >= 0) m = fmaxf(m, y);
+    if (c < 0) continue;
+    any |= !(y == -INFINITY);
+    top = fmaxf(top, y);
+    m = fmaxf(m, l.x[k]);
   }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  for (int o = 16; o > 0; o >>= 1) {
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  }
   t.bad = __any_sync(0xffffffffu, bad);
   t.some = __any_sync(0xffffffffu, any) || a.teacher_lse;
-  float s = 0.f;
-  if (a.teacher_lse) {
-    t.whole = j.lse;
+  t.m = m;
+  t.top = 0.f;
+  t.whole = j.lse;
+  if (!a.teacher_lse) {
+    float s = 0.f;
     for (int k = lane; k < a.K; k += 32)
-      if (l.cls[k] >= 0) s += expf(l.y[k] * inv_h - t.whole);
-    t.sum = warp_sum(s);
-  } else {
-    for (int k = lane; k < a.K; k += 32)
-      if (l.cls[k] >= 0) s += expf((l.y[k] - m) * inv_h);
-    t.whole = logf(warp_sum(s));  // on top of m / h
-    t.sum = m;
+      if (l.cls[k] >= 0) s += expf((l.y[k] - top) * inv_h);
+    t.top = top;
+    t.whole = logf(warp_sum(s));
   }
+  float sum = 0.f, v = 0.f;
+  for (int k = lane; k < a.K; k += 32) {
+    if (l.cls[k] < 0) continue;
+    const float lq = log_q_of(t, l.y[k], inv_h), q = expf(lq);
+    sum += q;
+    v += term(q, lq, (l.x[k] - m) * inv_h);
+  }
+  t.sum = warp_sum(sum);
+  t.t = warp_sum(v);
   return t;
 }
-// log q of an entry.
-__device__ __forceinline__ float log_q_of(const DistillArgs& a, const Teacher& t, float y, float inv_h) {
-  return a.teacher_lse ? y * inv_h - t.whole : (y - t.sum) * inv_h - t.whole;
-}
-__device__ __forceinline__ float term(float q, float log_q, float log_p) {
-  return q > 0.f || q != q ? q * (log_q - log_p) : 0.f;
+
+// The loss's sum over the list; none for a list of q = 0, whose maximum may be as far away as it likes.
+__device__ __forceinline__ float list_loss(const Sums& t, float lse_against_m) {
+  return t.sum == 0.f ? 0.f : fmaf(t.sum, lse_against_m, t.t);
 }
 
-// Whether entry k is its class's first, and the sum of q over the class's entries.
-__device__ __forceinline__ bool look_up(const List& l, int K, int k, int c, float& q_all) {
+// Whether entry k, of class c, is its class's first, and the sum of q over the class's entries, q its own.
+__device__ __forceinline__ bool look_up(const List& l, const Sums& t, int K, int k, int c, float q, float inv_h,
+                                        float& q_all) {
+  int same = 0;
   bool first = c >= 0;
-  q_all = 0.f;
   for (int i = 0; i < K; i += 4) {  // past K: no entries
     const int4 o = *reinterpret_cast<const int4*>(&l.cls[i]);
-    if (o.x == c) first &= i >= k, q_all += l.q[i];
-    if (o.y == c) first &= i + 1 >= k, q_all += l.q[i + 1];
-    if (o.z == c) first &= i + 2 >= k, q_all += l.q[i + 2];
-    if (o.w == c) first &= i + 3 >= k, q_all += l.q[i + 3];
+    same += (o.x == c) + (o.y == c) + (o.z == c) + (o.w == c);
+    first &= !((o.x == c && i < k) || (o.y == c && i + 1 < k) || (o.z == c && i + 2 < k) || (o.w == c && i + 3 < k));
+  }
+  q_all = q;
+  if (c >= 0 && same > 1) {
+    q_all = 0.f;
+    for (int i = 0; i < K; ++i)
+      if (l.cls[i] == c) q_all += expf(log_q_of(t, l.y[i], inv_h));
   }
   return first;
 }
@@ -167,7 +187,7 @@ __device__ __forceinline__ float block_add(float s, float* part) {
 
 // One block on row r, whose list is complete in shared memory.
 template <typename T>
-__device__ __noinline__ void slow_row(const DistillArgs& a, int r, const Job& j, List& l, float q_sum) {
+__device__ __noinline__ void slow_row(const DistillArgs& a, int r, const Job& j, List& l, const Sums& t) {
   __shared__ float part[kRowThreads / 32];
   const int tid = threadIdx.x, nt = blockDim.x;
   const T* const x = row_of<T>(a.logits, j.b, j.t);
@@ -199,22 +219,16 @@ __device__ __noinline__ void slow_row(const DistillArgs& a, int r, const Job& j,
     if (v != -INFINITY && listed(c) < 0) s += exp2_fast((v - m_r) * f);
   }
   const float s_r = block_add(s, part);
-  m = kLowest;
-  for (int k = tid; k < a.K; k += nt)
-    if (l.cls[k] >= 0) m = fmaxf(m, l.x[k]);
-  m = fmaxf(block_max(m, part), m_r);
+  m = fmaxf(t.m, m_r);
   s = 0.f;
   for (int k = tid; k < a.K; k += nt)
     if (l.first[k]) s += exp2_fast((l.x[k] - m) * f);
   s = block_add(s, part) + s_r * exp2_fast((m_r - m) * f);
   const float ls = s > 0.f ? logf(s) : NAN;  // no finite logit: NaN
   const float log_pr = (m_r - m) * inv_h + (logf(s_r) - ls);
-  const float q_r = a.teacher_lse && !whole ? fmaxf(0.f, 1.f - q_sum) : 0.f;
-  float v = 0.f;
-  for (int k = tid; k < a.K; k += nt)
-    if (l.cls[k] >= 0) v += term(l.q[k], l.log_q[k], (l.x[k] - m) * inv_h - ls);
-  v = block_add(v, part);
-  if (tid == 0) put_loss(a, r, j.w * (v + term(q_r, logf(q_r), log_pr)), m * inv_h + ls);
+  const float q_r = a.teacher_lse && !whole ? fmaxf(0.f, 1.f - t.sum) : 0.f;
+  if (tid == 0)
+    put_loss(a, r, j.w * (list_loss(t, (m - t.m) * inv_h + ls) + term(q_r, logf(q_r), log_pr)), m * inv_h + ls);
   if (!a.dlogits.p) return;
   T* const g = row_out<T>(a.dlogits, j.b, j.t);
   const float wt = j.w * inv_h;
@@ -232,7 +246,7 @@ __global__ void __launch_bounds__(kRowThreads) k_distill_rows(const DistillArgs 
   const int r = blockIdx.x, tid = threadIdx.x;
   const Job j = job_of(a, r);
   const float inv_h = 1.f / a.temperature;
-  Teacher t{0.f, 0.f, false, false};
+  Sums t{};
   if (j.kept) {
     if (tid < kListMax) {
       Entry e{-1, 0.f, 0.f};
@@ -242,7 +256,7 @@ __global__ void __launch_bounds__(kRowThreads) k_distill_rows(const DistillArgs 
       l.x[tid] = e.x;
     }
     __syncthreads();
-    t = teacher_of(a, l, j, inv_h);
+    t = sums_of(a, l, j, inv_h);
     if (t.bad && tid == 0) flag_status(status, EOGP_ST_DEVICE);
   }
   if (!j.kept || t.bad || !t.some) {
@@ -252,15 +266,10 @@ __global__ void __launch_bounds__(kRowThreads) k_distill_rows(const DistillArgs 
     for (int c = tid; c < a.V; c += kRowThreads) g[c] = from_f32<T>(0.f);
     return;
   }
-  if (tid < a.K) {
-    const float lq = log_q_of(a, t, l.y[tid], inv_h);
-    l.log_q[tid] = lq;
-    l.q[tid] = l.cls[tid] < 0 ? 0.f : expf(lq);
-  }
+  if (tid < a.K)
+    l.first[tid] = look_up(l, t, a.K, tid, l.cls[tid], expf(log_q_of(t, l.y[tid], inv_h)), inv_h, l.q_all[tid]);
   __syncthreads();
-  if (tid < a.K) l.first[tid] = look_up(l, a.K, tid, l.cls[tid], l.q_all[tid]);
-  __syncthreads();
-  slow_row<T>(a, r, j, l, t.sum);
+  slow_row<T>(a, r, j, l, t);
 }
 
 // ----------------------------------------------------------------- slices of rows
@@ -341,7 +350,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) k_distill(const DistillArgs 
     ask_list(jn, raw);
     Entry nxt[kEach];
     T* const g = GRAD ? row_out<T>(a.dlogits, p.j.b, p.j.t) : nullptr;
-    Teacher t{0.f, 0.f, false, false};
+    Sums t{};
     if (p.j.kept) {  // in every CTA of the cluster
 #pragma unroll
       for (int u = 0; u < kEach; ++u) {
@@ -354,7 +363,7 @@ __global__ void __launch_bounds__(kSliceThreads, 2) k_distill(const DistillArgs 
       }
       commit_async();
       __syncthreads();  // the list; what is done with it comes while the slice's copies arrive
-      t = teacher_of(a, l, p.j, inv_h);
+      t = sums_of(a, l, p.j, inv_h);
       if (t.bad && tid == 0 && first_cta) flag_status(status, EOGP_ST_DEVICE);
     }
     if (!p.j.kept || t.bad || !t.some) {  // likewise
@@ -376,19 +385,9 @@ __global__ void __launch_bounds__(kSliceThreads, 2) k_distill(const DistillArgs 
 #pragma unroll
       for (int u = 0; u < kEach; ++u) {
         const int k = tid + u * nt;
-        if (k < a.K) {
-          const float lq = log_q_of(a, t, own[u].y, inv_h);
-          l.log_q[k] = lq;
-          l.q[k] = own[u].c < 0 ? 0.f : expf(lq);
-        }
-      }
-      __syncthreads();
-#pragma unroll
-      for (int u = 0; u < kEach; ++u) {
-        const int k = tid + u * nt;
         first[u] = false;
         if (k < a.K) {
-          first[u] = look_up(l, a.K, k, own[u].c, q_all[u]);
+          first[u] = look_up(l, t, a.K, k, own[u].c, expf(log_q_of(t, own[u].y, inv_h)), inv_h, q_all[u]);
           l.first[k] = first[u];
           l.q_all[k] = q_all[u];
         }
@@ -409,6 +408,15 @@ __global__ void __launch_bounds__(kSliceThreads, 2) k_distill(const DistillArgs 
           if (o.x == ce || o.y == ce || o.z == ce || o.w == ce) xe = -INFINITY;
         }
       }
+      // The list's own sum, against its maximum, and its classes.
+      float s_l = 0.f, classes = 0.f;
+      for (int i = lane; i < a.K; i += 32)
+        if (l.first[i]) {
+          s_l += exp2_fast((l.x[i] - t.m) * f);
+          classes += 1.f;
+        }
+      s_l = warp_sum(s_l);
+      const bool whole = warp_sum(classes) == static_cast<float>(a.V);
       __syncthreads();  // the listed classes' places
       MaxSum v{-INFINITY, 0.f};
       int k = tid;
@@ -453,33 +461,17 @@ __global__ void __launch_bounds__(kSliceThreads, 2) k_distill(const DistillArgs 
       }
       const bool is_near = fabsf(v.m) * f <= kNearLogit * kLog2e;
       if (!is_near) {  // in every CTA of the cluster
-        if (first_cta) slow_row<T>(a, r, p.j, l, t.sum);
+        if (first_cta) slow_row<T>(a, r, p.j, l, t);
         if (GRAD)
           for (int i = tid; i < next.n; i += nt) ask(next, i);
       } else {
-        // Logarithms to base 2 against c: of the listed classes' logits, their sum, and all.
-        const float c = ref(v.m, f);
-        float top = 0.f, classes = 0.f, s = 0.f;
-        for (int i = lane; i < a.K; i += 32)
-          if (l.cls[i] >= 0) top = fmaxf(top, fmaf(l.x[i], f, -c));
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        for (int i = lane; i < a.K; i += 32)
-          if (l.first[i]) {
-            s += exp2_fast(fmaf(l.x[i], f, -c) - top);
-            classes += 1.f;
-          }
-        s = warp_sum(s) + v.s * exp2_fast(-top);
-        const bool whole = warp_sum(classes) == static_cast<float>(a.V);
-        const float ls = top + log2f(s), log_r = log2f(v.s) - ls;
+        // Logarithms to base 2 against c: of the list's maximum, of the sum over all classes, of the remainder's share.
+        const float c = ref(v.m, f), to_list = fmaf(t.m, f, -c), top = fmaxf(0.f, to_list);
+        const float ls = top + log2f(s_l * exp2_fast(to_list - top) + v.s * exp2_fast(-top)), log_r = log2f(v.s) - ls;
         const float q_r = a.teacher_lse && !whole ? fmaxf(0.f, 1.f - t.sum) : 0.f;
-        if (tid < 32 && first_cta) {
-          float sum = 0.f;
-          for (int i = lane; i < a.K; i += 32)
-            if (l.cls[i] >= 0) sum += term(l.q[i], l.log_q[i], kLn2 * (fmaf(l.x[i], f, -c) - ls));
-          sum = warp_sum(sum);
-          if (lane == 0) put_loss(a, r, p.j.w * (sum + term(q_r, logf(q_r), kLn2 * log_r)), kLn2 * (c + ls));
-        }
+        if (tid == 0 && first_cta)
+          put_loss(a, r, p.j.w * (list_loss(t, kLn2 * (ls - to_list)) + term(q_r, logf(q_r), kLn2 * log_r)),
+                   kLn2 * (c + ls));
         if (GRAD) {
           const RowVecs<T> out(g, a.V);
           const float wt = p.j.w * inv_h, to = wt * (exp2_fast(log_r) - q_r) / v.s;
