@@ -306,16 +306,15 @@ struct DistillArgs {
 };
 cudaError_t launch_distill(const DistillArgs& a, bool bf16, unsigned* status, int num_sms, cudaStream_t st);
 
-// k_head_tc.cu: the three products of a piece of the counted positions, on bf16 operands.
+// k_head_tc.cu: the three products of a piece of the counted positions, on operands of bf16 parts.
 // An operand of several parts has 64 columns of each in turn (parts * 64 columns a block).
 struct HeadTc {
   const int* count;  // counted positions in all; the piece has those from `first` on, at most `piece`
   int first, piece, d, V;
   const void *A, *B;
   uint64_t inner_a, rows_a, lda, inner_b, rows_b, ldb;  // elements as they lie
-  int parts_a, parts_b;
-  int pairs;           // products of parts that are summed,
-  uint32_t pair_list;  // four bits each: part of A | part of B << 2
+  int parts_a, parts_b;  // as they lie: 1 or 2 of A with 1 of B, or 3 and 3 (k_head_tc: PARTS)
+  int pairs;             // parts of an A of two that are summed over; else 1
   int bn;              // columns of a tile
   int run;             // steps of 64 (times pairs) that one accumulator sums
   // logits: z (NULL: not kept) [piece x ldz], -inf beyond V; (maximum, sum) of each row's half tiles

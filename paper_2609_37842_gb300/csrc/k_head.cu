@@ -26,21 +26,21 @@ constexpr size_t kPieceBytes = size_t(4) << 30;  // logits of a piece
 size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
 long long up(long long x, long long a) { return (x + a - 1) / a * a; }
 
-// Where everything lies in the workspace, and how the products are cut. bf16 only: from `W` on.
+// Where everything lies in the workspace, and how the products are cut.
 struct Plan {
   int find_blocks, per_block;  // blocks of the search, positions of each
+  bool few;                    // positions are found and gathered in one launch
   int piece, pieces;           // rows of a piece, most pieces
-  int ldz, ldx, ldw;           // row strides of the logits, of the gathered rows and of the matrix
-  int parts;                   // bf16 parts of D that are used
+  int ldz, ldx, ldw;           // row strides of the logits, of the gathered rows and of the matrix (bf16 elements)
+  int parts;                   // bf16 parts of D
   int bn_z, bn_d;              // columns of a tile of the logits, of dx and dW
   int ld_slab;
-  bool few;  // positions are found and gathered in one launch
   size_t slab_bytes;
-  size_t counts, idx, target, w, x, z, acc, W, part, zt, row, slabs, total;
+  size_t counts, idx, target, w, x, z, D, acc, W, part, zt, row, slabs, total;
 };
 
 bool w_fits(const HeadArgs& a) {
-  return reinterpret_cast<uintptr_t>(a.weight) % 16 == 0 &&
+  return a.bf16 && reinterpret_cast<uintptr_t>(a.weight) % 16 == 0 &&
          (a.V == 1 || (a.ld_weight % 8 == 0 && a.ld_weight >= a.d));
 }
 
@@ -54,16 +54,14 @@ Plan plan_of(const HeadArgs& a) {
   p.per_block = static_cast<int>(each * kFindThreads);
   p.find_blocks = static_cast<int>((tiles + each - 1) / each);
   p.ldz = static_cast<int>(up(a.V, 64));
-  p.ldx = static_cast<int>(up(a.d, 8));
-  p.parts = a.bf16 ? a.dweight && !a.grad_bf16 ? 2 : 1 : 0;
-  // A row of a piece: logits, or the gathered row and the sums of its half tiles.
-  const size_t row_bytes = grad || !a.bf16 ? static_cast<size_t>(p.ldz) * 4
-                                           : static_cast<size_t>(p.ldx) * 2 + p.ldz / 64 * 16;
+  p.ldx = p.ldw = static_cast<int>(a.bf16 ? up(a.d, 8) : up(a.d, 64) * 3);
+  p.parts = !a.bf16 ? 3 : a.dweight && !a.grad_bf16 ? 2 : 1;
+  // A row of a piece: logits (and D, where it is not in their place), or the sums of its half tiles; and the gathered row.
+  const size_t row_bytes = static_cast<size_t>(p.ldx) * 2 + (grad ? static_cast<size_t>(p.ldz) * (a.bf16 ? 4 : 10) : p.ldz / 64 * 16);
   const long long most = std::max<long long>(256, static_cast<long long>(kPieceBytes / row_bytes) / 256 * 256);
   p.pieces = static_cast<int>((M + most - 1) / most);
   p.piece = static_cast<int>(std::min(most, up((M + p.pieces - 1) / p.pieces, 256)));
   p.few = p.pieces == 1 && M <= kFewRows;
-  const int es = a.bf16 ? 2 : 4;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
@@ -74,30 +72,29 @@ Plan plan_of(const HeadArgs& a) {
   p.idx = take(M * 4);
   p.target = take(M * 4);
   p.w = take(M * 4);
-  p.x = take(static_cast<size_t>(p.piece) * p.ldx * es);
-  if (grad || !a.bf16) p.z = take(static_cast<size_t>(p.piece) * p.ldz * 4);
-  if (a.dweight && a.bf16 && a.grad_bf16 && p.pieces > 1) p.acc = take(static_cast<size_t>(a.V) * a.d * 4);
-  if (a.bf16) {
-    p.ldw = static_cast<int>(up(a.d, 8));
-    if (!w_fits(a)) p.W = take(static_cast<size_t>(a.V) * p.ldw * 2);
-    // Columns of a tile of the logits: the widest, but for few tiles those that 76 pairs share out best.
-    const long long mt = (std::min<long long>(M, p.piece) + 255) / 256;
-    p.bn_z = 256;
-    if (mt * ((a.V + 255) / 256) < 4 * 76)
-      for (int bn = 128; bn >= 64; bn /= 2)
-        if ((mt * ((a.V + bn - 1) / bn) + 75) / 76 * bn * 10 < (mt * ((a.V + p.bn_z - 1) / p.bn_z) + 75) / 76 * p.bn_z * 9)
-          p.bn_z = bn;
-    p.bn_d = up(a.d, 128) * 1.15 < up(a.d, 256) ? 128 : 256;
-    p.part = take(static_cast<size_t>((a.V + p.bn_z - 1) / p.bn_z) * 2 * p.piece * 8);
-    p.zt = take(static_cast<size_t>(p.piece) * 4);
-    p.row = take(static_cast<size_t>(p.piece) * 8);
-    if (grad) {
-      p.ld_slab = static_cast<int>(up(a.d, 8));
-      // Room for split sums: as many as there may be, half a GB at most.
-      const size_t most_rows = std::max<size_t>(a.dx.p ? p.piece : 0, a.dweight ? a.V : 0);
-      p.slab_bytes = std::min<size_t>(kSlabBytes, most_rows * p.ld_slab * 4 * kMostSplits);
-      p.slabs = take(p.slab_bytes);
-    }
+  p.x = take(static_cast<size_t>(p.piece) * p.ldx * 2);
+  if (!w_fits(a)) p.W = take(static_cast<size_t>(a.V) * p.ldw * 2);
+  // Columns of a tile of the logits: the widest, but for few tiles those that 76 pairs share out best. fp32: two
+  // accumulators of 128.
+  const long long mt = (std::min<long long>(M, p.piece) + 255) / 256;
+  p.bn_z = a.bf16 ? 256 : 128;
+  if (mt * ((a.V + 255) / 256) < 4 * 76)
+    for (int bn = 128; bn >= 64; bn /= 2)
+      if ((mt * ((a.V + bn - 1) / bn) + 75) / 76 * bn * 10 < (mt * ((a.V + p.bn_z - 1) / p.bn_z) + 75) / 76 * p.bn_z * 9)
+        p.bn_z = bn;
+  p.bn_d = !a.bf16 || up(a.d, 128) * 1.15 < up(a.d, 256) ? 128 : 256;
+  p.part = take(static_cast<size_t>((a.V + p.bn_z - 1) / p.bn_z) * 2 * p.piece * 8);
+  p.zt = take(static_cast<size_t>(p.piece) * 4);
+  p.row = take(static_cast<size_t>(p.piece) * 8);
+  if (grad) {
+    p.z = take(static_cast<size_t>(p.piece) * p.ldz * 4);
+    if (!a.bf16) p.D = take(static_cast<size_t>(p.piece) * p.ldz * 6);
+    if (a.dweight && a.grad_bf16 && p.pieces > 1) p.acc = take(static_cast<size_t>(a.V) * a.d * 4);
+    p.ld_slab = static_cast<int>(up(a.d, 8));
+    // Room for split sums: as many as there may be, half a GB at most.
+    const size_t most_rows = std::max<size_t>(a.dx.p ? p.piece : 0, a.dweight ? a.V : 0);
+    p.slab_bytes = std::min<size_t>(kSlabBytes, most_rows * p.ld_slab * 4 * kMostSplits);
+    p.slabs = take(p.slab_bytes);
   }
   p.total = at;
   return p;
@@ -190,21 +187,53 @@ __global__ void __launch_bounds__(256) k_head_zero(const HeadArgs a, int M) {
   }
 }
 
-// Row i of the gathered ones by a warp: x (NULL: zeros), and zeros from d to ldx.
-template <typename T>
-__device__ __forceinline__ void put_row(const T* x, int d, int ldx, bool vec, T* o) {
-  constexpr int N = 16 / sizeof(T);
-  const int lane = threadIdx.x & 31, nv = vec && x ? d / N : 0;
+// fp32 as the sum of three bf16, exactly: 8 bits of the mantissa each, the first two cut off. What is not finite
+// is its first part alone.
+__device__ __forceinline__ void split3(float v, bf16 (&p)[3]) {
+  if (!(fabsf(v) <= 3.402823466e38f)) {
+    p[0] = from_f32<bf16>(v);
+    p[1] = p[2] = from_f32<bf16>(0.f);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const float top = k < 2 ? __uint_as_float(__float_as_uint(v) & 0xffff0000u) : v;
+    p[k] = from_f32<bf16>(top);
+    v -= top;
+  }
+}
+// Place of part k of column c in a row of three parts.
+__device__ __forceinline__ int place3(int c, int k) { return (c >> 6) * 192 + k * 64 + (c & 63); }
+
+// A row as the products read it, by a warp: x (NULL: zeros) and zeros from d on; fp32 in three parts.
+__device__ __forceinline__ void put_row(const bf16* x, int d, int ldx, bool vec, bf16* o) {
+  const int lane = threadIdx.x & 31, nv = vec && x ? d / 8 : 0;
 #pragma unroll 4
   for (int c = lane; c < nv; c += 32)
-    *reinterpret_cast<uint4*>(o + c * N) = __ldcs(reinterpret_cast<const uint4*>(x) + c);
-  for (int c = nv * N + lane; c < ldx; c += 32) o[c] = x && c < d ? x[c] : from_f32<T>(0.f);
+    *reinterpret_cast<uint4*>(o + c * 8) = __ldcs(reinterpret_cast<const uint4*>(x) + c);
+  for (int c = nv * 8 + lane; c < ldx; c += 32) o[c] = x && c < d ? x[c] : from_f32<bf16>(0.f);
+}
+__device__ __forceinline__ void put_row(const float* x, int d, int ldx, bool, bf16* o) {
+  // Two columns a lane: 64 at a time, a block of each part.
+  const int lane = threadIdx.x & 31;
+#pragma unroll 4
+  for (int c = lane * 2; c < ldx / 3; c += 64) {
+    bf16 p[3] = {}, q[3] = {};
+    if (x && c < d) split3(x[c], p);
+    if (x && c + 1 < d) split3(x[c + 1], q);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      __nv_bfloat162 v;
+      v.x = p[k], v.y = q[k];
+      *reinterpret_cast<__nv_bfloat162*>(o + place3(c, k)) = v;
+    }
+  }
 }
 
 // Rows first .. of the counted positions, dense; zeros up to the next multiple of 64.
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_gather(const HeadArgs a, const int* counts, const int* idx, int first,
-                                                     int piece, int ldx, bool vec, T* out) {
+                                                     int piece, int ldx, bool vec, bf16* out) {
   const int n = min(piece, counts[kFindBlocks] - first), n64 = (max(n, 0) + 63) & ~63;
   for (int i = blockIdx.x * 8 + (threadIdx.x >> 5); i < n64; i += gridDim.x * 8) {
     const T* x = nullptr;
@@ -213,7 +242,7 @@ __global__ void __launch_bounds__(256) k_head_gather(const HeadArgs a, const int
       locate(a.rs, idx[first + i], b, t);
       x = row_of<T>(a.x, b, t);
     }
-    put_row<T>(x, a.d, ldx, vec, out + static_cast<size_t>(i) * ldx);
+    put_row(x, a.d, ldx, vec, out + static_cast<size_t>(i) * ldx);
   }
 }
 
@@ -221,7 +250,7 @@ __global__ void __launch_bounds__(256) k_head_gather(const HeadArgs a, const int
 // them, and each of its warps then has one.
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_few(const HeadArgs a, int M, int* counts, int* idx, int* target, float* w,
-                                                  int ldx, bool vec, T* out, unsigned* status) {
+                                                  int ldx, bool vec, bf16* out, unsigned* status) {
   __shared__ unsigned kept[kFewRows / 32];
   const int tid = threadIdx.x, lane = tid & 31, r = blockIdx.x * 8 + (tid >> 5);
 #pragma unroll
@@ -244,7 +273,7 @@ __global__ void __launch_bounds__(256) k_head_few(const HeadArgs a, int M, int* 
   }
   if (r == 0 && lane == 0) counts[kFindBlocks] = n;
   for (int i = n + r; i < ((n + 63) & ~63); i += gridDim.x * 8)
-    put_row<T>(nullptr, a.d, ldx, vec, out + static_cast<size_t>(i) * ldx);
+    put_row(static_cast<const T*>(nullptr), a.d, ldx, vec, out + static_cast<size_t>(i) * ldx);
   if (r >= M) return;
   const Job j = job_of(a, r, status);
   int b, t;
@@ -255,7 +284,7 @@ __global__ void __launch_bounds__(256) k_head_few(const HeadArgs a, int M, int* 
       target[before] = j.target;
       w[before] = j.w;
     }
-    put_row<T>(row_of<T>(a.x, b, t), a.d, ldx, vec, out + static_cast<size_t>(before) * ldx);
+    put_row(row_of<T>(a.x, b, t), a.d, ldx, vec, out + static_cast<size_t>(before) * ldx);
   } else {
     if (lane == 0) {
       a.loss[r] = 0.f;
@@ -268,137 +297,12 @@ __global__ void __launch_bounds__(256) k_head_few(const HeadArgs a, int M, int* 
   }
 }
 
-// ------------------------------------------------------------------ loss and D
-// One block on a row of logits: loss and lse, then D over them.
-__global__ void __launch_bounds__(512) k_head_rows(const HeadArgs a, const int* counts, const int* idx,
-                                                   const int* targets, const float* ws, int first, int piece, float* z,
-                                                   int ldz, bool grad) {
-  __shared__ float part[2][16];
-  const int n = min(piece, counts[kFindBlocks] - first), tid = threadIdx.x, i = blockIdx.x;
-  if (i >= n) return;
-  float* const x = z + static_cast<size_t>(i) * ldz;
-  const int target = targets[first + i], r = idx[first + i];
-  const float w = ws[first + i];
-  float m = -3.402823466e38f;
-  for (int c = tid; c < a.V; c += 512) m = fmaxf(m, x[c]);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if ((tid & 31) == 0) part[0][tid >> 5] = m;
-  __syncthreads();
-  m = part[0][0];
-  for (int k = 1; k < 16; ++k) m = fmaxf(m, part[0][k]);
-  float s = 0.f;
-  for (int c = tid; c < a.V; c += 512) s += exp2f((x[c] - m) * kLog2e);
-  s = block_sum<16>(s, part[1]);
-  if (tid == 0) {
-    const float ls = s > 0.f ? logf(s) : NAN;  // no finite logit: NaN
-    a.loss[r] = w * ((m - x[target]) + ls);
-    if (a.lse) a.lse[r] = m + ls;
-  }
-  if (!grad) return;
-  __syncthreads();
-  const float g = w * a.scale, inv = g / s;
-  for (int c = tid; c < ldz; c += 512)
-    x[c] = c < a.V ? exp2f((x[c] - m) * kLog2e) * inv - (c == target ? g : 0.f) : 0.f;
-}
-
-// ------------------------------------------------------------------ products
-// C[i][j] = alpha sum_k A(i, k) B(j, k) (+ add[i][j]), A(i, k) at A + i sai + k sak and
-// B likewise: 64 x 64 tiles, 4 x 4 outputs a thread, sums in fp32 in ascending order.
-template <typename TA, typename TB>
-struct Product {
-  const TA* A;
-  long long sai, sak;
-  const TB* B;
-  long long sbj, sbk;
-  int M, N, K;  // M or K: the piece's rows at most, then as many as there are
-  bool rows_m, rows_k;
-  float alpha;
-};
-
-// Where a product goes: rows of dx by position, or rows of an array, on top of what an
-// array of `add` holds.
-struct Out {
-  void* p;
-  long long ld;
-  bool bf16;
-  const void* add;  // NULL: nothing is added
-  long long ld_add;
-  bool add_bf16;
-};
-
-template <typename TA, typename TB>
-__global__ void __launch_bounds__(256) k_head_product(const Product<TA, TB> g, const HeadArgs a, const Out o,
-                                                      const int* counts, const int* idx, int first, bool to_dx) {
-  __shared__ float As[16][65], Bs[16][65];
-  const int n = max(0, counts[kFindBlocks] - first);
-  const int M = g.rows_m ? min(g.M, n) : g.M, K = g.rows_k ? min(g.K, n) : g.K;
-  const int nn = (g.N + 63) / 64;
-  const int m0 = static_cast<int>(blockIdx.x / nn) * 64, n0 = static_cast<int>(blockIdx.x % nn) * 64;
-  if (m0 >= M) return;
-  const int tid = threadIdx.x, ti = tid >> 4, tj = tid & 15;
-  float acc[4][4] = {};
-  for (int k0 = 0; k0 < K; k0 += 16) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      // neighbouring threads along whichever index is contiguous
-      const int q = tid + e * 256;
-      int i = g.sak == 1 ? q >> 4 : q & 63, k = g.sak == 1 ? q & 15 : q >> 6;
-      As[k][i] = m0 + i < M && k0 + k < K ? to_f32(g.A[(m0 + i) * g.sai + (k0 + k) * g.sak]) : 0.f;
-      i = g.sbk == 1 ? q >> 4 : q & 63, k = g.sbk == 1 ? q & 15 : q >> 6;
-      Bs[k][i] = n0 + i < g.N && k0 + k < K ? to_f32(g.B[(n0 + i) * g.sbj + (k0 + k) * g.sbk]) : 0.f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 16; ++k)
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) acc[u][v] = fmaf(As[k][ti + 16 * u], Bs[k][tj + 16 * v], acc[u][v]);
-    __syncthreads();
-  }
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int i = m0 + ti + 16 * u;
-    if (i >= M) continue;
-    long long row = i * o.ld;
-    if (to_dx) {
-      int b, t;
-      locate(a.rs, idx[first + i], b, t);
-      row = b * a.dx.bs + t * a.dx.ld;
-    }
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const int j = n0 + tj + 16 * v;
-      if (j >= g.N) continue;
-      float x = g.alpha * acc[u][v];
-      if (o.add) {
-        const long long at = i * o.ld_add + j;
-        x += o.add_bf16 ? to_f32(static_cast<const bf16*>(o.add)[at]) : static_cast<const float*>(o.add)[at];
-      }
-      if (o.bf16)
-        static_cast<bf16*>(o.p)[row + j] = from_f32<bf16>(x);
-      else
-        static_cast<float*>(o.p)[row + j] = x;
-    }
-  }
-}
-
-template <typename TA, typename TB>
-cudaError_t product(const Product<TA, TB>& g, const HeadArgs& a, const Out& o, const int* counts, const int* idx,
-                    int first, bool to_dx, cudaStream_t st) {
-  const long long tiles = static_cast<long long>((g.M + 63) / 64) * ((g.N + 63) / 64);
-  if (tiles > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
-  k_head_product<TA, TB><<<static_cast<unsigned>(tiles), 256, 0, st>>>(g, a, o, counts, idx, first, to_dx);
-  return cudaGetLastError();
-}
-
-// ------------------------------------------------------- between the tensor products
-// The matrix with rows that TMA can read.
-__global__ void __launch_bounds__(256) k_head_matrix(const bf16* W, long long ld, int V, int d, bf16* out, int ldo) {
-  const int lane = threadIdx.x & 31;
+// ------------------------------------------------------------ between the products
+// The matrix with rows that TMA can read; fp32 in three parts.
+template <typename T>
+__global__ void __launch_bounds__(256) k_head_matrix(const T* W, long long ld, int V, int d, bf16* out, int ldo) {
   for (long long r = blockIdx.x * 8 + (threadIdx.x >> 5); r < V; r += gridDim.x * 8)
-    for (int c = lane; c < d; c += 32) out[r * ldo + c] = W[r * ld + c];
+    put_row(W + r * ld, d, ldo, false, out + r * ldo);
 }
 
 // 32 rows a block: the (maximum, sum) pairs of a row's half tiles joined to its loss and lse,
@@ -437,12 +341,13 @@ __global__ void __launch_bounds__(1024) k_head_join(const HeadArgs a, const int*
 
 // D over the logits, in place: the 256 bytes of 64 columns become the 64 first bf16 parts and, with PARTS = 2,
 // the 64 second ones. Eight columns a thread, eight threads on such a block, which read it before one writes.
+// With PARTS = 3 (fp32) the parts go to an array of their own.
 // Zeros in the rows up to the next multiple of 64, which the sum over rows runs over. (4,096 x 50,000 to two parts: 255 us,
 // 6.4 TB/s.)
 template <int PARTS>
 __global__ void __launch_bounds__(256) k_head_d(const HeadArgs a, const int* counts, const int* targets,
                                                 const float* ws, int first, int piece, float* z, int ldz,
-                                                const float2* row) {
+                                                const float2* row, bf16* D) {
   const int n = min(piece, counts[kFindBlocks] - first), n64 = (max(n, 0) + 63) & ~63;
   for (int i = blockIdx.x; i < n64; i += gridDim.x) {
     float* const x = z + static_cast<size_t>(i) * ldz;
@@ -472,7 +377,20 @@ __global__ void __launch_bounds__(256) k_head_d(const HeadArgs a, const int* cou
       }
       __syncwarp();
       if (c >= ldz) continue;
-      bf16* const o = reinterpret_cast<bf16*>(x + (c & ~63)) + (c & 63);
+      bf16* const o = PARTS == 3 ? D + (static_cast<size_t>(i) * ldz + (c & ~63)) * 3 + (c & 63)
+                                 : reinterpret_cast<bf16*>(x + (c & ~63)) + (c & 63);
+      if (PARTS == 3) {
+        __align__(16) bf16 w[3][8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          bf16 q[3];
+          split3(v.get(e), q);
+          w[0][e] = q[0], w[1][e] = q[1], w[2][e] = q[2];
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(o + 64 * p) = *reinterpret_cast<const uint4*>(w[p]);
+        continue;
+      }
 #pragma unroll
       for (int p = 0; p < PARTS; ++p) {
         const Raw<bf16, 8> r = pack_raw<bf16, 8>(v);
@@ -542,7 +460,7 @@ bool vec_rows(const RowView& v, int es) {
 
 // The counted positions of the batch, zeros for the others, and, where there are few, their rows at `x`.
 template <typename T>
-cudaError_t find(const HeadArgs& a, const Plan& p, uint8_t* ws, T* x, bool vec, unsigned* status, int num_sms,
+cudaError_t find(const HeadArgs& a, const Plan& p, uint8_t* ws, bf16* x, bool vec, unsigned* status, int num_sms,
                  cudaStream_t st) {
   const int M = static_cast<int>(a.rs.rows());
   int* const counts = reinterpret_cast<int*>(ws + p.counts);
@@ -571,7 +489,8 @@ bool wide_rows(const void* p, long long bs, long long ld, int es) {
   return reinterpret_cast<uintptr_t>(p) % 32 == 0 && bs * es % 32 == 0 && ld * es % 32 == 0;
 }
 
-cudaError_t run_bf16(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, cudaStream_t st) {
+template <typename T>
+cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, cudaStream_t st) {
   const Plan p = plan_of(a);
   const int M = static_cast<int>(a.rs.rows());
   const bool grad = a.dx.p || a.dweight;
@@ -583,15 +502,17 @@ cudaError_t run_bf16(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_s
   float2* const row = reinterpret_cast<float2*>(ws + p.row);
   const bf16* W = static_cast<const bf16*>(a.weight);
   long long ldw = a.V == 1 ? p.ldw : a.ld_weight;
+  constexpr bool f32 = sizeof(T) == 4;
   if (!w_fits(a)) {
     bf16* const copy = reinterpret_cast<bf16*>(ws + p.W);
-    k_head_matrix<<<std::min((a.V + 7) / 8, num_sms * 8), 256, 0, st>>>(W, a.ld_weight, a.V, a.d, copy, p.ldw);
+    k_head_matrix<T><<<std::min((a.V + 7) / 8, num_sms * 8), 256, 0, st>>>(static_cast<const T*>(a.weight), a.ld_weight,
+                                                                           a.V, a.d, copy, p.ldw);
     TRY(cudaGetLastError());
     W = copy;
     ldw = p.ldw;
   }
-  const bool vec = vec_rows(a.x, 2);
-  TRY(find(a, p, ws, x, vec, status, num_sms, st));
+  const bool vec = vec_rows(a.x, sizeof(T));
+  TRY(find<T>(a, p, ws, x, vec, status, num_sms, st));
   HeadTc h{};
   h.count = counts + kFindBlocks;
   h.piece = p.piece;
@@ -605,47 +526,49 @@ cudaError_t run_bf16(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_s
   h.target = target;
   h.rs = a.rs;
   h.idx = idx;
-  h.parts_a = h.parts_b = h.pairs = 1;
+  h.parts_a = h.parts_b = f32 ? 3 : 1;
+  h.pairs = 1;
+  bf16* const D = f32 ? reinterpret_cast<bf16*>(ws + p.D) : reinterpret_cast<bf16*>(h.z);  // bf16: in the logits' place
   h.ld_slab = p.ld_slab;
   h.slabs = reinterpret_cast<float*>(ws + p.slabs);
   h.slab_bytes = p.slab_bytes;
   h.clusters = num_sms / 2;
   h.piece_rows = static_cast<int>(std::min<long long>(M, p.piece));
   h.rows_box = static_cast<int>(std::min<long long>(128, up(h.piece_rows, 8)));
-  const uint64_t ud = a.d, uv = a.V, rows = p.piece, dcols = static_cast<uint64_t>(p.ldz) * 2;  // D lies in the logits' place
+  const uint64_t xcols = f32 ? p.ldx : a.d, uv = a.V, rows = p.piece, dcols = static_cast<uint64_t>(p.ldz) * (f32 ? 3 : 2);
   for (int c = 0; c < p.pieces; ++c) {
     h.first = c * p.piece;
     if (!p.few)
-      k_head_gather<bf16><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, h.first, p.piece, p.ldx, vec, x);
+      k_head_gather<T><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, h.first, p.piece, p.ldx, vec, x);
     TRY(cudaGetLastError());
     HeadTc z = h;
-    z.A = x, z.inner_a = ud, z.rows_a = rows, z.lda = p.ldx;
-    z.B = W, z.inner_b = ud, z.rows_b = uv, z.ldb = ldw;
-    z.bn = p.bn_z, z.run = 16;
+    z.A = x, z.inner_a = xcols, z.rows_a = rows, z.lda = p.ldx;
+    z.B = W, z.inner_b = xcols, z.rows_b = uv, z.ldb = ldw;
+    z.bn = p.bn_z, z.run = f32 ? 8 : 16;
     TRY(launch_head_logits(z, status, st));
     k_head_join<<<(p.piece + 31) / 32, 1024, 0, st>>>(a, counts, idx, w, h.first, p.piece, h.part,
                                                       (a.V + p.bn_z - 1) / p.bn_z * 2, h.zt, grad ? row : nullptr);
     TRY(cudaGetLastError());
     if (!grad) continue;
-    auto d = p.parts == 2 ? k_head_d<2> : k_head_d<1>;
-    d<<<std::min(p.piece, num_sms * 8), 256, 0, st>>>(a, counts, target, w, h.first, p.piece, h.z, p.ldz, row);
+    auto d = f32 ? k_head_d<3> : p.parts == 2 ? k_head_d<2> : k_head_d<1>;
+    d<<<std::min(p.piece, num_sms * 8), 256, 0, st>>>(a, counts, target, w, h.first, p.piece, h.z, p.ldz, row, D);
     TRY(cudaGetLastError());
     if (a.dx.p) {
       HeadTc g = h;
-      g.A = h.z, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = 2;
-      g.B = W, g.inner_b = ud, g.rows_b = uv, g.ldb = ldw;
-      g.bn = p.bn_d, g.run = 64;
-      g.dx = a.dx, g.out_bf16 = true, g.wide = wide_rows(a.dx.p, a.dx.bs, a.dx.ld, 2);
+      g.A = D, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = f32 ? 3 : 2;
+      g.B = W, g.inner_b = xcols, g.rows_b = uv, g.ldb = ldw;
+      g.bn = p.bn_d, g.run = f32 ? 8 : 64;
+      g.dx = a.dx, g.out_bf16 = !f32, g.wide = wide_rows(a.dx.p, a.dx.bs, a.dx.ld, sizeof(T));
       TRY(launch_head_dx(g, status, st));
       k_head_slabs<<<num_sms * 8, 256, 0, st>>>(g, true);
       TRY(cudaGetLastError());
     }
     if (a.dweight) {
       HeadTc g = h;
-      g.A = h.z, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = 2;
-      g.B = x, g.inner_b = ud, g.rows_b = rows, g.ldb = p.ldx;
-      if (p.parts == 2) g.pairs = 2, g.pair_list = 0x10;  // D's parts with x
-      g.bn = p.bn_d, g.run = a.grad_bf16 ? 64 : 16;
+      g.A = D, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = f32 ? 3 : 2;
+      g.B = x, g.inner_b = xcols, g.rows_b = rows, g.ldb = p.ldx;
+      if (p.parts == 2) g.pairs = 2;
+      g.bn = p.bn_d, g.run = f32 ? 8 : a.grad_bf16 ? 64 : 16;
       // Sums of several pieces stay in fp32, in dweight itself or beside it; the last piece that has rows
       // ends them, and those after it do nothing.
       g.out = a.dweight, g.ld_out = a.ld_dweight, g.out_bf16 = a.grad_bf16;
@@ -660,53 +583,6 @@ cudaError_t run_bf16(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_s
       TRY(launch_head_dw(g, status, st));
       k_head_slabs<<<num_sms * 8, 256, 0, st>>>(g, false);
       TRY(cudaGetLastError());
-    }
-  }
-  return cudaSuccess;
-}
-
-cudaError_t run_f32(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, cudaStream_t st) {
-  const Plan p = plan_of(a);
-  const int M = static_cast<int>(a.rs.rows());
-  int* const counts = reinterpret_cast<int*>(ws + p.counts);
-  int* const idx = reinterpret_cast<int*>(ws + p.idx);
-  int* const target = reinterpret_cast<int*>(ws + p.target);
-  float* const w = reinterpret_cast<float*>(ws + p.w);
-  float* const x = reinterpret_cast<float*>(ws + p.x);
-  float* const z = reinterpret_cast<float*>(ws + p.z);
-  const float* const W = static_cast<const float*>(a.weight);
-  const bool grad = a.dx.p || a.dweight, vec = vec_rows(a.x, 4);
-  TRY(find(a, p, ws, x, vec, status, num_sms, st));
-  for (int c = 0; c < p.pieces; ++c) {
-    const int first = c * p.piece;
-    if (!p.few)
-      k_head_gather<float><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, first, p.piece, p.ldx, vec, x);
-    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
-    const Out logits{z, p.ldz, false, nullptr, 0, false};
-    if (cudaError_t e = product(Product<float, float>{x, p.ldx, 1, W, a.ld_weight, 1, p.piece, a.V, a.d, true, false, a.scale},
-                                a, logits, counts, idx, first, false, st);
-        e != cudaSuccess)
-      return e;
-    k_head_rows<<<p.piece, 512, 0, st>>>(a, counts, idx, target, w, first, p.piece, z, p.ldz, grad);
-    if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
-    if (a.dx.p) {
-      const Out dx{const_cast<void*>(a.dx.p), 0, a.bf16, nullptr, 0, false};
-      if (cudaError_t e = product(Product<float, float>{z, p.ldz, 1, W, 1, a.ld_weight, p.piece, a.d, a.V, true, false,
-                                                    1.f},
-                                  a, dx, counts, idx, first, true, st);
-          e != cudaSuccess)
-        return e;
-    }
-    if (a.dweight) {
-      Out o{a.dweight, a.ld_dweight, false, nullptr, 0, false};
-      if (c > 0 || a.accumulate) {
-        o.add = a.dweight;
-        o.ld_add = a.ld_dweight;
-      }
-      if (cudaError_t e = product(Product<float, float>{z, 1, p.ldz, x, 1, p.ldx, a.V, a.d, p.piece, false, true, 1.f}, a,
-                                  o, counts, idx, first, false, st);
-          e != cudaSuccess)
-        return e;
     }
   }
   return cudaSuccess;
@@ -733,6 +609,6 @@ cudaError_t launch_head_loss(const HeadArgs& a, void* ws, unsigned* status, int 
       k_head_clear<float><<<blocks, 256, 0, st>>>(static_cast<float*>(a.dweight), a.ld_dweight, a.V, a.d);
     return cudaGetLastError();
   }
-  return a.bf16 ? run_bf16(a, static_cast<uint8_t*>(ws), status, num_sms, st)
-                : run_f32(a, static_cast<uint8_t*>(ws), status, num_sms, st);
+  return a.bf16 ? run<bf16>(a, static_cast<uint8_t*>(ws), status, num_sms, st)
+                : run<float>(a, static_cast<uint8_t*>(ws), status, num_sms, st);
 }

@@ -11,8 +11,10 @@
 // Tensor cores cut an accumulator off where they add to it: towards 0, by up to 2^-23 of it every
 // 16 products. So a long sum goes through several accumulators, `run` steps of 64 each, which are
 // added up in registers, rounded.
-// An operand may come in several bf16 parts, blocks of 64 columns of each in turn; a sum then
-// runs over the products of parts that are listed.
+// An operand may come in several bf16 parts, blocks of 64 columns of each in turn. D of two parts: its sum
+// runs over both parts' products. fp32 operands are sums of three parts of 8 bits each, exactly; of the
+// nine products of parts the six down to 2^-16 are formed (PARTS = 3), the first parts' in one accumulator and
+// the others', 2^-8 and less of it, in a second one, where cutting off costs nothing that counts.
 //
 // Warps (384 threads): 0 issues TMA, 1 owns tensor memory and issues MMAs, 4-11 end tiles; these
 // take over registers from the first four (168 x 384 = 56 x 128 + 224 x 256).
@@ -27,7 +29,7 @@ namespace {
 
 constexpr int kThreads = 384;
 constexpr int kMostStages = 16;
-constexpr size_t kRingBytes = 6 * 32768;
+constexpr size_t kRingBytes = 221184;  // 6 stages of 32 KB, 3 of 72 KB
 constexpr uint32_t kABytes = 128u * 64u * 2u;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
@@ -226,6 +228,7 @@ __device__ __forceinline__ void end_tile(const TcArgs& g, const Shape& s, const 
 }
 
 // An accumulator, in place of the sums or added to them.
+template <int PARTS>
 __device__ __forceinline__ void take_sums(uint32_t tmem, int bn, bool more, Sums& sums) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -234,6 +237,12 @@ __device__ __forceinline__ void take_sums(uint32_t tmem, int bn, bool more, Sums
       for (int c = 0; c < 32; c += 16) {
         float v[16];
         tmem_ld16(tmem + k * 32 + c, v);
+        if (PARTS == 3) {
+          float w[16];
+          tmem_ld16(tmem + bn + k * 32 + c, w);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[e] += w[e];
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) sums.v[k][c + e] = (more ? sums.v[k][c + e] : 0.f) + v[e];
       }
@@ -241,7 +250,7 @@ __device__ __forceinline__ void take_sums(uint32_t tmem, int bn, bool more, Sums
   }
 }
 
-template <int MODE>
+template <int MODE, int PARTS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     k_head_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const TcArgs g) {
   constexpr bool kAmn = MODE == kDw, kBmn = MODE != kLogits;
@@ -250,14 +259,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int half = g.h.bn / 2;  // columns of B in this CTA
-  const uint32_t stage_bytes = kABytes + static_cast<uint32_t>(half) * 128u;
+  const uint32_t b_bytes = static_cast<uint32_t>(half) * 128u, b_at = PARTS * kABytes;
+  const uint32_t stage_bytes = b_at + PARTS * b_bytes;
   const int stages = g.stages;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + static_cast<size_t>(stages) * stage_bytes);
   uint64_t* empty = full + stages;
   uint64_t* tfull = empty + stages;
   uint64_t* tempty = tfull + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
-  const uint32_t tcols = static_cast<uint32_t>(g.h.bn) * 2u;
+  const uint32_t buf_cols = static_cast<uint32_t>(g.h.bn) * (PARTS == 3 ? 2u : 1u), tcols = buf_cols * 2u;
   const int cl = blockIdx.x >> 1, ncl = gridDim.x >> 1;
 
   if (threadIdx.x == 0) {
@@ -288,7 +298,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       // Few rows: those of A that there are, and none of the second CTA's. What lies in the others' place
       // only reaches outputs that are not taken.
       const bool a_there = kAmn || static_cast<int>(rank) * 128 < g.h.piece_rows;
-      const uint32_t bytes = (kAmn ? kABytes : a_there ? g.h.rows_box * 128u : 0u) + static_cast<uint32_t>(half) * 128u;
+      const uint32_t bytes = PARTS * ((kAmn ? kABytes : a_there ? g.h.rows_box * 128u : 0u) + b_bytes);
       int rs = 0;
       uint32_t rph = 0;
       bool ok = true;
@@ -306,22 +316,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             ok = false;
             break;
           }
-          const int kb = i / g.h.pairs, c = (g.h.pair_list >> (4 * (i % g.h.pairs))) & 15;
-          const int pa = c & 3, pb = c >> 2;
+          // PARTS = 3: all parts in one stage; else the part of A whose turn it is.
+          const int kb = i / g.h.pairs, turn = i - kb * g.h.pairs;
           const uint32_t st = smem_u32(smem + static_cast<size_t>(s) * stage_bytes);
           const uint32_t fl = mapa_shared(smem_u32(&full[s]), 0);
           mbar_arrive_expect_tx_cluster(fl, bytes);
-          if (kAmn) {
-            tma_load_2d_pair(st, &tmA, (am / 64 * g.h.parts_a + pa) * 64, kb * 64, fl);
-            tma_load_2d_pair(st + 8192, &tmA, ((am / 64 + 1) * g.h.parts_a + pa) * 64, kb * 64, fl);
-          } else if (a_there) {
-            tma_load_2d_pair(st, &tmA, (kb * g.h.parts_a + pa) * 64, am, fl);
-          }
-          if (kBmn) {
-            for (int j = 0; j < half / 64; ++j)
-              tma_load_2d_pair(st + kABytes + j * 8192, &tmB, ((bn / 64 + j) * g.h.parts_b + pb) * 64, kb * 64, fl);
-          } else {
-            tma_load_2d_pair(st + kABytes, &tmB, (kb * g.h.parts_b + pb) * 64, bn, fl);
+#pragma unroll
+          for (int q = 0; q < PARTS; ++q) {
+            const int pa = PARTS == 3 ? q : turn;
+            const uint32_t a = st + q * kABytes, b = st + b_at + q * b_bytes;
+            if (kAmn) {
+              tma_load_2d_pair(a, &tmA, (am / 64 * g.h.parts_a + pa) * 64, kb * 64, fl);
+              tma_load_2d_pair(a + 8192, &tmA, ((am / 64 + 1) * g.h.parts_a + pa) * 64, kb * 64, fl);
+            } else if (a_there) {
+              tma_load_2d_pair(a, &tmA, (kb * g.h.parts_a + pa) * 64, am, fl);
+            }
+            if (kBmn) {
+              for (int j = 0; j < half / 64; ++j)
+                tma_load_2d_pair(b + j * 8192, &tmB, ((bn / 64 + j) * PARTS + q) * 64, kb * 64, fl);
+            } else {
+              tma_load_2d_pair(b, &tmB, (kb * PARTS + q) * 64, bn, fl);
+            }
           }
         }
       }
@@ -345,7 +360,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           }
           ++i;
           tc_fence_after();
-          const uint32_t d = tmem + buf * g.h.bn;
+          const uint32_t d = tmem + buf * buf_cols;
           for (int k = k0; k < k1; ++k) {
             const int s = rs;
             const uint32_t ph = rph;
@@ -360,10 +375,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             tc_fence_after();
             const uint32_t st = smem_u32(smem + static_cast<size_t>(s) * stage_bytes);
             const uint64_t a = kAmn ? sdesc_sw128(st, 8192, 1024) : sdesc_sw128(st, 16, 1024);
-            const uint64_t b = kBmn ? sdesc_sw128(st + kABytes, 8192, 1024) : sdesc_sw128(st + kABytes, 16, 1024);
+            const uint64_t b = kBmn ? sdesc_sw128(st + b_at, 8192, 1024) : sdesc_sw128(st + b_at, 16, 1024);
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-              tc_mma_f16_pair(d, a + ka * kk, b + kb_ * kk, idesc, (k != k0 || kk != 0) ? 1u : 0u);
+            for (int kk = 0; kk < 4; ++kk) {
+              const uint64_t ak = a + ka * kk, bk = b + kb_ * kk;
+              const uint32_t on = (k != k0 || kk != 0) ? 1u : 0u;
+              tc_mma_f16_pair(d, ak, bk, idesc, on);
+              if (PARTS == 3) {
+                const uint64_t a1 = kABytes >> 4, b1 = b_bytes >> 4;
+                const uint32_t rest = d + g.h.bn;
+                tc_mma_f16_pair(rest, ak, bk + b1, idesc, on);
+                tc_mma_f16_pair(rest, ak + a1, bk, idesc, 1u);
+                tc_mma_f16_pair(rest, ak + a1, bk + b1, idesc, 1u);
+                tc_mma_f16_pair(rest, ak, bk + 2 * b1, idesc, 1u);
+                tc_mma_f16_pair(rest, ak + 2 * a1, bk, idesc, 1u);
+              }
+            }
             tc_commit_pair_mc(&empty[s], 0x3);
           }
           tc_commit_pair_mc(&tfull[buf], 0x3);
@@ -396,7 +423,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           break;
         }
         tc_fence_after();
-        take_sums(lanes + buf * g.h.bn + side * half, g.h.bn, k0 > tl.i0, sums);
+        take_sums<PARTS>(lanes + buf * buf_cols + side * half, g.h.bn, k0 > tl.i0, sums);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_relaxed_cluster(mapa_shared(smem_u32(&tempty[buf]), 0));
@@ -418,9 +445,9 @@ int tmap(CUtensorMap* tm, const void* base, uint64_t inner, uint64_t rows, uint6
   return make_tmap(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int MODE>
-cudaError_t launch(const HeadTc& h, int most_m, int N, unsigned* status, cudaStream_t st) {
-  const size_t stage = kABytes + h.bn / 2 * 128u;
+template <int MODE, int PARTS>
+cudaError_t launch_parts(const HeadTc& h, int most_m, int N, unsigned* status, cudaStream_t st) {
+  const size_t stage = PARTS * (kABytes + h.bn / 2 * 128u);
   TcArgs g{h, (N + h.bn - 1) / h.bn, static_cast<int>(std::min<size_t>(kMostStages, kRingBytes / stage)), status};
   CUtensorMap ta, tb;
   const bool a_mn = MODE == kDw, b_mn = MODE != kLogits;
@@ -430,10 +457,16 @@ cudaError_t launch(const HeadTc& h, int most_m, int N, unsigned* status, cudaStr
   const long long tiles = static_cast<long long>((most_m + 255) / 256) * g.nN * (MODE == kLogits ? 1 : kMostSplits);
   if (tiles > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
   const size_t smem = 1024 + g.stages * stage + (2 * g.stages + 4) * 8 + 16;
-  if (cudaError_t e = allow_smem(k_head_tc<MODE>, smem); e != cudaSuccess) return e;
+  if (cudaError_t e = allow_smem(k_head_tc<MODE, PARTS>, smem); e != cudaSuccess) return e;
   const unsigned grid = 2u * static_cast<unsigned>(std::min<long long>(tiles, h.clusters));
-  k_head_tc<MODE><<<grid, kThreads, smem, st>>>(ta, tb, g);
+  k_head_tc<MODE, PARTS><<<grid, kThreads, smem, st>>>(ta, tb, g);
   return cudaGetLastError();
+}
+
+template <int MODE>
+cudaError_t launch(const HeadTc& h, int most_m, int N, unsigned* status, cudaStream_t st) {
+  return h.parts_b == 3 ? launch_parts<MODE, 3>(h, most_m, N, status, st)
+                        : launch_parts<MODE, 1>(h, most_m, N, status, st);
 }
 
 }  // namespace
