@@ -334,9 +334,10 @@ struct HeadTc {
   long long ld_out;
   const void* add;
   long long ld_add;
-  bool add_bf16, add_wide;
+  bool add_bf16;
   float* acc;  // [V x d]: takes the sums instead where more pieces follow (NULL: out does)
-  bool out_bf16, wide;  // type of dx or dW; whether its rows allow 32-byte stores (add_wide: such loads)
+  bool out_bf16;          // type of dx or dW
+  int out_vec, add_vec;   // bytes that rows of dx or dW, and of what is added, are aligned to (32 at most)
   // of split sums of dx or dW: [splits][rows][ld_slab], as many as fit (head_splits)
   float* slabs;
   size_t slab_bytes;

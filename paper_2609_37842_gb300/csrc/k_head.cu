@@ -74,14 +74,15 @@ Plan plan_of(const HeadArgs& a) {
   p.w = take(M * 4);
   p.x = take(static_cast<size_t>(p.piece) * p.ldx * 2);
   if (!w_fits(a)) p.W = take(static_cast<size_t>(a.V) * p.ldw * 2);
-  // Columns of a tile of the logits: the widest, but for few tiles those that 76 pairs share out best. fp32: two
-  // accumulators of 128.
+  // Columns of a tile of the logits: those with which 76 pairs have the least in their rounds, a tile costing
+  // about 24 columns more than it has (50,000 classes, one row: 3 rounds of 224 instead of 256). fp32: two
+  // accumulators of 128 at most.
   const long long mt = (std::min<long long>(M, p.piece) + 255) / 256;
-  p.bn_z = a.bf16 ? 256 : 128;
-  if (mt * ((a.V + 255) / 256) < 4 * 76)
-    for (int bn = 128; bn >= 64; bn /= 2)
-      if ((mt * ((a.V + bn - 1) / bn) + 75) / 76 * bn * 10 < (mt * ((a.V + p.bn_z - 1) / p.bn_z) + 75) / 76 * p.bn_z * 9)
-        p.bn_z = bn;
+  long long least = 0;
+  for (int bn = a.bf16 ? 256 : 128; bn >= 64; bn -= 32) {
+    const long long cost = (mt * ((a.V + bn - 1) / bn) + 75) / 76 * (bn + 24);
+    if (p.bn_z == 0 || cost < least) p.bn_z = bn, least = cost;
+  }
   p.bn_d = !a.bf16 || up(a.d, 128) * 1.15 < up(a.d, 256) ? 128 : 256;
   p.part = take(static_cast<size_t>((a.V + p.bn_z - 1) / p.bn_z) * 2 * p.piece * 8);
   p.zt = take(static_cast<size_t>(p.piece) * 4);
@@ -484,9 +485,11 @@ cudaError_t find(const HeadArgs& a, const Plan& p, uint8_t* ws, bf16* x, bool ve
   return cudaSuccess;
 }
 
-// Whether rows of `es`-byte elements allow 32-byte stores at multiples of 32 columns.
-bool wide_rows(const void* p, long long bs, long long ld, int es) {
-  return reinterpret_cast<uintptr_t>(p) % 32 == 0 && bs * es % 32 == 0 && ld * es % 32 == 0;
+// Bytes that rows of es-byte elements are aligned to, 32 at most.
+int row_align(const void* p, long long bs, long long ld, int es) {
+  int v = 32;
+  while (v > es && (reinterpret_cast<uintptr_t>(p) % v || bs * es % v || ld * es % v)) v /= 2;
+  return v;
 }
 
 template <typename T>
@@ -558,7 +561,7 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
       g.A = D, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = f32 ? 3 : 2;
       g.B = W, g.inner_b = xcols, g.rows_b = uv, g.ldb = ldw;
       g.bn = p.bn_d, g.run = f32 ? 8 : 64;
-      g.dx = a.dx, g.out_bf16 = !f32, g.wide = wide_rows(a.dx.p, a.dx.bs, a.dx.ld, sizeof(T));
+      g.dx = a.dx, g.out_bf16 = !f32, g.out_vec = row_align(a.dx.p, a.dx.bs, a.dx.ld, sizeof(T));
       TRY(launch_head_dx(g, status, st));
       k_head_slabs<<<num_sms * 8, 256, 0, st>>>(g, true);
       TRY(cudaGetLastError());
@@ -578,8 +581,8 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
       else if (a.accumulate)
         g.add = a.dweight, g.ld_add = a.ld_dweight, g.add_bf16 = a.grad_bf16;
       g.acc = c < p.pieces - 1 ? acc : nullptr;
-      g.wide = wide_rows(g.out, 0, g.ld_out, g.out_bf16 ? 2 : 4);
-      g.add_wide = wide_rows(g.add, 0, g.ld_add, g.add_bf16 ? 2 : 4);
+      g.out_vec = row_align(g.out, 0, g.ld_out, g.out_bf16 ? 2 : 4);
+      g.add_vec = row_align(g.add, 0, g.ld_add, g.add_bf16 ? 2 : 4);
       TRY(launch_head_dw(g, status, st));
       k_head_slabs<<<num_sms * 8, 256, 0, st>>>(g, false);
       TRY(cudaGetLastError());

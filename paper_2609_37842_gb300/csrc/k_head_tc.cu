@@ -92,15 +92,24 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return r;
 }
 
-// 32 outputs of one row from column c0 on, where the row's columns end at `n`; `wide`: 32-byte stores fit.
-__device__ __forceinline__ void put_f32(float* p, int left, bool wide, const float (&v)[32]) {
-  if (left >= 32 && wide) {
+// Up to 32 outputs of one row, of which `left` are stored; `vec`: bytes that its start is aligned to (32 at most).
+__device__ __forceinline__ void put_row(float* p, int left, int vec, const float (&v)[32]) {
+  if (left >= 32 && vec >= 8) {
+    if (vec == 32) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      uint32_t w[8];
+      for (int q = 0; q < 32; q += 8) {
+        uint32_t w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[8 * q + e]);
-      st_global_v8(p + 8 * q, w);
+        for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[q + e]);
+        st_global_v8(p + q, w);
+      }
+    } else if (vec == 16) {
+#pragma unroll
+      for (int q = 0; q < 32; q += 4)
+        *reinterpret_cast<float4*>(p + q) = make_float4(v[q], v[q + 1], v[q + 2], v[q + 3]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 32; q += 2) *reinterpret_cast<float2*>(p + q) = make_float2(v[q], v[q + 1]);
     }
   } else {
 #pragma unroll
@@ -108,14 +117,27 @@ __device__ __forceinline__ void put_f32(float* p, int left, bool wide, const flo
       if (e < left) p[e] = v[e];
   }
 }
-__device__ __forceinline__ void put_bf16(bf16* p, int left, bool wide, const float (&v)[32]) {
-  if (left >= 32 && wide) {
+__device__ __forceinline__ void put_row(bf16* p, int left, int vec, const float (&v)[32]) {
+  if (left >= 32 && vec >= 4) {
+    uint32_t w[16];
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      uint32_t w[8];
+    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(make_float2(v[2 * e], v[2 * e + 1]));
+    if (vec == 32) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = pack_bf16(make_float2(v[16 * q + 2 * e], v[16 * q + 2 * e + 1]));
-      st_global_v8(p + 16 * q, w);
+      for (int q = 0; q < 16; q += 8) {
+        const uint32_t u[8] = {w[q], w[q + 1], w[q + 2], w[q + 3], w[q + 4], w[q + 5], w[q + 6], w[q + 7]};
+        st_global_v8(p + 2 * q, u);
+      }
+    } else if (vec == 16) {
+#pragma unroll
+      for (int q = 0; q < 16; q += 4)
+        *reinterpret_cast<uint4*>(p + 2 * q) = make_uint4(w[q], w[q + 1], w[q + 2], w[q + 3]);
+    } else if (vec == 8) {
+#pragma unroll
+      for (int q = 0; q < 16; q += 2) *reinterpret_cast<uint2*>(p + 2 * q) = make_uint2(w[q], w[q + 1]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 16; ++q) *reinterpret_cast<uint32_t*>(p + 2 * q) = w[q];
     }
   } else {
 #pragma unroll
@@ -141,95 +163,117 @@ __device__ __forceinline__ void add_row(const T* p, int left, bool wide, float (
   }
 }
 
-// What the sums of a thread's row of its side's columns of the tile become.
+// What the sums of a thread's row of its side's columns of the tile become: logits, with the maximum and the sum of
+// exponentials of the row's columns here. Two warps a scheduler run this: the chains are kept short.
+__device__ __forceinline__ void end_logits(const TcArgs& g, const Shape& s, const Tile& t, int row, int side, int target,
+                                           Sums& sums) {
+  const HeadTc& h = g.h;
+  if (row >= s.M) return;
+  const int half = h.bn / 2, c0 = t.n0 + side * half, cols = min(half, h.V - c0);
+  float top[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float(&v)[32] = sums.v[k];
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+      const float2 z = mul2(make_float2(v[e], v[e + 1]), pair(h.scale));
+      v[e] = z.x, v[e + 1] = z.y;
+    }
+    if (cols < k * 32 + 32) {
+#pragma unroll
+      for (int e = 0; e < 32; ++e) v[e] = k * 32 + e < cols ? v[e] : -INFINITY;
+    }
+    if (h.z) {
+      float* const z = h.z + static_cast<size_t>(row) * h.ldz + c0 + k * 32;
+      const int left = min(half, h.ldz - c0) - k * 32;  // a multiple of 8
+#pragma unroll
+      for (int q = 0; q < 32; q += 8) {
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[q + e]);
+        if (q < left) st_global_v8(z + q, w);
+      }
+    }
+    float a[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a[e] = fmaxf(fmaxf(v[e], v[e + 8]), fmaxf(v[e + 16], v[e + 24]));
+    top[k] = fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(a[4], a[5]), fmaxf(a[6], a[7])));
+  }
+  if (static_cast<unsigned>(target - c0) < static_cast<unsigned>(half)) {
+    float zt = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 32; ++e) zt = target - c0 == k * 32 + e ? sums.v[k][e] : zt;
+    h.zt[row] = zt;
+  }
+  const float m = fmaxf(kLowest, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
+  float2 sum[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    sum[k] = pair(0.f);
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+      const float2 d = mul2(add2(make_float2(sums.v[k][e], sums.v[k][e + 1]), pair(-m)), pair(kLog2e));
+      sum[k] = add2(sum[k], make_float2(exp2_fast(d.x), exp2_fast(d.y)));
+    }
+  }
+  const float2 all = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+  h.part[static_cast<size_t>(t.n0 / h.bn * 2 + side) * h.piece + row] = make_float2(m, all.x + all.y);
+}
+
+// Or outputs of dx or dW, or of a slab of them.
 template <int MODE>
 __device__ __forceinline__ void end_tile(const TcArgs& g, const Shape& s, const Tile& t, int row, int side,
                                          Sums& sums) {
   const HeadTc& h = g.h;
-  const bool mine = row < s.M;
-  float m = kLowest, sum = 0.f;
-  int target = -1;
+  if (row >= s.M) return;
   bf16* out16 = nullptr;
   float* out32 = nullptr;
-  bool wide = true;
-  const int N = MODE == kLogits ? h.V : h.d;
-  if (MODE == kLogits) {
-    if (mine) target = h.target[h.first + row];
-    if (h.z) out32 = h.z + static_cast<size_t>(row) * h.ldz;
-  } else if (s.splits > 1) {
+  int vec = 32;
+  if (s.splits > 1) {
     out32 = h.slabs + (static_cast<size_t>(t.split) * s.M + row) * h.ld_slab;
   } else if (MODE == kDx) {
-    if (mine) {
-      int b, tt;
-      locate(h.rs, h.idx[h.first + row], b, tt);
-      if (h.out_bf16)
-        out16 = row_out<bf16>(h.dx, b, tt);
-      else
-        out32 = row_out<float>(h.dx, b, tt);
-    }
-    wide = h.wide;
+    int b, tt;
+    locate(h.rs, h.idx[h.first + row], b, tt);
+    if (h.out_bf16)
+      out16 = row_out<bf16>(h.dx, b, tt);
+    else
+      out32 = row_out<float>(h.dx, b, tt);
+    vec = h.out_vec;
   } else if (h.acc && !s.last) {
     out32 = h.acc + static_cast<size_t>(row) * h.d;
-    wide = h.d % 8 == 0;
+    vec = h.d % 8 == 0 ? 32 : 4;
   } else {
     const long long at = static_cast<long long>(row) * h.ld_out;
     if (h.out_bf16)
       out16 = static_cast<bf16*>(h.out) + at;
     else
       out32 = static_cast<float*>(h.out) + at;
-    wide = h.wide;
+    vec = h.out_vec;
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const int col = t.n0 + side * (h.bn / 2) + k * 32, left = N - col;
-    float(&v)[32] = sums.v[k];
-    if (k * 64 < h.bn && mine && left > 0) {
-      if (MODE == kLogits) {
-        float top = kLowest;
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          v[e] = e < left ? v[e] * h.scale : -INFINITY;
-          top = fmaxf(top, v[e]);
-        }
-        if (out32) put_f32(out32 + col, h.ldz - col, true, v);
-        if (static_cast<unsigned>(target - col) < 32u) {
-          float zt = 0.f;
-#pragma unroll
-          for (int e = 0; e < 32; ++e) zt = target - col == e ? v[e] : zt;
-          h.zt[row] = zt;
-        }
-        if (top > m) {
-          sum *= exp2_fast((m - top) * kLog2e);
-          m = top;
-        }
-        float2 part = pair(0.f);
-#pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-          const float2 d = mul2(add2(make_float2(v[e], v[e + 1]), pair(-m)), pair(kLog2e));
-          part = add2(part, make_float2(exp2_fast(d.x), exp2_fast(d.y)));
-        }
-        sum += part.x + part.y;
-      } else {
-        if (MODE == kDw && s.splits == 1 && h.add) {
-          const long long at = static_cast<long long>(row) * h.ld_add + col;
-          if (h.add_bf16)
-            add_row(static_cast<const bf16*>(h.add) + at, left, h.add_wide, v);
-          else
-            add_row(static_cast<const float*>(h.add) + at, left, h.add_wide, v);
-        }
-        if (out16)
-          put_bf16(out16 + col, left, wide, v);
+    const int col = t.n0 + side * (h.bn / 2) + k * 32, left = h.d - col;
+    if (k * 64 < h.bn && left > 0) {
+      float(&v)[32] = sums.v[k];
+      if (MODE == kDw && s.splits == 1 && h.add) {
+        const long long at = static_cast<long long>(row) * h.ld_add + col;
+        if (h.add_bf16)
+          add_row(static_cast<const bf16*>(h.add) + at, left, h.add_vec >= 16, v);
         else
-          put_f32(out32 + col, left, wide, v);
+          add_row(static_cast<const float*>(h.add) + at, left, h.add_vec >= 16, v);
       }
+      if (out16)
+        put_row(out16 + col, left, vec, v);
+      else
+        put_row(out32 + col, left, vec, v);
     }
   }
-  if (MODE == kLogits && mine) h.part[static_cast<size_t>(t.n0 / h.bn * 2 + side) * h.piece + row] = make_float2(m, sum);
 }
 
 // An accumulator, in place of the sums or added to them.
-template <int PARTS>
-__device__ __forceinline__ void take_sums(uint32_t tmem, int bn, bool more, Sums& sums) {
+__device__ __forceinline__ void add_sums(uint32_t tmem, int bn, Sums& sums) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     if (k * 64 < bn) {
@@ -237,17 +281,31 @@ __device__ __forceinline__ void take_sums(uint32_t tmem, int bn, bool more, Sums
       for (int c = 0; c < 32; c += 16) {
         float v[16];
         tmem_ld16(tmem + k * 32 + c, v);
-        if (PARTS == 3) {
-          float w[16];
-          tmem_ld16(tmem + bn + k * 32 + c, w);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) v[e] += w[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sums.v[k][c + e] = (more ? sums.v[k][c + e] : 0.f) + v[e];
+        for (int e = 0; e < 16; ++e) sums.v[k][c + e] += v[e];
       }
     }
   }
+}
+template <int PARTS>
+__device__ __forceinline__ void take_sums(uint32_t tmem, int bn, bool more, Sums& sums) {
+  if (more) {
+    add_sums(tmem, bn, sums);
+  } else {
+    // All loads are under way before the first is waited for. Columns past the side's (the allocation has them: 512
+    // for every width) are not used.
+    uint32_t r[4][32];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      tmem_ld32_issue(tmem + k * 32, r[k]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      tmem_wait_ld(r[k]);
+#pragma unroll
+      for (int e = 0; e < 32; ++e) sums.v[k][e] = __uint_as_float(r[k][e]);
+    }
+  }
+  if (PARTS == 3) add_sums(tmem + bn, bn, sums);
 }
 
 template <int MODE, int PARTS>
@@ -259,15 +317,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int half = g.h.bn / 2;  // columns of B in this CTA
-  const uint32_t b_bytes = static_cast<uint32_t>(half) * 128u, b_at = PARTS * kABytes;
+  const uint32_t a_bytes = kAmn ? kABytes : g.h.rows_box * 128u;
+  const uint32_t b_bytes = static_cast<uint32_t>(half) * 128u, b_at = PARTS * a_bytes;
   const uint32_t stage_bytes = b_at + PARTS * b_bytes;
   const int stages = g.stages;
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + static_cast<size_t>(stages) * stage_bytes);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + static_cast<size_t>(stages) * stage_bytes + (kABytes - a_bytes));
   uint64_t* empty = full + stages;
   uint64_t* tfull = empty + stages;
   uint64_t* tempty = tfull + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
-  const uint32_t buf_cols = static_cast<uint32_t>(g.h.bn) * (PARTS == 3 ? 2u : 1u), tcols = buf_cols * 2u;
+  const uint32_t buf_cols = static_cast<uint32_t>(g.h.bn) * (PARTS == 3 ? 2u : 1u);
+  constexpr uint32_t tcols = 512;
   const int cl = blockIdx.x >> 1, ncl = gridDim.x >> 1;
 
   if (threadIdx.x == 0) {
@@ -295,10 +355,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
   if (warp == 0) {
     if (lane == 0) {
-      // Few rows: those of A that there are, and none of the second CTA's. What lies in the others' place
-      // only reaches outputs that are not taken.
+      // Few rows: those of A that there are, and none of the second CTA's. What the MMAs read in the others' place
+      // (the stage's B, the next stage, at the ring's end the space behind it) only reaches outputs that are not taken.
       const bool a_there = kAmn || static_cast<int>(rank) * 128 < g.h.piece_rows;
-      const uint32_t bytes = PARTS * ((kAmn ? kABytes : a_there ? g.h.rows_box * 128u : 0u) + b_bytes);
+      const uint32_t bytes = PARTS * ((a_there ? a_bytes : 0u) + b_bytes);
       int rs = 0;
       uint32_t rph = 0;
       bool ok = true;
@@ -324,7 +384,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int q = 0; q < PARTS; ++q) {
             const int pa = PARTS == 3 ? q : turn;
-            const uint32_t a = st + q * kABytes, b = st + b_at + q * b_bytes;
+            const uint32_t a = st + q * a_bytes, b = st + b_at + q * b_bytes;
             if (kAmn) {
               tma_load_2d_pair(a, &tmA, (am / 64 * g.h.parts_a + pa) * 64, kb * 64, fl);
               tma_load_2d_pair(a + 8192, &tmA, ((am / 64 + 1) * g.h.parts_a + pa) * 64, kb * 64, fl);
@@ -382,7 +442,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               const uint32_t on = (k != k0 || kk != 0) ? 1u : 0u;
               tc_mma_f16_pair(d, ak, bk, idesc, on);
               if (PARTS == 3) {
-                const uint64_t a1 = kABytes >> 4, b1 = b_bytes >> 4;
+                const uint64_t a1 = a_bytes >> 4, b1 = b_bytes >> 4;
                 const uint32_t rest = d + g.h.bn;
                 tc_mma_f16_pair(rest, ak, bk + b1, idesc, on);
                 tc_mma_f16_pair(rest, ak + a1, bk, idesc, 1u);
@@ -408,11 +468,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const Tile tl = tile_of<MODE>(g, sh, t);
       const int row = tl.m0 + static_cast<int>(rank) * 128 + q * 32 + lane;
       const uint32_t lanes = tmem + (static_cast<uint32_t>(q * 32) << 16);
+      // Asked for before the accumulator is waited for.
+      const int target = MODE == kLogits && row < sh.M ? g.h.target[g.h.first + row] : -1;
       Sums sums;
+      if (tl.i0 >= tl.i1) {  // a sum without terms
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int e = 0; e < 32; ++e) sums.v[k][e] = 0.f;  // what a sum without terms is
+          for (int e = 0; e < 32; ++e) sums.v[k][e] = 0.f;
+      }
       for (int k0 = tl.i0; k0 < tl.i1; k0 += g.h.run, ++i) {
         const int buf = i & 1;
         uint32_t there = 1;
@@ -428,7 +492,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive_relaxed_cluster(mapa_shared(smem_u32(&tempty[buf]), 0));
       }
-      if (ok) end_tile<MODE>(g, sh, tl, row, side, sums);
+      if (!ok) break;
+      if constexpr (MODE == kLogits)
+        end_logits(g, sh, tl, row, side, target, sums);
+      else
+        end_tile<MODE>(g, sh, tl, row, side, sums);
     }
   }
   tc_fence_before();
@@ -447,8 +515,9 @@ int tmap(CUtensorMap* tm, const void* base, uint64_t inner, uint64_t rows, uint6
 
 template <int MODE, int PARTS>
 cudaError_t launch_parts(const HeadTc& h, int most_m, int N, unsigned* status, cudaStream_t st) {
-  const size_t stage = PARTS * (kABytes + h.bn / 2 * 128u);
-  TcArgs g{h, (N + h.bn - 1) / h.bn, static_cast<int>(std::min<size_t>(kMostStages, kRingBytes / stage)), status};
+  const size_t a_bytes = MODE == kDw ? kABytes : h.rows_box * 128u, stage = PARTS * (a_bytes + h.bn / 2 * 128u);
+  const size_t behind = kABytes - a_bytes;
+  TcArgs g{h, (N + h.bn - 1) / h.bn, static_cast<int>(std::min<size_t>(kMostStages, (kRingBytes - behind) / stage)), status};
   CUtensorMap ta, tb;
   const bool a_mn = MODE == kDw, b_mn = MODE != kLogits;
   if (tmap(&ta, h.A, h.inner_a, h.rows_a, h.lda, a_mn ? 64 : h.rows_box) ||
@@ -456,7 +525,7 @@ cudaError_t launch_parts(const HeadTc& h, int most_m, int N, unsigned* status, c
     return cudaErrorInvalidValue;
   const long long tiles = static_cast<long long>((most_m + 255) / 256) * g.nN * (MODE == kLogits ? 1 : kMostSplits);
   if (tiles > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
-  const size_t smem = 1024 + g.stages * stage + (2 * g.stages + 4) * 8 + 16;
+  const size_t smem = 1024 + g.stages * stage + behind + (2 * g.stages + 4) * 8 + 16;
   if (cudaError_t e = allow_smem(k_head_tc<MODE, PARTS>, smem); e != cudaSuccess) return e;
   const unsigned grid = 2u * static_cast<unsigned>(std::min<long long>(tiles, h.clusters));
   k_head_tc<MODE, PARTS><<<grid, kThreads, smem, st>>>(ta, tb, g);
