@@ -1,7 +1,7 @@
 """Example: attribute a small language model's answers to its training examples,
 from tokens to a ranking.
 
-    python -m paper_2609_37842_gb300.attribute_lm
+    python -m paper_2609_37842_gb300.attribute_lm [logits | head | distill]
 
 One pass of the model with this library's model ends (token embedding,
 normalisation, token loss, each with its gradient) and plain matrix products
@@ -13,7 +13,9 @@ example, which has to rank first among all of them.
 The model, tokens x of an example (padding beyond its length):
     h0 = table[x] + pos,  n1 = layernorm(h0),  u = n1 W1^T,  g = gelu(u),
     h1 = h0 + g W2^T,     n2 = rmsnorm(h1),    logits = n2 table^T,
-with the loss of the next token at every position but an example's last.
+with the loss of the next token at every position but an example's last: from the
+logits ("logits"), or without keeping them ("head"); or with the distance from a
+second model's top logits at every position ("distill").
 """
 from __future__ import annotations
 
@@ -51,21 +53,45 @@ def next_tokens(tokens, lengths):
     return targets.masked_fill_(last, -100)
 
 
-def backward_pass(model: Model, tokens, lengths):
-    """One forward and backward pass. Returns loss [B, T], the modules' (a, s) pairs, and the gradients: of the
-    table (over the batch), of the position table, and of the normalisations' weights for each example."""
+def forward(model: Model, tokens, lengths):
+    """The hidden states up to the output matrix: h0, n1, mean1, rstd1, u, g, h1, n2, rstd2."""
     import torch
-    V, (B, T) = model.table.shape[0], tokens.shape
     h0 = E.embed(tokens, model.table, pos=model.pos, lengths=lengths)
     n1, mean1, rstd1 = E.norm(h0, *model.norm1, lengths=lengths)
     u = n1 @ model.W1.T
     g = torch.nn.functional.gelu(u)
     h1 = h0 + g @ model.W2.T
     n2, _, rstd2 = E.norm(h1, model.norm2, kind=E.NORM_RMS, lengths=lengths)
-    logits = n2 @ model.table.T
-    loss, _, dlogits = E.cross_entropy(logits, next_tokens(tokens, lengths), lengths=lengths, dlogits=logits)
+    return h0, n1, mean1, rstd1, u, g, h1, n2, rstd2
 
-    dn2 = dlogits @ model.table
+
+def top_logits(model: Model, tokens, lengths, K: int):
+    """A teacher's K best classes of each position, their logits, and the log-sum over all its classes."""
+    import torch
+    logits = (forward(model, tokens, lengths)[7] @ model.table.T).float()
+    best, classes = logits.topk(K, -1)
+    return classes, best, torch.logsumexp(logits, -1)
+
+
+def backward_pass(model: Model, tokens, lengths, loss_from: str = "logits", teacher=None):
+    """One forward and backward pass. Returns loss [B, T], the modules' (a, s) pairs, and the gradients: of the
+    table (over the batch), of the position table, and of the normalisations' weights for each example.
+    `teacher`: top_logits of a second model, for loss_from = "distill"."""
+    import torch
+    V, (B, T) = model.table.shape[0], tokens.shape
+    h0, n1, mean1, rstd1, u, g, h1, n2, rstd2 = forward(model, tokens, lengths)
+    if loss_from == "head":
+        loss, _, dn2, dtable = E.head_loss(n2, model.table, next_tokens(tokens, lengths), lengths=lengths,
+                                           dtype=torch.float32)
+    else:
+        logits = n2 @ model.table.T
+        if loss_from == "distill":
+            classes, best, lse = teacher
+            loss, _, dlogits = E.distill(logits, classes, best, teacher_lse=lse, lengths=lengths, dlogits=logits)
+        else:
+            loss, _, dlogits = E.cross_entropy(logits, next_tokens(tokens, lengths), lengths=lengths, dlogits=logits)
+        dn2 = dlogits @ model.table
+        dtable = (dlogits.reshape(-1, V).T @ n2.reshape(-1, n2.shape[-1])).float()      # the head's share
     dh1, dnorm2, _ = E.norm_grad(dn2, h1, None, rstd2, model.norm2, kind=E.NORM_RMS, lengths=lengths,
                                  per_example=True, want_dbias=False)
     uf = u.float()
@@ -73,7 +99,6 @@ def backward_pass(model: Model, tokens, lengths):
     du = ((dh1 @ model.W2).float() * dgelu).to(u.dtype)
     dx, dw1, db1 = E.norm_grad(du @ model.W1, h0, mean1, rstd1, model.norm1[0], lengths=lengths, per_example=True)
     dh0 = dh1 + dx
-    dtable = (dlogits.reshape(-1, V).T @ n2.reshape(-1, n2.shape[-1])).float()      # the head's share
     E.embed_grad(tokens, dh0, V, lengths=lengths, dtable=dtable, accumulate=True)   # the embedding's
     positions = torch.arange(T, device=tokens.device).expand(B, T)
     dpos = E.embed_grad(positions, dh0, T, lengths=lengths)
@@ -111,7 +136,7 @@ def codes_of(fits, pairs, lengths, k: int):
 
 
 def run(V: int = 1000, B: int = 192, T: int = 40, d: int = 128, f: int = 256, m: int = 512, k: int = 128,
-        queries: int = 16, dtype=None, seed: int = 0):
+        queries: int = 16, dtype=None, seed: int = 0, loss_from: str = "logits"):
     """Stores B examples, queries with `queries` of them. Returns the queried rows' ranks (0 = first)."""
     import torch
     dtype = dtype or torch.bfloat16
@@ -120,12 +145,16 @@ def run(V: int = 1000, B: int = 192, T: int = 40, d: int = 128, f: int = 256, m:
     model = make_model(V, T, d, f, dtype, g)
     tokens = torch.randint(0, V, (B, T), generator=g, device="cuda")
     lengths = torch.randint(T // 4, T + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
-    _, pairs, _ = backward_pass(model, tokens, lengths)
+    teacher = None
+    if loss_from == "distill":
+        teacher = top_logits(make_model(V, T, d, f, dtype, g), tokens, lengths, 32)
+    _, pairs, _ = backward_pass(model, tokens, lengths, loss_from, teacher)
     fits = {name: fit_module(a, s, lengths, m, k) for name, (a, s) in pairs.items()}
     codes, scales = codes_of(fits, pairs, lengths, k)
 
     asked = torch.randperm(B, generator=g, device="cuda")[:queries]
-    _, qpairs, _ = backward_pass(model, tokens[asked], lengths[asked])
+    _, qpairs, _ = backward_pass(model, tokens[asked], lengths[asked], loss_from,
+                                 teacher and tuple(t[asked].contiguous() for t in teacher))
     qcodes, qscales = codes_of(fits, qpairs, lengths[asked], k)
     scores = E.score(codes, scales, [k] * len(pairs), E.SCORE_CODES, qcodes, qscales)
     E.sync_status()
@@ -134,5 +163,6 @@ def run(V: int = 1000, B: int = 192, T: int = 40, d: int = 128, f: int = 256, m:
 
 
 if __name__ == "__main__":
-    ranks = run()
+    import sys
+    ranks = run(loss_from=sys.argv[1] if len(sys.argv) > 1 else "logits")
     print(f"{len(ranks)} queries, each repeating a stored example: {sum(r == 0 for r in ranks)} rank it first")
