@@ -8,12 +8,22 @@ namespace eogp {
 
 constexpr int kMostSplits = 32;
 
+// The kernels of a call follow each other by programmatic launch: each is let in as soon as the one before has
+// begun everywhere, sets itself up, and waits here for that one's end. (511 tokens with gradient: nine launches.)
+__device__ __forceinline__ void after_previous() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // How many slabs the sums of `tiles` tiles of 256 rows are split into, `steps` 64-deep steps each, so that
 // the pairs of multiprocessors take about the same share, by a whole warp. Tiles are taken in rounds;
 // a round costs its steps and about 8 more (filling the ring, ending a tile), and a split the
 // writing and reading of its slabs and the launch that joins them, in steps of 0.38 us (3,977 rows
 // of 4096 columns, 1,563 steps: 2.40 ms unsplit in four rounds of 76, the last a third full).
+// More than 16 rounds are not split: what the last one leaves idle is no more than that.
+__host__ __device__ __forceinline__ bool head_split_at_all(long long tiles, int clusters) { return tiles <= 16ll * clusters; }
 __device__ __forceinline__ int head_splits(const HeadTc& h, long long tiles, int steps, int rows) {
+  if (!head_split_at_all(tiles, h.clusters)) return 1;
   const int s = static_cast<int>(threadIdx.x & 31) + 1;
   const unsigned long long slab = static_cast<unsigned long long>(rows) * h.ld_slab;
   long long cost = (tiles * s + h.clusters - 1) / h.clusters * ((steps + s - 1) / s + 8);
@@ -26,3 +36,20 @@ __device__ __forceinline__ int head_splits(const HeadTc& h, long long tiles, int
 }
 
 }  // namespace eogp
+
+// Launches k after what was launched before on the stream, as after_previous() has it; `next` false: plainly.
+template <typename... P, typename... A>
+cudaError_t head_launch(void (*k)(P...), bool next, unsigned grid, unsigned block, size_t smem, cudaStream_t st,
+                        A... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = next ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, k, static_cast<P>(args)...);
+}

@@ -122,6 +122,7 @@ __device__ __forceinline__ Job job_of(const HeadArgs& a, int r, unsigned* status
 }
 
 __global__ void __launch_bounds__(kFindThreads) k_head_count(const HeadArgs a, int M, int per, int* counts) {
+  after_previous();
   const int r0 = blockIdx.x * per, r1 = min(M, r0 + per);
   int n = 0;
   for (int r = r0; r < r1; r += kFindThreads) {
@@ -135,6 +136,7 @@ __global__ void __launch_bounds__(kFindThreads) k_head_count(const HeadArgs a, i
 // number in counts[kFindBlocks]. Losses of the others are 0.
 __global__ void __launch_bounds__(kFindThreads) k_head_place(const HeadArgs a, int M, int per, int* counts, int* idx,
                                                              int* target, float* w, unsigned* status) {
+  after_previous();
   __shared__ int part[kFindThreads / 32], base;
   const int tid = threadIdx.x, lane = tid & 31;
   int before = 0;
@@ -178,6 +180,7 @@ __global__ void __launch_bounds__(kFindThreads) k_head_place(const HeadArgs a, i
 // Zeros in the rows of dx that are left out.
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_zero(const HeadArgs a, int M) {
+  after_previous();
   const int lane = threadIdx.x & 31;
   for (int r = blockIdx.x * 8 + (threadIdx.x >> 5); r < M; r += gridDim.x * 8) {
     if (job_of(a, r, nullptr).kept) continue;
@@ -235,6 +238,7 @@ __device__ __forceinline__ void put_row(const float* x, int d, int ldx, bool, bf
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_gather(const HeadArgs a, const int* counts, const int* idx, int first,
                                                      int piece, int ldx, bool vec, bf16* out) {
+  after_previous();
   const int n = min(piece, counts[kFindBlocks] - first), n64 = (max(n, 0) + 63) & ~63;
   for (int i = blockIdx.x * 8 + (threadIdx.x >> 5); i < n64; i += gridDim.x * 8) {
     const T* x = nullptr;
@@ -252,6 +256,7 @@ __global__ void __launch_bounds__(256) k_head_gather(const HeadArgs a, const int
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_few(const HeadArgs a, int M, int* counts, int* idx, int* target, float* w,
                                                   int ldx, bool vec, bf16* out, unsigned* status) {
+  after_previous();
   __shared__ unsigned kept[kFewRows / 32];
   const int tid = threadIdx.x, lane = tid & 31, r = blockIdx.x * 8 + (tid >> 5);
 #pragma unroll
@@ -302,6 +307,7 @@ __global__ void __launch_bounds__(256) k_head_few(const HeadArgs a, int M, int* 
 // The matrix with rows that TMA can read; fp32 in three parts.
 template <typename T>
 __global__ void __launch_bounds__(256) k_head_matrix(const T* W, long long ld, int V, int d, bf16* out, int ldo) {
+  after_previous();
   for (long long r = blockIdx.x * 8 + (threadIdx.x >> 5); r < V; r += gridDim.x * 8)
     put_row(W + r * ld, d, ldo, false, out + r * ldo);
 }
@@ -311,6 +317,7 @@ __global__ void __launch_bounds__(256) k_head_matrix(const T* W, long long ld, i
 __global__ void __launch_bounds__(1024) k_head_join(const HeadArgs a, const int* counts, const int* idx, const float* ws,
                                                     int first, int piece, const float2* parts, int n_parts,
                                                     const float* zt, float2* row) {
+  after_previous();
   __shared__ float2 all[32][33];
   const int n = min(piece, counts[kFindBlocks] - first), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int i = blockIdx.x * 32 + lane;
@@ -349,6 +356,7 @@ template <int PARTS>
 __global__ void __launch_bounds__(256) k_head_d(const HeadArgs a, const int* counts, const int* targets,
                                                 const float* ws, int first, int piece, float* z, int ldz,
                                                 const float2* row, bf16* D) {
+  after_previous();
   const int n = min(piece, counts[kFindBlocks] - first), n64 = (max(n, 0) + 63) & ~63;
   for (int i = blockIdx.x; i < n64; i += gridDim.x) {
     float* const x = z + static_cast<size_t>(i) * ldz;
@@ -408,6 +416,7 @@ __global__ void __launch_bounds__(256) k_head_d(const HeadArgs a, const int* cou
 
 // The slabs of a split sum joined, in order, four columns a thread: rows of dx by position, or rows of dW.
 __global__ void __launch_bounds__(256) k_head_slabs(const HeadTc h, bool to_dx) {
+  after_previous();
   const int there = *h.count - h.first, some = max(0, min(h.piece, there)), rows = to_dx ? some : h.V;
   if ((to_dx || h.first > 0) && some == 0) return;
   const int steps = ((to_dx ? h.V : some) + 63) / 64 * h.pairs, nv = h.ld_slab / 4;
@@ -461,27 +470,22 @@ bool vec_rows(const RowView& v, int es) {
 
 // The counted positions of the batch, zeros for the others, and, where there are few, their rows at `x`.
 template <typename T>
-cudaError_t find(const HeadArgs& a, const Plan& p, uint8_t* ws, bf16* x, bool vec, unsigned* status, int num_sms,
-                 cudaStream_t st) {
+cudaError_t find(const HeadArgs& a, const Plan& p, uint8_t* ws, bf16* x, bool vec, bool next, unsigned* status,
+                 int num_sms, cudaStream_t st) {
   const int M = static_cast<int>(a.rs.rows());
   int* const counts = reinterpret_cast<int*>(ws + p.counts);
   int* const idx = reinterpret_cast<int*>(ws + p.idx);
   int* const target = reinterpret_cast<int*>(ws + p.target);
   float* const w = reinterpret_cast<float*>(ws + p.w);
-  if (p.few) {
-    k_head_few<T><<<(M + 7) / 8, 256, 0, st>>>(a, M, counts, idx, target, w, p.ldx, vec, x, status);
-    return cudaGetLastError();
-  }
+  if (p.few)
+    return head_launch(k_head_few<T>, next, (M + 7) / 8, 256, 0, st, a, M, counts, idx, target, w, p.ldx, vec, x, status);
   if (p.find_blocks > 1) {
-    k_head_count<<<p.find_blocks, kFindThreads, 0, st>>>(a, M, p.per_block, counts);
-    TRY(cudaGetLastError());
+    TRY(head_launch(k_head_count, next, p.find_blocks, kFindThreads, 0, st, a, M, p.per_block, counts));
+    next = true;
   }
-  k_head_place<<<p.find_blocks, kFindThreads, 0, st>>>(a, M, p.per_block, counts, idx, target, w, status);
-  TRY(cudaGetLastError());
-  if (a.dx.p) {
-    k_head_zero<T><<<std::min((M + 7) / 8, num_sms * 8), 256, 0, st>>>(a, M);
-    TRY(cudaGetLastError());
-  }
+  TRY(head_launch(k_head_place, next, p.find_blocks, kFindThreads, 0, st, a, M, p.per_block, counts, idx, target, w,
+                  status));
+  if (a.dx.p) TRY(head_launch(k_head_zero<T>, true, std::min((M + 7) / 8, num_sms * 8), 256, 0, st, a, M));
   return cudaSuccess;
 }
 
@@ -508,14 +512,13 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
   constexpr bool f32 = sizeof(T) == 4;
   if (!w_fits(a)) {
     bf16* const copy = reinterpret_cast<bf16*>(ws + p.W);
-    k_head_matrix<T><<<std::min((a.V + 7) / 8, num_sms * 8), 256, 0, st>>>(static_cast<const T*>(a.weight), a.ld_weight,
-                                                                           a.V, a.d, copy, p.ldw);
-    TRY(cudaGetLastError());
+    TRY(head_launch(k_head_matrix<T>, false, std::min((a.V + 7) / 8, num_sms * 8), 256, 0, st,
+                    static_cast<const T*>(a.weight), a.ld_weight, a.V, a.d, copy, p.ldw));
     W = copy;
     ldw = p.ldw;
   }
   const bool vec = vec_rows(a.x, sizeof(T));
-  TRY(find<T>(a, p, ws, x, vec, status, num_sms, st));
+  TRY(find<T>(a, p, ws, x, vec, !w_fits(a), status, num_sms, st));
   HeadTc h{};
   h.count = counts + kFindBlocks;
   h.piece = p.piece;
@@ -542,20 +545,19 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
   for (int c = 0; c < p.pieces; ++c) {
     h.first = c * p.piece;
     if (!p.few)
-      k_head_gather<T><<<std::min(p.piece / 8, num_sms * 8), 256, 0, st>>>(a, counts, idx, h.first, p.piece, p.ldx, vec, x);
-    TRY(cudaGetLastError());
+      TRY(head_launch(k_head_gather<T>, true, std::min(p.piece / 8, num_sms * 8), 256, 0, st, a, counts, idx, h.first,
+                      p.piece, p.ldx, vec, x));
     HeadTc z = h;
     z.A = x, z.inner_a = xcols, z.rows_a = rows, z.lda = p.ldx;
     z.B = W, z.inner_b = xcols, z.rows_b = uv, z.ldb = ldw;
     z.bn = p.bn_z, z.run = f32 ? 8 : 16;
     TRY(launch_head_logits(z, status, st));
-    k_head_join<<<(p.piece + 31) / 32, 1024, 0, st>>>(a, counts, idx, w, h.first, p.piece, h.part,
-                                                      (a.V + p.bn_z - 1) / p.bn_z * 2, h.zt, grad ? row : nullptr);
-    TRY(cudaGetLastError());
+    TRY(head_launch(k_head_join, true, (p.piece + 31) / 32, 1024, 0, st, a, counts, idx, w, h.first, p.piece, h.part,
+                    (a.V + p.bn_z - 1) / p.bn_z * 2, h.zt, grad ? row : nullptr));
     if (!grad) continue;
     auto d = f32 ? k_head_d<3> : p.parts == 2 ? k_head_d<2> : k_head_d<1>;
-    d<<<std::min(p.piece, num_sms * 8), 256, 0, st>>>(a, counts, target, w, h.first, p.piece, h.z, p.ldz, row, D);
-    TRY(cudaGetLastError());
+    TRY(head_launch(d, true, std::min(p.piece, num_sms * 8), 256, 0, st, a, counts, target, w, h.first, p.piece, h.z,
+                    p.ldz, row, D));
     if (a.dx.p) {
       HeadTc g = h;
       g.A = D, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = f32 ? 3 : 2;
@@ -563,8 +565,7 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
       g.bn = p.bn_d, g.run = f32 ? 8 : 64;
       g.dx = a.dx, g.out_bf16 = !f32, g.out_vec = row_align(a.dx.p, a.dx.bs, a.dx.ld, sizeof(T));
       TRY(launch_head_dx(g, status, st));
-      k_head_slabs<<<num_sms * 8, 256, 0, st>>>(g, true);
-      TRY(cudaGetLastError());
+      TRY(head_launch(k_head_slabs, true, num_sms * 8, 256, 0, st, g, true));
     }
     if (a.dweight) {
       HeadTc g = h;
@@ -584,8 +585,8 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
       g.out_vec = row_align(g.out, 0, g.ld_out, g.out_bf16 ? 2 : 4);
       g.add_vec = row_align(g.add, 0, g.ld_add, g.add_bf16 ? 2 : 4);
       TRY(launch_head_dw(g, status, st));
-      k_head_slabs<<<num_sms * 8, 256, 0, st>>>(g, false);
-      TRY(cudaGetLastError());
+      if (head_split_at_all((a.V + 255ll) / 256 * ((a.d + g.bn - 1) / g.bn), g.clusters))
+        TRY(head_launch(k_head_slabs, true, num_sms * 8, 256, 0, st, g, false));
     }
   }
   return cudaSuccess;

@@ -349,6 +349,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  after_previous();
   const Shape sh = shape_of<MODE>(g);
 
   if (warp < 4) {
@@ -528,8 +529,7 @@ cudaError_t launch_parts(const HeadTc& h, int most_m, int N, unsigned* status, c
   const size_t smem = 1024 + g.stages * stage + behind + (2 * g.stages + 4) * 8 + 16;
   if (cudaError_t e = allow_smem(k_head_tc<MODE, PARTS>, smem); e != cudaSuccess) return e;
   const unsigned grid = 2u * static_cast<unsigned>(std::min<long long>(tiles, h.clusters));
-  k_head_tc<MODE, PARTS><<<grid, kThreads, smem, st>>>(ta, tb, g);
-  return cudaGetLastError();
+  return head_launch(k_head_tc<MODE, PARTS>, true, grid, kThreads, smem, st, ta, tb, g);
 }
 
 template <int MODE>
