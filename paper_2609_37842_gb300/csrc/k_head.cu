@@ -20,6 +20,7 @@ constexpr float kLowest = -3.402823466e38f;
 constexpr int kFindThreads = 1024;
 constexpr int kFindBlocks = 1024;
 constexpr int kFewRows = 1024;
+constexpr int kDSegment = 8192;  // columns of a row of D that a block forms at a time
 constexpr size_t kSlabBytes = size_t(512) << 20;
 constexpr size_t kPieceBytes = size_t(4) << 30;  // logits of a piece
 
@@ -325,26 +326,36 @@ __global__ void __launch_bounds__(1024) k_head_join(const HeadArgs a, const int*
   float m = kLowest, s = 0.f;
   if (i < n) {
     const float2* const v = parts + i;
-#pragma unroll 8
-    for (int p = warp; p < n_parts; p += 32) m = fmaxf(m, v[static_cast<size_t>(p) * piece].x);
-#pragma unroll 8
-    for (int p = warp; p < n_parts; p += 32) {
-      const float2 x = v[static_cast<size_t>(p) * piece];
-      s += x.y * exp2f((x.x - m) * kLog2e);
+    for (int p = warp; p < n_parts; p += 32 * 8) {
+      float2 x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        x[e] = p + 32 * e < n_parts ? v[static_cast<size_t>(p + 32 * e) * piece] : make_float2(kLowest, 0.f);
+      float top = m;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e].x);
+      s *= exp2f((m - top) * kLog2e);
+      m = top;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += x[e].y * exp2f((x[e].x - m) * kLog2e);
     }
   }
   all[warp][lane] = make_float2(m, s);
   __syncthreads();
-  if (warp > 0 || i >= n) return;
-  for (int p = 1; p < 32; ++p) m = fmaxf(m, all[p][lane].x);
-  s = 0.f;
-  for (int p = 0; p < 32; ++p) s += all[p][lane].y * exp2f((all[p][lane].x - m) * kLog2e);
+  const int mine = blockIdx.x * 32 + warp;  // a row a warp
+  if (mine >= n) return;
+  const float2 x = all[lane][warp];
+  m = x.x;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  s = warp_sum(x.y * exp2f((x.x - m) * kLog2e));
+  if (lane > 0) return;
   const float ls = s > 0.f ? logf(s) : NAN;  // no finite logit: NaN
-  const int r = idx[first + i];
-  const float w = ws[first + i];
-  a.loss[r] = w * ((m - zt[i]) + ls);
+  const int r = idx[first + mine];
+  const float w = ws[first + mine];
+  a.loss[r] = w * ((m - zt[mine]) + ls);
   if (a.lse) a.lse[r] = m + ls;
-  if (row) row[i] = make_float2(m, w * a.scale / s);
+  if (row) row[mine] = make_float2(m, w * a.scale / s);
 }
 
 // D over the logits, in place: the 256 bytes of 64 columns become the 64 first bf16 parts and, with PARTS = 2,
@@ -358,15 +369,17 @@ __global__ void __launch_bounds__(256) k_head_d(const HeadArgs a, const int* cou
                                                 const float2* row, bf16* D) {
   after_previous();
   const int n = min(piece, counts[kFindBlocks] - first), n64 = (max(n, 0) + 63) & ~63;
-  for (int i = blockIdx.x; i < n64; i += gridDim.x) {
+  const unsigned segments = (ldz + kDSegment - 1) / kDSegment, items = n64 * segments;
+  for (unsigned item = blockIdx.x; item < items; item += gridDim.x) {
+    const int i = item / segments, c0 = (item - i * segments) * kDSegment, c1 = min(ldz, c0 + kDSegment);
     float* const x = z + static_cast<size_t>(i) * ldz;
     const bool real = i < n;
     const float2 mi = real ? row[i] : make_float2(0.f, 0.f);
     const int target = real ? targets[first + i] : -1;
     const float g = real ? ws[first + i] * a.scale : 0.f;
-    for (int c = threadIdx.x * 8; (c & ~255) < ldz; c += 256 * 8) {
+    for (int c = c0 + threadIdx.x * 8; (c & ~255) < c1; c += 256 * 8) {
       Vals<8> v = fill<8>(0.f);
-      if (real && c < ldz) {
+      if (real && c < c1) {
         v = ld_floats<8>(x + c);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -385,7 +398,7 @@ __global__ void __launch_bounds__(256) k_head_d(const HeadArgs a, const int* cou
         }
       }
       __syncwarp();
-      if (c >= ldz) continue;
+      if (c >= c1) continue;
       bf16* const o = PARTS == 3 ? D + (static_cast<size_t>(i) * ldz + (c & ~63)) * 3 + (c & 63)
                                  : reinterpret_cast<bf16*>(x + (c & ~63)) + (c & 63);
       if (PARTS == 3) {
@@ -419,13 +432,20 @@ __global__ void __launch_bounds__(256) k_head_slabs(const HeadTc h, bool to_dx) 
   after_previous();
   const int there = *h.count - h.first, some = max(0, min(h.piece, there)), rows = to_dx ? some : h.V;
   if ((to_dx || h.first > 0) && some == 0) return;
-  const int steps = ((to_dx ? h.V : some) + 63) / 64 * h.pairs, nv = h.ld_slab / 4;
+  const int steps = ((to_dx ? h.V : some) + 63) / 64 * h.pairs, lane = threadIdx.x & 31;
   const int splits = head_splits(h, static_cast<long long>((rows + 255) / 256) * ((h.d + h.bn - 1) / h.bn), steps, rows);
   if (splits == 1) return;
   const bool to_acc = !to_dx && h.acc && there > h.piece;
   const size_t slab = static_cast<size_t>(rows) * h.ld_slab;
-  for (long long k = blockIdx.x * 256ll + threadIdx.x; k < static_cast<long long>(rows) * nv; k += gridDim.x * 256ll) {
-    const int i = static_cast<int>(k / nv), c = static_cast<int>(k - static_cast<long long>(i) * nv) * 4;
+  // A warp has 128 columns of a row at a time.
+  const long long chunks = (h.d + 127) / 128, items = rows * chunks;
+  for (long long k = blockIdx.x * 8ll + (threadIdx.x >> 5); k < items; k += gridDim.x * 8ll) {
+    const int i = items <= 0x7fffffff ? static_cast<int>(static_cast<unsigned>(k) / static_cast<unsigned>(chunks))
+                                      : static_cast<int>(k / chunks);
+    const int c = static_cast<int>(k - i * chunks) * 128 + lane * 4;
+    if (c >= h.d) continue;
+    int b = 0, t = 0;
+    if (to_dx) locate(h.rs, h.idx[h.first + i], b, t);
     const float* const from = h.slabs + static_cast<size_t>(i) * h.ld_slab + c;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
@@ -434,14 +454,8 @@ __global__ void __launch_bounds__(256) k_head_slabs(const HeadTc h, bool to_dx) 
       v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
     }
     const float w[4] = {v.x, v.y, v.z, v.w};
-    long long at = to_acc ? static_cast<long long>(i) * h.d : i * h.ld_out;
-    void* out = to_acc ? h.acc : h.out;
-    if (to_dx) {
-      int b, t;
-      locate(h.rs, h.idx[h.first + i], b, t);
-      at = b * h.dx.bs + t * h.dx.ld;
-      out = const_cast<void*>(h.dx.p);
-    }
+    const long long at = to_dx ? b * h.dx.bs + t * h.dx.ld : to_acc ? static_cast<long long>(i) * h.d : i * h.ld_out;
+    void* const out = to_dx ? const_cast<void*>(h.dx.p) : to_acc ? h.acc : h.out;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (c + e >= h.d) break;
@@ -556,7 +570,8 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
                     (a.V + p.bn_z - 1) / p.bn_z * 2, h.zt, grad ? row : nullptr));
     if (!grad) continue;
     auto d = f32 ? k_head_d<3> : p.parts == 2 ? k_head_d<2> : k_head_d<1>;
-    TRY(head_launch(d, true, std::min(p.piece, num_sms * 8), 256, 0, st, a, counts, target, w, h.first, p.piece, h.z,
+    const long long segments = static_cast<long long>(p.piece) * ((p.ldz + kDSegment - 1) / kDSegment);
+    TRY(head_launch(d, true, std::min<long long>(segments, num_sms * 8), 256, 0, st, a, counts, target, w, h.first, p.piece, h.z,
                     p.ldz, row, D));
     if (a.dx.p) {
       HeadTc g = h;
