@@ -662,8 +662,8 @@ int eogp_cross_entropy(const void* logits, int dtype, long long logits_bs, long 
  *                                         with `accumulate` the sums are added instead).
  * dx and dweight may each be NULL; dx may be x with the same strides. Positions left out cost
  * nothing but their zeros: the others are gathered first. With a gradient, the logits of a piece
- * of the positions at a time lie in the workspace, in fp32, of at most about 4 GB (more only where
- * 256 positions take more); without one none are stored.
+ * of the positions at a time lie in the workspace, in fp32, or D in bf16, of at most about 4 GB (more
+ * only where 256 positions take more); without one none are stored.
  * EOGP_BF16: products of bf16 on the tensor cores, sums in fp32. D enters the products for dx, and
  * for a dweight of EOGP_BF16, rounded to bf16, as dlogits of eogp_cross_entropy would; for one of
  * EOGP_F32 it enters as two bf16 parts (about 2^-16 relative). EOGP_F32: products to fp32.

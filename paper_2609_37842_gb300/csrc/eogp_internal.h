@@ -306,17 +306,17 @@ struct DistillArgs {
 };
 cudaError_t launch_distill(const DistillArgs& a, bool bf16, unsigned* status, int num_sms, cudaStream_t st);
 
-// k_head_tc.cu: the three products of a piece of the counted positions, on operands of bf16 parts.
+// k_head_tc.cu: the products of a piece of the counted positions, on operands of bf16 parts.
 // An operand of several parts has 64 columns of each in turn (parts * 64 columns a block).
 struct HeadTc {
   const int* count;  // counted positions in all; the piece has those from `first` on, at most `piece`
   int first, piece, d, V;
   const void *A, *B;
   uint64_t inner_a, rows_a, lda, inner_b, rows_b, ldb;  // elements as they lie
-  int parts_a, parts_b;  // as they lie: 1 or 2 of A with 1 of B, or 3 and 3 (k_head_tc: PARTS)
-  int pairs;             // parts of an A of two that are summed over; else 1
+  int parts_a;  // of A as it lies: 1 or 2 with 1 of B, or 3 and 3
+  int used_a;   // those that enter the sum: 1, 2 or 3 (k_head_tc: PARTS)
   int bn;              // columns of a tile
-  int run;             // steps of 64 (times pairs) that one accumulator sums
+  int run;             // steps of 64 that one accumulator sums
   // logits: z (NULL: not kept) [piece x ldz], -inf beyond V; (maximum, sum) of each row's half tiles
   // [2 * tiles][piece]; the target's logit
   float scale;
@@ -325,6 +325,12 @@ struct HeadTc {
   float2* part;
   float* zt;
   const int* target;
+  bool early;  // 256 rows at most, and B is as it was before the call
+  // D of logits that are not kept: [piece x ldz * parts_d], of a row's maximum and w scale / sum
+  void* D;
+  int parts_d;
+  const float2* row;
+  const float* w;
   // dx, by position
   RowSet rs;
   const int* idx;
@@ -345,5 +351,6 @@ struct HeadTc {
   int piece_rows, rows_box;  // most rows of this piece; rows of a K-major A that a CTA loads
 };
 cudaError_t launch_head_logits(const HeadTc& h, unsigned* status, cudaStream_t st);
+cudaError_t launch_head_d(const HeadTc& h, unsigned* status, cudaStream_t st);
 cudaError_t launch_head_dx(const HeadTc& h, unsigned* status, cudaStream_t st);
 cudaError_t launch_head_dw(const HeadTc& h, unsigned* status, cudaStream_t st);

@@ -26,7 +26,7 @@ __device__ __forceinline__ int head_splits(const HeadTc& h, long long tiles, int
   if (!head_split_at_all(tiles, h.clusters)) return 1;
   const int s = static_cast<int>(threadIdx.x & 31) + 1;
   const unsigned long long slab = static_cast<unsigned long long>(rows) * h.ld_slab;
-  long long cost = (tiles * s + h.clusters - 1) / h.clusters * ((steps + s - 1) / s + 8);
+  long long cost = (tiles * s + h.clusters - 1) / h.clusters * ((steps + s - 1) / s * (h.used_a == 2 ? 2 : 1) + 8);
   if (s > 1) cost += 8 + static_cast<long long>(s * slab / 323000);
   if (s > 1 && (s > steps || s * slab * 4 > h.slab_bytes)) cost = 0x7fffffffffffffffll;
   unsigned long long best = static_cast<unsigned long long>(cost);

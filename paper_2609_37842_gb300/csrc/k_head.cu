@@ -6,7 +6,12 @@
 // The counted positions (inside their example's length, target not ignored, weight not
 // 0) are found first and their rows of x gathered, a piece of them at a time: what is
 // left out costs no products. The logits of one piece lie in the workspace in fp32 and
-// become D in place.
+// become D in place; those of narrow rows of bf16 are formed again for D instead.
+//
+// Bound by the products, 6 m V d operations with both gradients (GB300: 4 x 2048 positions, 3,979 of them counted,
+// 4096 columns, 100,000 classes: FIG_BATCH), for few rows by the launches, one after the other, and the
+// matrix's way through the multiprocessors (511 positions, 768 columns, 50,001 classes: FIG_EXAMPLE); the loss of
+// one position by reading the matrix (FIG_TOKEN).
 #include <algorithm>
 
 #include "head_dev.cuh"
@@ -20,6 +25,7 @@ constexpr float kLowest = -3.402823466e38f;
 constexpr int kFindThreads = 1024;
 constexpr int kFindBlocks = 1024;
 constexpr int kFewRows = 1024;
+constexpr int kAgainRows = 256, kAgainWidth = 1024;
 constexpr int kDSegment = 8192;  // columns of a row of D that a block forms at a time
 constexpr size_t kSlabBytes = size_t(512) << 20;
 constexpr size_t kPieceBytes = size_t(4) << 30;  // logits of a piece
@@ -34,6 +40,7 @@ struct Plan {
   int piece, pieces;           // rows of a piece, most pieces
   int ldz, ldx, ldw;           // row strides of the logits, of the gathered rows and of the matrix (bf16 elements)
   int parts;                   // bf16 parts of D
+  bool again;                  // the logits are not kept but formed again for D
   int bn_z, bn_d;              // columns of a tile of the logits, of dx and dW
   int ld_slab;
   size_t slab_bytes;
@@ -57,8 +64,14 @@ Plan plan_of(const HeadArgs& a) {
   p.ldz = static_cast<int>(up(a.V, 64));
   p.ldx = p.ldw = static_cast<int>(a.bf16 ? up(a.d, 8) : up(a.d, 64) * 3);
   p.parts = !a.bf16 ? 3 : a.dweight && !a.grad_bf16 ? 2 : 1;
+  // Narrow rows: the logits are not kept, D is formed from them where they are computed a second time. That costs
+  // 2 d operations a logit and spares 8 bytes of traffic, 6 where D has one part (us, kept / formed again, dW in
+  // bf16: 16,384 rows of 64 columns, 50,000 classes 2,404 / 1,334; of 768 3,390 / 3,111, of 1024 4,047 / 4,104, of
+  // 1536 5,608 / 6,229; 511 rows of 768 171 / 163). For few rows the matrix, read once more, counts too.
+  p.again = grad && a.bf16 && M >= kAgainRows && a.d <= std::min<long long>(kAgainWidth, 2 * M);
   // A row of a piece: logits (and D, where it is not in their place), or the sums of its half tiles; and the gathered row.
-  const size_t row_bytes = static_cast<size_t>(p.ldx) * 2 + (grad ? static_cast<size_t>(p.ldz) * (a.bf16 ? 4 : 10) : p.ldz / 64 * 16);
+  const size_t row_bytes = static_cast<size_t>(p.ldx) * 2 + (grad ? static_cast<size_t>(p.ldz) * (p.again ? p.parts * 2 : a.bf16 ? 4 : 10) : 0) +
+                           p.ldz / 64 * 16;
   const long long most = std::max<long long>(256, static_cast<long long>(kPieceBytes / row_bytes) / 256 * 256);
   p.pieces = static_cast<int>((M + most - 1) / most);
   p.piece = static_cast<int>(std::min(most, up((M + p.pieces - 1) / p.pieces, 256)));
@@ -89,8 +102,8 @@ Plan plan_of(const HeadArgs& a) {
   p.zt = take(static_cast<size_t>(p.piece) * 4);
   p.row = take(static_cast<size_t>(p.piece) * 8);
   if (grad) {
-    p.z = take(static_cast<size_t>(p.piece) * p.ldz * 4);
-    if (!a.bf16) p.D = take(static_cast<size_t>(p.piece) * p.ldz * 6);
+    if (!p.again) p.z = take(static_cast<size_t>(p.piece) * p.ldz * 4);
+    if (!a.bf16 || p.again) p.D = take(static_cast<size_t>(p.piece) * p.ldz * p.parts * 2);
     if (a.dweight && a.grad_bf16 && p.pieces > 1) p.acc = take(static_cast<size_t>(a.V) * a.d * 4);
     p.ld_slab = static_cast<int>(up(a.d, 8));
     // Room for split sums: as many as there may be, half a GB at most.
@@ -432,7 +445,7 @@ __global__ void __launch_bounds__(256) k_head_slabs(const HeadTc h, bool to_dx) 
   after_previous();
   const int there = *h.count - h.first, some = max(0, min(h.piece, there)), rows = to_dx ? some : h.V;
   if ((to_dx || h.first > 0) && some == 0) return;
-  const int steps = ((to_dx ? h.V : some) + 63) / 64 * h.pairs, lane = threadIdx.x & 31;
+  const int steps = ((to_dx ? h.V : some) + 63) / 64, lane = threadIdx.x & 31;
   const int splits = head_splits(h, static_cast<long long>((rows + 255) / 256) * ((h.d + h.bn - 1) / h.bn), steps, rows);
   if (splits == 1) return;
   const bool to_acc = !to_dx && h.acc && there > h.piece;
@@ -539,23 +552,23 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
   h.d = a.d;
   h.V = a.V;
   h.scale = a.scale;
-  h.z = grad ? reinterpret_cast<float*>(ws + p.z) : nullptr;
+  h.z = grad && !p.again ? reinterpret_cast<float*>(ws + p.z) : nullptr;
   h.ldz = p.ldz;
   h.part = reinterpret_cast<float2*>(ws + p.part);
   h.zt = reinterpret_cast<float*>(ws + p.zt);
   h.target = target;
   h.rs = a.rs;
   h.idx = idx;
-  h.parts_a = h.parts_b = f32 ? 3 : 1;
-  h.pairs = 1;
-  bf16* const D = f32 ? reinterpret_cast<bf16*>(ws + p.D) : reinterpret_cast<bf16*>(h.z);  // bf16: in the logits' place
+  h.parts_a = h.used_a = f32 ? 3 : 1;
+  bf16* const D = reinterpret_cast<bf16*>(ws + (f32 || p.again ? p.D : p.z));  // else in the logits' place
+  const int parts_d = f32 ? 3 : p.again ? p.parts : 2;  // as they lie
   h.ld_slab = p.ld_slab;
   h.slabs = reinterpret_cast<float*>(ws + p.slabs);
   h.slab_bytes = p.slab_bytes;
   h.clusters = num_sms / 2;
   h.piece_rows = static_cast<int>(std::min<long long>(M, p.piece));
   h.rows_box = static_cast<int>(std::min<long long>(128, up(h.piece_rows, 8)));
-  const uint64_t xcols = f32 ? p.ldx : a.d, uv = a.V, rows = p.piece, dcols = static_cast<uint64_t>(p.ldz) * (f32 ? 3 : 2);
+  const uint64_t xcols = f32 ? p.ldx : a.d, uv = a.V, rows = p.piece, dcols = static_cast<uint64_t>(p.ldz) * parts_d;
   for (int c = 0; c < p.pieces; ++c) {
     h.first = c * p.piece;
     if (!p.few)
@@ -565,17 +578,24 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
     z.A = x, z.inner_a = xcols, z.rows_a = rows, z.lda = p.ldx;
     z.B = W, z.inner_b = xcols, z.rows_b = uv, z.ldb = ldw;
     z.bn = p.bn_z, z.run = f32 ? 8 : 16;
+    z.early = w_fits(a) && h.piece_rows <= 256;
     TRY(launch_head_logits(z, status, st));
     TRY(head_launch(k_head_join, true, (p.piece + 31) / 32, 1024, 0, st, a, counts, idx, w, h.first, p.piece, h.part,
                     (a.V + p.bn_z - 1) / p.bn_z * 2, h.zt, grad ? row : nullptr));
     if (!grad) continue;
-    auto d = f32 ? k_head_d<3> : p.parts == 2 ? k_head_d<2> : k_head_d<1>;
-    const long long segments = static_cast<long long>(p.piece) * ((p.ldz + kDSegment - 1) / kDSegment);
-    TRY(head_launch(d, true, std::min<long long>(segments, num_sms * 8), 256, 0, st, a, counts, target, w, h.first, p.piece, h.z,
-                    p.ldz, row, D));
+    if (p.again) {
+      z.bn = 256;
+      z.D = D, z.parts_d = parts_d, z.row = row, z.w = w;
+      TRY(launch_head_d(z, status, st));
+    } else {
+      auto d = f32 ? k_head_d<3> : p.parts == 2 ? k_head_d<2> : k_head_d<1>;
+      const long long segments = static_cast<long long>(p.piece) * ((p.ldz + kDSegment - 1) / kDSegment);
+      TRY(head_launch(d, true, std::min<long long>(segments, num_sms * 8), 256, 0, st, a, counts, target, w, h.first,
+                      p.piece, h.z, p.ldz, row, D));
+    }
     if (a.dx.p) {
       HeadTc g = h;
-      g.A = D, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = f32 ? 3 : 2;
+      g.A = D, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = parts_d;
       g.B = W, g.inner_b = xcols, g.rows_b = uv, g.ldb = ldw;
       g.bn = p.bn_d, g.run = f32 ? 8 : 64;
       g.dx = a.dx, g.out_bf16 = !f32, g.out_vec = row_align(a.dx.p, a.dx.bs, a.dx.ld, sizeof(T));
@@ -584,10 +604,10 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
     }
     if (a.dweight) {
       HeadTc g = h;
-      g.A = D, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = f32 ? 3 : 2;
+      g.A = D, g.inner_a = dcols, g.rows_a = rows, g.lda = dcols, g.parts_a = parts_d;
       g.B = x, g.inner_b = xcols, g.rows_b = rows, g.ldb = p.ldx;
-      if (p.parts == 2) g.pairs = 2;
-      g.bn = p.bn_d, g.run = f32 ? 8 : a.grad_bf16 ? 64 : 16;
+      g.used_a = p.parts;
+      g.bn = p.bn_d, g.run = f32 || p.parts == 2 ? 8 : 64;
       // Sums of several pieces stay in fp32, in dweight itself or beside it; the last piece that has rows
       // ends them, and those after it do nothing.
       g.out = a.dweight, g.ld_out = a.ld_dweight, g.out_bf16 = a.grad_bf16;

@@ -1,6 +1,6 @@
 // The products of the token loss through the output matrix, on the tensor cores (see
-// k_head.cu for the formulas): z = scale x W^T with the sums of the loss, dx = D W and
-// dW = D^T x, all sums in fp32.
+// k_head.cu for the formulas): z = scale x W^T with the sums of the loss, or once more as D of
+// them, dx = D W and dW = D^T x, all sums in fp32.
 //
 // k_head_tc: a pair of CTAs (tcgen05 cta_group::2) works on tiles of 256 x BN outputs, one
 // after the other. Each CTA loads its 128 rows of A and its half of B's columns, 64 steps of the
@@ -11,14 +11,18 @@
 // Tensor cores cut an accumulator off where they add to it: towards 0, by up to 2^-23 of it every
 // 16 products. So a long sum goes through several accumulators, `run` steps of 64 each, which are
 // added up in registers, rounded.
-// An operand may come in several bf16 parts, blocks of 64 columns of each in turn. D of two parts: its sum
-// runs over both parts' products. fp32 operands are sums of three parts of 8 bits each, exactly; of the
+// An operand may come in several bf16 parts, blocks of 64 columns of each in turn. D of two parts (PARTS = 2): both
+// are in a stage and meet the same x. fp32 operands are sums of three parts of 8 bits each, exactly; of the
 // nine products of parts the six down to 2^-16 are formed (PARTS = 3), the first parts' in one accumulator and
 // the others', 2^-8 and less of it, in a second one, where cutting off costs nothing that counts.
 //
 // Warps (384 threads): 0 issues TMA, 1 owns tensor memory and issues MMAs, 4-11 end tiles; these
 // take over registers from the first four (168 x 384 = 56 x 128 + 224 x 256).
 // Every wait is bounded; after one that ran out each role goes to the common end.
+//
+// 3,979 rows, 4096 columns, 100,000 classes: z FIG_Z, dx FIG_DX, dW FIG_DW, each alone; in a row they meet the power limit.
+// Tried without gain: operands asked for in L2 ten steps ahead (7.2 against 6.7 ms for that batch), a thread of its
+// own for each operand's copies.
 #include <algorithm>
 
 #include "head_dev.cuh"
@@ -34,7 +38,7 @@ constexpr uint32_t kABytes = 128u * 64u * 2u;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
 
-enum { kLogits = 0, kDx = 1, kDw = 2 };
+enum { kLogits = 0, kDx = 1, kDw = 2, kD = 3 };
 
 struct TcArgs {
   HeadTc h;
@@ -64,9 +68,9 @@ __device__ __forceinline__ Shape shape_of(const TcArgs& g) {
   s.last = left <= g.h.piece;
   s.M = MODE == kDw ? g.h.V : s.rows;
   s.mt = (s.M + 255) / 256;
-  const int K = MODE == kLogits ? g.h.d : MODE == kDx ? g.h.V : s.rows;
-  s.steps = (K + 63) / 64 * g.h.pairs;
-  s.splits = MODE == kLogits ? 1 : head_splits(g.h, s.mt * g.nN, s.steps, s.M);
+  const int K = MODE == kDx ? g.h.V : MODE == kDw ? s.rows : g.h.d;
+  s.steps = (K + 63) / 64;
+  s.splits = MODE == kLogits || MODE == kD ? 1 : head_splits(g.h, s.mt * g.nN, s.steps, s.M);
   s.per = (s.steps + s.splits - 1) / s.splits;
   s.tiles = s.rows == 0 && g.h.first > 0 ? 0 : s.mt * g.nN * s.splits;
   return s;
@@ -78,7 +82,8 @@ __device__ __forceinline__ Tile tile_of(const TcArgs& g, const Shape& s, int t) 
   const int mn = s.mt * g.nN;
   r.split = t / mn;
   t -= r.split * mn;
-  const int m = MODE == kLogits ? t % s.mt : t / g.nN, n = MODE == kLogits ? t / s.mt : t % g.nN;
+  constexpr bool by_n = MODE == kLogits || MODE == kD;
+  const int m = by_n ? t % s.mt : t / g.nN, n = by_n ? t / s.mt : t % g.nN;
   r.m0 = m * 256;
   r.n0 = n * g.h.bn;
   r.i0 = r.split * s.per;
@@ -222,6 +227,53 @@ __device__ __forceinline__ void end_logits(const TcArgs& g, const Shape& s, cons
   h.part[static_cast<size_t>(t.n0 / h.bn * 2 + side) * h.piece + row] = make_float2(m, all.x + all.y);
 }
 
+// Or D of logits that are not kept, in one or two bf16 parts: zeros from V on and in the rows up to the next multiple
+// of 64. Sixteen columns of a part are 32 bytes of a block of 64.
+__device__ __forceinline__ void end_d(const TcArgs& g, const Shape& s, const Tile& t, int row, int side, int target,
+                                      Sums& sums) {
+  const HeadTc& h = g.h;
+  if (row >= ((s.M + 63) & ~63)) return;
+  const bool real = row < s.M;
+  const float2 mi = real ? h.row[row] : make_float2(0.f, 0.f);
+  const int c0 = t.n0 + side * (h.bn / 2), cols = real ? h.V - c0 : 0, out = h.ldz - c0;
+  bf16* const D = static_cast<bf16*>(h.D) + static_cast<size_t>(row) * h.ldz * h.parts_d;
+  const float gt = static_cast<unsigned>(target - c0) < 128u ? h.w[h.first + row] * h.scale : 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float(&v)[32] = sums.v[k];
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+      const float2 z = mul2(make_float2(v[e], v[e + 1]), pair(h.scale));
+      const float2 x = mul2(add2(z, pair(-mi.x)), pair(kLog2e));
+      const float2 p = mul2(make_float2(exp2_fast(x.x), exp2_fast(x.y)), pair(mi.y));
+      v[e] = p.x, v[e + 1] = p.y;
+    }
+    if (cols < k * 32 + 32) {
+#pragma unroll
+      for (int e = 0; e < 32; ++e) v[e] = k * 32 + e < cols ? v[e] : 0.f;
+    }
+    if (static_cast<unsigned>(target - c0 - k * 32) < 32u) {
+#pragma unroll
+      for (int e = 0; e < 32; ++e) v[e] -= target - c0 == k * 32 + e ? gt : 0.f;
+    }
+    if (out < k * 32 + 32) continue;
+    bf16* const o = D + static_cast<size_t>((c0 + k * 32) >> 6) * 64 * h.parts_d + (c0 + k * 32 & 63);
+#pragma unroll
+    for (int q = 0; q < 32; q += 16) {
+      uint32_t w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = pack_bf16(make_float2(v[q + 2 * e], v[q + 2 * e + 1]));
+      st_global_v8(o + q, w);
+      if (h.parts_d == 1) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        w[e] = pack_bf16(make_float2(v[q + 2 * e] - __uint_as_float(w[e] << 16),
+                                     v[q + 2 * e + 1] - __uint_as_float(w[e] & 0xffff0000u)));
+      st_global_v8(o + 64 + q, w);
+    }
+  }
+}
+
 // Or outputs of dx or dW, or of a slab of them.
 template <int MODE>
 __device__ __forceinline__ void end_tile(const TcArgs& g, const Shape& s, const Tile& t, int row, int side,
@@ -311,7 +363,8 @@ __device__ __forceinline__ void take_sums(uint32_t tmem, int bn, bool more, Sums
 template <int MODE, int PARTS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     k_head_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const TcArgs g) {
-  constexpr bool kAmn = MODE == kDw, kBmn = MODE != kLogits;
+  constexpr bool kAmn = MODE == kDw, kBmn = MODE == kDx || MODE == kDw;
+  constexpr int kPartsB = PARTS == 3 ? 3 : 1;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = align1024(smem_raw);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -319,7 +372,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const int half = g.h.bn / 2;  // columns of B in this CTA
   const uint32_t a_bytes = kAmn ? kABytes : g.h.rows_box * 128u;
   const uint32_t b_bytes = static_cast<uint32_t>(half) * 128u, b_at = PARTS * a_bytes;
-  const uint32_t stage_bytes = b_at + PARTS * b_bytes;
+  const uint32_t stage_bytes = b_at + kPartsB * b_bytes;
   const int stages = g.stages;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + static_cast<size_t>(stages) * stage_bytes + (kABytes - a_bytes));
   uint64_t* empty = full + stages;
@@ -349,6 +402,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  // Rows of one tile at most, and a matrix that no launch of this call writes: the first copies of it are under way
+  // before the rows are there. (One row, 50,000 x 768: FIG_EARLY.)
+  int early = 0;  // stages whose B comes already
+  if (MODE == kLogits && PARTS == 1 && g.h.early && threadIdx.x == 0) {
+    const int steps = (g.h.d + 63) / 64;
+    const uint32_t full0 = mapa_shared(smem_u32(full), 0);
+    for (int t = cl, i = 0; early < stages && t < g.nN; ++early) {
+      tma_load_2d_pair(smem_u32(smem) + early * stage_bytes + b_at, &tmB, i * 64,
+                       t * g.h.bn + static_cast<int>(rank) * half, full0 + early * 8);
+      if (++i == steps) i = 0, t += ncl;
+    }
+  }
   after_previous();
   const Shape sh = shape_of<MODE>(g);
 
@@ -359,46 +424,63 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       // Few rows: those of A that there are, and none of the second CTA's. What the MMAs read in the others' place
       // (the stage's B, the next stage, at the ring's end the space behind it) only reaches outputs that are not taken.
       const bool a_there = kAmn || static_cast<int>(rank) * 128 < g.h.piece_rows;
-      const uint32_t bytes = PARTS * ((a_there ? a_bytes : 0u) + b_bytes);
-      int rs = 0;
-      uint32_t rph = 0;
+      const uint32_t bytes = PARTS * (a_there ? a_bytes : 0u) + kPartsB * b_bytes;
+      const uint32_t ring = smem_u32(smem), full0 = mapa_shared(smem_u32(full), 0);
+      int s = 0;
+      uint32_t ph = 1;
       bool ok = true;
+      if (sh.tiles == 0) {  // no rows
+        for (int k = 0; k < early; ++k) {
+          mbar_arrive_expect_tx_cluster(full0 + k * 8, b_bytes);
+          if (rank == 0 && !mbar_wait(&full[k], 0, g.status)) break;
+        }
+      }
       for (int t = cl; t < sh.tiles && ok; t += ncl) {
         const Tile tl = tile_of<MODE>(g, sh, t);
         const int am = tl.m0 + static_cast<int>(rank) * 128, bn = tl.n0 + static_cast<int>(rank) * half;
+        const int ac = kAmn ? am * g.h.parts_a : 0, bc = kBmn ? bn * kPartsB : 0;
+        const int ai = 64 * g.h.parts_a;
         for (int i = tl.i0; i < tl.i1; ++i) {
-          const int s = rs;
-          const uint32_t ph = rph;
-          if (++rs == stages) {
-            rs = 0;
-            rph ^= 1u;
-          }
-          if (!mbar_wait(&empty[s], ph ^ 1u, g.status)) {
+          if (!mbar_wait(&empty[s], ph, g.status)) {
             ok = false;
             break;
           }
-          // PARTS = 3: all parts in one stage; else the part of A whose turn it is.
-          const int kb = i / g.h.pairs, turn = i - kb * g.h.pairs;
-          const uint32_t st = smem_u32(smem + static_cast<size_t>(s) * stage_bytes);
-          const uint32_t fl = mapa_shared(smem_u32(&full[s]), 0);
+          const uint32_t st = ring + s * stage_bytes, fl = full0 + s * 8;
           mbar_arrive_expect_tx_cluster(fl, bytes);
 #pragma unroll
           for (int q = 0; q < PARTS; ++q) {
-            const int pa = PARTS == 3 ? q : turn;
-            const uint32_t a = st + q * a_bytes, b = st + b_at + q * b_bytes;
+            const uint32_t a = st + q * a_bytes;
             if (kAmn) {
-              tma_load_2d_pair(a, &tmA, (am / 64 * g.h.parts_a + pa) * 64, kb * 64, fl);
-              tma_load_2d_pair(a + 8192, &tmA, ((am / 64 + 1) * g.h.parts_a + pa) * 64, kb * 64, fl);
+              tma_load_2d_pair(a, &tmA, ac + q * 64, i * 64, fl);
+              tma_load_2d_pair(a + 8192, &tmA, ac + ai + q * 64, i * 64, fl);
             } else if (a_there) {
-              tma_load_2d_pair(a, &tmA, (kb * g.h.parts_a + pa) * 64, am, fl);
-            }
-            if (kBmn) {
-              for (int j = 0; j < half / 64; ++j)
-                tma_load_2d_pair(b + j * 8192, &tmB, ((bn / 64 + j) * PARTS + q) * 64, kb * 64, fl);
-            } else {
-              tma_load_2d_pair(b, &tmB, (kb * PARTS + q) * 64, bn, fl);
+              tma_load_2d_pair(a, &tmA, i * ai + q * 64, am, fl);
             }
           }
+          const bool comes = early > 0;
+          early -= comes;
+#pragma unroll
+          for (int q = 0; q < kPartsB && !comes; ++q) {
+            const uint32_t b = st + b_at + q * b_bytes;
+            if (kBmn) {
+              tma_load_2d_pair(b, &tmB, bc + q * 64, i * 64, fl);
+              if (half > 64) tma_load_2d_pair(b + 8192, &tmB, bc + (kPartsB + q) * 64, i * 64, fl);
+            } else {
+              tma_load_2d_pair(b, &tmB, (i * kPartsB + q) * 64, bn, fl);
+            }
+          }
+          if (++s == stages) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+      }
+      // The copies under way are not left behind: every stage is free again, or its wait has run out meanwhile.
+      for (int k = 0; k < stages; ++k) {
+        if (!mbar_wait(&empty[s], ph, g.status)) break;
+        if (++s == stages) {
+          s = 0;
+          ph ^= 1u;
         }
       }
     }
@@ -408,6 +490,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const uint32_t idesc = idesc_bf16_f32(256, g.h.bn, kAmn, kBmn);
       // Step of 16 along the sum: 32 bytes of a K-major row, 16 rows of 128 bytes of MN-major ones.
       constexpr uint64_t ka = kAmn ? 128 : 2, kb_ = kBmn ? 128 : 2;
+      const uint32_t st = smem_u32(smem);
+      const uint64_t a0 = kAmn ? sdesc_sw128(st, 8192, 1024) : sdesc_sw128(st, 16, 1024);
+      const uint64_t b0 = kBmn ? sdesc_sw128(st + b_at, 8192, 1024) : sdesc_sw128(st + b_at, 16, 1024);
       int rs = 0, i = 0;
       uint32_t rph = 0;
       bool ok = true;
@@ -434,14 +519,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               break;
             }
             tc_fence_after();
-            const uint32_t st = smem_u32(smem + static_cast<size_t>(s) * stage_bytes);
-            const uint64_t a = kAmn ? sdesc_sw128(st, 8192, 1024) : sdesc_sw128(st, 16, 1024);
-            const uint64_t b = kBmn ? sdesc_sw128(st + b_at, 8192, 1024) : sdesc_sw128(st + b_at, 16, 1024);
+            const uint32_t at = static_cast<uint32_t>(s) * stage_bytes >> 4;
+            const uint64_t a = a0 + at, b = b0 + at;
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
               const uint64_t ak = a + ka * kk, bk = b + kb_ * kk;
               const uint32_t on = (k != k0 || kk != 0) ? 1u : 0u;
               tc_mma_f16_pair(d, ak, bk, idesc, on);
+              if (PARTS == 2) tc_mma_f16_pair(d, ak + (a_bytes >> 4), bk, idesc, 1u);
               if (PARTS == 3) {
                 const uint64_t a1 = a_bytes >> 4, b1 = b_bytes >> 4;
                 const uint32_t rest = d + g.h.bn;
@@ -470,7 +555,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const int row = tl.m0 + static_cast<int>(rank) * 128 + q * 32 + lane;
       const uint32_t lanes = tmem + (static_cast<uint32_t>(q * 32) << 16);
       // Asked for before the accumulator is waited for.
-      const int target = MODE == kLogits && row < sh.M ? g.h.target[g.h.first + row] : -1;
+      const int target = (MODE == kLogits || MODE == kD) && row < sh.M ? g.h.target[g.h.first + row] : -1;
       Sums sums;
       if (tl.i0 >= tl.i1) {  // a sum without terms
 #pragma unroll
@@ -496,6 +581,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       if (!ok) break;
       if constexpr (MODE == kLogits)
         end_logits(g, sh, tl, row, side, target, sums);
+      else if constexpr (MODE == kD)
+        end_d(g, sh, tl, row, side, target, sums);
       else
         end_tile<MODE>(g, sh, tl, row, side, sums);
     }
@@ -516,15 +603,15 @@ int tmap(CUtensorMap* tm, const void* base, uint64_t inner, uint64_t rows, uint6
 
 template <int MODE, int PARTS>
 cudaError_t launch_parts(const HeadTc& h, int most_m, int N, unsigned* status, cudaStream_t st) {
-  const size_t a_bytes = MODE == kDw ? kABytes : h.rows_box * 128u, stage = PARTS * (a_bytes + h.bn / 2 * 128u);
+  const size_t a_bytes = MODE == kDw ? kABytes : h.rows_box * 128u, stage = PARTS * a_bytes + (PARTS == 3 ? 3 : 1) * (h.bn / 2 * 128u);
   const size_t behind = kABytes - a_bytes;
   TcArgs g{h, (N + h.bn - 1) / h.bn, static_cast<int>(std::min<size_t>(kMostStages, (kRingBytes - behind) / stage)), status};
   CUtensorMap ta, tb;
-  const bool a_mn = MODE == kDw, b_mn = MODE != kLogits;
+  const bool a_mn = MODE == kDw, b_mn = MODE == kDx || MODE == kDw;
   if (tmap(&ta, h.A, h.inner_a, h.rows_a, h.lda, a_mn ? 64 : h.rows_box) ||
       tmap(&tb, h.B, h.inner_b, h.rows_b, h.ldb, b_mn ? 64 : h.bn / 2))
     return cudaErrorInvalidValue;
-  const long long tiles = static_cast<long long>((most_m + 255) / 256) * g.nN * (MODE == kLogits ? 1 : kMostSplits);
+  const long long tiles = static_cast<long long>((most_m + 255) / 256) * g.nN * (b_mn ? kMostSplits : 1);
   if (tiles > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
   const size_t smem = 1024 + g.stages * stage + behind + (2 * g.stages + 4) * 8 + 16;
   if (cudaError_t e = allow_smem(k_head_tc<MODE, PARTS>, smem); e != cudaSuccess) return e;
@@ -532,20 +619,21 @@ cudaError_t launch_parts(const HeadTc& h, int most_m, int N, unsigned* status, c
   return head_launch(k_head_tc<MODE, PARTS>, true, grid, kThreads, smem, st, ta, tb, g);
 }
 
-template <int MODE>
-cudaError_t launch(const HeadTc& h, int most_m, int N, unsigned* status, cudaStream_t st) {
-  return h.parts_b == 3 ? launch_parts<MODE, 3>(h, most_m, N, status, st)
-                        : launch_parts<MODE, 1>(h, most_m, N, status, st);
-}
-
 }  // namespace
 
 cudaError_t launch_head_logits(const HeadTc& h, unsigned* status, cudaStream_t st) {
-  return launch<kLogits>(h, h.piece_rows, h.V, status, st);
+  return h.used_a == 3 ? launch_parts<kLogits, 3>(h, h.piece_rows, h.V, status, st)
+                       : launch_parts<kLogits, 1>(h, h.piece_rows, h.V, status, st);
+}
+cudaError_t launch_head_d(const HeadTc& h, unsigned* status, cudaStream_t st) {
+  return launch_parts<kD, 1>(h, h.piece_rows, h.V, status, st);
 }
 cudaError_t launch_head_dx(const HeadTc& h, unsigned* status, cudaStream_t st) {
-  return launch<kDx>(h, h.piece_rows, h.d, status, st);
+  return h.used_a == 3 ? launch_parts<kDx, 3>(h, h.piece_rows, h.d, status, st)
+                       : launch_parts<kDx, 1>(h, h.piece_rows, h.d, status, st);
 }
 cudaError_t launch_head_dw(const HeadTc& h, unsigned* status, cudaStream_t st) {
-  return launch<kDw>(h, h.V, h.d, status, st);
+  return h.used_a == 3   ? launch_parts<kDw, 3>(h, h.V, h.d, status, st)
+         : h.used_a == 2 ? launch_parts<kDw, 2>(h, h.V, h.d, status, st)
+                         : launch_parts<kDw, 1>(h, h.V, h.d, status, st);
 }

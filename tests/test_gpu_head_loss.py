@@ -433,3 +433,47 @@ def test_refusals():
     with pytest.raises(E.EOGPError) as e:
         E.head_loss(x, W, tgt, ws=E.workspace(512, DEV))
     assert e.value.code == E.EWORKSPACE
+
+
+@pytest.mark.parametrize("B,T,d,V,dt,gdt", [
+    (2, 2600, 64, 400_000, BF, BF),   # D kept alone, in one part
+    (1, 2100, 1032, 600_000, BF, BF),  # wide rows: D in the logits' place
+    (1, 1500, 40, 300_001, F32, F32),
+])
+def test_pieces_of_each_form(B, T, d, V, dt, gdt):
+    """More than a piece holds in each of the forms that D is kept in; dW's sum over the pieces, and on top of old ones."""
+    x, W, tgt, w, ln = make(23, B, T, d, V, dt, ignored=0.01)
+    loss, lse, dx, dW = E.head_loss(x, W, tgt, dtype=gdt)
+    old = torch.randn((V, d), generator=gen(5), device=DEV).to(gdt)
+    acc = old.clone()
+    E.head_loss(x, W, tgt, dweight=acc, accumulate=True, want_dx=False)
+    counted = counted_of(x, tgt, None, None)
+    at = counted.nonzero()
+    dW64 = tol = 0.0
+    for i in range(0, at.shape[0], 550):
+        m = torch.zeros_like(counted)
+        b = at[i:i + 550]
+        m[b[:, 0], b[:, 1]] = True
+        r = reference(x, W, tgt, None, None, 1.0, dt, gdt, counted=m)
+        for got, name in ((loss, "loss"), (lse, "lse"), (dx, "dx")):
+            check(got[m], r[name][m], r["t" + name][m], name)
+        dW64, tol = dW64 + r["dW"], tol + r["tdW"] + chain(counted.sum().item()) * r["dW"].abs()
+    for got, before in ((dW, None), (acc, old)):
+        want, t = rounded(dict(dW=dW64, tdW=tol), before, gdt)
+        check(got, want, t, "dweight")
+
+
+@pytest.mark.parametrize("gdt", [BF, F32])
+@pytest.mark.parametrize("B,T,d,V", [(1, 2048, 64, 257), (3, 1000, 72, 1001), (2, 1030, 513, 700), (1, 2500, 768, 4099),
+                                     (4, 700, 1024, 321), (2, 1300, 1032, 511), (1, 2304, 8, 63)])
+def test_many_positions(B, T, d, V, gdt):
+    """Enough positions that the logits may be formed twice instead of kept, at widths on both sides of that choice."""
+    x, W, tgt, w, ln = make(B * T + d, B, T, d, V, BF, lengths=[T] + [T // 3] * (B - 1), weighted=True, ignored=0.1)
+    got = E.head_loss(x, W, tgt, scale=0.7, weights=w, lengths=ln, dtype=gdt)
+    check_all(got, reference(x, W, tgt, w, ln, 0.7, BF, gdt), gdt)
+    for a, b in zip(got, E.head_loss(x, W, tgt, scale=0.7, weights=w, lengths=ln, dtype=gdt)):
+        assert torch.equal(a, b)
+    few = tgt.clone()
+    few.view(-1)[5:] = IGNORE  # hardly any of them counted
+    got = E.head_loss(x, W, few, dtype=gdt, lengths=ln)
+    check_all(got, reference(x, W, few, None, ln, 1.0, BF, gdt), gdt)
