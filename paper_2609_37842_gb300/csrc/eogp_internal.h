@@ -331,6 +331,7 @@ struct HeadTc {
   int parts_d;
   const float2* row;
   const float* w;
+  float* rest;  // what rounding took from D at the row's target (its first part)
   // dx, by position
   RowSet rs;
   const int* idx;

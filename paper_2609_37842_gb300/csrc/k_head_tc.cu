@@ -35,6 +35,7 @@ constexpr int kThreads = 384;
 constexpr int kMostStages = 16;
 constexpr size_t kRingBytes = 221184;  // 6 stages of 32 KB, 3 of 72 KB
 constexpr uint32_t kABytes = 128u * 64u * 2u;
+constexpr int kNear = 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
 
@@ -253,8 +254,12 @@ __device__ __forceinline__ void end_d(const TcArgs& g, const Shape& s, const Til
       for (int e = 0; e < 32; ++e) v[e] = k * 32 + e < cols ? v[e] : 0.f;
     }
     if (static_cast<unsigned>(target - c0 - k * 32) < 32u) {
+      float at = 0.f;
 #pragma unroll
-      for (int e = 0; e < 32; ++e) v[e] -= target - c0 == k * 32 + e ? gt : 0.f;
+      for (int e = 0; e < 32; ++e) {
+        if (target - c0 == k * 32 + e) at = v[e] -= gt;
+      }
+      h.rest[row] = at - to_f32(from_f32<bf16>(at));
     }
     if (out < k * 32 + 32) continue;
     bf16* const o = D + static_cast<size_t>((c0 + k * 32) >> 6) * 64 * h.parts_d + (c0 + k * 32 & 63);
@@ -271,6 +276,136 @@ __device__ __forceinline__ void end_d(const TcArgs& g, const Shape& s, const Til
                                      v[q + 2 * e + 1] - __uint_as_float(w[e] & 0xffff0000u)));
       st_global_v8(o + 64 + q, w);
     }
+  }
+}
+
+// A thread's row and side of a tile with r times row `b` of the B operand added; r = 0: not.
+__device__ __forceinline__ void add_rest(const HeadTc& h, const Tile& t, int side, float r, long long b, Sums& sums) {
+  const int c0 = t.n0 + side * (h.bn / 2);
+  if (r == 0.f) return;
+  const bf16* const p = static_cast<const bf16*>(h.B) + b * static_cast<long long>(h.ldb) + c0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int left = h.d - c0 - k * 32;
+    if (k * 64 >= h.bn || left <= 0) continue;
+    if (left >= 32) {
+      Raw<bf16, 8> w[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) w[q] = ld_keep<bf16, 8>(p + k * 32 + q * 8);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const Vals<8> x = unpack<bf16, 8>(w[q]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums.v[k][q * 8 + e] = fmaf(r, x.get(e), sums.v[k][q * 8 + e]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 32; ++e)
+        if (e < left) sums.v[k][e] = fmaf(r, to_f32(p[k * 32 + e]), sums.v[k][e]);
+    }
+  }
+}
+
+// One rounding of D to bf16 tells most where it is largest, at the targets: a class whose gradient is one position's
+// would have two roundings in place of one. So what was rounded off there is added in fp32 (dW of 3,979 rows, 100,000
+// classes: FIG_REST).
+// That row's part of B is asked for ahead.
+__device__ __forceinline__ void ask_rest(const HeadTc& h, const Tile& t, int side, long long b) {
+  const int c0 = t.n0 + side * (h.bn / 2);
+  const bf16* const p = static_cast<const bf16*>(h.B) + b * static_cast<long long>(h.ldb) + c0;
+  for (int c = 0; c < min(h.bn / 2, h.d - c0); c += 64)
+    asm volatile("prefetch.global.L1 [%0];" ::"l"(__cvta_generic_to_global(p + c)));
+}
+// dW. Targets and rests of the first positions lie in shared memory.
+struct Near {
+  int target[kNear];
+  float rest[kNear];
+};
+struct Found {
+  unsigned bits;    // bit b of lane w: position r0 + w / 4 * 128 + b * 4 + w % 4 of 1024 has a class of the warp's 32
+  int mine;         // the first one of this lane's class, taken out of the bits; -1: none
+  Raw<bf16, 8> x[16];  // its row of x, on its way
+};
+__device__ __forceinline__ int position_of(int r0, int w, int b) { return r0 + (w >> 2) * 128 + b * 4 + (w & 3); }
+
+// Of 1024 positions from r0 on, below r1.
+__device__ __forceinline__ unsigned find_bits(const HeadTc& h, const Near& near, int row0, int r0, int r1) {
+  const int lane = threadIdx.x & 31;
+  unsigned bits = 0;
+  for (int i = 0; i < 8 && r0 + i * 128 < r1; ++i) {
+    const int r = r0 + i * 128 + lane * 4;
+    int4 t = make_int4(-1, -1, -1, -1);
+    if (r < r1) t = *reinterpret_cast<const int4*>(r < kNear ? &near.target[r] : &h.target[h.first + r]);
+    const int v[4] = {t.x, t.y, t.z, t.w};
+    bool hit[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) hit[e] = r + e < r1 && static_cast<unsigned>(v[e] - row0) < 32u;
+    if (!__any_sync(0xffffffffu, hit[0] || hit[1] || hit[2] || hit[3])) continue;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const unsigned found = __ballot_sync(0xffffffffu, hit[e]);
+      if (lane == i * 4 + e) bits = found;
+    }
+  }
+  return bits;
+}
+// Takes positions out of the bits, one a class at most, up to the first whose class has one.
+__device__ __forceinline__ int take_bits(const HeadTc& h, const Near& near, int row0, int r0, unsigned& bits) {
+  const int lane = threadIdx.x & 31;
+  int mine = -1;
+  for (unsigned words = __ballot_sync(0xffffffffu, bits != 0); words; words &= words - 1) {
+    const int w = __ffs(words) - 1;
+    for (unsigned left = __shfl_sync(0xffffffffu, bits, w); left; left &= left - 1) {
+      const int r = position_of(r0, w, __ffs(left) - 1);
+      const bool me = (r < kNear ? near.target[r] : h.target[h.first + r]) - row0 == lane;
+      if (__any_sync(0xffffffffu, me && mine >= 0)) return mine;
+      if (me) mine = r;
+      if (lane == w) bits &= bits - 1;
+    }
+  }
+  return mine;
+}
+// Before the sums are there: the first of them, whose rows are under way then.
+__device__ __forceinline__ void find_rest(const TcArgs& g, const Shape& s, const Tile& t, int row, int side, const Near& near,
+                                          Found& f) {
+  const HeadTc& h = g.h;
+  const int lane = threadIdx.x & 31, row0 = row - lane, r0 = t.i0 * 64;
+  f.bits = find_bits(h, near, row0, r0, min(s.rows, t.i1 * 64));
+  f.mine = take_bits(h, near, row0, r0, f.bits);
+  const int c0 = t.n0 + side * (h.bn / 2);
+  const bf16* const p = static_cast<const bf16*>(h.B) + f.mine * static_cast<long long>(h.ldb) + c0;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) {
+    f.x[q] = {};
+    if (f.mine >= 0 && q * 16 < h.bn && c0 + q * 8 < h.d) f.x[q] = ld_keep<bf16, 8>(p + q * 8);
+  }
+}
+// They are added in a fixed order, then the others. A class's next one waits for its last; a warp stops after a number of
+// such turns that its MMAs cover (many positions of one class, whose roundings go either way).
+__device__ __forceinline__ void add_rest_dw(const TcArgs& g, const Shape& s, const Tile& t, int row, int side,
+                                            const Near& near, Found& f, Sums& sums) {
+  const HeadTc& h = g.h;
+  const int row0 = row - static_cast<int>(threadIdx.x & 31), r1 = min(s.rows, t.i1 * 64);
+  auto rest_of = [&](int r) { return r < 0 ? 0.f : r < kNear ? near.rest[r] : h.rest[r]; };
+  if (__any_sync(0xffffffffu, f.mine >= 0)) {
+    const float r = rest_of(f.mine);
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      const Vals<8> x = unpack<bf16, 8>(f.x[q]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sums.v[q / 4][q % 4 * 8 + e] = fmaf(r, x.get(e), sums.v[q / 4][q % 4 * 8 + e]);
+    }
+  }
+  int turns = 4 + (t.i1 - t.i0) / 4;
+  for (int r0 = t.i0 * 64;;) {
+    while (turns > 0 && __any_sync(0xffffffffu, f.bits != 0)) {
+      const int mine = take_bits(h, near, row0, r0, f.bits);
+      add_rest(h, t, side, rest_of(mine), mine, sums);
+      --turns;
+    }
+    r0 += 1024;
+    if (r0 >= r1 || turns <= 0) break;
+    f.bits = find_bits(h, near, row0, r0, r1);
   }
 }
 
@@ -379,6 +514,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   uint64_t* tfull = empty + stages;
   uint64_t* tempty = tfull + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
+  Near& near = *reinterpret_cast<Near*>(tmem_slot + 4);
   const uint32_t buf_cols = static_cast<uint32_t>(g.h.bn) * (PARTS == 3 ? 2u : 1u);
   constexpr uint32_t tcols = 512;
   const int cl = blockIdx.x >> 1, ncl = gridDim.x >> 1;
@@ -548,6 +684,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
     const int q = warp & 3, side = (warp - 4) >> 2;
+    if (MODE == kDw && PARTS == 1) {
+      for (int r = threadIdx.x - 128; r < min(kNear, sh.rows); r += 256) {
+        near.target[r] = g.h.target[g.h.first + r];
+        near.rest[r] = g.h.rest[r];
+      }
+      named_bar_sync(1, 256);
+    }
     int i = 0;
     bool ok = true;
     for (int t = cl; t < sh.tiles && ok; t += ncl) {
@@ -555,7 +698,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const int row = tl.m0 + static_cast<int>(rank) * 128 + q * 32 + lane;
       const uint32_t lanes = tmem + (static_cast<uint32_t>(q * 32) << 16);
       // Asked for before the accumulator is waited for.
-      const int target = (MODE == kLogits || MODE == kD) && row < sh.M ? g.h.target[g.h.first + row] : -1;
+      const bool one = MODE == kLogits || MODE == kD || (MODE == kDx && PARTS == 1 && tl.split == 0);
+      const int target = one && row < sh.M ? g.h.target[g.h.first + row] : -1;
+      float rest = 0.f;
+      if (MODE == kDx && target >= 0) {
+        rest = g.h.rest[row];
+        ask_rest(g.h, tl, side, target);
+      }
+      Found found;
+      if constexpr (MODE == kDw && PARTS == 1) find_rest(g, sh, tl, row, side, near, found);
       Sums sums;
       if (tl.i0 >= tl.i1) {  // a sum without terms
 #pragma unroll
@@ -583,8 +734,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         end_logits(g, sh, tl, row, side, target, sums);
       else if constexpr (MODE == kD)
         end_d(g, sh, tl, row, side, target, sums);
-      else
+      else {
+        if constexpr (MODE == kDx && PARTS == 1) add_rest(g.h, tl, side, rest, target, sums);
+        if constexpr (MODE == kDw && PARTS == 1) add_rest_dw(g, sh, tl, row, side, near, found, sums);
         end_tile<MODE>(g, sh, tl, row, side, sums);
+      }
     }
   }
   tc_fence_before();
@@ -604,7 +758,7 @@ int tmap(CUtensorMap* tm, const void* base, uint64_t inner, uint64_t rows, uint6
 template <int MODE, int PARTS>
 cudaError_t launch_parts(const HeadTc& h, int most_m, int N, unsigned* status, cudaStream_t st) {
   const size_t a_bytes = MODE == kDw ? kABytes : h.rows_box * 128u, stage = PARTS * a_bytes + (PARTS == 3 ? 3 : 1) * (h.bn / 2 * 128u);
-  const size_t behind = kABytes - a_bytes;
+  const size_t behind = (kABytes - a_bytes) + (MODE == kDw && PARTS == 1 ? sizeof(Near) : 0);  // the ring
   TcArgs g{h, (N + h.bn - 1) / h.bn, static_cast<int>(std::min<size_t>(kMostStages, (kRingBytes - behind) / stage)), status};
   CUtensorMap ta, tb;
   const bool a_mn = MODE == kDw, b_mn = MODE == kDx || MODE == kDw;

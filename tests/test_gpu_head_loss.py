@@ -90,8 +90,8 @@ def counted_of(x, tgt, w, ln):
     return c
 
 
-def reference(x, W, tgt, w, ln, scale, dt, gdt, counted=None):
-    """Results and tolerances, positions left out at 0."""
+def reference(x, W, tgt, w, ln, scale, dt, gdt, counted=None, whole_targets=False):
+    """Results and tolerances, positions left out at 0. whole_targets: without a rounding of D at the targets."""
     counted = counted_of(x, tgt, w, ln) if counted is None else counted
     B, T, d = x.shape
     V = W.shape[0]
@@ -116,6 +116,10 @@ def reference(x, W, tgt, w, ln, scale, dt, gdt, counted=None):
     tD = exact_D + (VB if dt == BF else U) * (D.abs() + exact_D)
     part = VB if dt == BF and gdt == BF else VB * VB if dt == BF else U
     tDw = exact_D + part * (D.abs() + exact_D)
+    if whole_targets:
+        tD[rows, t] = exact_D[rows, t] + U * D[rows, t].abs()
+        if gdt == BF:  # else two parts, both rounded: v^2 |D| as everywhere
+            tDw[rows, t] = tD[rows, t]
     dx = D @ W64
     tdx = tD @ W64.abs() + chain(V) * (D.abs() @ W64.abs())
     tdx = tdx + out_u(dt) * (dx.abs() + tdx)
@@ -477,3 +481,25 @@ def test_many_positions(B, T, d, V, gdt):
     few.view(-1)[5:] = IGNORE  # hardly any of them counted
     got = E.head_loss(x, W, few, dtype=gdt, lengths=ln)
     check_all(got, reference(x, W, few, None, ln, 1.0, BF, gdt), gdt)
+
+
+@pytest.mark.parametrize("gdt", [BF, F32])
+@pytest.mark.parametrize("B,T,d,V", [(1, 1, 64, 500), (1, 60, 72, 4099), (2, 300, 770, 2000), (1, 511, 768, 30_001),
+                                     (1, 2300, 136, 9000), (3, 900, 1032, 8191)])
+def test_targets_are_not_rounded(B, T, d, V, gdt):
+    """D's largest entry in a row, at the target, enters dx and a dW of bf16 as in fp32: rounded to bf16 and the rest
+    added; a dW of fp32 in two parts (a few positions a class here, fewer than a dW of bf16 has turns for)."""
+    x, W, tgt, w, ln = make(B * T + d + 3, B, T, d, V, BF, weighted=True, ignored=0.1 * (T > 8))
+    tgt = torch.where(tgt == IGNORE, tgt, torch.randperm(V, generator=gen(1), device=DEV).repeat(2)[:B * T].view(B, T))
+    ref = reference(x, W, tgt, w, ln, 1.0, BF, gdt, whole_targets=True)
+    check_all(E.head_loss(x, W, tgt, weights=w, dtype=gdt), ref, gdt)
+
+
+def test_one_class_for_all():
+    """Every position has the same target: more positions of a class than have their own turn."""
+    x, W, tgt, _, _ = make(24, 2, 1000, 64, 1000, BF)
+    tgt.fill_(777)
+    got = E.head_loss(x, W, tgt)
+    check_all(got, reference(x, W, tgt, None, None, 1.0, BF, BF), BF)
+    for a, b in zip(got, E.head_loss(x, W, tgt)):
+        assert torch.equal(a, b)
