@@ -67,8 +67,8 @@ Plan plan_of(const HeadArgs& a) {
   // Narrow rows: the logits are not kept, D is formed from them where they are computed a second time. That costs
   // 2 d operations a logit and spares 8 bytes of traffic, 6 where D has one part (us, kept / formed again, dW in
   // bf16: 16,384 rows of 64 columns, 50,000 classes 2,404 / 1,334; of 768 3,390 / 3,111, of 1024 4,047 / 4,104, of
-  // 1536 5,608 / 6,229; 511 rows of 768 171 / 163). For few rows the matrix, read once more, counts too.
-  p.again = grad && a.bf16 && M >= kAgainRows && a.d <= std::min<long long>(kAgainWidth, 2 * M);
+  // 1536 5,608 / 6,229; 511 rows of 256 124 / 101, of 768 169 / 173). For few rows the matrix, read once more, counts too.
+  p.again = grad && a.bf16 && M >= kAgainRows && a.d <= std::min<long long>(kAgainWidth, M);
   // A row of a piece: logits (and D, where it is not in their place), or the sums of its half tiles; and the gathered row.
   const size_t row_bytes = static_cast<size_t>(p.ldx) * 2 + (grad ? static_cast<size_t>(p.ldz) * (p.again ? p.parts * 2 : a.bf16 ? 4 : 10) : 0) +
                            p.ldz / 64 * 16;

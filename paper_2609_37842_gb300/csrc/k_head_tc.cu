@@ -309,23 +309,47 @@ __device__ __forceinline__ void add_rest(const HeadTc& h, const Tile& t, int sid
 // One rounding of D to bf16 tells most where it is largest, at the targets: a class whose gradient is one position's
 // would have two roundings in place of one. So what was rounded off there is added in fp32 (dW of 3,979 rows, 100,000
 // classes: FIG_REST).
-// That row's part of B is asked for ahead.
-__device__ __forceinline__ void ask_rest(const HeadTc& h, const Tile& t, int side, long long b) {
-  const int c0 = t.n0 + side * (h.bn / 2);
-  const bf16* const p = static_cast<const bf16*>(h.B) + b * static_cast<long long>(h.ldb) + c0;
-  for (int c = 0; c < min(h.bn / 2, h.d - c0); c += 64)
-    asm volatile("prefetch.global.L1 [%0];" ::"l"(__cvta_generic_to_global(p + c)));
-}
-// dW. Targets and rests of the first positions lie in shared memory.
+// dx: a thread's row has one target. dW: targets and rests of the first positions lie in shared memory.
 struct Near {
   int target[kNear];
   float rest[kNear];
 };
+// What is added first, found before the sums are there.
 struct Found {
-  unsigned bits;    // bit b of lane w: position r0 + w / 4 * 128 + b * 4 + w % 4 of 1024 has a class of the warp's 32
-  int mine;         // the first one of this lane's class, taken out of the bits; -1: none
-  Raw<bf16, 8> x[16];  // its row of x, on its way
+  unsigned bits;       // dW: bit b of lane w: position r0 + w / 4 * 128 + b * 4 + w % 4 of 1024 has a class of the warp's 32
+  int mine;            // row of B: dx: the target; dW: the first position of the lane's class, taken out of the bits; -1: none
+  float rest;
+  Raw<bf16, 8> x[16];  // that row's part, on its way
 };
+__device__ __forceinline__ void ask_rest(const HeadTc& h, const Tile& t, int side, Found& f) {
+  const int c0 = t.n0 + side * (h.bn / 2);
+  const bf16* const p = static_cast<const bf16*>(h.B) + f.mine * static_cast<long long>(h.ldb) + c0;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) {
+    f.x[q] = {};
+    const int left = q * 16 < h.bn ? h.d - c0 - q * 8 : 0;
+    if (f.mine < 0 || left <= 0) continue;
+    if (left >= 8) {
+      f.x[q] = ld_keep<bf16, 8>(p + q * 8);
+    } else {
+      // A row's end: what lies behind it may not be there.
+      uint32_t w[4] = {};
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (e < left) w[e / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(p[q * 8 + e])) << (e & 1) * 16;
+      f.x[q].w = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+__device__ __forceinline__ void add_found(const Found& f, Sums& sums) {
+  if (!__any_sync(0xffffffffu, f.mine >= 0)) return;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) {
+    const Vals<8> x = unpack<bf16, 8>(f.x[q]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums.v[q / 4][q % 4 * 8 + e] = fmaf(f.rest, x.get(e), sums.v[q / 4][q % 4 * 8 + e]);
+  }
+}
 __device__ __forceinline__ int position_of(int r0, int w, int b) { return r0 + (w >> 2) * 128 + b * 4 + (w & 3); }
 
 // Of 1024 positions from r0 on, below r1.
@@ -365,42 +389,27 @@ __device__ __forceinline__ int take_bits(const HeadTc& h, const Near& near, int 
   }
   return mine;
 }
-// Before the sums are there: the first of them, whose rows are under way then.
-__device__ __forceinline__ void find_rest(const TcArgs& g, const Shape& s, const Tile& t, int row, int side, const Near& near,
-                                          Found& f) {
-  const HeadTc& h = g.h;
-  const int lane = threadIdx.x & 31, row0 = row - lane, r0 = t.i0 * 64;
-  f.bits = find_bits(h, near, row0, r0, min(s.rows, t.i1 * 64));
-  f.mine = take_bits(h, near, row0, r0, f.bits);
-  const int c0 = t.n0 + side * (h.bn / 2);
-  const bf16* const p = static_cast<const bf16*>(h.B) + f.mine * static_cast<long long>(h.ldb) + c0;
-#pragma unroll
-  for (int q = 0; q < 16; ++q) {
-    f.x[q] = {};
-    if (f.mine >= 0 && q * 16 < h.bn && c0 + q * 8 < h.d) f.x[q] = ld_keep<bf16, 8>(p + q * 8);
-  }
+__device__ __forceinline__ float rest_of(const HeadTc& h, const Near& near, int r) {
+  return r < 0 ? 0.f : r < kNear ? near.rest[r] : h.rest[r];
 }
-// They are added in a fixed order, then the others. A class's next one waits for its last; a warp stops after a number of
+__device__ __forceinline__ void find_rest(const TcArgs& g, const Shape& s, const Tile& t, int row, const Near& near,
+                                          Found& f) {
+  const int row0 = row - static_cast<int>(threadIdx.x & 31), r0 = t.i0 * 64;
+  f.bits = find_bits(g.h, near, row0, r0, min(s.rows, t.i1 * 64));
+  f.mine = take_bits(g.h, near, row0, r0, f.bits);
+  f.rest = rest_of(g.h, near, f.mine);
+}
+// The others, in a fixed order. A class's next one waits for its last; a warp stops after a number of
 // such turns that its MMAs cover (many positions of one class, whose roundings go either way).
 __device__ __forceinline__ void add_rest_dw(const TcArgs& g, const Shape& s, const Tile& t, int row, int side,
                                             const Near& near, Found& f, Sums& sums) {
   const HeadTc& h = g.h;
   const int row0 = row - static_cast<int>(threadIdx.x & 31), r1 = min(s.rows, t.i1 * 64);
-  auto rest_of = [&](int r) { return r < 0 ? 0.f : r < kNear ? near.rest[r] : h.rest[r]; };
-  if (__any_sync(0xffffffffu, f.mine >= 0)) {
-    const float r = rest_of(f.mine);
-#pragma unroll
-    for (int q = 0; q < 16; ++q) {
-      const Vals<8> x = unpack<bf16, 8>(f.x[q]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sums.v[q / 4][q % 4 * 8 + e] = fmaf(r, x.get(e), sums.v[q / 4][q % 4 * 8 + e]);
-    }
-  }
   int turns = 4 + (t.i1 - t.i0) / 4;
   for (int r0 = t.i0 * 64;;) {
     while (turns > 0 && __any_sync(0xffffffffu, f.bits != 0)) {
       const int mine = take_bits(h, near, row0, r0, f.bits);
-      add_rest(h, t, side, rest_of(mine), mine, sums);
+      add_rest(h, t, side, rest_of(h, near, mine), mine, sums);
       --turns;
     }
     r0 += 1024;
@@ -700,13 +709,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       // Asked for before the accumulator is waited for.
       const bool one = MODE == kLogits || MODE == kD || (MODE == kDx && PARTS == 1 && tl.split == 0);
       const int target = one && row < sh.M ? g.h.target[g.h.first + row] : -1;
-      float rest = 0.f;
-      if (MODE == kDx && target >= 0) {
-        rest = g.h.rest[row];
-        ask_rest(g.h, tl, side, target);
-      }
       Found found;
-      if constexpr (MODE == kDw && PARTS == 1) find_rest(g, sh, tl, row, side, near, found);
+      if constexpr (PARTS == 1 && (MODE == kDx || MODE == kDw)) {
+        if (MODE == kDw) {
+          find_rest(g, sh, tl, row, near, found);
+        } else {
+          found.mine = target;
+          found.rest = target >= 0 ? g.h.rest[row] : 0.f;
+        }
+        if (found.rest == 0.f) found.mine = -1;
+        ask_rest(g.h, tl, side, found);
+      }
       Sums sums;
       if (tl.i0 >= tl.i1) {  // a sum without terms
 #pragma unroll
@@ -735,7 +748,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       else if constexpr (MODE == kD)
         end_d(g, sh, tl, row, side, target, sums);
       else {
-        if constexpr (MODE == kDx && PARTS == 1) add_rest(g.h, tl, side, rest, target, sums);
+        if constexpr (PARTS == 1) add_found(found, sums);
         if constexpr (MODE == kDw && PARTS == 1) add_rest_dw(g, sh, tl, row, side, near, found, sums);
         end_tile<MODE>(g, sh, tl, row, side, sums);
       }
