@@ -666,7 +666,9 @@ int eogp_cross_entropy(const void* logits, int dtype, long long logits_bs, long 
  * only where 256 positions take more); without one none are stored.
  * EOGP_BF16: products of bf16 on the tensor cores, sums in fp32. D enters the products for dx, and
  * for a dweight of EOGP_BF16, rounded to bf16, as dlogits of eogp_cross_entropy would; for one of
- * EOGP_F32 it enters as two bf16 parts (about 2^-16 relative). EOGP_F32: products to fp32.
+ * EOGP_F32 it enters as two bf16 parts (about 2^-16 relative). What that takes from the target's
+ * entry is added in fp32 (to a row of dweight for a limited number of its class's positions, the same
+ * ones every time). EOGP_F32: products to fp32.
  * A NaN or infinity in a counted position's x, or in weight, reaches all that it is multiplied
  * with: that position's loss, and dx or dweight. */
 int eogp_head_loss_workspace_size(const void* weight, int dtype, long long ld_weight, int V, int d, int B, int T,
@@ -692,7 +694,8 @@ int eogp_head_loss(const void* x, int dtype, long long x_bs, long long x_ld, con
  *   lse[b][t] = log sum_v exp(x_v / h),
  *   dlogits[b][t] = (w / h) * (p - q) at listed classes and (w / h) * p * (1 - q_r / p_r), without
  *     teacher_lse (w / h) * p, at the others.
- * Where a list holds all V classes there is no such class more. Terms of q = 0 are 0. Multiply the weights by h^2 for the usual scaling of softened targets.
+ * Where a list holds all V classes there is no such class more. Terms of q = 0 are 0. Multiply the
+ * weights by h^2 for the usual scaling of softened targets.
  * A class that is listed twice counts as one entry with the sum of both q in the gradient, and as two
  * in the loss. A position is left out (loss, lse and gradient 0, whatever its logits hold)
  * when it is padding, when its weight is 0, or, without teacher_lse, when no entry has a logit above -inf; a class

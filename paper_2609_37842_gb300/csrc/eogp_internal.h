@@ -325,13 +325,12 @@ struct HeadTc {
   float2* part;
   float* zt;
   const int* target;
-  bool early;  // 256 rows at most, and B is as it was before the call
   // D of logits that are not kept: [piece x ldz * parts_d], of a row's maximum and w scale / sum
   void* D;
   int parts_d;
   const float2* row;
   const float* w;
-  float* rest;  // what rounding took from D at the row's target (its first part)
+  float *rest, *rest_w;  // what is left of D at the row's target: after its first part, for dx; after all parts, for dW
   // dx, by position
   RowSet rs;
   const int* idx;

@@ -44,7 +44,7 @@ struct Plan {
   int bn_z, bn_d;              // columns of a tile of the logits, of dx and dW
   int ld_slab;
   size_t slab_bytes;
-  size_t counts, idx, target, w, x, z, D, acc, W, part, zt, row, rest, slabs, total;
+  size_t counts, idx, target, w, x, z, D, acc, W, part, zt, row, rest, rest_w, slabs, total;
 };
 
 bool w_fits(const HeadArgs& a) {
@@ -101,7 +101,8 @@ Plan plan_of(const HeadArgs& a) {
   p.part = take(static_cast<size_t>((a.V + p.bn_z - 1) / p.bn_z) * 2 * p.piece * 8);
   p.zt = take(static_cast<size_t>(p.piece) * 4);
   p.row = take(static_cast<size_t>(p.piece) * 8);
-  p.rest = take(static_cast<size_t>(p.piece) * 4);
+  p.rest = p.rest_w = take(static_cast<size_t>(p.piece) * 4);
+  if (p.parts == 2) p.rest_w = take(static_cast<size_t>(p.piece) * 4);
   if (grad) {
     if (!p.again) p.z = take(static_cast<size_t>(p.piece) * p.ldz * 4);
     if (!a.bf16 || p.again) p.D = take(static_cast<size_t>(p.piece) * p.ldz * p.parts * 2);
@@ -380,7 +381,8 @@ __global__ void __launch_bounds__(1024) k_head_join(const HeadArgs a, const int*
 template <int PARTS>
 __global__ void __launch_bounds__(256) k_head_d(const HeadArgs a, const int* counts, const int* targets,
                                                 const float* ws, int first, int piece, float* z, int ldz,
-                                                const float2* row, bf16* D, float* rest) {
+                                                const float2* row, bf16* D, float* rest,
+                                                float* rest_w) {
   after_previous();
   const int n = min(piece, counts[kFindBlocks] - first), n64 = (max(n, 0) + 63) & ~63;
   const unsigned segments = (ldz + kDSegment - 1) / kDSegment, items = n64 * segments;
@@ -413,7 +415,11 @@ __global__ void __launch_bounds__(256) k_head_d(const HeadArgs a, const int* cou
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             if (target - c == e) at = v.get(e);
-          if (PARTS < 3) rest[i] = at - to_f32(from_f32<bf16>(at));
+          if (PARTS < 3) {
+            const float left = at - to_f32(from_f32<bf16>(at));
+            rest[i] = left;
+            if (PARTS == 2) rest_w[i] = left - to_f32(from_f32<bf16>(left));
+          }
         }
       }
       __syncwarp();
@@ -563,6 +569,7 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
   h.part = reinterpret_cast<float2*>(ws + p.part);
   h.zt = reinterpret_cast<float*>(ws + p.zt);
   h.rest = reinterpret_cast<float*>(ws + p.rest);
+  h.rest_w = reinterpret_cast<float*>(ws + p.rest_w);
   h.target = target;
   h.rs = a.rs;
   h.idx = idx;
@@ -585,7 +592,6 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
     z.A = x, z.inner_a = xcols, z.rows_a = rows, z.lda = p.ldx;
     z.B = W, z.inner_b = xcols, z.rows_b = uv, z.ldb = ldw;
     z.bn = p.bn_z, z.run = 8;
-    z.early = w_fits(a) && h.piece_rows <= 256;
     TRY(launch_head_logits(z, status, st));
     TRY(head_launch(k_head_join, true, (p.piece + 31) / 32, 1024, 0, st, a, counts, idx, w, h.first, p.piece, h.part,
                     (a.V + p.bn_z - 1) / p.bn_z * 2, h.zt, grad ? row : nullptr));
@@ -598,7 +604,7 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
       auto d = f32 ? k_head_d<3> : p.parts == 2 ? k_head_d<2> : k_head_d<1>;
       const long long segments = static_cast<long long>(p.piece) * ((p.ldz + kDSegment - 1) / kDSegment);
       TRY(head_launch(d, true, std::min<long long>(segments, num_sms * 8), 256, 0, st, a, counts, target, w, h.first,
-                      p.piece, h.z, p.ldz, row, D, h.rest));
+                      p.piece, h.z, p.ldz, row, D, h.rest, h.rest_w));
     }
     if (a.dx.p) {
       HeadTc g = h;

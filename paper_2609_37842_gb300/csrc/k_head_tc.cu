@@ -20,7 +20,9 @@
 // take over registers from the first four (168 x 384 = 56 x 128 + 224 x 256).
 // Every wait is bounded; after one that ran out each role goes to the common end.
 //
-// 3,979 rows, 4096 columns, 100,000 classes: z FIG_Z, dx FIG_DX, dW FIG_DW, each alone; in a row they meet the power limit.
+// 875 rows, 4096 columns, 50,000 classes: z 457 us, dx 404, dW 416 (73, 85, 74 % of the tensor cores' cycles) at 15 to
+// 17 TB/s from L2 to shared memory, which bounds them; dW of two parts, with 3/4 of those bytes a product, 96 %. Many
+// such launches in a row meet the power limit.
 // Tried without gain: operands asked for in L2 ten steps ahead (7.2 against 6.7 ms for that batch), a thread of its
 // own for each operand's copies.
 #include <algorithm>
@@ -259,7 +261,9 @@ __device__ __forceinline__ void end_d(const TcArgs& g, const Shape& s, const Til
       for (int e = 0; e < 32; ++e) {
         if (target - c0 == k * 32 + e) at = v[e] -= gt;
       }
-      h.rest[row] = at - to_f32(from_f32<bf16>(at));
+      const float rest = at - to_f32(from_f32<bf16>(at));
+      h.rest[row] = rest;
+      if (h.parts_d == 2) h.rest_w[row] = rest - to_f32(from_f32<bf16>(rest));
     }
     if (out < k * 32 + 32) continue;
     bf16* const o = D + static_cast<size_t>((c0 + k * 32) >> 6) * 64 * h.parts_d + (c0 + k * 32 & 63);
@@ -307,8 +311,8 @@ __device__ __forceinline__ void add_rest(const HeadTc& h, const Tile& t, int sid
 }
 
 // One rounding of D to bf16 tells most where it is largest, at the targets: a class whose gradient is one position's
-// would have two roundings in place of one. So what was rounded off there is added in fp32 (dW of 3,979 rows, 100,000
-// classes: FIG_REST).
+// would have two roundings in place of one. So what was rounded off there is added in fp32 (3,979 rows,
+// 100,000 classes: 0.0017 of dW's and dx's norms off float64, 0.0024 without; 447 rows of 768 columns: 10 of 171 us).
 // dx: a thread's row has one target. dW: targets and rests of the first positions lie in shared memory.
 struct Near {
   int target[kNear];
@@ -390,7 +394,7 @@ __device__ __forceinline__ int take_bits(const HeadTc& h, const Near& near, int 
   return mine;
 }
 __device__ __forceinline__ float rest_of(const HeadTc& h, const Near& near, int r) {
-  return r < 0 ? 0.f : r < kNear ? near.rest[r] : h.rest[r];
+  return r < 0 ? 0.f : r < kNear ? near.rest[r] : h.rest_w[r];
 }
 __device__ __forceinline__ void find_rest(const TcArgs& g, const Shape& s, const Tile& t, int row, const Near& near,
                                           Found& f) {
@@ -547,18 +551,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  // Rows of one tile at most, and a matrix that no launch of this call writes: the first copies of it are under way
-  // before the rows are there. (One row, 50,000 x 768: FIG_EARLY.)
-  int early = 0;  // stages whose B comes already
-  if (MODE == kLogits && PARTS == 1 && g.h.early && threadIdx.x == 0) {
-    const int steps = (g.h.d + 63) / 64;
-    const uint32_t full0 = mapa_shared(smem_u32(full), 0);
-    for (int t = cl, i = 0; early < stages && t < g.nN; ++early) {
-      tma_load_2d_pair(smem_u32(smem) + early * stage_bytes + b_at, &tmB, i * 64,
-                       t * g.h.bn + static_cast<int>(rank) * half, full0 + early * 8);
-      if (++i == steps) i = 0, t += ncl;
-    }
-  }
   after_previous();
   const Shape sh = shape_of<MODE>(g);
 
@@ -574,12 +566,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       int s = 0;
       uint32_t ph = 1;
       bool ok = true;
-      if (sh.tiles == 0) {  // no rows
-        for (int k = 0; k < early; ++k) {
-          mbar_arrive_expect_tx_cluster(full0 + k * 8, b_bytes);
-          if (rank == 0 && !mbar_wait(&full[k], 0, g.status)) break;
-        }
-      }
       for (int t = cl; t < sh.tiles && ok; t += ncl) {
         const Tile tl = tile_of<MODE>(g, sh, t);
         const int am = tl.m0 + static_cast<int>(rank) * 128, bn = tl.n0 + static_cast<int>(rank) * half;
@@ -602,10 +588,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               tma_load_2d_pair(a, &tmA, i * ai + q * 64, am, fl);
             }
           }
-          const bool comes = early > 0;
-          early -= comes;
 #pragma unroll
-          for (int q = 0; q < kPartsB && !comes; ++q) {
+          for (int q = 0; q < kPartsB; ++q) {
             const uint32_t b = st + b_at + q * b_bytes;
             if (kBmn) {
               tma_load_2d_pair(b, &tmB, bc + q * 64, i * 64, fl);
@@ -693,10 +677,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
     const int q = warp & 3, side = (warp - 4) >> 2;
-    if (MODE == kDw && PARTS == 1) {
+    if (MODE == kDw && PARTS < 3) {
       for (int r = threadIdx.x - 128; r < min(kNear, sh.rows); r += 256) {
         near.target[r] = g.h.target[g.h.first + r];
-        near.rest[r] = g.h.rest[r];
+        near.rest[r] = g.h.rest_w[r];
       }
       named_bar_sync(1, 256);
     }
@@ -710,7 +694,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const bool one = MODE == kLogits || MODE == kD || (MODE == kDx && PARTS == 1 && tl.split == 0);
       const int target = one && row < sh.M ? g.h.target[g.h.first + row] : -1;
       Found found;
-      if constexpr (PARTS == 1 && (MODE == kDx || MODE == kDw)) {
+      if constexpr (PARTS < 3 && (MODE == kDx || MODE == kDw)) {
         if (MODE == kDw) {
           find_rest(g, sh, tl, row, near, found);
         } else {
@@ -748,8 +732,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       else if constexpr (MODE == kD)
         end_d(g, sh, tl, row, side, target, sums);
       else {
-        if constexpr (PARTS == 1) add_found(found, sums);
-        if constexpr (MODE == kDw && PARTS == 1) add_rest_dw(g, sh, tl, row, side, near, found, sums);
+        if constexpr (PARTS < 3) add_found(found, sums);
+        if constexpr (MODE == kDw && PARTS < 3) add_rest_dw(g, sh, tl, row, side, near, found, sums);
         end_tile<MODE>(g, sh, tl, row, side, sums);
       }
     }
@@ -771,7 +755,7 @@ int tmap(CUtensorMap* tm, const void* base, uint64_t inner, uint64_t rows, uint6
 template <int MODE, int PARTS>
 cudaError_t launch_parts(const HeadTc& h, int most_m, int N, unsigned* status, cudaStream_t st) {
   const size_t a_bytes = MODE == kDw ? kABytes : h.rows_box * 128u, stage = PARTS * a_bytes + (PARTS == 3 ? 3 : 1) * (h.bn / 2 * 128u);
-  const size_t behind = (kABytes - a_bytes) + (MODE == kDw && PARTS == 1 ? sizeof(Near) : 0);  // the ring
+  const size_t behind = (kABytes - a_bytes) + (MODE == kDw && PARTS < 3 ? sizeof(Near) : 0);  // the ring
   TcArgs g{h, (N + h.bn - 1) / h.bn, static_cast<int>(std::min<size_t>(kMostStages, (kRingBytes - behind) / stage)), status};
   CUtensorMap ta, tb;
   const bool a_mn = MODE == kDw, b_mn = MODE == kDx || MODE == kDw;

@@ -503,3 +503,17 @@ def test_one_class_for_all():
     check_all(got, reference(x, W, tgt, None, None, 1.0, BF, BF), BF)
     for a, b in zip(got, E.head_loss(x, W, tgt)):
         assert torch.equal(a, b)
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, one after the other on the host, each with a workspace of its own."""
+    sets = [make(30 + k, 2, 400, 256, 3000, (BF, F32)[k], lengths=[400, 100 + k]) for k in range(2)]
+    want = [E.head_loss(x, W, tgt, lengths=ln) for x, W, tgt, _, ln in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(5):
+        got = [E.head_loss(x, W, tgt, lengths=ln, stream=s) for (x, W, tgt, _, ln), s in zip(sets, streams)]
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            for a, b in zip(g, w):
+                assert torch.equal(a, b)
