@@ -6,10 +6,11 @@
 // with a given log-sum the classes not listed are one more class on both sides,
 //   q_r = max(0, 1 - sum q_k), p_r = sum of their p: loss += w q_r (log q_r - log p_r), and
 //   dx = (w / h) p (1 - q_r / p_r) for them.
-// The sum over the classes not listed has its own maximum m_r, and so log p_r has all its digits; with
-// e = 2^(x f - c), f = log2(e) / h, c = m_r f, and s_r = sum e over those classes,
-// dx = (w / h) (p_r - q_r) e / s_r there, whatever the sizes: p_r is no difference, and may be too
-// small for a float.
+// The sum over the classes not listed has its own maximum m_r, and that over the listed ones theirs, m_l; the
+// difference m_l - m_r is formed before it is scaled, and logarithms are taken against the larger of the two: each
+// keeps all its digits however far the two lie apart. With e = 2^(x f - c), f = log2(e) / h, c = m_r f rounded, and
+// s_r = sum e over the classes not listed, dx = (w / h) (p_r - q_r) e / s_r there, whatever the sizes: p_r is no
+// difference, and may be too small for a float.
 //
 // HBM-bound: a row is read once and its gradient written once.
 // k_distill: a row lies in the shared memory of a CTA, or in slices in that of the CTAs
@@ -436,16 +437,21 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
         if (GRAD)
           for (int i = tid; i < next.n; i += nt) ask(next, i);
       } else {
-        // Logarithms to base 2 against c: of the list's maximum, of the sum over all classes, of the remainder's share.
-        const float c = ref(v.m, f), to_list = fmaf(l.m, f, -c), top = fmaxf(0.f, to_list);
-        const float ls = top + log2f(l.s * exp2_fast(to_list - top) + v.s * exp2_fast(-top)), log_r = log2f(v.s) - ls;
+        // The larger of the list's maximum and the others', and how far each lies below it; logarithms to base 2
+        // against it: of the sum over all classes, `ls`, and of that over the others, 2^(log_s + to_rest log2(e)), which
+        // knows what c was rounded by.
+        const float c = ref(v.m, f), gap = (l.m - v.m) * inv_h, to_list = fminf(gap, 0.f), to_rest = fminf(-gap, 0.f);
+        const float log_s = log2f(v.s) + fmaf(-v.m, f, c);
+        const float ls = log2f(l.s * exp2_fast(to_list * kLog2e) + exp2_fast(fmaf(to_rest, kLog2e, log_s)));
+        const float log_pr = fmaf(kLn2, log_s - ls, to_rest);
         const float q_r = a.teacher_lse && !l.whole ? fmaxf(0.f, 1.f - l.sum) : 0.f;
         if (tid == 0 && first_cta)
-          put_loss(a, r, p.j.w * (list_loss(l, kLn2 * (ls - to_list)) + term(q_r, logf(q_r), kLn2 * log_r)),
-                   kLn2 * (c + ls));
+          put_loss(a, r, p.j.w * (list_loss(l, fmaf(kLn2, ls, -to_list)) + term(q_r, logf(q_r), log_pr)),
+                   fmaf(kLn2, ls, fmaxf(l.m, v.m) * inv_h));
         if (GRAD) {
           const RowVecs<T> out(g, a.V);
-          const float wt = p.j.w * inv_h, to = wt * (exp2_fast(log_r) - q_r) / v.s;
+          const float wt = p.j.w * inv_h, to = wt * (expf(log_pr) - q_r) / v.s;
+          const float at = fmaf(to_list, kLog2e, -ls);
           if (ce >= 0) g[ce] = from_f32<T>(exp2_fast(fmaf(xe, f, -c)) * to);
           if (out.ph == p.row.ph) {
             T* o = g + col0 + tid * N;
@@ -475,7 +481,7 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
             const int ck = l.cls[k];
             const bool edge = ck < p.row.head || ck >= inner;
             if (l.first[k] && (edge ? first_cta : static_cast<unsigned>(ck - col0) < static_cast<unsigned>(p.n * N)))
-              g[ck] = from_f32<T>(wt * (exp2_fast(fmaf(l.x[k], f, -c) - ls) - l.q_all[k]));
+              g[ck] = from_f32<T>(wt * (exp2_fast(fmaf(l.x[k] - l.m, f, at)) - l.q_all[k]));
           }
         }
       }
