@@ -437,12 +437,12 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
         if (GRAD)
           for (int i = tid; i < next.n; i += nt) ask(next, i);
       } else {
-        // The larger of the list's maximum and the others', and how far each lies below it; logarithms to base 2
-        // against it: of the sum over all classes, `ls`, and of that over the others, 2^(log_s + to_rest log2(e)), which
-        // knows what c was rounded by.
+        // How far the list's maximum and the others' lie below the larger of the two, and logarithms to base 2 against
+        // that: of the sums over the list, over the others (which knows what c was rounded by), and over both.
         const float c = ref(v.m, f), gap = (l.m - v.m) * inv_h, to_list = fminf(gap, 0.f), to_rest = fminf(-gap, 0.f);
         const float log_s = log2f(v.s) + fmaf(-v.m, f, c);
-        const float ls = log2f(l.s * exp2_fast(to_list * kLog2e) + exp2_fast(fmaf(to_rest, kLog2e, log_s)));
+        const float to_l = fmaf(to_list, kLog2e, log2f(l.s)), to_r = fmaf(to_rest, kLog2e, log_s);
+        const float ls = fmaxf(to_l, to_r) + log2f(1.f + exp2_fast(-fabsf(to_l - to_r)));  // = to_r beside an empty list
         const float log_pr = fmaf(kLn2, log_s - ls, to_rest);
         const float q_r = a.teacher_lse && !l.whole ? fmaxf(0.f, 1.f - l.sum) : 0.f;
         if (tid == 0 && first_cta)

@@ -61,3 +61,14 @@ def test_all_far_from_zero(tail, V, dt, h):
     x, cls, y, ylse, _ = lists(V + 2, len(at), V, 6, dt, tail, h)
     x = (x.float() * h + torch.tensor(at, device=DEV)[None, :, None]).to(dt)
     check_all(E.distill(x, cls, y, teacher_lse=ylse, temperature=h), reference(x, cls, y, ylse, h, None, None, dt))
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("V", [64, 3000, 50_001, 70_001])
+def test_empty_list_beside_a_log_sum(V, dt):
+    """All of the teacher's mass and all of the student's on one class: no loss and no gradient, to the bit."""
+    x, cls, y, ylse, _, _ = make(V, 2, 60, V, 3, dt, tail=True)
+    cls.fill_(-1)
+    loss, lse, dx = E.distill(x, cls, y, teacher_lse=ylse)
+    assert not loss.any() and not dx.any()
+    check_all((loss, lse, dx), reference(x, cls, y, ylse, 1.0, None, None, dt))
