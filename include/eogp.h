@@ -692,8 +692,9 @@ int eogp_head_loss(const void* x, int dtype, long long x_bs, long long x_ld, con
  *     q_r = max(0, 1 - sum q_k), p_r = 1 - sum p_k over the listed classes, summed without them,
  *     loss[b][t] = w * (sum_k q_k (log q_k - log p_k) + q_r (log q_r - log p_r));
  *   lse[b][t] = log sum_v exp(x_v / h),
- *   dlogits[b][t] = (w / h) * (p - q) at listed classes and (w / h) * p * (1 - q_r / p_r), without
- *     teacher_lse (w / h) * p, at the others.
+ *   dlogits[b][t] = (w / h) * (p - q) at listed classes and (w / h) * p at the others; with teacher_lse
+ *     (w / h) * (Q p - q) and (w / h) * p * (Q - q_r / p_r), Q = sum q_k + q_r. Q is 1 unless the q_k add up to
+ *     more than 1 (rounded logits beside the log-sum of others) or all V classes are listed.
  * Where a list holds all V classes there is no such class more. Terms of q = 0 are 0. Multiply the
  * weights by h^2 for the usual scaling of softened targets.
  * A class that is listed twice counts as one entry with the sum of both q in the gradient, and as two

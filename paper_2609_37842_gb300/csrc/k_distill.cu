@@ -4,12 +4,14 @@
 //   the list's own),
 //   loss = w sum q_k (log q_k - log p_jk),  dx = (w / h) (p - sum_k q_k e_jk);
 // with a given log-sum the classes not listed are one more class on both sides,
-//   q_r = max(0, 1 - sum q_k), p_r = sum of their p: loss += w q_r (log q_r - log p_r), and
-//   dx = (w / h) p (1 - q_r / p_r) for them.
+//   q_r = max(0, 1 - sum q_k), p_r = sum of their p: loss += w q_r (log q_r - log p_r), and, with
+//   Q = q_r + sum q_k the teacher's whole mass, dx = (w / h) (Q p - sum_k q_k e_jk) for the listed classes and
+//   dx = (w / h) p (Q - q_r / p_r) for the others. Q is 1 unless the list's mass is above 1 (rounded logits beside the
+//   log-sum of others, say) or all classes are listed.
 // The sum over the classes not listed has its own maximum m_r, and that over the listed ones theirs, m_l; the
 // difference m_l - m_r is formed before it is scaled, and logarithms are taken against the larger of the two: each
 // keeps all its digits however far the two lie apart. With e = 2^(x f - c), f = log2(e) / h, c = m_r f rounded, and
-// s_r = sum e over the classes not listed, dx = (w / h) (p_r - q_r) e / s_r there, whatever the sizes: p_r is no
+// s_r = sum e over the classes not listed, dx = (w / h) (Q p_r - q_r) e / s_r there, whatever the sizes: p_r is no
 // difference, and may be too small for a float.
 //
 // HBM-bound: a row is read once and its gradient written once.
@@ -40,8 +42,8 @@ struct __align__(16) List {
   float q_all[kListMax];   // sum of q of the entries of this class
   uint8_t first[kListMax]; // the first entry of its class
   float sum, m, t, s;
+  float rest, mass;        // q_r and Q
   bool live;               // the row takes part
-  bool whole;              // all V classes are listed
 };
 using Seen = unsigned[kSeen / 32];  // of slow_row: bit c % kSeen: a class like c is listed
 struct Lists {
@@ -197,7 +199,8 @@ __device__ __forceinline__ void make_list(const DistillArgs& a, const Job& j, Li
     l.t = t;
     l.s = s;
     l.live = true;
-    l.whole = classes == static_cast<float>(a.V);
+    l.rest = a.teacher_lse && classes != static_cast<float>(a.V) ? fmaxf(0.f, 1.f - sum) : 0.f;
+    l.mass = a.teacher_lse && !(l.rest > 0.f) ? sum : 1.f;
   }
   __syncwarp();
 }
@@ -269,17 +272,16 @@ __device__ __noinline__ void slow_row(const DistillArgs& a, int r, const Job& j,
   s = l.s * exp2_fast((l.m - m) * f) + s_r * exp2_fast((m_r - m) * f);
   const float ls = s > 0.f ? logf(s) : NAN;  // no finite logit: NaN
   const float log_pr = (m_r - m) * inv_h + (logf(s_r) - ls);
-  const float q_r = a.teacher_lse && !l.whole ? fmaxf(0.f, 1.f - l.sum) : 0.f;
   if (tid == 0)
-    put_loss(a, r, j.w * (list_loss(l, (m - l.m) * inv_h + ls) + term(q_r, logf(q_r), log_pr)), m * inv_h + ls);
+    put_loss(a, r, j.w * (list_loss(l, (m - l.m) * inv_h + ls) + term(l.rest, logf(l.rest), log_pr)), m * inv_h + ls);
   if (!a.dlogits.p) return;
   T* const g = row_out<T>(a.dlogits, j.b, j.t);
   const float wt = j.w * inv_h;
-  const float out = s_r > 0.f ? wt * (expf(log_pr) - q_r) / s_r : ls * 0.f;
+  const float out = s_r > 0.f ? wt * (l.mass * expf(log_pr) - l.rest) / s_r : ls * 0.f;
   for (int c = tid; c < a.V; c += nt) {
     const float xc = to_f32(x[c]);
     const int k = listed(c);
-    g[c] = from_f32<T>(k >= 0 ? wt * (expf((xc - m) * inv_h - ls) - l.q_all[k]) : exp2_fast((xc - m_r) * f) * out);
+    g[c] = from_f32<T>(k >= 0 ? wt * (l.mass * expf((xc - m) * inv_h - ls) - l.q_all[k]) : exp2_fast((xc - m_r) * f) * out);
   }
 }
 
@@ -444,13 +446,12 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
         const float to_l = fmaf(to_list, kLog2e, log2f(l.s)), to_r = fmaf(to_rest, kLog2e, log_s);
         const float ls = fmaxf(to_l, to_r) + log2f(1.f + exp2_fast(-fabsf(to_l - to_r)));  // = to_r beside an empty list
         const float log_pr = fmaf(kLn2, log_s - ls, to_rest);
-        const float q_r = a.teacher_lse && !l.whole ? fmaxf(0.f, 1.f - l.sum) : 0.f;
         if (tid == 0 && first_cta)
-          put_loss(a, r, p.j.w * (list_loss(l, fmaf(kLn2, ls, -to_list)) + term(q_r, logf(q_r), log_pr)),
+          put_loss(a, r, p.j.w * (list_loss(l, fmaf(kLn2, ls, -to_list)) + term(l.rest, logf(l.rest), log_pr)),
                    fmaf(kLn2, ls, fmaxf(l.m, v.m) * inv_h));
         if (GRAD) {
           const RowVecs<T> out(g, a.V);
-          const float wt = p.j.w * inv_h, to = wt * (expf(log_pr) - q_r) / v.s;
+          const float wt = p.j.w * inv_h, to = wt * (l.mass * expf(log_pr) - l.rest) / v.s;
           const float at = fmaf(to_list, kLog2e, -ls);
           if (ce >= 0) g[ce] = from_f32<T>(exp2_fast(fmaf(xe, f, -c)) * to);
           if (out.ph == p.row.ph) {
@@ -481,7 +482,7 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
             const int ck = l.cls[k];
             const bool edge = ck < p.row.head || ck >= inner;
             if (l.first[k] && (edge ? first_cta : static_cast<unsigned>(ck - col0) < static_cast<unsigned>(p.n * N)))
-              g[ck] = from_f32<T>(wt * (exp2_fast(fmaf(l.x[k] - l.m, f, at)) - l.q_all[k]));
+              g[ck] = from_f32<T>(wt * (l.mass * exp2_fast(fmaf(l.x[k] - l.m, f, at)) - l.q_all[k]));
           }
         }
       }

@@ -1,5 +1,5 @@
-"""GPU checks of distillation where list and remainder lie far apart, against the formulas in
-float64 with the tolerances of test_gpu_distill.py."""
+"""GPU checks of distillation where list and remainder lie far apart, and where the teacher's mass is not 1, against
+the formulas in float64 with the tolerances of test_gpu_distill.py."""
 import numpy as np
 import pytest
 
@@ -7,7 +7,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from paper_2609_37842_gb300 import eogp as E  # noqa: E402
-from test_gpu_distill import BF, DEV, F32, _lib, _status, check_all, make, reference  # noqa: E402,F401
+from test_gpu_distill import BF, DEV, F32, U, _lib, _status, check_all, gen, make, out_u, reference  # noqa: E402,F401
 
 
 def lists(seed, rows, V, K, dt, tail, h):
@@ -72,3 +72,114 @@ def test_empty_list_beside_a_log_sum(V, dt):
     loss, lse, dx = E.distill(x, cls, y, teacher_lse=ylse)
     assert not loss.any() and not dx.any()
     check_all((loss, lse, dx), reference(x, cls, y, ylse, 1.0, None, None, dt))
+
+
+def with_mass(x, cls, y, ylse, h, dt):
+    """`reference` of one class each entry with a log-sum, its gradient of a teacher of mass Q = sum q + q_r, not 1:
+    (w / h) (Q - 1) p more at every class. Its tolerance grows by the errors of that p (a logarithm 4 u (max - x) / h
+    off, sums) and of Q (each q off by its logarithm's error and the sum's), and by the rounding."""
+    r = reference(x, cls, y, ylse, h, None, None, dt)
+    V, K = x.shape[-1], cls.shape[-1]
+    z = x.double() / h
+    z = z - z.amax(-1, keepdim=True)
+    p = torch.softmax(z, -1)
+    yy = y.double() / h
+    q = torch.exp(yy - ylse.double()[..., None])
+    listed = torch.zeros(x.shape, dtype=torch.bool, device=DEV).scatter_(2, cls.long(), True)
+    q_r = torch.where(listed.all(-1), 0.0, (1 - q.sum(-1)).clamp_min(0))
+    more = (q.sum(-1) + q_r - 1)[..., None]
+    sums = (V / 32 + K / 32 + 160) * U
+    e_q = (4 * U * (yy.abs().amax(-1) + ylse.double().abs()) + sums)[..., None] * q.sum(-1, keepdim=True) + 2 * U
+    extra = more.abs() * p * (4 * U * z.abs() + 2 * sums) + p * e_q
+    r["dx"] = r["dx"] + more * p / h
+    r["tdx"] = r["tdx"] + (extra + (out_u(dt) + 4 * U) * (more.abs() * p + extra)) / h
+    return r
+
+
+def derivative(x, cls, y, ylse, h):
+    """The loss's derivative by automatic differentiation in float64, the teacher's probabilities constants."""
+    x = (x.double()).requires_grad_()
+    z = x / h
+    log_p = torch.log_softmax(z, -1)
+    log_q = y.double() / h - ylse.double()[..., None]
+    q = torch.exp(log_q)
+    listed = torch.zeros(x.shape, dtype=torch.bool, device=DEV).scatter_(2, cls.long(), True)
+    whole = listed.all(-1)
+    q_r = torch.where(whole, 0.0, (1 - q.sum(-1)).clamp_min(0))
+    log_pr = torch.logsumexp(z.masked_fill(listed & ~whole[..., None], float("-inf")), -1) - torch.logsumexp(z, -1)
+    loss = (q * (log_q - log_p.gather(-1, cls.long()))).sum(-1) + torch.xlogy(q_r, q_r) - q_r * log_pr
+    return torch.autograd.grad(loss.sum(), x)[0]
+
+
+def check_mass(x, cls, y, ylse, h, dt):
+    ref = with_mass(x, cls, y, ylse, h, dt)
+    d = derivative(x, cls, y, ylse, h)
+    assert (d - ref["dx"]).abs().max() <= 1e-9 * (1 + d.abs().max())
+    check_all(E.distill(x, cls, y, teacher_lse=ylse, temperature=h), ref)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("by", [1e-3, 0.05, 0.7, 2.0])
+@pytest.mark.parametrize("V", [100, 5000, 60_001, 70_001])
+def test_mass_above_one(V, by, dt):
+    """A log-sum too small for its list: the rest is 0, and p counts as often as the list's mass."""
+    h = (1.0, 2.0, 0.7)[V % 3]
+    x, cls, y, ylse, _, _ = make(V, 2, 9, V, 6, dt, tail=True, h=h)
+    check_mass(x, cls, y, torch.logsumexp(y.double() / h, -1).float() - by, h, dt)
+
+
+@pytest.mark.parametrize("V", [100, 5000, 60_001])
+def test_mass_of_rounded_logits(V):
+    """What a store of teachers' logits holds: the best ones in bf16, and the log-sum of all of them unrounded."""
+    x, cls, _, _, _, _ = make(V, 1, 200, V, 8, BF, tail=True)
+    g = gen(V)
+    exact = 14.0 + 2.0 * torch.randn(cls.shape, generator=g, device=DEV)
+    ylse = torch.logsumexp(exact.double(), -1).float() + 1e-3
+    y = exact.to(BF)
+    above = torch.logsumexp(y.double(), -1) > ylse.double()
+    assert 0 < above.sum() < above.numel()
+    check_mass(x, cls, y, ylse, 1.0, BF)
+
+
+@pytest.mark.parametrize("V", [1, 7, 200])
+@pytest.mark.parametrize("by", [-0.5, 0.0, 0.5])
+def test_mass_of_all_classes(by, V):
+    """Lists of every class: no rest, whatever their mass, below 1 or above."""
+    x, cls, y, _, _, _ = make(V, 2, 15, V, V, F32)
+    check_mass(x, cls, y, torch.logsumexp(y.double(), -1).float() + by, 1.0, F32)
+
+
+@pytest.mark.parametrize("V", [300, 60_001, 70_001])
+def test_mass_of_far_rows(V):
+    """Rows that take the slow way: logits beyond 2^27, and others masked to -inf."""
+    x, cls, y, _, free = lists(V, 4, V, 5, F32, True, 1.0)
+    x[:, :2] += 1e9
+    x[:, 2:] = torch.where(free[:, 2:], float("-inf"), x[:, 2:])
+    ylse = torch.logsumexp(y.double(), -1).float() - 0.5
+    ref = with_mass(x, cls, y, ylse, 1.0, F32)
+    # Classes of p = 0 have a gradient of 0, to the bit; the formulas' shares of their empty sum are no numbers.
+    none = x == float("-inf")
+    ref["dx"], ref["tdx"] = torch.where(none, 0.0, ref["dx"]), torch.where(none, 0.0, ref["tdx"])
+    check_all(E.distill(x, cls, y, teacher_lse=ylse), ref)
+
+
+def test_mass_of_longest_rows():
+    x, cls, y, _, _, _ = make(3, 1, 3, 1_000_003, 5, BF)
+    check_mass(x, cls, y, torch.logsumexp(y.double(), -1).float() - 0.5, 1.0, BF)
+
+
+@pytest.mark.parametrize("by", [0.3, 1.5])
+def test_gradient_against_differences_above_one(by):
+    """As test_gradient_against_differences of test_gpu_distill.py, with a log-sum that is too small: third
+    derivatives grow with the list's mass."""
+    h, s = 1.3, 2.0 ** -5
+    x, cls, y, _, _, _ = make(10, 2, 12, 400, 20, F32, tail=True, h=h)
+    ylse = torch.logsumexp(y.double() / h, -1).float() - by
+    _, _, dx = E.distill(x, cls, y, teacher_lse=ylse, temperature=h)
+    v = torch.randn(x.shape, generator=gen(11), device=DEV) * 0.2
+    L = [E.distill(x + k * s * v, cls, y, teacher_lse=ylse, temperature=h)[0].double().sum().item() for k in (1, -1)]
+    ref = reference(x, cls, y, ylse, h, None, None, F32)
+    slope = (dx.double() * v.double()).sum().item()
+    bend = float(np.exp(by)) * (((v.amax(-1) - v.amin(-1)).double() / h) ** 3).sum().item() * 2 * s * s / 6
+    noise = 4 * ref["tloss"].sum().item() / (2 * s) + 2 * U * x.abs().sum().item() / x.shape[-1] / (2 * s)
+    assert abs((L[0] - L[1]) / (2 * s) - slope) <= bend + noise + 1e-4 * abs(slope)
