@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
   constexpr int N = 16 / sizeof(T), K = 4;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ MaxSum part[kSliceThreads / 32], peers[2][kMaxCluster], all;
-  __shared__ bool lost;
+  __shared__ volatile int lost;  // the row whose exchange ran out; r1: none
   __shared__ uint64_t bar[2];
   const int tid = threadIdx.x, nt = blockDim.x - 32, nw = nt >> 5;
   const int rank = cs > 1 ? static_cast<int>(blockIdx.x % cs) : 0;
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
   Lists& ls_ = *reinterpret_cast<Lists*>(smem);
   Raw<T, N>* const slice = reinterpret_cast<Raw<T, N>*>(smem + sizeof(Lists));
   const float inv_h = 1.f / a.temperature, f = kLog2e * inv_h;
-  if (tid == 0) lost = false;
+  if (tid == 0) lost = r1;
   if (cs > 1) {
     if (tid == 0) {
       mbar_init(&bar[0], 1);
@@ -335,7 +335,9 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
     for (int r = r0; r < r1; ++r) {
       make_list<T>(a, job_of(a, r), ls_.l[(r - r0) & 1], inv_h, first_cta, status);
       named_bar_sync(2, nt + 32);
-      if (lost) break;
+      // Of an earlier row: the others came to barrier 2 once more, with that written before, and not again. Of this
+      // row, which may be written meanwhile: they will come once more.
+      if (lost < r) break;
     }
     if (cs > 1) cluster_wait();
     return;
@@ -422,7 +424,7 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
           if (tid < cs) put_peer(&peers[set][rank], &bar[set], tid, v);
           const bool came = __all_sync(0xffffffffu, mbar_wait_cluster(&bar[set], (turn >> 1) & 1, status));
           if (tid == 0) {
-            lost = !came;
+            if (!came) lost = r;
             if (came) {
               mbar_arrive_expect_tx(&bar[set], cs * sizeof(MaxSum));  // for the turn after next
               all = join_all(peers[set], cs, f);
@@ -430,7 +432,7 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
           }
         }
         meet(nt);
-        if (lost) break;
+        if (lost < r1) break;
         v = all;
         ++turn;
       }
@@ -492,7 +494,7 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
     xe = ce >= 0 ? to_f32(p.x[ce]) : 0.f;
   }
   if (!met) cluster_wait();
-  if (cs > 1 && met && lost) {
+  if (cs > 1 && met && lost < r1) {
     if (r + 1 < r1) named_bar_sync(2, nt + 32);  // the last warp stops too
     commit_async();
     wait_async<0>();
