@@ -183,3 +183,23 @@ def test_gradient_against_differences_above_one(by):
     bend = float(np.exp(by)) * (((v.amax(-1) - v.amin(-1)).double() / h) ** 3).sum().item() * 2 * s * s / 6
     noise = 4 * ref["tloss"].sum().item() / (2 * s) + 2 * U * x.abs().sum().item() / x.shape[-1] / (2 * s)
     assert abs((L[0] - L[1]) / (2 * s) - slope) <= bend + noise + 1e-4 * abs(slope)
+
+
+@pytest.mark.parametrize("K", [1, 20, 64, 256])
+@pytest.mark.parametrize("V", [300, 9000, 70_001])
+def test_small_rest(V, K):
+    """q_r = 1 - sum q keeps its digits where little is left over. A listed class of p = 0 has the gradient -q, which
+    gives each q as the kernel has it; with p = 0 at the others and their logits equal, their gradients add up to -q_r.
+    So q_r is known from the q: the sum in 64 bits is off by K 2^-53; the difference, the share and the sum of the
+    others' gradients round it by u a step (V / 32 + 160 u covers a sum over the classes)."""
+    x, cls, y, _, free = lists(V + K, 12, V, K, F32, True, 1.0)
+    mass = torch.logspace(-6, -1, 12, dtype=torch.float64, device=DEV)
+    ylse = (torch.logsumexp(y.double(), -1) - torch.log1p(-mass)).float()
+    _, _, dx = E.distill(torch.where(free, 0.0, -1e4), cls, y, teacher_lse=ylse)
+    q = -dx.gather(-1, cls).double()
+    want = 1 - q.sum(-1)
+    assert bool((q > 0).all()) and bool((want > 0).sum() > 8)
+    _, _, dx = E.distill(torch.where(free, -1e4, 0.0), cls, y, teacher_lse=ylse)
+    got = -torch.where(free, dx, 0.0).double().sum(-1)
+    off = (got - want.clamp_min(0)).abs()
+    assert bool((off <= (V / 32 + 160) * U * want.clamp_min(0) + K * 2.0 ** -53).all())
