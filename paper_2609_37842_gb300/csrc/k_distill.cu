@@ -31,7 +31,7 @@ namespace {
 constexpr int kListMax = EOGP_DISTILL_MAX;
 constexpr int kSeen = 8192;
 constexpr int kRowThreads = 512;
-constexpr float kLowest = -3.402823466e38f;
+constexpr float kLargest = 3.402823466e38f, kLowest = -kLargest;
 
 // A row's list in shared memory, and what it comes to by itself: log q of an entry is (y - top) / h - whole; `sum` of q;
 // the largest of the student's logits m, and t = sum q (log q - (x - m) / h), so that the loss's sum over the list
@@ -78,6 +78,12 @@ __device__ __forceinline__ float warp_max(float m) {
   return m;
 }
 
+// (a - b) k: the difference first, which keeps its digits; for finite a and b whose difference is no float, their
+// products with k.
+__device__ __forceinline__ float scaled(float a, float b, float k) {
+  const float d = a - b;
+  return fabsf(d) > kLargest && fabsf(a) <= kLargest && fabsf(b) <= kLargest ? a * k - b * k : d * k;
+}
 // hi += x; lo += what that rounds off.
 __device__ __forceinline__ void add_exactly(float& hi, float& lo, float x) {
   const float s = hi + x, b = s - hi;
@@ -144,14 +150,14 @@ __device__ __forceinline__ void make_list(const DistillArgs& a, const Job& j, Li
     float s = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e)
-      if (c[e] >= 0) s += expf((y[e] - top) * inv_h);
+      if (c[e] >= 0) s += expf(scaled(y[e], top, inv_h));
     whole = logf(warp_sum(s));
   }
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const float lq = (y[e] - top) * inv_h - whole, q = c[e] >= 0 ? expf(lq) : 0.f;
+    const float lq = scaled(y[e], top, inv_h) - whole, q = c[e] >= 0 ? expf(lq) : 0.f;
     sum += q;
-    t += term(q, lq, (x[e] - m) * inv_h);
+    t += term(q, lq, scaled(x[e], m, inv_h));
     y[e] = q;
     l.x[lane + 32 * e] = x[e];
     l.q_all[lane + 32 * e] = q;
@@ -198,7 +204,7 @@ __device__ __forceinline__ void make_list(const DistillArgs& a, const Job& j, Li
     twice |= c[e] >= 0 && same[e] > 1;
     l.first[lane + 32 * e] = first[e];
     if (first[e]) {
-      s += expf((x[e] - m) * inv_h);
+      s += expf(scaled(x[e], m, inv_h));
       classes += 1.f;
     }
   }
@@ -289,15 +295,15 @@ __device__ __noinline__ void slow_row(const DistillArgs& a, int r, const Job& j,
   float s = 0.f;
   for (int c = tid; c < a.V; c += nt) {
     const float v = to_f32(x[c]);
-    if (v != -INFINITY && listed(c) < 0) s += exp2_fast((v - m_r) * f);
+    if (v != -INFINITY && listed(c) < 0) s += exp2_fast(scaled(v, m_r, f));
   }
   const float s_r = block_add(s, part, nt);
   m = fmaxf(l.m, m_r);
-  s = l.s * exp2_fast((l.m - m) * f) + s_r * exp2_fast((m_r - m) * f);
+  s = l.s * exp2_fast(scaled(l.m, m, f)) + s_r * exp2_fast(scaled(m_r, m, f));
   const float ls = s > 0.f ? logf(s) : NAN;  // no finite logit: NaN
-  const float log_pr = (m_r - m) * inv_h + (logf(s_r) - ls);
+  const float log_pr = scaled(m_r, m, inv_h) + (logf(s_r) - ls);
   if (tid == 0)
-    put_loss(a, r, j.w * (list_loss(l, (m - l.m) * inv_h + ls) + term(l.rest, logf(l.rest), log_pr)), m * inv_h + ls);
+    put_loss(a, r, j.w * (list_loss(l, scaled(m, l.m, inv_h) + ls) + term(l.rest, logf(l.rest), log_pr)), m * inv_h + ls);
   if (!a.dlogits.p) return;
   T* const g = row_out<T>(a.dlogits, j.b, j.t);
   const float wt = j.w * inv_h;
@@ -305,7 +311,7 @@ __device__ __noinline__ void slow_row(const DistillArgs& a, int r, const Job& j,
   for (int c = tid; c < a.V; c += nt) {
     const float xc = to_f32(x[c]);
     const int k = listed(c);
-    g[c] = from_f32<T>(k >= 0 ? wt * (l.mass * expf((xc - m) * inv_h - ls) - l.q_all[k]) : exp2_fast((xc - m_r) * f) * out);
+    g[c] = from_f32<T>(k >= 0 ? wt * (l.mass * expf(scaled(xc, m, inv_h) - ls) - l.q_all[k]) : exp2_fast(scaled(xc, m_r, f)) * out);
   }
 }
 
@@ -467,7 +473,7 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
       } else {
         // How far the list's maximum and the others' lie below the larger of the two, and logarithms to base 2 against
         // that: of the sums over the list, over the others (which knows what c was rounded by), and over both.
-        const float c = ref(v.m, f), gap = (l.m - v.m) * inv_h, to_list = fminf(gap, 0.f), to_rest = fminf(-gap, 0.f);
+        const float c = ref(v.m, f), gap = scaled(l.m, v.m, inv_h), to_list = fminf(gap, 0.f), to_rest = fminf(-gap, 0.f);
         const float log_s = log2f(v.s) + fmaf(-v.m, f, c);
         const float to_l = fmaf(to_list, kLog2e, log2f(l.s)), to_r = fmaf(to_rest, kLog2e, log_s);
         const float ls = fmaxf(to_l, to_r) + log2f(1.f + exp2_fast(-fabsf(to_l - to_r)));  // = to_r beside an empty list
@@ -508,7 +514,7 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
             const int ck = l.cls[k];
             const bool edge = ck < p.row.head || ck >= inner;
             if (l.first[k] && (edge ? first_cta : static_cast<unsigned>(ck - col0) < static_cast<unsigned>(p.n * N)))
-              g[ck] = from_f32<T>(wt * (l.mass * exp2_fast(fmaf(l.x[k] - l.m, f, at)) - l.q_all[k]));
+              g[ck] = from_f32<T>(wt * (l.mass * exp2_fast(scaled(l.x[k], l.m, f) + at) - l.q_all[k]));
           }
         }
       }

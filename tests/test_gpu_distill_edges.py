@@ -203,3 +203,35 @@ def test_small_rest(V, K):
     got = -torch.where(free, dx, 0.0).double().sum(-1)
     off = (got - want.clamp_min(0)).abs()
     assert bool((off <= (V / 32 + 160) * U * want.clamp_min(0) + K * 2.0 ** -53).all())
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("V", [300, 9000, 70_001])
+@pytest.mark.parametrize("tail", [False, True])
+def test_differences_beyond_floats(tail, V, dt):
+    """Logits of 3e38 and -3e38 in one row, at temperatures that make ordinary numbers of them: their differences
+    are no floats. On either side, listed and not, the student's and the teacher's."""
+    for h in (1e37, 5e37):
+        h = float(np.float32(h))
+        x, cls, y, ylse, free = lists(V, 8, V, 4, dt, tail, h)
+        big = 3e38
+        x = x.float() * (h / 4)
+        x[:, 0] = torch.where(free[:, 0], -big, big)
+        x[:, 1] = torch.where(free[:, 1], big, -big)
+        x[:, 2] = torch.where(torch.arange(V, device=DEV) % 2 == 0, -big, big)
+        x[:, 3] = torch.where(torch.arange(V, device=DEV) == cls[:, 3, :1], big, -big)
+        x[:, 4, V // 2:] = -big
+        x[:, 4, : V // 2] = big
+        x = x.to(dt)
+        if not tail:
+            y[:, 5, 0], y[:, 5, 1] = big, -big
+            y[:, 0, 2] = -big
+        ref = reference(x, cls, y, ylse, h, None, None, dt)
+        # Gradients of 1 / h are below 2^-126, where steps no longer shrink: half of one, 2^-134 in bf16, for the result,
+        # and 2^-150 each for the share's factor, its product (with at most 1) and w / h times a difference.
+        ref["tdx"] = ref["tdx"] + (2.0 ** -134 if dt == BF else 2.0 ** -150) + 3 * 2.0 ** -150
+        got = E.distill(x, cls, y, teacher_lse=ylse, temperature=h)
+        # Of 4 h times a normal number some of the teacher's logits are +inf: their rows have no finite loss.
+        fine = ~(y == float("inf")).any(-1)[0]
+        assert not bool(torch.isfinite(got[0][0, ~fine]).any())
+        check_all([t[:, fine] for t in got], {k: v[:, fine] for k, v in ref.items()})
