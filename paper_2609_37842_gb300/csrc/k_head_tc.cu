@@ -356,8 +356,9 @@ __device__ __forceinline__ void add_found(const Found& f, Sums& sums) {
 }
 __device__ __forceinline__ int position_of(int r0, int w, int b) { return r0 + (w >> 2) * 128 + b * 4 + (w & 3); }
 
-// Of 1024 positions from r0 on, below r1.
-__device__ __forceinline__ unsigned find_bits(const HeadTc& h, const Near& near, int row0, int r0, int r1) {
+// Of 1024 positions from r0 on, below r1; none of the classes in `done`.
+__device__ __forceinline__ unsigned find_bits(const HeadTc& h, const Near& near, int row0, int r0, int r1,
+                                              unsigned done) {
   const int lane = threadIdx.x & 31;
   unsigned bits = 0;
   for (int i = 0; i < 8 && r0 + i * 128 < r1; ++i) {
@@ -367,7 +368,10 @@ __device__ __forceinline__ unsigned find_bits(const HeadTc& h, const Near& near,
     const int v[4] = {t.x, t.y, t.z, t.w};
     bool hit[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) hit[e] = r + e < r1 && static_cast<unsigned>(v[e] - row0) < 32u;
+    for (int e = 0; e < 4; ++e) {
+      const unsigned c = static_cast<unsigned>(v[e] - row0);
+      hit[e] = r + e < r1 && c < 32u && !(done >> (c & 31u) & 1u);
+    }
     if (!__any_sync(0xffffffffu, hit[0] || hit[1] || hit[2] || hit[3])) continue;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -377,48 +381,75 @@ __device__ __forceinline__ unsigned find_bits(const HeadTc& h, const Near& near,
   }
   return bits;
 }
-// Takes positions out of the bits, one a class at most, up to the first whose class has one.
+// Class of position r among the warp's 32, which has it.
+__device__ __forceinline__ int class_of(const HeadTc& h, const Near& near, int row0, int r) {
+  return (r < kNear ? near.target[r] : h.target[h.first + r]) - row0;
+}
+// Takes the next position of every class that has one out of the bits: of the lane's class, -1 for none.
 __device__ __forceinline__ int take_bits(const HeadTc& h, const Near& near, int row0, int r0, unsigned& bits) {
   const int lane = threadIdx.x & 31;
   int mine = -1;
+  unsigned taken = 0;  // classes
   for (unsigned words = __ballot_sync(0xffffffffu, bits != 0); words; words &= words - 1) {
     const int w = __ffs(words) - 1;
     for (unsigned left = __shfl_sync(0xffffffffu, bits, w); left; left &= left - 1) {
-      const int r = position_of(r0, w, __ffs(left) - 1);
-      const bool me = (r < kNear ? near.target[r] : h.target[h.first + r]) - row0 == lane;
-      if (__any_sync(0xffffffffu, me && mine >= 0)) return mine;
-      if (me) mine = r;
-      if (lane == w) bits &= bits - 1;
+      const int r = position_of(r0, w, __ffs(left) - 1), c = class_of(h, near, row0, r);
+      if (taken >> c & 1u) continue;
+      taken |= 1u << c;
+      if (lane == c) mine = r;
+      if (lane == w) bits &= ~(left & -left);
     }
   }
   return mine;
 }
+// Drops positions beyond their class's share, of which the lane's has `share` left.
+__device__ __forceinline__ void keep_share(const HeadTc& h, const Near& near, int row0, int r0, int share,
+                                           unsigned& bits) {
+  const int lane = threadIdx.x & 31;
+  if (!__any_sync(0xffffffffu, share < static_cast<int>(__reduce_add_sync(0xffffffffu, __popc(bits))))) return;
+  for (unsigned words = __ballot_sync(0xffffffffu, bits != 0); words; words &= words - 1) {
+    const int w = __ffs(words) - 1;
+    for (unsigned left = __shfl_sync(0xffffffffu, bits, w); left; left &= left - 1) {
+      const bool me = lane == class_of(h, near, row0, position_of(r0, w, __ffs(left) - 1));
+      const bool over = __any_sync(0xffffffffu, me && share <= 0);
+      if (me) --share;
+      if (over && lane == w) bits &= ~(left & -left);
+    }
+  }
+}
 __device__ __forceinline__ float rest_of(const HeadTc& h, const Near& near, int r) {
   return r < 0 ? 0.f : r < kNear ? near.rest[r] : h.rest_w[r];
 }
+// Positions of a class that are added to its row, in each part of a split sum: turns that a tile's MMAs cover.
+__device__ __forceinline__ int share_of(const Shape& s) { return min(64, 4 + s.steps / 4); }
+
 __device__ __forceinline__ void find_rest(const TcArgs& g, const Shape& s, const Tile& t, int row, const Near& near,
                                           Found& f) {
   const int row0 = row - static_cast<int>(threadIdx.x & 31), r0 = t.i0 * 64;
-  f.bits = find_bits(g.h, near, row0, r0, min(s.rows, t.i1 * 64));
+  f.bits = find_bits(g.h, near, row0, r0, min(s.rows, t.i1 * 64), 0);
+  keep_share(g.h, near, row0, r0, share_of(s), f.bits);
   f.mine = take_bits(g.h, near, row0, r0, f.bits);
   f.rest = rest_of(g.h, near, f.mine);
 }
-// The others, in a fixed order. A class's next one waits for its last; a warp stops after a number of
-// such turns that its MMAs cover (many positions of one class, whose roundings go either way).
+// The others, in a fixed order: in a turn, the next one of every class that has one. A class has no more than its
+// share, so that one with many positions, whose roundings go either way, neither holds up the tile for long nor takes
+// anything from its neighbours.
 __device__ __forceinline__ void add_rest_dw(const TcArgs& g, const Shape& s, const Tile& t, int row, int side,
                                             const Near& near, Found& f, Sums& sums) {
   const HeadTc& h = g.h;
   const int row0 = row - static_cast<int>(threadIdx.x & 31), r1 = min(s.rows, t.i1 * 64);
-  int turns = 4 + (t.i1 - t.i0) / 4;
+  int share = share_of(s) - (f.mine >= 0);
   for (int r0 = t.i0 * 64;;) {
-    while (turns > 0 && __any_sync(0xffffffffu, f.bits != 0)) {
+    while (__any_sync(0xffffffffu, f.bits != 0)) {
       const int mine = take_bits(h, near, row0, r0, f.bits);
       add_rest(h, t, side, rest_of(h, near, mine), mine, sums);
-      --turns;
+      share -= mine >= 0;
     }
     r0 += 1024;
-    if (r0 >= r1 || turns <= 0) break;
-    f.bits = find_bits(h, near, row0, r0, r1);
+    const unsigned done = __ballot_sync(0xffffffffu, share <= 0);
+    if (r0 >= r1 || done == 0xffffffffu) break;
+    f.bits = find_bits(h, near, row0, r0, r1, done);
+    keep_share(h, near, row0, r0, share, f.bits);
   }
 }
 
