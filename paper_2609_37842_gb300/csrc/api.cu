@@ -1694,6 +1694,7 @@ extern "C" int eogp_head_loss_workspace_size(const void* weight, int dtype, long
   a.V = V;
   a.dx.p = want_dx ? &a : nullptr;
   a.dweight = want_dweight ? &a : nullptr;
+  a.clusters = sm_count() / 2;
   *bytes = head_loss_ws_bytes(a);
   return EOGP_OK;
 }
@@ -1732,8 +1733,8 @@ extern "C" int eogp_head_loss(const void* x, int dtype, long long x_bs, long lon
   const HeadArgs a{RowSet{B, T, lengths}, RowView{x, x_bs, x_ld}, RowView{dx, dx_bs, dx_ld}, weight, ld_weight,
                    dtype == EOGP_BF16, grad_dtype == EOGP_BF16, accumulate != 0, scale,
                    TokenView{targets, index_type == EOGP_I64, targets_bs}, weights, ignore_index, d, V, loss, lse,
-                   dweight, ld_dweight};
-  CUDA_TRY(launch_head_loss(a, ws, status, sm_count(), st));
+                   dweight, ld_dweight, sm_count() / 2};
+  CUDA_TRY(launch_head_loss(a, ws, status, st));
   return EOGP_OK;
 }
 

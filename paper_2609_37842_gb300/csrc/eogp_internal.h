@@ -289,9 +289,10 @@ struct HeadArgs {
   float *loss, *lse;
   void* dweight;  // NULL: not wanted
   long long ld_dweight;
+  int clusters;  // pairs of multiprocessors
 };
 size_t head_loss_ws_bytes(const HeadArgs& a);
-cudaError_t launch_head_loss(const HeadArgs& a, void* ws, unsigned* status, int num_sms, cudaStream_t st);
+cudaError_t launch_head_loss(const HeadArgs& a, void* ws, unsigned* status, cudaStream_t st);
 
 // k_distill.cu
 struct DistillArgs {

@@ -2,6 +2,8 @@
 // (k_head.cu, k_head_tc.cu).
 #pragma once
 
+#include <algorithm>
+
 #include "rows_dev.cuh"
 
 namespace eogp {
@@ -33,6 +35,18 @@ __device__ __forceinline__ int head_splits(const HeadTc& h, long long tiles, int
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, o));
   return __ffs(__ballot_sync(0xffffffffu, static_cast<unsigned long long>(cost) == best));
+}
+
+// Most floats of slabs that head_splits may choose for such a sum, of `weight` (2: D in two parts) times the steps and
+// slabs of `slab` floats. From cost(s) < cost(1), with rounds(s) >= tiles s / clusters and steps of a split >= steps / s:
+//   s (slab / 323000 + 8 tiles / clusters) < (rounds(1) - tiles / clusters) weight steps + 8 rounds(1) - 7.
+// It grows with the steps.
+inline size_t head_slab_floats(long long tiles, long long steps, int weight, size_t slab, int clusters) {
+  if (!head_split_at_all(tiles, clusters)) return 0;
+  const double each = static_cast<double>(tiles) / clusters, rounds = static_cast<double>((tiles + clusters - 1) / clusters);
+  const double s = ((rounds - each) * weight * steps + 8 * rounds - 7) / (slab / 323000.0 + 8 * each) + 1e-6;
+  const long long most = std::min<long long>(steps, s < 2 ? 1 : s < kMostSplits ? static_cast<long long>(s) : kMostSplits);
+  return most < 2 ? 0 : most * slab;
 }
 
 }  // namespace eogp

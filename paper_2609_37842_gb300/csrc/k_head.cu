@@ -88,13 +88,13 @@ Plan plan_of(const HeadArgs& a) {
   p.w = take(M * 4);
   p.x = take(static_cast<size_t>(p.piece) * p.ldx * 2);
   if (!w_fits(a)) p.W = take(static_cast<size_t>(a.V) * p.ldw * 2);
-  // Columns of a tile of the logits: those with which 76 pairs have the least in their rounds, a tile costing
-  // about 24 columns more than it has (50,000 classes, one row: 3 rounds of 224 instead of 256). fp32: two
+  // Columns of a tile of the logits: those with which the pairs have the least in their rounds, a tile costing
+  // about 24 columns more than it has (50,000 classes, one row, 76 pairs: 3 rounds of 224 instead of 256). fp32: two
   // accumulators of 128 at most.
   const long long mt = (std::min<long long>(M, p.piece) + 255) / 256;
   long long least = 0;
   for (int bn = a.bf16 ? 256 : 128; bn >= 64; bn -= 32) {
-    const long long cost = (mt * ((a.V + bn - 1) / bn) + 75) / 76 * (bn + 24);
+    const long long cost = (mt * ((a.V + bn - 1) / bn) + a.clusters - 1) / a.clusters * (bn + 24);
     if (p.bn_z == 0 || cost < least) p.bn_z = bn, least = cost;
   }
   p.bn_d = !a.bf16 || up(a.d, 128) * 1.15 < up(a.d, 256) ? 128 : 256;
@@ -108,9 +108,16 @@ Plan plan_of(const HeadArgs& a) {
     if (!a.bf16 || p.again) p.D = take(static_cast<size_t>(p.piece) * p.ldz * p.parts * 2);
     if (a.dweight && a.grad_bf16 && p.pieces > 1) p.acc = take(static_cast<size_t>(a.V) * a.d * 4);
     p.ld_slab = static_cast<int>(up(a.d, 8));
-    // Room for split sums: as many as there may be, half a GB at most.
-    const size_t most_rows = std::max<size_t>(a.dx.p ? p.piece : 0, a.dweight ? a.V : 0);
-    p.slab_bytes = std::min<size_t>(kSlabBytes, most_rows * p.ld_slab * 4 * kMostSplits);
+    // Room for split sums: as many as there may be, of dx for any number of rows, half a GB at most.
+    const long long most = std::min<long long>(M, p.piece), across = (a.d + p.bn_d - 1) / p.bn_d;
+    size_t floats = 0;
+    if (a.dweight)
+      floats = head_slab_floats((a.V + 255ll) / 256 * across, (most + 63) / 64, p.parts == 2 ? 2 : 1,
+                                static_cast<size_t>(a.V) * p.ld_slab, a.clusters);
+    for (long long rows = 256; a.dx.p && rows < most + 256 && head_split_at_all(rows / 256 * across, a.clusters); rows += 256)
+      floats = std::max(floats, head_slab_floats(rows / 256 * across, (a.V + 63ll) / 64, 1,
+                                                 static_cast<size_t>(std::min(rows, most)) * p.ld_slab, a.clusters));
+    p.slab_bytes = std::min(kSlabBytes, floats * 4);
     p.slabs = take(p.slab_bytes);
   }
   p.total = at;
@@ -536,8 +543,9 @@ int row_align(const void* p, long long bs, long long ld, int es) {
 }
 
 template <typename T>
-cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, cudaStream_t st) {
+cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, cudaStream_t st) {
   const Plan p = plan_of(a);
+  const int num_sms = 2 * a.clusters;
   const int M = static_cast<int>(a.rs.rows());
   const bool grad = a.dx.p || a.dweight;
   int* const counts = reinterpret_cast<int*>(ws + p.counts);
@@ -579,7 +587,7 @@ cudaError_t run(const HeadArgs& a, uint8_t* ws, unsigned* status, int num_sms, c
   h.ld_slab = p.ld_slab;
   h.slabs = reinterpret_cast<float*>(ws + p.slabs);
   h.slab_bytes = p.slab_bytes;
-  h.clusters = num_sms / 2;
+  h.clusters = a.clusters;
   h.piece_rows = static_cast<int>(std::min<long long>(M, p.piece));
   h.rows_box = static_cast<int>(std::min<long long>(128, up(h.piece_rows, 8)));
   const uint64_t xcols = f32 ? p.ldx : a.d, uv = a.V, rows = p.piece, dcols = static_cast<uint64_t>(p.ldz) * parts_d;
@@ -651,16 +659,16 @@ __global__ void __launch_bounds__(256) k_head_clear(T* p, long long ld, int V, i
 
 size_t head_loss_ws_bytes(const HeadArgs& a) { return plan_of(a).total; }
 
-cudaError_t launch_head_loss(const HeadArgs& a, void* ws, unsigned* status, int num_sms, cudaStream_t st) {
+cudaError_t launch_head_loss(const HeadArgs& a, void* ws, unsigned* status, cudaStream_t st) {
   if (a.rs.rows() == 0) {
     if (a.accumulate) return cudaSuccess;
-    const int blocks = std::min(a.V, num_sms * 8);
+    const int blocks = std::min(a.V, a.clusters * 16);
     if (a.grad_bf16)
       k_head_clear<bf16><<<blocks, 256, 0, st>>>(static_cast<bf16*>(a.dweight), a.ld_dweight, a.V, a.d);
     else
       k_head_clear<float><<<blocks, 256, 0, st>>>(static_cast<float*>(a.dweight), a.ld_dweight, a.V, a.d);
     return cudaGetLastError();
   }
-  return a.bf16 ? run<bf16>(a, static_cast<uint8_t*>(ws), status, num_sms, st)
-                : run<float>(a, static_cast<uint8_t*>(ws), status, num_sms, st);
+  return a.bf16 ? run<bf16>(a, static_cast<uint8_t*>(ws), status, st)
+                : run<float>(a, static_cast<uint8_t*>(ws), status, st);
 }

@@ -5,10 +5,25 @@ import pytest
 pytest.importorskip("torch")
 
 from paper_2609_37842_gb300 import eogp as E  # noqa: E402
-from test_more_losses_cpu import DISTILL, built, call  # noqa: E402,F401
+from test_more_losses_cpu import DISTILL, built, call, size  # noqa: E402,F401
 
 
 @pytest.mark.parametrize("temperature", [3.0e-39, 4.0e-39, 5.8e-39])
 def test_temperatures_whose_exponents_are_no_floats(temperature):
     """log2(e) / h, which logits are scaled by, is beyond a float there: every answer would be NaN."""
     assert call("eogp_distill", DISTILL, temperature=temperature) == E.EINVAL
+
+
+@pytest.mark.parametrize("dtype,grad,T,d,V", [(E.BF16, E.BF16, 511, 768, 50_001), (E.F32, E.F32, 509, 770, 32_001),
+                                              (E.BF16, E.F32, 511, 768, 50_001), (E.BF16, E.BF16, 64, 4096, 100_000)])
+def test_workspace_of_one_example(dtype, grad, T, d, V):
+    """What one example's workspace holds: its logits in fp32, D where it lies beside them (fp32: three bf16 parts),
+    a copy of an fp32 matrix in such parts, and slabs of dx for sums split 32 times at most; not slabs of dW, whose
+    sum over so few positions is not split."""
+    rows, cols = -(-T // 256) * 256, -(-V // 64) * 64
+    most = rows * cols * (4 if dtype == E.BF16 else 4 + 6) + 32 * T * (d + 8) * 4
+    if dtype == E.F32:
+        most += V * (d + 64) * 6
+    most += rows * (d + 64) * 6 + rows * cols // 8  # rows of x; sums of half tiles, positions
+    rc, n = size(dtype=dtype, grad_dtype=grad, T=T, B=1, d=d, V=V, ld_weight=d)
+    assert rc == E.OK and n <= most
