@@ -1683,6 +1683,8 @@ extern "C" int eogp_head_loss_workspace_size(const void* weight, int dtype, long
     return set_error(EOGP_EUNSUPPORTED, "the gradient of an fp32 weight is fp32");
   if (int rc = check_extent(V, "V")) return rc;
   if (int rc = check_extent(d, "d")) return rc;
+  // Rows of three bf16 parts, 64 columns of each in turn, are counted by ints.
+  if (dtype == EOGP_F32 && (d + 63ll) / 64 * 192 > 0x7FFFFFFFLL) return set_error(EOGP_EUNSUPPORTED, "d too large for EOGP_F32");
   if (ld_weight < 0) return set_error(EOGP_EINVAL, "negative stride");
   HeadArgs a{};
   a.rs = RowSet{B, T, nullptr};

@@ -5,7 +5,7 @@ import pytest
 pytest.importorskip("torch")
 
 from paper_2609_37842_gb300 import eogp as E  # noqa: E402
-from test_more_losses_cpu import DISTILL, built, call, size  # noqa: E402,F401
+from test_more_losses_cpu import DISTILL, HEAD, built, call, size  # noqa: E402,F401
 
 
 @pytest.mark.parametrize("temperature", [3.0e-39, 4.0e-39, 5.8e-39])
@@ -27,3 +27,16 @@ def test_workspace_of_one_example(dtype, grad, T, d, V):
     most += rows * (d + 64) * 6 + rows * cols // 8  # rows of x; sums of half tiles, positions
     rc, n = size(dtype=dtype, grad_dtype=grad, T=T, B=1, d=d, V=V, ld_weight=d)
     assert rc == E.OK and n <= most
+
+
+def test_widest_rows():
+    """Rows of an fp32 x are three bf16 rows side by side, whose columns are counted by ints; the sizes of those that
+    are taken do not wrap."""
+    for V, d in ((1, 1 << 30), (50, 800_000_000), (1000, 715_827_841)):
+        assert size(dtype=E.F32, B=1, T=1, V=V, d=d, ld_weight=d)[0] == E.EUNSUPPORTED
+        assert call("eogp_head_loss", HEAD, dtype=E.F32, V=V, d=d, ld_weight=d, dx_ld=d, dx_bs=4 * d, ld_dweight=d,
+                    ws_bytes=1 << 62) == E.EUNSUPPORTED
+    rc, n = size(dtype=E.F32, B=1, T=1, V=2, d=715_827_840, ld_weight=715_827_840)
+    assert rc == E.OK and n >= 258 * 715_827_840 * 6
+    rc, n = size(dtype=E.BF16, B=1, T=1, V=2, d=1 << 30, ld_weight=1 << 30)
+    assert rc == E.OK and n >= 256 << 31
