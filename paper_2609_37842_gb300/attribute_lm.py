@@ -14,8 +14,8 @@ The model, tokens x of an example (padding beyond its length):
     h0 = table[x] + pos,  n1 = layernorm(h0),  u = n1 W1^T,  g = gelu(u),
     h1 = h0 + g W2^T,     n2 = rmsnorm(h1),    logits = n2 table^T,
 with the loss of the next token at every position but an example's last: from the
-logits ("logits"), or without keeping them ("head"); or with the distance from a
-second model's top logits at every position ("distill").
+logits ("logits"), or from n2 and the table in one call ("head"); or with the distance
+from a second model's top logits at every position ("distill").
 """
 from __future__ import annotations
 
@@ -78,6 +78,10 @@ def backward_pass(model: Model, tokens, lengths, loss_from: str = "logits", teac
     table (over the batch), of the position table, and of the normalisations' weights for each example.
     `teacher`: top_logits of a second model, for loss_from = "distill"."""
     import torch
+    if loss_from not in ("logits", "head", "distill"):
+        raise ValueError(f'loss_from must be "logits", "head" or "distill", not {loss_from!r}')
+    if loss_from == "distill" and teacher is None:
+        raise ValueError('loss_from = "distill" needs a teacher')
     V, (B, T) = model.table.shape[0], tokens.shape
     h0, n1, mean1, rstd1, u, g, h1, n2, rstd2 = forward(model, tokens, lengths)
     if loss_from == "head":

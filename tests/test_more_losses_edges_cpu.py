@@ -40,3 +40,10 @@ def test_widest_rows():
     assert rc == E.OK and n >= 258 * 715_827_840 * 6
     rc, n = size(dtype=E.BF16, B=1, T=1, V=2, d=1 << 30, ld_weight=1 << 30)
     assert rc == E.OK and n >= 256 << 31
+
+
+def test_example_refuses_unknown_losses():
+    from paper_2609_37842_gb300 import attribute_lm as L
+    for loss_from, message in (("logit", "loss_from must be"), ("distill", "needs a teacher")):
+        with pytest.raises(ValueError, match=message):
+            L.backward_pass(None, None, None, loss_from)
