@@ -652,7 +652,7 @@ int eogp_cross_entropy(const void* logits, int dtype, long long logits_bs, long 
                        long long ignore_index, const int32_t* lengths, int B, int T, int V, float* loss, float* lse,
                        void* dlogits, long long dlogits_bs, long long dlogits_ld, eogp_stream_t stream);
 
-/* Token loss through the output matrix, without the logits of the whole batch:
+/* Token loss through the output matrix, without logits in and out of the call:
  *   z = scale * x W^T,  x = x[b][t] [d], W = weight [V x d],
  *   lse[b][t]  = log sum_v exp(z_v),
  *   loss[b][t] = w * (lse - z_target),   w and what is left out as in eogp_cross_entropy,
@@ -661,12 +661,13 @@ int eogp_cross_entropy(const void* logits, int dtype, long long logits_bs, long 
  *   dweight (+)= sum D^T x               (type `grad_dtype`, [V x ld_dweight]; every row is written,
  *                                         with `accumulate` the sums are added instead).
  * dx and dweight may each be NULL; dx may be x with the same strides. Positions left out cost
- * nothing but their zeros: the others are gathered first. With a gradient, the logits of a piece
- * of the positions at a time lie in the workspace, in fp32, or D in bf16, of at most about 4 GB (more
- * only where 256 positions take more); without one none are stored.
+ * nothing but their zeros: the others are gathered first. Without a gradient no logits are stored. With one, those of a
+ * piece of the positions at a time are in the workspace, in fp32, or D in bf16: of all positions (B * T * V * 4 bytes)
+ * where that is at most about 4 GB, else of as many as 4 GB hold (256 at least). The workspace's size is fixed by
+ * the arguments; a smaller one is refused.
  * EOGP_BF16: products of bf16 on the tensor cores, sums in fp32. D enters the products for dx, and
  * for a dweight of EOGP_BF16, rounded to bf16, as dlogits of eogp_cross_entropy would; for one of
- * EOGP_F32 it enters as two bf16 parts (about 2^-16 relative). What that takes from the target's
+ * EOGP_F32 it enters that one as two bf16 parts (about 2^-16 relative). What that takes from the target's
  * entry is added in fp32 (to a row of dweight for the positions of its class, or of many in a piece of n positions for
  * min(64, 4 + n / 256) at least, the same ones every time). EOGP_F32: products to fp32.
  * A NaN or infinity in a counted position's x, or in weight, reaches all that it is multiplied

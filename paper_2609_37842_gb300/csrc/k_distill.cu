@@ -31,7 +31,6 @@ namespace {
 constexpr int kListMax = EOGP_DISTILL_MAX;
 constexpr int kSeen = 8192;
 constexpr int kRowThreads = 512;
-constexpr float kLargest = 3.402823466e38f, kLowest = -kLargest;
 
 // A row's list in shared memory, and what it comes to by itself: log q of an entry is (y - top) / h - whole; `sum` of q;
 // the largest of the student's logits m, and t = sum q (log q - (x - m) / h), so that the loss's sum over the list

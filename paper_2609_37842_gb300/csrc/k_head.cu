@@ -20,8 +20,6 @@ using namespace eogp;
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLowest = -3.402823466e38f;
 constexpr int kFindThreads = 1024;
 constexpr int kFindBlocks = 1024;
 constexpr int kFewRows = 1024;
@@ -65,9 +63,12 @@ Plan plan_of(const HeadArgs& a) {
   p.ldx = p.ldw = static_cast<int>(a.bf16 ? up(a.d, 8) : up(a.d, 64) * 3);
   p.parts = !a.bf16 ? 3 : a.dweight && !a.grad_bf16 ? 2 : 1;
   // Narrow rows: the logits are not kept, D is formed from them where they are computed a second time. That costs
-  // 2 d operations a logit and spares 8 bytes of traffic, 6 where D has one part (us, kept / formed again, dW in
-  // bf16: 16,384 rows of 64 columns, 50,000 classes 2,404 / 1,334; of 768 3,390 / 3,111, of 1024 4,047 / 4,104, of
-  // 1536 5,608 / 6,229; 511 rows of 256 124 / 101, of 768 169 / 173). For few rows the matrix, read once more, counts too.
+  // 2 d operations a logit and spares 8 bytes of traffic, 6 or 4 where D has one part or two. us, kept / formed again, of
+  // 16,384 rows and 50,000 classes, dW in bf16 and in fp32 (two parts):
+  //   64 columns 2,437 / 1,319 and 2,802 / 2,163, 256 2,562 / 1,538 and 2,937 / 2,307, 768 3,598 / 3,414 and
+  //   4,598 / 4,416, 896 4,202 / 4,072 and 5,469 / 5,418, 1024 4,380 / 4,308 and 5,789 / 5,798, 1536 6,020 / 6,502 and
+  //   7,879 / 8,431;
+  // 511 rows, in bf16: 256 columns 124 / 101, 768 169 / 173. For few rows the matrix, read once more, counts too.
   p.again = grad && a.bf16 && M >= kAgainRows && a.d <= std::min<long long>(kAgainWidth, M);
   // A row of a piece: logits (and D, where it is not in their place), or the sums of its half tiles; and the gathered row.
   const size_t row_bytes = static_cast<size_t>(p.ldx) * 2 + (grad ? static_cast<size_t>(p.ldz) * (p.again ? p.parts * 2 : a.bf16 ? 4 : 10) : 0) +
@@ -114,9 +115,9 @@ Plan plan_of(const HeadArgs& a) {
     if (a.dweight)
       floats = head_slab_floats((a.V + 255ll) / 256 * across, (most + 63) / 64, p.parts == 2 ? 2 : 1,
                                 static_cast<size_t>(a.V) * p.ld_slab, a.clusters);
-    for (long long rows = 256; a.dx.p && rows < most + 256 && head_split_at_all(rows / 256 * across, a.clusters); rows += 256)
-      floats = std::max(floats, head_slab_floats(rows / 256 * across, (a.V + 63ll) / 64, 1,
-                                                 static_cast<size_t>(std::min(rows, most)) * p.ld_slab, a.clusters));
+    for (long long m = 1; a.dx.p && (m - 1) * 256 < most && head_split_at_all(m * across, a.clusters); ++m)
+      floats = std::max(floats, head_slab_floats(m * across, (a.V + 63ll) / 64, 1,
+                                                 static_cast<size_t>(std::min(m * 256, most)) * p.ld_slab, a.clusters));
     p.slab_bytes = std::min(kSlabBytes, floats * 4);
     p.slabs = take(p.slab_bytes);
   }
@@ -217,7 +218,7 @@ __global__ void __launch_bounds__(256) k_head_zero(const HeadArgs a, int M) {
 // fp32 as the sum of three bf16, exactly: 8 bits of the mantissa each, the first two cut off. What is not finite
 // is its first part alone.
 __device__ __forceinline__ void split3(float v, bf16 (&p)[3]) {
-  if (!(fabsf(v) <= 3.402823466e38f)) {
+  if (!(fabsf(v) <= kLargest)) {
     p[0] = from_f32<bf16>(v);
     p[1] = p[2] = from_f32<bf16>(0.f);
     return;

@@ -9,15 +9,8 @@
 
 namespace eogp {
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNearLogit = 134217728.f;  // 2^27: c's last place is 16 at most
-
-__device__ __forceinline__ float exp2_fast(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 
 // Maximum m and s = sum 2^(x f - ref(m, f)) of some logits, f = log2(e) over the temperature;
 // m = -inf: none yet.

@@ -1,5 +1,6 @@
-// Device helpers of the model-end kernels (k_embed.cu, k_norm.cu, k_loss.cu):
-// element conversion, row addressing and block-wide sums in a fixed order.
+// Device helpers of the model-end kernels (k_embed.cu, k_norm.cu, k_loss.cu, k_head.cu,
+// k_head_tc.cu, k_distill.cu): element conversion, row addressing, exponentials and block-wide
+// sums in a fixed order.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -10,6 +11,15 @@
 namespace eogp {
 
 using bf16 = __nv_bfloat16;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLargest = 3.402823466e38f, kLowest = -kLargest;
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(bf16 v) { return __bfloat162float(v); }

@@ -1106,9 +1106,10 @@ def head_loss(x, weight, targets, scale: float = 1.0, weights=None, lengths=None
               want_dx: bool = True, want_dweight: bool = True, dx=None, dweight=None, dtype=None,
               accumulate: bool = False, ws=None, stream=None):
     """eogp_head_loss: token loss of the logits scale * x weight^T for x [B, T, d] or [T, d], weight [V, d] and targets
-    [B, T] or [T], without keeping the logits. Returns (loss, lse, dx, dweight): fp32 per position, and the gradients of
-    the sum of the losses (None where not wanted). `dx` may be x. dweight may be given, and added to with accumulate,
-    else it is a new tensor of `dtype` (default that of weight; float32 always possible)."""
+    [B, T] or [T], without a tensor of logits (with a gradient the workspace holds them, about 4 GB at a time at most).
+    Returns (loss, lse, dx, dweight): fp32 per position, and the gradients of the sum of the losses (None where not
+    wanted). `dx` may be x. dweight may be given, and added to with accumulate, else it is a new tensor of `dtype`
+    (default that of weight; float32 always possible)."""
     import torch
     dev = _device_of(x, weight, targets, weights, lengths, dx, dweight, ws)
     B, T, d, xbs, xld = _rows_of(x, "x")
