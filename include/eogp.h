@@ -706,7 +706,7 @@ int eogp_head_loss(const void* x, int dtype, long long x_bs, long long x_ld, con
  * may have any size.
  * loss and lse fp32 [B x T], dense; lse and dlogits may be NULL; dlogits has the type of logits
  * and may be logits itself with the same strides. Rows of lists have the strides classes_bs / _ld
- * and teacher_bs / _ld, K <= EOGP_DISTILL_MAX; temperature is finite and > 0, and 2 / temperature is finite. */
+ * and teacher_bs / _ld, K <= EOGP_DISTILL_MAX; temperature is finite and > 0, and 3 / temperature is finite. */
 #define EOGP_DISTILL_MAX 256
 int eogp_distill(const void* logits, int dtype, long long logits_bs, long long logits_ld, const void* classes,
                  int index_type, long long classes_bs, long long classes_ld, const void* teacher,

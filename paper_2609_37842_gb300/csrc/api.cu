@@ -1752,8 +1752,8 @@ extern "C" int eogp_distill(const void* logits, int dtype, long long logits_bs, 
   if (!index_type_ok(index_type)) return set_error(EOGP_EINVAL, "bad index_type");
   if (int rc = check_extent(V, "V")) return rc;
   if (K < 1 || K > EOGP_DISTILL_MAX) return set_error(EOGP_EINVAL, "K must be in [1, %d]", EOGP_DISTILL_MAX);
-  if (!std::isfinite(temperature) || !(temperature > 0.f) || !std::isfinite(2.f / temperature))
-    return set_error(EOGP_EINVAL, "temperature and twice its reciprocal must be finite and > 0");  // log2(e) / h too
+  if (!std::isfinite(temperature) || !(temperature > 0.f) || !std::isfinite(3.f / temperature))  // 2 log2(e) / h
+    return set_error(EOGP_EINVAL, "temperature must be finite and > 0, and 3 / temperature finite");
   if (B == 0 || T == 0) return EOGP_OK;
   if (!logits || !classes || !teacher || !loss) return set_error(EOGP_EINVAL, "NULL argument");
   if (!aligned_to(logits, dtype) || !aligned_to(dlogits, dtype) || !aligned_to(classes, index_type) ||

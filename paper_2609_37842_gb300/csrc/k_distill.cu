@@ -40,7 +40,7 @@ struct __align__(16) List {
   float x[kListMax];       // the student's logit
   float q_all[kListMax];   // sum of q of the entries of this class
   uint8_t first[kListMax]; // the first entry of its class
-  float sum, m, t, s;
+  float sum, m, t, s, log_s;  // log_s = log2 s
   float rest, mass;        // q_r and Q
   bool live;               // the row takes part
 };
@@ -77,12 +77,9 @@ __device__ __forceinline__ float warp_max(float m) {
   return m;
 }
 
-// (a - b) k: the difference first, which keeps its digits; for finite a and b whose difference is no float, their
-// products with k.
-__device__ __forceinline__ float scaled(float a, float b, float k) {
-  const float d = a - b;
-  return fabsf(d) > kLargest && fabsf(a) <= kLargest && fabsf(b) <= kLargest ? a * k - b * k : d * k;
-}
+// (a - b) k of k2 = 2 k: the difference first, which keeps its digits, and of halves, for it may be no float. (What
+// halving takes from numbers below 2^-125 is below 2^-22 even at the largest k2.)
+__device__ __forceinline__ float scaled(float a, float b, float k2) { return fmaf(a, 0.5f, -0.5f * b) * k2; }
 // hi += x; lo += what that rounds off.
 __device__ __forceinline__ void add_exactly(float& hi, float& lo, float x) {
   const float s = hi + x, b = s - hi;
@@ -92,7 +89,7 @@ __device__ __forceinline__ void add_exactly(float& hi, float& lo, float x) {
 
 // One warp makes row r's list.
 template <typename T>
-__device__ __forceinline__ void make_list(const DistillArgs& a, const Job& j, List& l, float inv_h, bool flag,
+__device__ __forceinline__ void make_list(const DistillArgs& a, const Job& j, List& l, float inv2, bool flag,
                                           unsigned* status) {
   constexpr int E = kListMax / 32;
   const int lane = threadIdx.x & 31;
@@ -149,14 +146,14 @@ __device__ __forceinline__ void make_list(const DistillArgs& a, const Job& j, Li
     float s = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e)
-      if (c[e] >= 0) s += expf(scaled(y[e], top, inv_h));
+      if (c[e] >= 0) s += expf(scaled(y[e], top, inv2));
     whole = logf(warp_sum(s));
   }
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const float lq = scaled(y[e], top, inv_h) - whole, q = c[e] >= 0 ? expf(lq) : 0.f;
+    const float lq = scaled(y[e], top, inv2) - whole, q = c[e] >= 0 ? expf(lq) : 0.f;
     sum += q;
-    t += term(q, lq, scaled(x[e], m, inv_h));
+    t += term(q, lq, scaled(x[e], m, inv2));
     y[e] = q;
     l.x[lane + 32 * e] = x[e];
     l.q_all[lane + 32 * e] = q;
@@ -203,7 +200,7 @@ __device__ __forceinline__ void make_list(const DistillArgs& a, const Job& j, Li
     twice |= c[e] >= 0 && same[e] > 1;
     l.first[lane + 32 * e] = first[e];
     if (first[e]) {
-      s += expf(scaled(x[e], m, inv_h));
+      s += expf(scaled(x[e], m, inv2));
       classes += 1.f;
     }
   }
@@ -227,6 +224,7 @@ __device__ __forceinline__ void make_list(const DistillArgs& a, const Job& j, Li
     l.m = m;
     l.t = t;
     l.s = s;
+    l.log_s = log2f(s);
     l.live = true;
     l.rest = classes != static_cast<float>(a.V) ? rest : 0.f;
     l.mass = a.teacher_lse && !(l.rest > 0.f) ? sum : 1.f;
@@ -271,7 +269,7 @@ __device__ __noinline__ void slow_row(const DistillArgs& a, int r, const Job& j,
   __shared__ float part[kRowThreads / 32];
   const int tid = threadIdx.x;
   const T* const x = row_of<T>(a.logits, j.b, j.t);
-  const float inv_h = 1.f / a.temperature, f = kLog2e * inv_h;
+  const float inv_h = 1.f / a.temperature, f = kLog2e * inv_h, inv2 = 2.f * inv_h, f2 = 2.f * f;
   for (int k = tid; k < kSeen / 32; k += nt) seen[k] = 0u;
   meet(nt);
   for (int k = tid; k < a.K; k += nt) {
@@ -294,15 +292,15 @@ __device__ __noinline__ void slow_row(const DistillArgs& a, int r, const Job& j,
   float s = 0.f;
   for (int c = tid; c < a.V; c += nt) {
     const float v = to_f32(x[c]);
-    if (v != -INFINITY && listed(c) < 0) s += exp2_fast(scaled(v, m_r, f));
+    if (v != -INFINITY && listed(c) < 0) s += exp2_fast(scaled(v, m_r, f2));
   }
   const float s_r = block_add(s, part, nt);
   m = fmaxf(l.m, m_r);
-  s = l.s * exp2_fast(scaled(l.m, m, f)) + s_r * exp2_fast(scaled(m_r, m, f));
+  s = l.s * exp2_fast(scaled(l.m, m, f2)) + s_r * exp2_fast(scaled(m_r, m, f2));
   const float ls = s > 0.f ? logf(s) : NAN;  // no finite logit: NaN
-  const float log_pr = scaled(m_r, m, inv_h) + (logf(s_r) - ls);
+  const float log_pr = scaled(m_r, m, inv2) + (logf(s_r) - ls);
   if (tid == 0)
-    put_loss(a, r, j.w * (list_loss(l, scaled(m, l.m, inv_h) + ls) + term(l.rest, logf(l.rest), log_pr)), m * inv_h + ls);
+    put_loss(a, r, j.w * (list_loss(l, scaled(m, l.m, inv2) + ls) + term(l.rest, logf(l.rest), log_pr)), m * inv_h + ls);
   if (!a.dlogits.p) return;
   T* const g = row_out<T>(a.dlogits, j.b, j.t);
   const float wt = j.w * inv_h;
@@ -310,7 +308,7 @@ __device__ __noinline__ void slow_row(const DistillArgs& a, int r, const Job& j,
   for (int c = tid; c < a.V; c += nt) {
     const float xc = to_f32(x[c]);
     const int k = listed(c);
-    g[c] = from_f32<T>(k >= 0 ? wt * (l.mass * expf(scaled(xc, m, inv_h) - ls) - l.q_all[k]) : exp2_fast(scaled(xc, m_r, f)) * out);
+    g[c] = from_f32<T>(k >= 0 ? wt * (l.mass * expf(scaled(xc, m, inv2) - ls) - l.q_all[k]) : exp2_fast(scaled(xc, m_r, f2)) * out);
   }
 }
 
@@ -320,7 +318,7 @@ __global__ void __launch_bounds__(kRowThreads) k_distill_rows(const DistillArgs 
   __shared__ Seen seen;
   const int r = blockIdx.x, tid = threadIdx.x;
   const Job j = job_of(a, r);
-  if (tid < 32) make_list<T>(a, j, l, 1.f / a.temperature, true, status);
+  if (tid < 32) make_list<T>(a, j, l, 2.f * (1.f / a.temperature), true, status);
   __syncthreads();
   if (l.live) return slow_row<T>(a, r, j, l, seen, kRowThreads);
   if (tid == 0) put_loss(a, r, 0.f, 0.f);
@@ -347,7 +345,7 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
   const bool first_cta = rank == 0;
   Lists& ls_ = *reinterpret_cast<Lists*>(smem);
   Raw<T, N>* const slice = reinterpret_cast<Raw<T, N>*>(smem + sizeof(Lists));
-  const float inv_h = 1.f / a.temperature, f = kLog2e * inv_h;
+  const float inv_h = 1.f / a.temperature, f = kLog2e * inv_h, inv2 = 2.f * inv_h, f2 = 2.f * f;
   if (tid == 0) lost = r1;
   if (cs > 1) {
     if (tid == 0) {
@@ -362,7 +360,7 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
   }
   if (tid >= nt) {
     for (int r = r0; r < r1; ++r) {
-      make_list<T>(a, job_of(a, r), ls_.l[(r - r0) & 1], inv_h, first_cta, status);
+      make_list<T>(a, job_of(a, r), ls_.l[(r - r0) & 1], inv2, first_cta, status);
       named_bar_sync(2, nt + 32);
       // Of an earlier row: the others came to barrier 2 once more, with that written before, and not again. Of this
       // row, which may be written meanwhile: they will come once more.
@@ -472,9 +470,9 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
       } else {
         // How far the list's maximum and the others' lie below the larger of the two, and logarithms to base 2 against
         // that: of the sums over the list, over the others (which knows what c was rounded by), and over both.
-        const float c = ref(v.m, f), gap = scaled(l.m, v.m, inv_h), to_list = fminf(gap, 0.f), to_rest = fminf(-gap, 0.f);
+        const float c = ref(v.m, f), gap = scaled(l.m, v.m, inv2), to_list = fminf(gap, 0.f), to_rest = fminf(-gap, 0.f);
         const float log_s = log2f(v.s) + fmaf(-v.m, f, c);
-        const float to_l = fmaf(to_list, kLog2e, log2f(l.s)), to_r = fmaf(to_rest, kLog2e, log_s);
+        const float to_l = fmaf(to_list, kLog2e, l.log_s), to_r = fmaf(to_rest, kLog2e, log_s);
         const float ls = fmaxf(to_l, to_r) + log2f(1.f + exp2_fast(-fabsf(to_l - to_r)));  // = to_r beside an empty list
         const float log_pr = fmaf(kLn2, log_s - ls, to_rest);
         if (tid == 0 && first_cta)
@@ -482,7 +480,7 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
                    fmaf(kLn2, ls, fmaxf(l.m, v.m) * inv_h));
         if (GRAD) {
           const RowVecs<T> out(g, a.V);
-          const float wt = p.j.w * inv_h, to = wt * (l.mass * expf(log_pr) - l.rest) / v.s;
+          const float wt = p.j.w * inv_h, to = wt * (l.mass * exp2_fast(to_r - ls) - l.rest) / v.s;
           const float at = fmaf(to_list, kLog2e, -ls);
           if (ce >= 0) g[ce] = from_f32<T>(exp2_fast(fmaf(xe, f, -c)) * to);
           if (out.ph == p.row.ph) {
@@ -513,7 +511,7 @@ __global__ void __launch_bounds__(kSliceThreads + 32, 2) k_distill(const Distill
             const int ck = l.cls[k];
             const bool edge = ck < p.row.head || ck >= inner;
             if (l.first[k] && (edge ? first_cta : static_cast<unsigned>(ck - col0) < static_cast<unsigned>(p.n * N)))
-              g[ck] = from_f32<T>(wt * (l.mass * exp2_fast(scaled(l.x[k], l.m, f) + at) - l.q_all[k]));
+              g[ck] = from_f32<T>(wt * (l.mass * exp2_fast(scaled(l.x[k], l.m, f2) + at) - l.q_all[k]));
           }
         }
       }

@@ -8,9 +8,9 @@ from paper_2609_37842_gb300 import eogp as E  # noqa: E402
 from test_more_losses_cpu import DISTILL, HEAD, built, call, size  # noqa: E402,F401
 
 
-@pytest.mark.parametrize("temperature", [3.0e-39, 4.0e-39, 5.8e-39])
+@pytest.mark.parametrize("temperature", [3.0e-39, 4.0e-39, 5.8e-39, 8.8e-39])
 def test_temperatures_whose_exponents_are_no_floats(temperature):
-    """log2(e) / h, which logits are scaled by, is beyond a float there: every answer would be NaN."""
+    """log2(e) / h or twice that, which differences are scaled by, is beyond a float there: answers would be NaN."""
     assert call("eogp_distill", DISTILL, temperature=temperature) == E.EINVAL
 
 
