@@ -669,7 +669,7 @@ int eogp_cross_entropy(const void* logits, int dtype, long long logits_bs, long 
  * for a dweight of EOGP_BF16, rounded to bf16, as dlogits of eogp_cross_entropy would; for one of
  * EOGP_F32 it enters that one as two bf16 parts (about 2^-16 relative). What that takes from the target's
  * entry is added in fp32 (to a row of dweight for the positions of its class, or of many in a piece of n positions for
- * min(64, 4 + n / 256) at least, the same ones every time). EOGP_F32: products to fp32.
+ * min(12, 4 + n / 256) at least, the same ones every time). EOGP_F32: products to fp32.
  * A NaN or infinity in a counted position's x, or in weight, reaches all that it is multiplied
  * with: that position's loss, and dx or dweight. */
 int eogp_head_loss_workspace_size(const void* weight, int dtype, long long ld_weight, int V, int d, int B, int T,
